@@ -464,6 +464,134 @@ gbmw_status gbmw_cost_model(const gbmw_layer_shape* layers, int32_t L,
                             int32_t* O_f, int32_t* O_b, int32_t* O_ms, int32_t* M, float* R,
                             void* stream);
 
+/* ---- Operators of a transformer layer's training -------------------------------
+ *
+ * The cost model above prices a layer by its FLOPs; Section 5 takes its time from
+ * the layer itself, run on one device.  Beside matrix products such a run needs the
+ * operators below, forward and backward.  They share these rules:
+ *   - every data pointer is a DEVICE pointer; work is enqueued on p->stream and the
+ *     call returns without waiting; nothing is allocated and nothing is kept from
+ *     one call for the next, so the calls can be captured in a HIP graph;
+ *   - arguments are checked on the host before anything is enqueued;
+ *   - arrays may lie anywhere an element of their type may (16-byte alignment is
+ *     faster, not required); outputs must not overlap one another or the inputs
+ *     unless a text below says so;
+ *   - sums, softmax statistics and products are accumulated in fp32 (sums of squares
+ *     of gradients in fp64) and outputs are rounded once, to nearest even;
+ *   - results do not depend on timing: the same call gives the same bits.
+ */
+enum { GBMW_F32 = 0, GBMW_F16 = 1, GBMW_BF16 = 2 };
+
+/*
+ * Attention.  Query head h reads key head h / (Hq / Hk); with n = len_q[b] queries and
+ * m = len_k[b] keys in sample b,
+ *   x_ij  = scale * <q_i, k_j>      for i < n, j < m and, if causal, j <= i + m - n,
+ *   lse_i = log sum_j exp x_ij,  p_ij = exp(x_ij - lse_i),  out_i = sum_j p_ij v_j.
+ * A row that sees no key, and every row i >= n, has out_i = 0 and lse_i = -inf.
+ * Backward, from dout, out and lse (as the forward call left them):
+ *   ds_ij = p_ij (<dout_i, v_j> - <dout_i, out_i>),
+ *   dq_i = scale sum_j ds_ij k_j,  dk_j = scale sum_i ds_ij q_i,  dv_j = sum_i p_ij dout_i,
+ * dk and dv summed over the query heads that read the key head.  Rows without keys
+ * give and get no gradient (0), nor do keys that no row sees.
+ * q, k, v, dout beyond the lengths are not used, whatever they hold.  Inside the
+ * lengths values should be finite: a NaN or an infinity reaches the rows that see it,
+ * and may reach rows from which only the causal mask hides it.
+ *
+ * Layout: element (b, row, head, d) of an array X is at X + b * X_stride[0] +
+ * row * X_stride[1] + head * X_stride[2] + d, in elements; strides are >= 0, so inputs
+ * may be broadcast.  lse is [B][Hq][Lq], dense.
+ */
+typedef struct {
+  int32_t dtype;             /* GBMW_F16 or GBMW_BF16, of all arrays but lse         */
+  int32_t B, Hq, Hk;         /* samples >= 0, heads >= 1, Hq a multiple of Hk        */
+  int32_t Lq, Lk;            /* rows of the arrays, >= 0                             */
+  int32_t D;                 /* head size, 1..128                                    */
+  int32_t causal;            /* 0 or 1                                               */
+  float scale;               /* >= 0                                                 */
+  const int32_t* len_q;      /* [B] or NULL (all Lq); values are clamped to 0..Lq    */
+  const int32_t* len_k;      /* [B] or NULL (all Lk); values are clamped to 0..Lk    */
+  const void *q, *k, *v;
+  int64_t q_stride[3], k_stride[3], v_stride[3];
+  void* out;                 /* forward: written; backward: read                     */
+  int64_t out_stride[3];
+  float* lse;                /* forward: written; backward: read                     */
+  const void* dout;          /* from here on backward only                           */
+  int64_t dout_stride[3];
+  void *dq, *dk, *dv;
+  int64_t dq_stride[3], dk_stride[3], dv_stride[3];
+  void* workspace;           /* scratch of at least gbmw_attention_workspace() bytes, */
+  int64_t workspace_bytes;   /* 16-byte aligned; may be used by one call at a time   */
+  void* stream;
+} gbmw_attention_problem;
+
+gbmw_status gbmw_attention_forward(const gbmw_attention_problem* p);
+gbmw_status gbmw_attention_backward(const gbmw_attention_problem* p);
+
+/* Bytes of workspace that a call on this problem needs (the sizes alone are read; may
+ * be 0); -1 with a message if the sizes are out of range. */
+int64_t gbmw_attention_workspace(const gbmw_attention_problem* p, int32_t backward);
+
+/*
+ * Layer norm over rows of `cols` values:
+ *   mean = sum x / cols, rstd = 1 / sqrt(sum (x - mean)^2 / cols + eps),
+ *   xhat = (x - mean) rstd,  y = xhat * weight + bias.
+ * Backward, from dy, x and the forward call's mean and rstd, with g = dy * weight:
+ *   dx = (g - sum(g) / cols - xhat sum(g xhat) / cols) rstd,
+ *   dweight = sum over rows of dy xhat,  dbias = sum over rows of dy.
+ * weight may be NULL (ones), bias may be NULL (zeros), dweight and dbias may each be
+ * NULL (not wanted).  y may be x, and dx may be dy, with the same row stride.
+ */
+typedef struct {
+  int32_t dtype;             /* of x, y, dy, dx                                      */
+  int32_t wdtype;            /* of weight, bias, dweight, dbias: dtype or GBMW_F32   */
+  int64_t rows;              /* >= 0                                                 */
+  int32_t cols;              /* 1..32768                                             */
+  float eps;                 /* >= 0                                                 */
+  const void* x;
+  int64_t x_stride;          /* elements from row to row, >= cols (x, dy: >= 0)      */
+  const void *weight, *bias; /* [cols]                                               */
+  void* y;                   /* forward                                              */
+  int64_t y_stride;
+  float *mean, *rstd;        /* [rows]; forward: written, backward: read             */
+  const void* dy;            /* from here on backward only                           */
+  int64_t dy_stride;
+  void* dx;
+  int64_t dx_stride;
+  void *dweight, *dbias;     /* [cols]                                               */
+  void* workspace;           /* at least gbmw_layer_norm_workspace() bytes, 16-byte  */
+  int64_t workspace_bytes;   /* aligned; backward with dweight or dbias only         */
+  void* stream;
+} gbmw_layer_norm_problem;
+
+gbmw_status gbmw_layer_norm_forward(const gbmw_layer_norm_problem* p);
+gbmw_status gbmw_layer_norm_backward(const gbmw_layer_norm_problem* p);
+int64_t gbmw_layer_norm_workspace(const gbmw_layer_norm_problem* p);
+
+/*
+ * The global norm of a model's gradients, and clipping:
+ *   norm = scale * sqrt(sum of squares of all elements of all tensors),
+ *   out  = grad * (scale * (norm > max_norm ? max_norm / norm : 1)),
+ * scale being the inverse of a loss scale (1 without one).  The sum is kept in fp64, so
+ * no square overflows.  A norm that is NaN or infinite (a gradient is) leaves the
+ * factor at `scale`: `norm` tells, and the step is the caller's to skip.
+ *
+ * A list is made once for tensors that stay where they are: it copies the addresses and
+ * sizes to the device and owns a workspace for the sums.  It holds no tensor alive.
+ * numel[i] >= 0 elements of type in_dtype at in[i]; out_dtype is in_dtype or GBMW_F32;
+ * out[i] may be in[i] if the types are the same.  Making a list allocates and waits;
+ * gbmw_clip_gradients does neither.  One list serves one stream at a time.
+ */
+typedef struct gbmw_gradient_list gbmw_gradient_list;
+
+gbmw_status gbmw_gradient_list_create(int32_t n, const void* const* in, void* const* out,
+                                      const int64_t* numel, int32_t in_dtype, int32_t out_dtype,
+                                      gbmw_gradient_list** list);
+/* norm: DEVICE pointer to one float, or NULL.  max_norm > 0 (may be +inf), scale > 0. */
+gbmw_status gbmw_clip_gradients(gbmw_gradient_list* list, float max_norm, float scale, float* norm,
+                                void* stream);
+/* Waits for the device.  NULL is allowed. */
+void gbmw_gradient_list_destroy(gbmw_gradient_list* list);
+
 /* Lmax of the last solve (row length of `plan` above); 0 if none. */
 int32_t gbmw_max_layers(const gbmw_ctx* ctx);
 

@@ -39,6 +39,9 @@ GBMW_STATIC_SCRATCH_BYTES = 1 << 20
 EXPORTS = [
     "gbmw_dp_solve_batched", "gbmw_backtrack", "gbmw_backtrack_static", "gbmw_select_forward_budget", "gbmw_pipeline_cost",
     "gbmw_partition_search", "gbmw_enumerate_strategies", "gbmw_cost_model",
+    "gbmw_attention_forward", "gbmw_attention_backward", "gbmw_attention_workspace",
+    "gbmw_layer_norm_forward", "gbmw_layer_norm_backward", "gbmw_layer_norm_workspace",
+    "gbmw_gradient_list_create", "gbmw_clip_gradients", "gbmw_gradient_list_destroy",
     "gbmw_max_layers", "gbmw_get_best",
     "gbmw_export_tables", "gbmw_synchronize", "gbmw_last_solve_ms", "gbmw_last_solve_work", "gbmw_destroy",
     "gbmw_last_error", "gbmw_version",
@@ -78,6 +81,30 @@ class gbmw_hardware(ct.Structure):
                 ("unit_bytes", ct.c_double), ("island", ct.c_int32)]
 
 
+GBMW_F32, GBMW_F16, GBMW_BF16 = 0, 1, 2
+
+
+class gbmw_attention_problem(ct.Structure):
+    _fields_ = ([(n, ct.c_int32) for n in ("dtype", "B", "Hq", "Hk", "Lq", "Lk", "D", "causal")] +
+                [("scale", ct.c_float)] +
+                [(n, ct.c_void_p) for n in ("len_q", "len_k", "q", "k", "v")] +
+                [(n, ct.c_int64 * 3) for n in ("q_stride", "k_stride", "v_stride")] +
+                [("out", ct.c_void_p), ("out_stride", ct.c_int64 * 3), ("lse", ct.c_void_p),
+                 ("dout", ct.c_void_p), ("dout_stride", ct.c_int64 * 3)] +
+                [(n, ct.c_void_p) for n in ("dq", "dk", "dv")] +
+                [(n, ct.c_int64 * 3) for n in ("dq_stride", "dk_stride", "dv_stride")] +
+                [("workspace", ct.c_void_p), ("workspace_bytes", ct.c_int64), ("stream", ct.c_void_p)])
+
+
+class gbmw_layer_norm_problem(ct.Structure):
+    _fields_ = [("dtype", ct.c_int32), ("wdtype", ct.c_int32), ("rows", ct.c_int64), ("cols", ct.c_int32),
+                ("eps", ct.c_float), ("x", ct.c_void_p), ("x_stride", ct.c_int64), ("weight", ct.c_void_p),
+                ("bias", ct.c_void_p), ("y", ct.c_void_p), ("y_stride", ct.c_int64), ("mean", ct.c_void_p),
+                ("rstd", ct.c_void_p), ("dy", ct.c_void_p), ("dy_stride", ct.c_int64), ("dx", ct.c_void_p),
+                ("dx_stride", ct.c_int64), ("dweight", ct.c_void_p), ("dbias", ct.c_void_p),
+                ("workspace", ct.c_void_p), ("workspace_bytes", ct.c_int64), ("stream", ct.c_void_p)]
+
+
 STRATEGY_DTYPE = np.dtype([("n_levels", np.int32), ("kind", np.int32, 3), ("degree", np.int32, 3), ("ckpt", np.int32)])
 GBMW_DP, GBMW_SDP, GBMW_TP = 1, 2, 3
 
@@ -107,6 +134,22 @@ _lib.gbmw_partition_search.argtypes = [ct.POINTER(gbmw_partition_problem), ct.c_
 _lib.gbmw_partition_search.restype = ct.c_int
 _lib.gbmw_enumerate_strategies.argtypes = [ct.c_int32, ct.c_int32, ct.c_int32, ct.c_void_p, ct.c_int32]
 _lib.gbmw_enumerate_strategies.restype = ct.c_int32
+for _name in ("gbmw_attention_forward", "gbmw_attention_backward"):
+    getattr(_lib, _name).argtypes = [ct.POINTER(gbmw_attention_problem)]
+    getattr(_lib, _name).restype = ct.c_int
+_lib.gbmw_attention_workspace.argtypes = [ct.POINTER(gbmw_attention_problem), ct.c_int32]
+_lib.gbmw_attention_workspace.restype = ct.c_int64
+for _name in ("gbmw_layer_norm_forward", "gbmw_layer_norm_backward"):
+    getattr(_lib, _name).argtypes = [ct.POINTER(gbmw_layer_norm_problem)]
+    getattr(_lib, _name).restype = ct.c_int
+_lib.gbmw_layer_norm_workspace.argtypes = [ct.POINTER(gbmw_layer_norm_problem)]
+_lib.gbmw_layer_norm_workspace.restype = ct.c_int64
+_lib.gbmw_gradient_list_create.argtypes = [ct.c_int32] + [ct.c_void_p] * 3 + [ct.c_int32] * 2 + [ct.POINTER(ct.c_void_p)]
+_lib.gbmw_gradient_list_create.restype = ct.c_int
+_lib.gbmw_clip_gradients.argtypes = [ct.c_void_p, ct.c_float, ct.c_float, ct.c_void_p, ct.c_void_p]
+_lib.gbmw_clip_gradients.restype = ct.c_int
+_lib.gbmw_gradient_list_destroy.argtypes = [ct.c_void_p]
+_lib.gbmw_gradient_list_destroy.restype = None
 _lib.gbmw_cost_model.argtypes = [ct.c_void_p, ct.c_int32, ct.c_void_p, ct.c_int32, ct.POINTER(gbmw_hardware),
                                  ct.c_double, ct.c_int32, ct.c_int32] + [ct.c_void_p] * 8
 _lib.gbmw_cost_model.restype = ct.c_int
@@ -355,6 +398,288 @@ def gbmw_cost_model(layers, strategies, hw: dict, Bm: float, P: int, device: boo
                                 GBMW_PTR_DEVICE if device else GBMW_PTR_HOST,
                                 *[_ptr(out[k]) for k in ("c", "c_nosync", "O_f", "O_b", "O_ms", "M", "R")], stream))
     return out
+
+
+# ---- operators of a transformer layer's training ------------------------------------------------------------------
+
+_DTYPE = {torch.float32: GBMW_F32, torch.float16: GBMW_F16, torch.bfloat16: GBMW_BF16}
+
+
+def _refuse(message: str):
+    raise GbmwError(GBMW_ERR_INVALID_ARG, message)
+
+
+def _device_tensor(name: str, t, dtype=None, shape=None):
+    """t, or an error: the kernels take plain addresses, so type and shape are checked here."""
+    if not isinstance(t, torch.Tensor) or not t.is_cuda:
+        _refuse(f"{name} is not a tensor on the GPU")
+    if t.device.index != torch.cuda.current_device():
+        _refuse(f"{name} is on {t.device}, device {torch.cuda.current_device()} is current")
+    if t.dtype not in _DTYPE and t.dtype != torch.int32:
+        _refuse(f"{name} has type {t.dtype}")
+    if dtype is not None and t.dtype != dtype:
+        _refuse(f"{name} has type {t.dtype}, not {dtype}")
+    if shape is not None and tuple(t.shape) != tuple(shape):
+        _refuse(f"{name} has shape {tuple(t.shape)}, not {tuple(shape)}")
+    return t
+
+
+class _on_stream:
+    """Outputs and scratch memory that a call makes belong to the stream its kernels run on, so that the memory
+    is not handed to anybody else before they have run.  Inputs on another stream than that are the caller's to
+    keep until the stream has got to the call, as with any work on a second stream."""
+
+    def __init__(self, stream):
+        current = torch.cuda.current_stream()
+        self.handle = current.cuda_stream if stream is None else int(getattr(stream, "cuda_stream", stream))
+        other = self.handle != current.cuda_stream
+        self.guard = torch.cuda.stream(torch.cuda.ExternalStream(self.handle)) if other else None
+
+    def __enter__(self):
+        if self.guard is not None:
+            self.guard.__enter__()
+        return self.handle
+
+    def __exit__(self, *exc):
+        if self.guard is not None:
+            self.guard.__exit__(*exc)
+
+
+def _workspace(p, given, need: int):
+    """Sets p's workspace: the caller's uint8 tensor, or a new one.  Returns what has to live until the call is made."""
+    if need < 0:
+        raise GbmwError(GBMW_ERR_INVALID_ARG, gbmw_last_error())
+    if given is None:
+        given = torch.empty(max(16, need), dtype=torch.uint8, device="cuda")
+    elif not given.is_cuda or given.dtype != torch.uint8 or not given.is_contiguous():
+        _refuse("workspace is not a contiguous uint8 tensor on the GPU")
+    p.workspace, p.workspace_bytes = given.data_ptr(), given.numel()
+    return given
+
+
+def _attention_problem(q, k, v, causal, scale, len_q, len_k) -> gbmw_attention_problem:
+    _device_tensor("q", q)
+    if q.dim() != 4:
+        _refuse(f"q has {q.dim()} dimensions, not [B][Lq][Hq][D]")
+    B, Lq, Hq, D = q.shape
+    if not isinstance(k, torch.Tensor) or k.dim() != 4:
+        _refuse("k is not a tensor [B][Lk][Hk][D]")
+    Lk, Hk = k.shape[1], k.shape[2]
+    _device_tensor("k", k, q.dtype, (B, Lk, Hk, D))
+    _device_tensor("v", v, q.dtype, (B, Lk, Hk, D))
+    p = gbmw_attention_problem()
+    if q.dtype not in _DTYPE:
+        _refuse(f"q has type {q.dtype}")
+    p.dtype, p.B, p.Hq, p.Hk, p.Lq, p.Lk, p.D = _DTYPE[q.dtype], B, Hq, Hk, Lq, Lk, D
+    p.causal, p.scale = int(bool(causal)), (1.0 / D ** 0.5 if D else 1.0) if scale is None else float(scale)
+    for name, t in (("q", q), ("k", k), ("v", v)):
+        _set_array(p, name, t)
+    for name, t in (("len_q", len_q), ("len_k", len_k)):
+        if t is not None:
+            if not _device_tensor(name, t, torch.int32, (B,)).is_contiguous():
+                _refuse(f"{name} is not contiguous")
+            setattr(p, name, t.data_ptr())
+    return p
+
+
+def _set_array(p, name: str, t) -> None:
+    s = t.stride()
+    if s[3] != 1 and t.shape[3] > 1:
+        _refuse(f"{name}: the values of one head are not next to each other")
+    setattr(p, name, t.data_ptr())
+    setattr(p, name + "_stride", (ct.c_int64 * 3)(s[0], s[1], s[2]))
+
+
+def gbmw_attention_workspace(q, k, backward: bool) -> int:
+    """Bytes of workspace of a call on q [B][Lq][Hq][D] and k [B][Lk][Hk][D]."""
+    p = gbmw_attention_problem()
+    p.dtype, (p.B, p.Lq, p.Hq, p.D), (p.Lk, p.Hk) = _DTYPE.get(q.dtype, -1), q.shape, (k.shape[1], k.shape[2])
+    n = _lib.gbmw_attention_workspace(ct.byref(p), int(backward))
+    if n < 0:
+        raise GbmwError(GBMW_ERR_INVALID_ARG, gbmw_last_error())
+    return n
+
+
+def gbmw_attention_forward(q, k, v, causal: bool = False, scale: float | None = None, len_q=None, len_k=None,
+                           out=None, lse=None, workspace=None, stream=None):
+    """out [B][Lq][Hq][D] and lse [B][Hq][Lq] (float32) of q [B][Lq][Hq][D], k and v [B][Lk][Hk][D]: float16 or
+    bfloat16 GPU tensors with any strides whose last one is 1.  scale: 1 / sqrt(D) by default.  len_q, len_k:
+    int32 [B], the samples' lengths.  out, lse, workspace (uint8): made here unless given."""
+    p = _attention_problem(q, k, v, causal, scale, len_q, len_k)
+    with _on_stream(stream) as p.stream:
+        if out is None:
+            out = torch.empty((p.B, p.Lq, p.Hq, p.D), dtype=q.dtype, device="cuda")
+        if lse is None:
+            lse = torch.empty((p.B, p.Hq, p.Lq), dtype=torch.float32, device="cuda")
+        _set_array(p, "out", _device_tensor("out", out, q.dtype, q.shape))
+        p.lse = _device_tensor("lse", lse, torch.float32, (p.B, p.Hq, p.Lq)).data_ptr()
+        if not lse.is_contiguous():
+            _refuse("lse is not contiguous")
+        need = _lib.gbmw_attention_workspace(ct.byref(p), 0)
+        keep = _workspace(p, workspace, need) if need else None
+        _check(_lib.gbmw_attention_forward(ct.byref(p)))
+    return out, lse
+
+
+def gbmw_attention_backward(dout, q, k, v, out, lse, causal: bool = False, scale: float | None = None, len_q=None,
+                            len_k=None, dq=None, dk=None, dv=None, workspace=None, stream=None):
+    """dq, dk, dv from dout and the forward call's arguments and results."""
+    p = _attention_problem(q, k, v, causal, scale, len_q, len_k)
+    with _on_stream(stream) as p.stream:
+        if dq is None:
+            dq = torch.empty((p.B, p.Lq, p.Hq, p.D), dtype=q.dtype, device="cuda")
+        if dk is None:
+            dk = torch.empty((p.B, p.Lk, p.Hk, p.D), dtype=q.dtype, device="cuda")
+        if dv is None:
+            dv = torch.empty((p.B, p.Lk, p.Hk, p.D), dtype=q.dtype, device="cuda")
+        for name, t, like in (("dout", dout, q), ("out", out, q), ("dq", dq, q), ("dk", dk, k), ("dv", dv, k)):
+            _set_array(p, name, _device_tensor(name, t, q.dtype, like.shape))
+        p.lse = _device_tensor("lse", lse, torch.float32, (p.B, p.Hq, p.Lq)).data_ptr()
+        if not lse.is_contiguous():
+            _refuse("lse is not contiguous")
+        keep = _workspace(p, workspace, _lib.gbmw_attention_workspace(ct.byref(p), 1))
+        _check(_lib.gbmw_attention_backward(ct.byref(p)))
+    return dq, dk, dv
+
+
+def _norm_rows(name: str, t, like=None):
+    """(rows, cols, row stride) of a tensor whose last axis is normed; the axes before it have to be one stride."""
+    _device_tensor(name, t, None if like is None else like.dtype, None if like is None else like.shape)
+    if t.dim() < 1:
+        _refuse(f"{name} has no axis")
+    cols, rows = t.shape[-1], t.numel() // max(1, t.shape[-1])
+    if t.stride(-1) != 1 and cols > 1:
+        _refuse(f"{name}: the values of a row are not next to each other")
+    stride = cols
+    if rows > 1:
+        axes = [(n, s) for n, s in zip(t.shape[:-1], t.stride()[:-1]) if n > 1]
+        stride = axes[-1][1]
+        for (n, s), (n1, s1) in zip(axes, axes[1:]):
+            if s != n1 * s1:
+                _refuse(f"{name}: its rows are not one stride apart")
+    return rows, cols, stride
+
+
+def _norm_problem(x, weight, bias) -> gbmw_layer_norm_problem:
+    p = gbmw_layer_norm_problem()
+    p.rows, p.cols, p.x_stride = _norm_rows("x", x)
+    if x.dtype not in _DTYPE:
+        _refuse(f"x has type {x.dtype}")
+    p.x, p.dtype = x.data_ptr(), _DTYPE[x.dtype]
+    wdtype = x.dtype if weight is None and bias is None else (bias if weight is None else weight).dtype
+    p.wdtype = _DTYPE.get(wdtype, -1)
+    for name, t in (("weight", weight), ("bias", bias)):
+        if t is not None:
+            if not _device_tensor(name, t, wdtype, (p.cols,)).is_contiguous():
+                _refuse(f"{name} is not contiguous")
+            setattr(p, name, t.data_ptr())
+    return p
+
+
+def gbmw_layer_norm_workspace(x, weight=None) -> int:
+    """Bytes of workspace of the backward call."""
+    n = _lib.gbmw_layer_norm_workspace(ct.byref(_norm_problem(x, weight, None)))
+    if n < 0:
+        raise GbmwError(GBMW_ERR_INVALID_ARG, gbmw_last_error())
+    return n
+
+
+def gbmw_layer_norm_forward(x, weight=None, bias=None, eps: float = 1e-5, y=None, stream=None):
+    """y like x, mean and rstd float32 of x's shape without its last axis.  x: float32, float16 or bfloat16 GPU
+    tensor; weight, bias: of x's type or float32.  y: made here unless given (it may be x)."""
+    p = _norm_problem(x, weight, bias)
+    p.eps = eps
+    with _on_stream(stream) as p.stream:
+        if y is None:
+            y = torch.empty(x.shape, dtype=x.dtype, device="cuda")
+        _, _, p.y_stride = _norm_rows("y", y, x)
+        mean = torch.empty(x.shape[:-1], dtype=torch.float32, device="cuda")
+        rstd = torch.empty(x.shape[:-1], dtype=torch.float32, device="cuda")
+        p.y, p.mean, p.rstd = y.data_ptr(), mean.data_ptr(), rstd.data_ptr()
+        _check(_lib.gbmw_layer_norm_forward(ct.byref(p)))
+    return y, mean, rstd
+
+
+def gbmw_layer_norm_backward(dy, x, weight, mean, rstd, bias: bool = True, dx=None, workspace=None, stream=None):
+    """dx, dweight, dbias from dy and the forward call's x, weight, mean and rstd.  weight None: no dweight; bias
+    False: no dbias.  Both are of weight's type (x's without one)."""
+    p = _norm_problem(x, weight, None)
+    with _on_stream(stream) as p.stream:
+        if dx is None:
+            dx = torch.empty(x.shape, dtype=x.dtype, device="cuda")
+        _, _, p.dx_stride = _norm_rows("dx", dx, x)
+        _, _, p.dy_stride = _norm_rows("dy", dy, x)
+        p.dx, p.dy = dx.data_ptr(), dy.data_ptr()
+        for name, t in (("mean", mean), ("rstd", rstd)):
+            if not _device_tensor(name, t, torch.float32, x.shape[:-1]).is_contiguous():
+                _refuse(f"{name} is not contiguous")
+            setattr(p, name, t.data_ptr())
+        wdtype = x.dtype if weight is None else weight.dtype
+        dweight = None if weight is None else torch.empty(p.cols, dtype=wdtype, device="cuda")
+        dbias = torch.empty(p.cols, dtype=wdtype, device="cuda") if bias else None
+        keep = None
+        if dweight is not None or dbias is not None:
+            p.dweight, p.dbias = (None if t is None else t.data_ptr() for t in (dweight, dbias))
+            keep = _workspace(p, workspace, _lib.gbmw_layer_norm_workspace(ct.byref(p)))
+        _check(_lib.gbmw_layer_norm_backward(ct.byref(p)))
+    return dx, dweight, dbias
+
+
+class GradientList:
+    """Owns a gbmw_gradient_list and keeps its tensors; freed by gbmw_gradient_list_destroy or with this object."""
+
+    def __init__(self):
+        self.handle = ct.c_void_p(None)
+        self._keep = ()
+
+    def __del__(self):
+        try:
+            gbmw_gradient_list_destroy(self)
+        except Exception:
+            pass
+
+
+def gbmw_gradient_list_create(grads, outs=None) -> GradientList:
+    """A list of gradients (GPU tensors of one type, contiguous) and of the tensors that their clipped values go to:
+    of the same type or float32; by default the gradients themselves.  The tensors have to stay where they are."""
+    grads = list(grads)
+    outs = grads if outs is None else list(outs)
+    if len(outs) != len(grads):
+        _refuse(f"{len(grads)} gradients, {len(outs)} outputs")
+    dtype = grads[0].dtype if grads else torch.float32
+    odtype = outs[0].dtype if outs else torch.float32
+    for i, (g, o) in enumerate(zip(grads, outs)):
+        _device_tensor(f"gradient {i}", g, dtype)
+        _device_tensor(f"output {i}", o, odtype)
+        if o.numel() != g.numel() or not g.is_contiguous() or not o.is_contiguous():
+            _refuse(f"tensor {i}: sizes {g.numel()} and {o.numel()}, or not contiguous")
+    n = len(grads)
+    arr = lambda ts: (ct.c_void_p * max(1, n))(*[t.data_ptr() or None for t in ts])
+    numel = (ct.c_int64 * max(1, n))(*[g.numel() for g in grads])
+    lst = GradientList()
+    _check(_lib.gbmw_gradient_list_create(n, arr(grads), arr(outs), numel, _DTYPE.get(dtype, -1),
+                                          _DTYPE.get(odtype, -1), ct.byref(lst.handle)))
+    lst._keep = (grads, outs)
+    return lst
+
+
+def gbmw_clip_gradients(lst: GradientList, max_norm: float, scale: float = 1.0, norm=None, stream=None):
+    """Writes the list's outputs; returns the norm before clipping, a float32 GPU tensor [1] (norm, if given)."""
+    with _on_stream(stream) as handle:
+        if norm is None:
+            norm = torch.empty(1, dtype=torch.float32, device="cuda")
+        _device_tensor("norm", norm, torch.float32)
+        if norm.numel() < 1:
+            _refuse("norm is empty")
+        _check(_lib.gbmw_clip_gradients(lst.handle, float(max_norm), float(scale), norm.data_ptr(), handle))
+    return norm
+
+
+def gbmw_gradient_list_destroy(lst: GradientList) -> None:
+    if lst.handle:
+        _lib.gbmw_gradient_list_destroy(lst.handle)
+        lst.handle = ct.c_void_p(None)
+        lst._keep = ()
 
 
 def gbmw_export_tables(ctx: Context, instance: int, l0: int = 0, l1: int | None = None,
