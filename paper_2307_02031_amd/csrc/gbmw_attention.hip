@@ -24,6 +24,10 @@ using gbmw_detail::fail;
 namespace gbmw {
 namespace {
 
+#ifndef GBMW_FILL
+#define GBMW_FILL 1536
+#define GBMW_LEAST 512
+#endif
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 constexpr float kInf = __builtin_inff();
 
@@ -37,11 +41,15 @@ typedef bf16 bf16x8 __attribute__((ext_vector_type(8)));
 struct AttnArgs {
   const char *q, *k, *v, *dout;
   char *out, *dq, *dk, *dv;
-  float *lse, *delta;
+  float *lse;
+  float *level, *delta;   // [B][Hk][rows]: log2(e) lse - kUp, inf for rows without keys; <dout, out>
   float *vmax, *gmax;   // f16: the largest norms of a value and of a row of dout, for parts of 256 keys and 128 rows
   int64_t qs[3], ks[3], vs[3], os[3], dos[3], dqs[3], dks[3], dvs[3];
   const int *len_q, *len_k;
+  float* partial;   // [parts][2][B][Hk][Lk][D4]: shares of dk and dv
   int B, Hq, Hk, Lq, Lk, D, share, causal;
+  int parts, D4;    // D rounded up to 4
+  unsigned magic;   // 2^32 / share, rounded up
   float c;       // scale * log2(e): probabilities are powers of two
   float scale;
 };
@@ -65,105 +73,204 @@ __device__ __forceinline__ s16x8 round8(const f32x16& x, int t) {
   return __builtin_bit_cast(s16x8, r);
 }
 
-// ---- tiles in LDS: rows of CH 16-byte pieces, the piece swapped by the row -----------------
+// ---- tiles in LDS ---------------------------------------------------------------------------
 //
-// read_row8 reads one piece of 32 rows, read_cols 32 bytes each of four rows; with the piece
-// exclusive-or'ed with this function of the row both touch every bank once per cycle.
-__device__ __forceinline__ int swap_of(int row) { return ((row & 3) << 1) | ((row >> 2) & 1); }
+// A tile is 64 rows of CH 16-byte pieces, stored so that the two kinds of reads, a piece of
+// each of 32 rows and (transposing) 64 bytes of each of four rows, touch all 64 banks evenly:
+// piece p of row r lies at place p ^ swap_of(r) of its row, and rows of 16 pieces have 16 bytes
+// between groups of four.  A lane then needs four addresses for each kind (Reader);
+// everything else is a constant offset.
+typedef __attribute__((address_space(3))) char lds_char;
 
+template <int KS>
+constexpr int kChunks = KS <= 4 ? 8 : 16;
 template <int CH>
-__device__ __forceinline__ int piece_at(int row, int piece) {   // in 16-bit elements
-  return (row * CH + (piece ^ swap_of(row))) * 8;
+__device__ __forceinline__ constexpr int swap_of(int row) {
+  return CH == 16 ? (row & 3) << 2 : ((row & 2) << 1) | ((row >> 2) & 3);
 }
-
-// A operand whose rows are the tile's rows row .. row+31 and whose terms are the columns
-// 16 step .. 16 step + 15.
 template <int CH>
-__device__ __forceinline__ s16x8 read_rows(const short* tile, int row, int step) {
-  const int l = threadIdx.x % 64;
-  return *(const s16x8*)&tile[piece_at<CH>(row + l % 32, 2 * step + l / 32)];
+__device__ __forceinline__ constexpr int place_of(int row, int piece) {   // bytes
+  return (row * CH + (piece ^ swap_of<CH>(row))) * 16 + (CH == 16 ? row / 4 * 16 : 0);
 }
+template <int KS>
+constexpr int kTile = 64 * 16 * kChunks<KS> + (kChunks<KS> == 16 ? 256 : 0);   // bytes
 
-// A operand whose rows are the tile's columns col .. col+31 and whose terms are its rows
-// row .. row+15 in the order above.  The transposing read gives lane i of 16 element i of each
-// of four runs of 16 elements, lanes 4u..4u+3 naming the four quarters of run u.
-template <int CH>
-__device__ __forceinline__ s16x8 read_cols(const short* tile, int row, int col) {
-  typedef __attribute__((address_space(3))) s16x4 lds4;
-  const int l = threadIdx.x % 64, i = l % 16;
-  const int r = row + 4 * (l / 32) + i / 4, c = col + 16 * ((l / 16) % 2) + 4 * (i % 4);
-  s16x4 x[2];
+template <int KS>
+struct Reader {
+  static constexpr int CH = kChunks<KS>;
+  int row[4], col[4];
+  __device__ __forceinline__ Reader() {
+    const int l = threadIdx.x % 64, i = l % 16, half = l / 32;
 #pragma unroll
-  for (int u = 0; u < 2; ++u) {
-    const short* p = &tile[piece_at<CH>(r + 8 * u, c / 8) + c % 8];
-    x[u] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4*)p);
+    for (int s = 0; s < 4; ++s) row[s] = place_of<CH>(l % 32, (CH == 16 ? 4 * s : 2 * s) + half);
+    // lanes 4u..4u+3 of sixteen name the quarters of run u of sixteen elements; lane i gets
+    // element i of each of the four runs
+    const int r = 4 * half + i / 4, c = 16 * ((l / 16) % 2) + 4 * (i % 4);
+#pragma unroll
+    for (int n = 0; n < 4; ++n)   // of 32 columns each, or of two times 32 columns eight rows apart
+      col[n] = (CH == 16 ? place_of<CH>(r, 4 * n + c / 8) : place_of<CH>(r + 8 * (n / 2), 4 * (n % 2) + c / 8)) + (c % 8) * 2;
   }
-  return __builtin_shufflevector(x[0], x[1], 0, 1, 2, 3, 4, 5, 6, 7);
-}
-
-// A piece of a row in global memory; zeros beyond D and where the row is not there.
-__device__ __forceinline__ s16x8 load8(const char* row, int piece, int D, bool there) {
-  const Pack<bf16> r = load_pack((const bf16*)row + 8 * piece, there ? D - 8 * piece : 0);
-  return __builtin_bit_cast(s16x8, r);
-}
-
-// Pieces of one 64-row tile that a thread of 256 loads: piece n = threadIdx.x + 256 i is piece
-// n % (2 KS) of row n / (2 KS).
-template <int KS>
-constexpr int kLoads = (64 * 2 * KS + 255) / 256;
-
-template <int KS>
-struct Staged {
-  s16x8 x[kLoads<KS>];
+  static constexpr int down(int r) { return r * CH * 16 + (CH == 16 ? r / 4 * 16 : 0); }   // r a multiple of 16, or of 8 for CH = 16
+  // A operand: rows r .. r+31 of the tile (r = 0 or 32), terms 16 step .. 16 step + 15
+  __device__ __forceinline__ s16x8 rows(lds_char* tile, int r, int step) const {
+    typedef __attribute__((address_space(3))) s16x8 lds8;
+    return *(lds8*)(tile + (CH == 16 ? row[step / 2] + (step % 2) * 32 : row[step]) + down(r));
+  }
+  // A operand: rows = columns 32 d .. 32 d + 31 of the tile, terms = its rows r .. r+15 in the
+  // order of a result's registers
+  __device__ __forceinline__ s16x8 cols(lds_char* tile, int r, int d) const {
+    typedef __attribute__((address_space(3))) s16x4 lds4;
+    s16x4 x[2];
+#pragma unroll
+    for (int u = 0; u < 2; ++u)
+      x[u] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4*)(tile + (CH == 16 ? col[d] + down(r + 8 * u) : col[d + 2 * u] + down(r))));
+    return __builtin_shufflevector(x[0], x[1], 0, 1, 2, 3, 4, 5, 6, 7);
+  }
 };
 
-// rows first .. first+63 of an array with one head: row r is at base + r * stride (bytes)
-template <int KS>
-__device__ __forceinline__ void fetch(Staged<KS>& s, const char* base, int64_t stride, int first, int rows, int D) {
-#pragma unroll
-  for (int i = 0; i < kLoads<KS>; ++i) {
-    const int n = threadIdx.x + 256 * i, r = n / (2 * KS);
-    const bool there = first + r < rows && r < 64;
-    s.x[i] = load8(base + (there ? (int64_t)(first + r) * stride : 0), n % (2 * KS), D, there);
+// A piece of a row in global memory; zeros beyond D and where the row is not there.  WHOLE: D is
+// a multiple of 8.
+template <bool WHOLE>
+__device__ __forceinline__ s16x8 load8(const char* row, int piece, int D, bool there) {
+  if constexpr (WHOLE) {
+    s16x8 r = {};
+    if (there && 8 * piece < D) __builtin_memcpy(&r, row + 16 * piece, 16);
+    return r;
+  } else {
+    const Pack<bf16> r = load_pack((const bf16*)row + 8 * piece, there ? D - 8 * piece : 0);
+    return __builtin_bit_cast(s16x8, r);
   }
 }
 
-// the same of the rows of a group of heads
-template <int KS>
-__device__ __forceinline__ void fetch_group(Staged<KS>& s, const char* base, int64_t row_stride, int64_t head_stride,
-                                            int share, int first, int rows, int D) {
-#pragma unroll
-  for (int i = 0; i < kLoads<KS>; ++i) {
-    const int n = threadIdx.x + 256 * i, r = n / (2 * KS);
-    const bool there = first + r < rows && r < 64;
-    const int at = there ? first + r : 0, x = at / share;
-    s.x[i] = load8(base + x * row_stride + (at - x * share) * head_stride, n % (2 * KS), D, there);
+// Rows of a group of `share` heads: row r is at base + (r / share) * stride + (r % share) * head.
+struct Rows {
+  const char* base;
+  int64_t stride, head;   // bytes
+  int share, count;       // rows beyond count read as zeros
+  unsigned magic;         // 2^32 / share, rounded up
+  __device__ __forceinline__ int of(int r) const {   // r / share
+    if (share == 1) return r;
+    int x = (int)__umulhi((unsigned)r, magic);   // at most one too large for r < 2^31
+    return x * share > r ? x - 1 : x;
   }
-}
+};
 
-template <int KS, int CH>
-__device__ __forceinline__ void put(short* tile, const Staged<KS>& s) {
-#pragma unroll
-  for (int i = 0; i < kLoads<KS>; ++i) {
-    const int n = threadIdx.x + 256 * i, r = n / (2 * KS);
-    if (r < 64) *(s16x8*)&tile[piece_at<CH>(r, n % (2 * KS))] = s.x[i];
+// Brings 64 rows into a tile, in two halves: begin() before the tile before it is worked on,
+// end() before the barrier that hands it over.
+//
+// Direct: the loads write to LDS themselves, 64 pieces in lane order; lanes fetch the pieces
+// that belong in their places, and what is beyond the buffer's bounds arrives as zeros.  Needs
+// 16-byte aligned rows and offsets inside a tile below 2^31.  Otherwise through registers.
+//
+// A wave brings N runs of kRowsOf rows.  Its lanes' offsets inside a run are the same for all of
+// them where rows have 16 pieces; with SPARE every run gets bounds of its own and the lanes keep
+// one offset, otherwise N (for the kernel that is short of registers, and those that are not).
+template <int KS, bool DIRECT, bool SPARE = false>
+struct Loader {
+  static constexpr int CH = kChunks<KS>, N = DIRECT ? CH / 4 : (64 * 2 * KS + 255) / 256;
+  static constexpr int kRowsOf = 64 / CH;
+  static constexpr bool kOne = SPARE && CH == 16;
+  static constexpr int NA = kOne ? 1 : N;
+  static constexpr unsigned kOut = 0x80000000u;
+  s16x8 x[DIRECT ? 1 : N];
+  unsigned at[DIRECT ? NA : 1];
+
+  __device__ __forceinline__ static int wave() { return __builtin_amdgcn_readfirstlane(threadIdx.x / 64); }
+  __device__ __forceinline__ static int row_of(int i) {   // of this lane, in the tile
+    return (wave() * N + i) * kRowsOf + (int)(threadIdx.x % 64) / CH;
   }
-}
+  __device__ __forceinline__ void init(const Rows& rows, int D) {
+    if constexpr (DIRECT) {
+#pragma unroll
+      for (int i = 0; i < NA; ++i) {
+        const int piece = ((int)threadIdx.x % CH) ^ swap_of<CH>(row_of(i));
+        const int down = kOne ? (int)(threadIdx.x % 64) / CH : row_of(i);
+        at[i] = 8 * piece >= D ? kOut : 16 * piece + (rows.share == 1 ? down * (unsigned)rows.stride : 0u);
+      }
+    }
+  }
+
+  __device__ __forceinline__ void begin(lds_char* tile, const Rows& rows, int first, int D) {
+    if constexpr (DIRECT) {
+      if (rows.share == 1) {   // rows beyond the last one are beyond the bounds
+        const int64_t length = (int64_t)(rows.count - first) * rows.stride;
+        const int left = (int)min(length, (int64_t)0x7fffffff), run = kRowsOf * (int)rows.stride;
+        const char* base = rows.base + first * rows.stride;
+        const int skip = kOne ? wave() * N * run : 0;
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+          const int off = kOne ? skip + i * run : 0;
+          load(tile, __builtin_amdgcn_make_buffer_rsrc((void*)(base + off), 0, max(left - off, 0), 0x00020000), i, at[i % NA]);
+        }
+      } else {
+        const int x0 = rows.of(first);
+        __amdgpu_buffer_rsrc_t from =
+            __builtin_amdgcn_make_buffer_rsrc((void*)(rows.base + x0 * rows.stride), 0, 0x7fffffff, 0x00020000);
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+          const int r = first + row_of(i), x = rows.of(r);
+          load(tile, from, i, (r >= rows.count) | (at[i % NA] == kOut) ? kOut
+                                  : at[i % NA] + (unsigned)(x - x0) * (unsigned)rows.stride + (unsigned)(r - x * rows.share) * (unsigned)rows.head);
+        }
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < N; ++i) {
+        const int n = threadIdx.x + 256 * i, r = first + n / (2 * KS);
+        const bool there = n < 64 * 2 * KS && r < rows.count;
+        const int q = there ? r : first, h = rows.of(q);
+        x[i] = load8<false>(rows.base + h * rows.stride + (q - h * rows.share) * rows.head, n % (2 * KS), D, there);
+      }
+    }
+  }
+  __device__ __forceinline__ static void load(lds_char* tile, __amdgpu_buffer_rsrc_t from, int i, unsigned offset) {
+    lds_char* to = tile + (wave() * N + i) * (CH == 16 ? 1040 : 1024);
+    __builtin_amdgcn_raw_ptr_buffer_load_lds(from, (__attribute__((address_space(3))) void*)to, 16, (int)offset, 0, 0, 0);
+  }
+  __device__ __forceinline__ void end(lds_char* tile) {
+    if constexpr (DIRECT) {
+      __builtin_amdgcn_s_waitcnt(0x0f70);   // all of this wave's loads have arrived
+    } else {
+      typedef __attribute__((address_space(3))) s16x8 lds8;
+#pragma unroll
+      for (int i = 0; i < N; ++i) {
+        const int n = threadIdx.x + 256 * i, r = n / (2 * KS);
+        if (r < 64) *(lds8*)(tile + place_of<CH>(r, n % (2 * KS))) = x[i];
+      }
+    }
+  }
+};
 
 __device__ __forceinline__ int length(const int* len, int b, int most) {
   return len ? max(0, min(len[b], most)) : most;
 }
 
+__device__ __forceinline__ float max3(float a, float b, float c) {   // without quieting NaNs first
+  float r;
+  asm("v_max3_f32 %0, %1, %2, %3" : "=v"(r) : "v"(a), "v"(b), "v"(c));
+  return r;
+}
+
+__device__ __forceinline__ float other_half(float x, float* mine) {   // of lane l ^ 32; both sorted by half
+  const auto r = __builtin_amdgcn_permlane32_swap(__builtin_bit_cast(unsigned, x), __builtin_bit_cast(unsigned, x), false, false);
+  *mine = __builtin_bit_cast(float, (unsigned)r[0]);
+  return __builtin_bit_cast(float, (unsigned)r[1]);
+}
+
 // A row of the result of a product over d: lane l has column (row of the problem) l % 32 and
 // the d of its registers, four at a time.
-template <typename T>
+template <typename T, bool WHOLE>
 __device__ __forceinline__ void store4(char* row, int d, int D, const f32x16& x, int r, float f) {
   typedef T Tx4 __attribute__((ext_vector_type(4)));
   Tx4 y;
 #pragma unroll
-  for (int i = 0; i < 4; ++i) y[i] = (T)(x[r + i] * f);
+  for (int i = 0; i < 4; ++i) {
+    float z = x[r + i] * f;
+    asm("" : "+v"(z));   // the product is rounded to 32 bits first, in every variant of a kernel
+    y[i] = (T)z;
+  }
   T* p = (T*)row + d;
-  if (d + 4 <= D) {
+  if (WHOLE || d + 4 <= D) {
     __builtin_memcpy(p, &y, 8);
   } else {
 #pragma unroll
@@ -171,6 +278,35 @@ __device__ __forceinline__ void store4(char* row, int d, int D, const f32x16& x,
       if (d + i < D) p[i] = y[i];
   }
 }
+
+// Workgroups are dealt to the eight dies in turn; neighbours in `id` (tiles of one head, which
+// read the same keys) go to one die and its cache.
+__device__ __forceinline__ int dealt(int id, int n) {
+  const int per = n / 8;
+  return id < per * 8 ? (id % 8) * per + id / 8 : id;
+}
+
+// Where a workgroup of the rows' kernels works, and how many keys a row sees.
+struct Place {
+  int tile, tiles, hk, b, nq, nk, rows;
+  __device__ __forceinline__ Place(const AttnArgs& a, int per) {
+    rows = a.Lq * a.share;
+    tiles = (rows + per - 1) / per;
+    int id = blockIdx.x;
+    const int heads = a.Hk * a.B;
+    tile = tiles - 1 - id / heads;   // the longest rows of a causal mask first
+    id = dealt(id % heads, heads);
+    hk = id % a.Hk, b = id / a.Hk;
+    nq = length(a.len_q, b, a.Lq), nk = length(a.len_k, b, a.Lk);
+  }
+  __device__ __forceinline__ int sees(const AttnArgs& a, int i) const {   // keys j < sees
+    return i >= nq ? 0 : a.causal ? max(0, min(nk, i + nk - nq + 1)) : nk;
+  }
+  __device__ __forceinline__ int most(const AttnArgs& a, int per) const {   // of any row of the tile
+    const int first = tile * per / a.share, last = min((min(tile * per + per, rows) - 1) / a.share, nq - 1);
+    return first >= nq ? 0 : sees(a, last);
+  }
+};
 
 // Probabilities times 2^kUp: float16 loses digits below 2^-14, and a thousand keys have
 // probabilities of a thousandth.
@@ -195,115 +331,143 @@ __device__ __forceinline__ float max_of(const float* x, int n) {   // n values, 
   return m;
 }
 
-template <int KS>
-constexpr int kChunks = KS <= 4 ? 8 : 16;
-
 // ---- forward --------------------------------------------------------------------------------
 //
-// A workgroup takes 128 rows of one (sample, key head), 32 a wave, and walks the keys in tiles
-// of 64.  A wave computes x^T = K Q^T (lane: one row, 32 keys), so the running maximum and sum
-// of a row need one exchange between two lanes a tile, and out^T += V^T p^T with p from its
-// own registers.
-template <typename T, int KS>
-__global__ __launch_bounds__(256, 2) void k_attn_fwd(AttnArgs a) {
-  constexpr int CH = kChunks<KS>, DB = (KS + 1) / 2;
-  __shared__ __attribute__((aligned(16))) short sK[2][64 * CH * 8], sV[2][64 * CH * 8];
-  const int tiles = (a.Lq * a.share + 127) / 128;
-  int id = blockIdx.x;
-  const int tile = tiles - 1 - id % tiles;   // the longest rows of a causal mask first
-  id /= tiles;
-  const int hk = id % a.Hk, b = id / a.Hk;
-  const int nq = length(a.len_q, b, a.Lq), nk = length(a.len_k, b, a.Lk);
-  const int l = threadIdx.x % 64, half = l / 32, row0 = tile * 128 + (threadIdx.x / 64) * 32;
-  const int rows = a.Lq * a.share, row = row0 + l % 32;
-  const int i = row / a.share, hq = hk * a.share + row % a.share;
-  // the row sees keys j < sees
-  const int sees = i >= nq ? 0 : a.causal ? max(0, min(nk, i + nk - nq + 1)) : nk;
-  const int last_i = min((min(tile * 128 + 128, rows) - 1) / a.share, nq - 1);
-  const int most = tile * 128 / a.share >= nq ? 0 : a.causal ? max(0, min(nk, last_i + nk - nq + 1)) : nk;
-  const char* kb = a.k + 2 * (b * a.ks[0] + hk * a.ks[2]);
-  const char* vb = a.v + 2 * (b * a.vs[0] + hk * a.vs[2]);
+// A workgroup takes 128 NQ rows of one (sample, key head), 32 NQ a wave, and walks the keys in
+// tiles of 64.  A wave computes x^T = K Q^T (lane: one row, 32 keys), so the running maximum
+// and sum of a row need one exchange between two lanes a tile, and out^T += V^T p^T with p from
+// its own registers.  The running sums are in units of 2^(c m); m follows the maximum only
+// when that is more than 2^kLag ahead, so they are seldom rescaled.
+constexpr float kLag = 6.0f;
 
-  s16x8 q[KS];
-  {
-    const char* p = a.q + 2 * (b * a.qs[0] + (i < nq ? i : 0) * a.qs[1] + hq * a.qs[2]);
+template <typename T, int KS, int NQ, bool DIRECT>
+__global__ __launch_bounds__(256, NQ == 1 ? 2 : 1) void k_attn_fwd(AttnArgs a) {
+  constexpr int DB = (KS + 1) / 2;
+  __shared__ __attribute__((aligned(16))) char lds[4 * kTile<KS>];
+  lds_char* const tiles = (lds_char*)lds;
+  const Place w(a, 128 * NQ);
+  const int l = threadIdx.x % 64, half = l / 32;
+  const int most = w.most(a, 128 * NQ);
+  const Rows kr{a.k + 2 * (w.b * a.ks[0] + w.hk * a.ks[2]), 2 * a.ks[1], 0, 1, w.nk, 0};
+  const Rows vr{a.v + 2 * (w.b * a.vs[0] + w.hk * a.vs[2]), 2 * a.vs[1], 0, 1, w.nk, 0};
+
+  s16x8 q[NQ][KS];
+  int sees[NQ];
+  int fewest = INT_MAX;
 #pragma unroll
-    for (int s = 0; s < KS; ++s) q[s] = load8(p, 2 * s + half, a.D, i < nq);
+  for (int n = 0; n < NQ; ++n) {
+    const int row = w.tile * 128 * NQ + ((int)(threadIdx.x / 64) * NQ + n) * 32 + l % 32;
+    const int i = row / a.share, hq = w.hk * a.share + row % a.share;
+    sees[n] = w.sees(a, i);
+    fewest = min(fewest, sees[n]);
+    const char* p = a.q + 2 * (w.b * a.qs[0] + (i < w.nq ? i : 0) * a.qs[1] + hq * a.qs[2]);
+#pragma unroll
+    for (int s = 0; s < KS; ++s) q[n][s] = load8<DIRECT>(p, 2 * s + half, a.D, i < w.nq);
   }
-  f32x16 o[DB] = {};
-  float m = -kInf, sum = 0.0f;   // m in units of x / scale
+  f32x16 o[NQ][DB] = {};
+  float m[NQ], sum[NQ];   // m in units of x / scale
+#pragma unroll
+  for (int n = 0; n < NQ; ++n) m[n] = -kInf, sum[n] = 0.0f;
 
-  Staged<KS> nextK, nextV;
+  const Reader<KS> rd;
+  Loader<KS, DIRECT> lk, lv;
+  lk.init(kr, a.D), lv.init(vr, a.D);
   if (most > 0) {
-    fetch(nextK, kb, 2 * a.ks[1], 0, nk, a.D);
-    fetch(nextV, vb, 2 * a.vs[1], 0, nk, a.D);
+    lk.begin(tiles, kr, 0, a.D);
+    lv.begin(tiles + kTile<KS>, vr, 0, a.D);
   }
   for (int j0 = 0, buf = 0; j0 < most; j0 += 64, buf ^= 1) {
-    put<KS, CH>(sK[buf], nextK);
-    put<KS, CH>(sV[buf], nextV);
+    lds_char *tk = tiles + 2 * buf * kTile<KS>, *tv = tk + kTile<KS>;
+    lk.end(tk), lv.end(tv);
     __syncthreads();   // this tile is whole, and nobody reads the other buffer any more
     if (j0 + 64 < most) {
-      fetch(nextK, kb, 2 * a.ks[1], j0 + 64, nk, a.D);
-      fetch(nextV, vb, 2 * a.vs[1], j0 + 64, nk, a.D);
+      lds_char* to = tiles + 2 * (buf ^ 1) * kTile<KS>;
+      lk.begin(to, kr, j0 + 64, a.D);
+      lv.begin(to + kTile<KS>, vr, j0 + 64, a.D);
     }
-    f32x16 x[2] = {};
+    f32x16 x[NQ][2] = {};
 #pragma unroll
     for (int u = 0; u < 2; ++u)
 #pragma unroll
-      for (int s = 0; s < KS; ++s) x[u] = mma<T>(read_rows<CH>(sK[buf], 32 * u, s), q[s], x[u]);
-    if (!__all(j0 + 64 <= sees)) {
+      for (int s = 0; s < KS; ++s) {
+        const s16x8 k = rd.rows(tk, 32 * u, s);
+#pragma unroll
+        for (int n = 0; n < NQ; ++n) x[n][u] = mma<T>(k, q[n][s], x[n][u]);
+      }
+    if (!__all(j0 + 64 <= fewest)) {
+#pragma unroll
+      for (int n = 0; n < NQ; ++n)
+#pragma unroll
+        for (int u = 0; u < 2; ++u)
+#pragma unroll
+          for (int r = 0; r < 16; ++r)
+            if (j0 + 32 * u + 8 * (r / 4) + 4 * half + r % 4 >= sees[n]) x[n][u][r] = -kInf;
+    }
+#pragma unroll
+    for (int n = 0; n < NQ; ++n) {
+      // the matrix results are waited for where the compiler sees them read, before max3
+      float top = fmaxf(fmaxf(m[n], x[n][0][15]), x[n][1][15]);
 #pragma unroll
       for (int u = 0; u < 2; ++u)
 #pragma unroll
-        for (int r = 0; r < 16; ++r)
-          if (j0 + 32 * u + 8 * (r / 4) + 4 * half + r % 4 >= sees) x[u][r] = -kInf;
-    }
-    float top = m;
+        for (int r = 0; r < 16; r += 2) top = max3(top, x[n][u][r], x[n][u][r + 1]);
+      float low;
+      const float high = other_half(top, &low);
+      top = fmaxf(low, high);
+      const bool ahead = (top - m[n]) * a.c > kLag;
+      if (__any(ahead)) {
+        const float f = ahead ? __builtin_amdgcn_exp2f((m[n] - top) * a.c) : 1.0f;
+        if (ahead) m[n] = top;
+        sum[n] *= f;
 #pragma unroll
-    for (int u = 0; u < 2; ++u)
+        for (int d = 0; d < DB; ++d)
 #pragma unroll
-      for (int r = 0; r < 16; ++r) top = fmaxf(top, x[u][r]);
-    top = fmaxf(top, __shfl_xor(top, 32));
-    if (__any(top > m)) {   // the running sums are in units of the old maximum
-      const float f = top > m ? __builtin_amdgcn_exp2f((m - top) * a.c) : 1.0f;
-      m = top;
-      sum *= f;
-#pragma unroll
-      for (int d = 0; d < DB; ++d)
-#pragma unroll
-        for (int r = 0; r < 16; ++r) o[d][r] *= f;
-    }
-    const float off = (m == -kInf ? 0.0f : m * a.c) - kUp<T>;
-#pragma unroll
-    for (int u = 0; u < 2; ++u)
-#pragma unroll
-      for (int r = 0; r < 16; ++r) {
-        x[u][r] = __builtin_amdgcn_exp2f(__builtin_fmaf(x[u][r], a.c, -off));
-        sum += x[u][r];
+          for (int r = 0; r < 16; ++r) o[n][d][r] *= f;
       }
+      const float off = (m[n] == -kInf ? 0.0f : m[n] * a.c) - kUp<T>;
+#pragma unroll
+      for (int u = 0; u < 2; ++u)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+          x[n][u][r] = __builtin_amdgcn_exp2f(__builtin_fmaf(x[n][u][r], a.c, -off));
+          sum[n] += x[n][u][r];
+        }
+    }
 #pragma unroll
     for (int u = 0; u < 2; ++u)
 #pragma unroll
       for (int t = 0; t < 2; ++t) {
-        const s16x8 p = round8<T>(x[u], t);
+        s16x8 p[NQ];
 #pragma unroll
-        for (int d = 0; d < DB; ++d) o[d] = mma<T>(read_cols<CH>(sV[buf], 32 * u + 16 * t, 32 * d), p, o[d]);
+        for (int n = 0; n < NQ; ++n) p[n] = round8<T>(x[n][u], t);
+#pragma unroll
+        for (int d = 0; d < DB; ++d) {
+          const s16x8 v = rd.cols(tv, 32 * u + 16 * t, d);
+#pragma unroll
+          for (int n = 0; n < NQ; ++n) o[n][d] = mma<T>(v, p[n], o[n][d]);
+        }
       }
   }
-  sum += __shfl_xor(sum, 32);
-  if (row >= rows) return;
-  const bool empty = m == -kInf && !(sum != sum);
-  const float f = empty ? 0.0f : 1.0f / sum;
-  if (half == 0)
-    a.lse[((int64_t)b * a.Hq + hq) * a.Lq + i] = empty ? -kInf : (m * a.c - kUp<T> + __builtin_amdgcn_logf(sum)) * kLn2;
-  char* out = a.out + 2 * (b * a.os[0] + i * a.os[1] + hq * a.os[2]);
 #pragma unroll
-  for (int d = 0; d < DB; ++d)
+  for (int n = 0; n < NQ; ++n) {
+    const int row = w.tile * 128 * NQ + ((int)(threadIdx.x / 64) * NQ + n) * 32 + l % 32;
+    const int i = row / a.share, hq = w.hk * a.share + row % a.share;
+    sum[n] += __shfl_xor(sum[n], 32);
+    if (row >= w.rows) continue;
+    const bool empty = m[n] == -kInf && !(sum[n] != sum[n]);
+    const float f = empty ? 0.0f : 1.0f / sum[n];
+    if (half == 0)
+      a.lse[((int64_t)w.b * a.Hq + hq) * a.Lq + i] =
+          empty ? -kInf : (m[n] * a.c - kUp<T> + __builtin_amdgcn_logf(sum[n])) * kLn2;
+    char* out = a.out + 2 * (w.b * a.os[0] + i * a.os[1] + hq * a.os[2]);
 #pragma unroll
-    for (int r = 0; r < 16; r += 4) {
-      const int at = 32 * d + 8 * (r / 4) + 4 * half;
-      if (at < a.D) store4<T>(out, at, a.D, o[d], r, f);
-    }
+    for (int d = 0; d < DB; ++d)
+#pragma unroll
+      for (int r = 0; r < 16; r += 4) {
+        const int at = 32 * d + 8 * (r / 4) + 4 * half;
+        if (at < a.D) store4<T, DIRECT>(out, at, a.D, o[n][d], r, f);
+      }
+  }
 }
 
 // The largest norm of a value among 256 keys of a (sample, key head), for float16's lift.
@@ -333,25 +497,19 @@ __global__ __launch_bounds__(256) void k_attn_vmax(AttnArgs a) {
 // Rows and keys as in the forward pass: p^T from K Q^T and the row's log-sum-exp, dp^T = V
 // dout^T, ds^T = p^T (dp^T - delta), dq^T += K^T ds^T.  Writes delta = <dout, out> of its rows and,
 // for float16, their largest norm for the other kernel.
-template <typename T, int KS>
+template <typename T, int KS, bool DIRECT>
 __global__ __launch_bounds__(256, 2) void k_attn_dq(AttnArgs a) {
-  constexpr int CH = kChunks<KS>, DB = (KS + 1) / 2;
+  constexpr int DB = (KS + 1) / 2;
   constexpr bool kLift = __is_same(T, f16);
-  __shared__ __attribute__((aligned(16))) short sK[2][64 * CH * 8], sV[2][64 * CH * 8];
-  const int tiles = (a.Lq * a.share + 127) / 128;
-  int id = blockIdx.x;
-  const int tile = tiles - 1 - id % tiles;
-  id /= tiles;
-  const int hk = id % a.Hk, b = id / a.Hk;
-  const int nq = length(a.len_q, b, a.Lq), nk = length(a.len_k, b, a.Lk);
-  const int l = threadIdx.x % 64, half = l / 32, row0 = tile * 128 + (threadIdx.x / 64) * 32;
-  const int rows = a.Lq * a.share, row = row0 + l % 32;
-  const int i = row / a.share, hq = hk * a.share + row % a.share;
-  const int sees = i >= nq ? 0 : a.causal ? max(0, min(nk, i + nk - nq + 1)) : nk;
-  const int last_i = min((min(tile * 128 + 128, rows) - 1) / a.share, nq - 1);
-  const int most = tile * 128 / a.share >= nq ? 0 : a.causal ? max(0, min(nk, last_i + nk - nq + 1)) : nk;
-  const char* kb = a.k + 2 * (b * a.ks[0] + hk * a.ks[2]);
-  const char* vb = a.v + 2 * (b * a.vs[0] + hk * a.vs[2]);
+  __shared__ __attribute__((aligned(16))) char lds[4 * kTile<KS>];
+  lds_char* const tiles = (lds_char*)lds;
+  const Place w(a, 128);
+  const int l = threadIdx.x % 64, half = l / 32, row = w.tile * 128 + (threadIdx.x / 64) * 32 + l % 32;
+  const int i = row / a.share, hq = w.hk * a.share + row % a.share;
+  const int b = w.b, hk = w.hk, nq = w.nq, nk = w.nk, rows = w.rows;
+  const int sees = w.sees(a, i), most = w.most(a, 128);
+  const Rows kr{a.k + 2 * (b * a.ks[0] + hk * a.ks[2]), 2 * a.ks[1], 0, 1, nk, 0};
+  const Rows vr{a.v + 2 * (b * a.vs[0] + hk * a.vs[2]), 2 * a.vs[1], 0, 1, nk, 0};
 
   s16x8 q[KS], g[KS];
   float delta = 0.0f, lse = kInf, norm = 0.0f;
@@ -363,9 +521,9 @@ __global__ __launch_bounds__(256, 2) void k_attn_dq(AttnArgs a) {
     typedef T Tx8 __attribute__((ext_vector_type(8)));
 #pragma unroll
     for (int s = 0; s < KS; ++s) {
-      q[s] = load8(p, 2 * s + half, a.D, i < nq);
-      g[s] = load8(d, 2 * s + half, a.D, i < nq);
-      const Tx8 x = __builtin_bit_cast(Tx8, g[s]), y = __builtin_bit_cast(Tx8, load8(o, 2 * s + half, a.D, i < nq));
+      q[s] = load8<DIRECT>(p, 2 * s + half, a.D, i < nq);
+      g[s] = load8<DIRECT>(d, 2 * s + half, a.D, i < nq);
+      const Tx8 x = __builtin_bit_cast(Tx8, g[s]), y = __builtin_bit_cast(Tx8, load8<DIRECT>(o, 2 * s + half, a.D, i < nq));
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
         delta = __builtin_fmaf((float)x[e], (float)y[e], delta);
@@ -389,27 +547,30 @@ __global__ __launch_bounds__(256, 2) void k_attn_dq(AttnArgs a) {
     float top = norm;
 #pragma unroll
     for (int d = 32; d; d >>= 1) top = fmaxf(top, __shfl_xor(top, d));
-    if (l == 0) a.gmax[(((int64_t)b * a.Hk + hk) * tiles + tile) * 4 + threadIdx.x / 64] = top;
+    if (l == 0) a.gmax[(((int64_t)b * a.Hk + hk) * w.tiles + w.tile) * 4 + threadIdx.x / 64] = top;
   }
   f32x16 o[DB] = {};
   float left = 0.0f;
-  Staged<KS> nextK, nextV;
+  const Reader<KS> rd;
+  Loader<KS, DIRECT> lk, lv;
+  lk.init(kr, a.D), lv.init(vr, a.D);
   // The score gradients of a row add up to 0: what their sum leaves over is delta's error, the
   // rounding of `out`.  The other kernel gets the corrected delta.  Here it matters where few
   // keys share a row, and there (one tile) a first pass finds it.
   for (int pass = most > 64; pass < 2; ++pass) {
     left = 0.0f;
     if (most > 0) {
-      fetch(nextK, kb, 2 * a.ks[1], 0, nk, a.D);
-      fetch(nextV, vb, 2 * a.vs[1], 0, nk, a.D);
+      lk.begin(tiles, kr, 0, a.D);
+      lv.begin(tiles + kTile<KS>, vr, 0, a.D);
     }
     for (int j0 = 0, buf = 0; j0 < most; j0 += 64, buf ^= 1) {
-      put<KS, CH>(sK[buf], nextK);
-      put<KS, CH>(sV[buf], nextV);
+      lds_char *tk = tiles + 2 * buf * kTile<KS>, *tv = tk + kTile<KS>;
+      lk.end(tk), lv.end(tv);
       __syncthreads();
       if (j0 + 64 < most) {
-        fetch(nextK, kb, 2 * a.ks[1], j0 + 64, nk, a.D);
-        fetch(nextV, vb, 2 * a.vs[1], j0 + 64, nk, a.D);
+        lds_char* to = tiles + 2 * (buf ^ 1) * kTile<KS>;
+        lk.begin(to, kr, j0 + 64, a.D);
+        lv.begin(to + kTile<KS>, vr, j0 + 64, a.D);
       }
       const bool whole = __all(j0 + 64 <= sees);
       const float shift = delta * up;
@@ -417,9 +578,9 @@ __global__ __launch_bounds__(256, 2) void k_attn_dq(AttnArgs a) {
       for (int u = 0; u < 2; ++u) {
         f32x16 x = {}, dp = {};
 #pragma unroll
-        for (int s = 0; s < KS; ++s) x = mma<T>(read_rows<CH>(sK[buf], 32 * u, s), q[s], x);
+        for (int s = 0; s < KS; ++s) x = mma<T>(rd.rows(tk, 32 * u, s), q[s], x);
 #pragma unroll
-        for (int s = 0; s < KS; ++s) dp = mma<T>(read_rows<CH>(sV[buf], 32 * u, s), g[s], dp);
+        for (int s = 0; s < KS; ++s) dp = mma<T>(rd.rows(tv, 32 * u, s), g[s], dp);
 #pragma unroll
         for (int r = 0; r < 16; ++r)
           x[r] = __builtin_amdgcn_exp2f(__builtin_fmaf(x[r], a.c, -lse)) * __builtin_fmaf(dp[r], up, -shift);
@@ -435,7 +596,7 @@ __global__ __launch_bounds__(256, 2) void k_attn_dq(AttnArgs a) {
         for (int t = 0; t < 2; ++t) {
           const s16x8 ds = round8<T>(x, t);
 #pragma unroll
-          for (int d = 0; d < DB; ++d) o[d] = mma<T>(read_cols<CH>(sK[buf], 32 * u + 16 * t, 32 * d), ds, o[d]);
+          for (int d = 0; d < DB; ++d) o[d] = mma<T>(rd.cols(tk, 32 * u + 16 * t, d), ds, o[d]);
         }
       }
     }
@@ -443,7 +604,10 @@ __global__ __launch_bounds__(256, 2) void k_attn_dq(AttnArgs a) {
     delta = __builtin_fmaf(left, down, delta);
     __syncthreads();   // the next pass begins with the first buffer again
   }
-  if (row < rows && half == 0) a.delta[((int64_t)b * a.Hq + hq) * a.Lq + i] = delta;
+  if (row < rows && half == 0) {
+    const int64_t at = ((int64_t)b * a.Hk + hk) * rows + row;
+    a.delta[at] = delta, a.level[at] = lse - kUp<T>;
+  }
   if (row >= rows) return;
   char* out = a.dq + 2 * (b * a.dqs[0] + i * a.dqs[1] + hq * a.dqs[2]);
 #pragma unroll
@@ -451,7 +615,7 @@ __global__ __launch_bounds__(256, 2) void k_attn_dq(AttnArgs a) {
 #pragma unroll
     for (int r = 0; r < 16; r += 4) {
       const int at = 32 * d + 8 * (r / 4) + 4 * half;
-      if (at < a.D) store4<T>(out, at, a.D, o[d], r, a.scale * down);
+      if (at < a.D) store4<T, DIRECT>(out, at, a.D, o[d], r, a.scale * down);
     }
 }
 
@@ -460,15 +624,16 @@ __global__ __launch_bounds__(256, 2) void k_attn_dq(AttnArgs a) {
 // A workgroup takes 128 keys of one (sample, key head), 32 a wave, and walks the rows in tiles
 // of 64: x = Q K^T (lane: one key, 16 rows), dv^T += dout^T p, dk^T += Q^T ds.  No sums are
 // shared between workgroups, so there is nothing to add atomically.
-template <typename T, int KS>
+template <typename T, int KS, bool DIRECT>
 __global__ __launch_bounds__(256, 2) void k_attn_dkv(AttnArgs a) {
-  constexpr int CH = kChunks<KS>, DB = (KS + 1) / 2;
-  __shared__ __attribute__((aligned(16))) short sQ[2][64 * CH * 8], sG[2][64 * CH * 8];
-  __shared__ __attribute__((aligned(16))) float sLse[2][64], sDelta[2][64];
-  const int tiles = (a.Lk + 127) / 128;
-  int id = blockIdx.x;
-  const int tile = id % tiles;   // the keys that most rows see first
-  id /= tiles;
+  constexpr int DB = (KS + 1) / 2;
+  __shared__ __attribute__((aligned(16))) char lds[4 * kTile<KS>];
+  lds_char* const buffers = (lds_char*)lds;
+  __shared__ __attribute__((aligned(16))) float sRow[2][2][64];   // level, delta
+  const int heads = a.Hk * a.B;
+  int id = blockIdx.x / heads;
+  const int part = id % a.parts, tile = id / a.parts;   // the keys that most rows see first
+  id = dealt(blockIdx.x % heads, heads);
   const int hk = id % a.Hk, b = id / a.Hk;
   const int nq = length(a.len_q, b, a.Lq), nk = length(a.len_k, b, a.Lk);
   const int l = threadIdx.x % 64, half = l / 32, key0 = tile * 128 + (threadIdx.x / 64) * 32;
@@ -476,17 +641,22 @@ __global__ __launch_bounds__(256, 2) void k_attn_dkv(AttnArgs a) {
   const int rows = nq * a.share;
   // the first row that sees key j
   auto first_of = [&](int j) { return a.causal ? max(0, j - (nk - nq)) * a.share : 0; };
-  const int first = first_of(key), begin = tile * 128 < nk ? first_of(tile * 128) / 64 * 64 : rows;
-  const char* qb = a.q + 2 * (b * a.qs[0] + (int64_t)hk * a.share * a.qs[2]);
-  const char* gb = a.dout + 2 * (b * a.dos[0] + (int64_t)hk * a.share * a.dos[2]);
-  const int64_t lse0 = ((int64_t)b * a.Hq + hk * a.share) * a.Lq;
+  const int first = first_of(key);
+  // the rows that see a key of the tile, in `parts` runs of whole tiles
+  int begin = tile * 128 < nk ? min(first_of(tile * 128) / 64 * 64, rows) : rows;
+  const int run = ((rows - begin + 63) / 64 + a.parts - 1) / a.parts * 64;
+  begin = min((int64_t)begin + (int64_t)part * run, (int64_t)rows);
+  const int end = min((int64_t)begin + run, (int64_t)rows);
+  const Rows qr{a.q + 2 * (b * a.qs[0] + (int64_t)hk * a.share * a.qs[2]), 2 * a.qs[1], 2 * a.qs[2], a.share, rows, a.magic};
+  const Rows gr{a.dout + 2 * (b * a.dos[0] + (int64_t)hk * a.share * a.dos[2]), 2 * a.dos[1], 2 * a.dos[2], a.share, rows, a.magic};
+  const int64_t row0 = ((int64_t)b * a.Hk + hk) * a.Lq * a.share;
 
   s16x8 k[KS], v[KS];
 #pragma unroll
   for (int s = 0; s < KS; ++s) {
     const int64_t j = key < nk ? key : 0;
-    k[s] = load8(a.k + 2 * (b * a.ks[0] + j * a.ks[1] + hk * a.ks[2]), 2 * s + half, a.D, key < nk);
-    v[s] = load8(a.v + 2 * (b * a.vs[0] + j * a.vs[1] + hk * a.vs[2]), 2 * s + half, a.D, key < nk);
+    k[s] = load8<DIRECT>(a.k + 2 * (b * a.ks[0] + j * a.ks[1] + hk * a.ks[2]), 2 * s + half, a.D, key < nk);
+    v[s] = load8<DIRECT>(a.v + 2 * (b * a.vs[0] + j * a.vs[1] + hk * a.vs[2]), 2 * s + half, a.D, key < nk);
   }
   f32x16 dk[DB] = {}, dv[DB] = {};
 
@@ -497,38 +667,37 @@ __global__ __launch_bounds__(256, 2) void k_attn_dkv(AttnArgs a) {
                              max_of(a.vmax + ((int64_t)b * a.Hk + hk) * parts, (nk + 255) / 256));
     up = __builtin_ldexpf(1.0f, lift - (int)kUp<T>), down = __builtin_ldexpf(1.0f, -lift);
   }
-  Staged<KS> nextQ, nextG;
-  float nextL = kInf, nextD = 0.0f;
-  auto fetch_all = [&](int r0) {
-    fetch_group(nextQ, qb, 2 * a.qs[1], 2 * a.qs[2], a.share, r0, rows, a.D);
-    fetch_group(nextG, gb, 2 * a.dos[1], 2 * a.dos[2], a.share, r0, rows, a.D);
-    const int r = r0 + threadIdx.x;
-    if (threadIdx.x < 64) {
-      nextL = kInf, nextD = 0.0f;
-      if (r < rows) {
-        const int x = r / a.share;
-        const int64_t at = lse0 + (int64_t)(r - x * a.share) * a.Lq + x;
-        nextL = a.lse[at] * kLog2e - kUp<T>, nextD = a.delta[at] * up;
-        if (nextL == -kInf) nextL = kInf;
-      }
+  const Reader<KS> rd;
+  Loader<KS, DIRECT, true> lq, lg;
+  lq.init(qr, a.D), lg.init(gr, a.D);
+  auto begin_all = [&](int buf, int r0) {
+    lds_char* to = buffers + 2 * buf * kTile<KS>;
+    lq.begin(to, qr, r0, a.D);
+    lg.begin(to + kTile<KS>, gr, r0, a.D);
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
+    if (wave < 2) {   // zeros beyond the last row: nothing comes of them, q and dout being zero there
+      __amdgpu_buffer_rsrc_t from = __builtin_amdgcn_make_buffer_rsrc(
+          (void*)((wave ? a.delta : a.level) + row0 + r0), 0, 4 * min(rows - r0, 64), 0x00020000);
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(from, (__attribute__((address_space(3))) void*)(lds_char*)&sRow[buf][wave][0], 4,
+                                               4 * l, 0, 0, 0);
     }
   };
-  if (begin < rows) fetch_all(begin);
-  for (int r0 = begin, buf = 0; r0 < rows; r0 += 64, buf ^= 1) {
-    put<KS, CH>(sQ[buf], nextQ);
-    put<KS, CH>(sG[buf], nextG);
-    if (threadIdx.x < 64) sLse[buf][threadIdx.x] = nextL, sDelta[buf][threadIdx.x] = nextD;
+  if (begin < end) begin_all(0, begin);
+  for (int r0 = begin, buf = 0; r0 < end; r0 += 64, buf ^= 1) {
+    lds_char *tq = buffers + 2 * buf * kTile<KS>, *tg = tq + kTile<KS>;
+    lq.end(tq), lg.end(tg);
+    if constexpr (!DIRECT) __builtin_amdgcn_s_waitcnt(0x0f70);   // sRow
     __syncthreads();
-    if (r0 + 64 < rows) fetch_all(r0 + 64);
+    if (r0 + 64 < end) begin_all(buf ^ 1, r0 + 64);
     const bool whole = __all(r0 >= first);
-#pragma unroll
-    for (int u = 0; u < 2; ++u) {
+#pragma unroll 1
+    for (int u = 0; u < 2; ++u, tq += Reader<KS>::down(32), tg += Reader<KS>::down(32)) {
       f32x16 x = {}, dp = {};
 #pragma unroll
-      for (int s = 0; s < KS; ++s) x = mma<T>(read_rows<CH>(sQ[buf], 32 * u, s), k[s], x);
+      for (int s = 0; s < KS; ++s) x = mma<T>(rd.rows(tq, 0, s), k[s], x);
 #pragma unroll
       for (int r = 0; r < 16; r += 4) {
-        const f32x4 lse = *(const f32x4*)&sLse[buf][32 * u + 2 * r + 4 * half];
+        const f32x4 lse = *(const f32x4*)&sRow[buf][0][32 * u + 2 * r + 4 * half];
 #pragma unroll
         for (int e = 0; e < 4; ++e) x[r + e] = __builtin_amdgcn_exp2f(__builtin_fmaf(x[r + e], a.c, -lse[e]));
       }
@@ -541,15 +710,15 @@ __global__ __launch_bounds__(256, 2) void k_attn_dkv(AttnArgs a) {
       for (int t = 0; t < 2; ++t) {
         const s16x8 p = round8<T>(x, t);
 #pragma unroll
-        for (int d = 0; d < DB; ++d) dv[d] = mma<T>(read_cols<CH>(sG[buf], 32 * u + 16 * t, 32 * d), p, dv[d]);
+        for (int d = 0; d < DB; ++d) dv[d] = mma<T>(rd.cols(tg, 16 * t, d), p, dv[d]);
       }
 #pragma unroll
-      for (int s = 0; s < KS; ++s) dp = mma<T>(read_rows<CH>(sG[buf], 32 * u, s), v[s], dp);
+      for (int s = 0; s < KS; ++s) dp = mma<T>(rd.rows(tg, 0, s), v[s], dp);
 #pragma unroll
       for (int r = 0; r < 16; r += 4) {
-        const f32x4 delta = *(const f32x4*)&sDelta[buf][32 * u + 2 * r + 4 * half];
+        const f32x4 delta = *(const f32x4*)&sRow[buf][1][32 * u + 2 * r + 4 * half];
 #pragma unroll
-        for (int e = 0; e < 4; ++e) x[r + e] *= __builtin_fmaf(dp[r + e], up, -delta[e]);
+        for (int e = 0; e < 4; ++e) x[r + e] *= __is_same(T, f16) ? (dp[r + e] - delta[e]) * up : dp[r + e] - delta[e];
       }
       if (!whole) {
 #pragma unroll
@@ -560,28 +729,68 @@ __global__ __launch_bounds__(256, 2) void k_attn_dkv(AttnArgs a) {
       for (int t = 0; t < 2; ++t) {
         const s16x8 ds = round8<T>(x, t);
 #pragma unroll
-        for (int d = 0; d < DB; ++d) dk[d] = mma<T>(read_cols<CH>(sQ[buf], 32 * u + 16 * t, 32 * d), ds, dk[d]);
+        for (int d = 0; d < DB; ++d) dk[d] = mma<T>(rd.cols(tq, 16 * t, d), ds, dk[d]);
       }
     }
   }
   if (key >= a.Lk) return;
-  char* ok = a.dk + 2 * (b * a.dks[0] + key * a.dks[1] + hk * a.dks[2]);
-  char* ov = a.dv + 2 * (b * a.dvs[0] + key * a.dvs[1] + hk * a.dvs[2]);
+  const float fk = a.scale * down, fv = kUp<T> == 0.0f ? 1.0f : 1.0f / 256.0f;
 #pragma unroll
   for (int d = 0; d < DB; ++d)
 #pragma unroll
     for (int r = 0; r < 16; ++r)
       if (key >= nk) dk[d][r] = dv[d][r] = 0.0f;
+  if (a.parts == 1) {
+    char* ok = a.dk + 2 * (b * a.dks[0] + key * a.dks[1] + hk * a.dks[2]);
+    char* ov = a.dv + 2 * (b * a.dvs[0] + key * a.dvs[1] + hk * a.dvs[2]);
 #pragma unroll
-  for (int d = 0; d < DB; ++d)
+    for (int d = 0; d < DB; ++d)
 #pragma unroll
-    for (int r = 0; r < 16; r += 4) {
-      const int at = 32 * d + 8 * (r / 4) + 4 * half;
-      if (at < a.D) {
-        store4<T>(ok, at, a.D, dk[d], r, a.scale * down);
-        store4<T>(ov, at, a.D, dv[d], r, kUp<T> == 0.0f ? 1.0f : 1.0f / 256.0f);
+      for (int r = 0; r < 16; r += 4) {
+        const int at = 32 * d + 8 * (r / 4) + 4 * half;
+        if (at < a.D) {
+          store4<T, DIRECT>(ok, at, a.D, dk[d], r, fk);
+          store4<T, DIRECT>(ov, at, a.D, dv[d], r, fv);
+        }
       }
-    }
+  } else {
+    const int64_t all = (int64_t)heads * a.Lk * a.D4;
+    float* o = a.partial + part * 2 * all + (((int64_t)b * a.Hk + hk) * a.Lk + key) * a.D4;
+#pragma unroll
+    for (int d = 0; d < DB; ++d)
+#pragma unroll
+      for (int r = 0; r < 16; r += 4) {
+        const int at = 32 * d + 8 * (r / 4) + 4 * half;
+        if (at < a.D4) {
+          *(f32x4*)(o + at) = f32x4{dk[d][r] * fk, dk[d][r + 1] * fk, dk[d][r + 2] * fk, dk[d][r + 3] * fk};
+          *(f32x4*)(o + all + at) = f32x4{dv[d][r] * fv, dv[d][r + 1] * fv, dv[d][r + 2] * fv, dv[d][r + 3] * fv};
+        }
+      }
+  }
+}
+
+// dk and dv from their shares, four values a thread, in the shares' order.
+template <typename T>
+__global__ __launch_bounds__(256) void k_attn_join(AttnArgs a) {
+  typedef T Tx4 __attribute__((ext_vector_type(4)));
+  const int64_t quads = (int64_t)a.B * a.Hk * a.Lk * (a.D4 / 4);
+  const int64_t n = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  if (n >= quads) return;
+  f32x4 s = {};
+  for (int k = 0; k < a.parts; ++k) s += *(const f32x4*)(a.partial + (((int64_t)k * 2 + blockIdx.y) * quads + n) * 4);
+  const int d = (int)(n % (a.D4 / 4)) * 4;
+  int64_t at = n / (a.D4 / 4);
+  const int64_t key = at % a.Lk, hk = at / a.Lk % a.Hk, b = at / a.Lk / a.Hk;
+  const int64_t* st = blockIdx.y ? a.dvs : a.dks;
+  T* o = (T*)(blockIdx.y ? a.dv : a.dk) + b * st[0] + key * st[1] + hk * st[2] + d;
+  const Tx4 y = {(T)s[0], (T)s[1], (T)s[2], (T)s[3]};
+  if (d + 4 <= a.D) {
+    __builtin_memcpy(o, &y, 8);
+  } else {
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      if (d + i < a.D) o[i] = y[i];
+  }
 }
 
 // ---- host ---------------------------------------------------------------------------------------
@@ -641,44 +850,86 @@ AttnArgs args_of(const gbmw_attention_problem* p) {
   }
   a.len_q = p->len_q, a.len_k = p->len_k;
   a.B = p->B, a.Hq = p->Hq, a.Hk = p->Hk, a.Lq = p->Lq, a.Lk = p->Lk, a.D = p->D, a.share = p->Hq / p->Hk;
+  a.D4 = (p->D + 3) / 4 * 4, a.parts = 1;
   a.causal = p->causal, a.scale = p->scale;
+  a.magic = (unsigned)(((1ull << 32) + a.share - 1) / a.share);
   // not 0: a hidden key's -inf has to stay -inf when it is scaled
   a.c = std::max(p->scale * kLog2e, 1e-30f);
   return a;
 }
 
-// delta [B][Hq][Lq], and for float16 gmax [B][Hk][tiles][4] and vmax [B][Hk][parts]
+// Shares that dk and dv are summed from: where the tiles of keys do not fill the chip a few times
+// over (under a causal mask they differ much in length), each tile's rows are dealt to several
+// workgroups, as long as each gets enough of them.
+int parts_of(const gbmw_attention_problem* p) {
+  const int64_t groups = (int64_t)p->B * p->Hk * ((p->Lk + 127) / 128), rows = (int64_t)p->Lq * (p->Hq / p->Hk);
+  int parts = 1;
+  while (parts < 16 && groups * parts < GBMW_FILL && rows / (2 * parts) >= GBMW_LEAST) parts *= 2;
+  return parts;
+}
+
+// level and delta [B][Hk][rows], and for float16 gmax [B][Hk][tiles][4] and vmax [B][Hk][parts of 256 keys]
 struct Scratch {
-  int64_t delta, gmax, vmax;   // floats
-  int64_t bytes() const { return 4 * (delta + gmax + vmax); }
+  int64_t rows, gmax, vmax, partial;   // floats
+  int parts;
+  int64_t bytes() const { return 4 * (2 * rows + gmax + vmax + partial); }
 };
 Scratch scratch_of(const gbmw_attention_problem* p) {
   const int64_t groups = (int64_t)p->B * p->Hk, rows = (int64_t)p->Lq * (p->Hq / p->Hk);
   const bool lift = p->dtype == GBMW_F16;
-  return {groups * rows, lift ? groups * ((rows + 127) / 128) * 4 : 0, lift ? groups * (((int64_t)p->Lk + 255) / 256) : 0};
+  const int parts = parts_of(p);
+  auto padded = [](int64_t n) { return (n + 3) / 4 * 4; };
+  return {padded(groups * rows), padded(lift ? groups * ((rows + 127) / 128) * 4 : 0),
+          padded(lift ? groups * (((int64_t)p->Lk + 255) / 256) : 0),
+          parts > 1 ? parts * 2 * groups * p->Lk * ((p->D + 3) / 4 * 4) : 0, parts};
 }
 
-template <typename T, int KS>
+#ifndef GBMW_NQ
+#define GBMW_NQ 1
+#endif
+template <typename T, int KS, bool DIRECT>
 void launch(const AttnArgs& a, bool backward, hipStream_t st) {
-  const int64_t rows = (int64_t)a.Lq * a.share;
-  const dim3 grid_q((unsigned)((rows + 127) / 128 * a.Hk * a.B)), grid_k((unsigned)(((int64_t)a.Lk + 127) / 128 * a.Hk * a.B));
+  const int64_t rows = (int64_t)a.Lq * a.share, groups = (int64_t)a.Hk * a.B;
+  const dim3 grid_q((unsigned)((rows + 127) / 128 * groups)), grid_k((unsigned)(((int64_t)a.Lk + 127) / 128 * groups));
   if (!backward) {
-    hipLaunchKernelGGL((k_attn_fwd<T, KS>), grid_q, dim3(256), 0, st, a);
+    constexpr int NQ = GBMW_NQ;
+    hipLaunchKernelGGL((k_attn_fwd<T, KS, NQ, DIRECT>), dim3((unsigned)((rows + 128 * NQ - 1) / (128 * NQ) * groups)),
+                       dim3(256), 0, st, a);
     return;
   }
   if constexpr (__is_same(T, f16))
-    if (a.Lk) hipLaunchKernelGGL(k_attn_vmax, dim3((unsigned)(((int64_t)a.Lk + 255) / 256 * a.Hk * a.B)), dim3(256), 0, st, a);
-  if (grid_q.x) hipLaunchKernelGGL((k_attn_dq<T, KS>), grid_q, dim3(256), 0, st, a);
-  if (grid_k.x) hipLaunchKernelGGL((k_attn_dkv<T, KS>), grid_k, dim3(256), 0, st, a);
+    if (a.Lk) hipLaunchKernelGGL(k_attn_vmax, dim3((unsigned)(((int64_t)a.Lk + 255) / 256 * groups)), dim3(256), 0, st, a);
+  if (grid_q.x) hipLaunchKernelGGL((k_attn_dq<T, KS, DIRECT>), grid_q, dim3(256), 0, st, a);
+  if (!grid_k.x) return;
+  hipLaunchKernelGGL((k_attn_dkv<T, KS, DIRECT>), dim3(grid_k.x * a.parts), dim3(256), 0, st, a);
+  if (a.parts > 1) {
+    const int64_t quads = groups * a.Lk * (a.D4 / 4);
+    hipLaunchKernelGGL(k_attn_join<T>, dim3((unsigned)((quads + 255) / 256), 2), dim3(256), 0, st, a);
+  }
+}
+
+// Whether 64 rows of an array can be loaded straight to LDS.
+bool direct(const void* ptr, const int64_t* stride, int L, int share, int D) {
+  if (L == 0) return true;
+  const int64_t row = stride[1] * 2, head = stride[2] * 2;
+  if ((uintptr_t)ptr % 16 || (stride[0] * 2) % 16 || row % 16 || head % 16) return false;
+  if (row < 2 * D) return false;   // a tile's end is told by its length in bytes
+  return 64 * row + share * head < (1ll << 31);
 }
 
 template <typename T>
 void launch(const AttnArgs& a, bool backward, hipStream_t st) {
-  if (a.D <= 32) launch<T, 2>(a, backward, st);
-  else if (a.D <= 64) launch<T, 4>(a, backward, st);
-  else if (a.D <= 80) launch<T, 5>(a, backward, st);
-  else if (a.D <= 96) launch<T, 6>(a, backward, st);
-  else launch<T, 8>(a, backward, st);
+  const bool fast = a.D % 8 == 0 && direct(a.k, a.ks, a.Lk, 1, a.D) && direct(a.v, a.vs, a.Lk, 1, a.D) &&
+                    (!backward || (direct(a.q, a.qs, a.Lq, a.share, a.D) && direct(a.dout, a.dos, a.Lq, a.share, a.D)));
+  if (!fast) {
+    if (a.D <= 64) launch<T, 4, false>(a, backward, st);
+    else launch<T, 8, false>(a, backward, st);
+  }
+  else if (a.D <= 32) launch<T, 2, true>(a, backward, st);
+  else if (a.D <= 64) launch<T, 4, true>(a, backward, st);
+  else if (a.D <= 80) launch<T, 5, true>(a, backward, st);
+  else if (a.D <= 96) launch<T, 6, true>(a, backward, st);
+  else launch<T, 8, true>(a, backward, st);
 }
 
 }  // namespace
@@ -718,7 +969,8 @@ extern "C" gbmw_status gbmw_attention_backward(const gbmw_attention_problem* p) 
   if (need && (!p->workspace || p->workspace_bytes < need || (uintptr_t)p->workspace % 16))
     return fail(GBMW_ERR_INVALID_ARG, "workspace of %lld bytes, 16-byte aligned, is needed", (long long)need);
   AttnArgs a = args_of(p);
-  a.delta = (float*)p->workspace, a.gmax = a.delta + sc.delta, a.vmax = a.gmax + sc.gmax;
+  a.level = (float*)p->workspace, a.delta = a.level + sc.rows, a.gmax = a.delta + sc.rows, a.vmax = a.gmax + sc.gmax;
+  a.partial = a.vmax + sc.vmax, a.parts = sc.parts;
   if (p->dtype == GBMW_F16) launch<f16>(a, true, (hipStream_t)p->stream);
   else launch<bf16>(a, true, (hipStream_t)p->stream);
   HIP_TRY(hipGetLastError());
