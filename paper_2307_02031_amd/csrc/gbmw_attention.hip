@@ -25,7 +25,7 @@ namespace gbmw {
 namespace {
 
 #ifndef GBMW_FILL
-#define GBMW_FILL 1536
+#define GBMW_FILL 1024
 #define GBMW_LEAST 512
 #endif
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
@@ -49,6 +49,7 @@ struct AttnArgs {
   float* partial;   // [parts][2][B][Hk][Lk][D4]: shares of dk and dv
   int B, Hq, Hk, Lq, Lk, D, share, causal;
   int parts, D4;    // D rounded up to 4
+  int near;         // heads that a die works on at a time
   unsigned magic;   // 2^32 / share, rounded up
   float c;       // scale * log2(e): probabilities are powers of two
   float scale;
@@ -279,12 +280,26 @@ __device__ __forceinline__ void store4(char* row, int d, int D, const f32x16& x,
   }
 }
 
-// Workgroups are dealt to the eight dies in turn; neighbours in `id` (tiles of one head, which
-// read the same keys) go to one die and its cache.
-__device__ __forceinline__ int dealt(int id, int n) {
-  const int per = n / 8;
-  return id < per * 8 ? (id % 8) * per + id / 8 : id;
-}
+// Which head and which of its `units` pieces of work a workgroup takes.  Workgroups are dealt to
+// the eight dies in turn.  A die works on its own heads, `near` of them at a time, so that what
+// their units read alike stays in its cache; of those the first units (the longest under a
+// causal mask) come first.  Heads that eight does not divide are dealt to all dies at the end.
+struct Deal {
+  int head, unit;
+  __device__ __forceinline__ Deal(int heads, int units, int near) {
+    const int per = heads / 8, id = blockIdx.x;
+    near = min(near, max(per, 1));
+    if (id < 8 * per * units) {
+      const int at = id / 8, first = at / (near * units) * near, n = min(near, per - first);
+      unit = (at - first * units) / n;
+      head = id % 8 * per + first + (at - first * units) % n;
+    } else {
+      const int n = heads - 8 * per, at = id - 8 * per * units;
+      unit = at / n;
+      head = 8 * per + at % n;
+    }
+  }
+};
 
 // Where a workgroup of the rows' kernels works, and how many keys a row sees.
 struct Place {
@@ -292,11 +307,9 @@ struct Place {
   __device__ __forceinline__ Place(const AttnArgs& a, int per) {
     rows = a.Lq * a.share;
     tiles = (rows + per - 1) / per;
-    int id = blockIdx.x;
-    const int heads = a.Hk * a.B;
-    tile = tiles - 1 - id / heads;   // the longest rows of a causal mask first
-    id = dealt(id % heads, heads);
-    hk = id % a.Hk, b = id / a.Hk;
+    const Deal d(a.Hk * a.B, tiles, a.near);
+    tile = tiles - 1 - d.unit;   // the longest rows of a causal mask first
+    hk = d.head % a.Hk, b = d.head / a.Hk;
     nq = length(a.len_q, b, a.Lq), nk = length(a.len_k, b, a.Lk);
   }
   __device__ __forceinline__ int sees(const AttnArgs& a, int i) const {   // keys j < sees
@@ -353,13 +366,13 @@ __global__ __launch_bounds__(256, NQ == 1 ? 2 : 1) void k_attn_fwd(AttnArgs a) {
 
   s16x8 q[NQ][KS];
   int sees[NQ];
-  int fewest = INT_MAX;
+  int fewest = INT_MAX, furthest = 0;
 #pragma unroll
   for (int n = 0; n < NQ; ++n) {
     const int row = w.tile * 128 * NQ + ((int)(threadIdx.x / 64) * NQ + n) * 32 + l % 32;
     const int i = row / a.share, hq = w.hk * a.share + row % a.share;
     sees[n] = w.sees(a, i);
-    fewest = min(fewest, sees[n]);
+    fewest = min(fewest, sees[n]), furthest = max(furthest, sees[n]);
     const char* p = a.q + 2 * (w.b * a.qs[0] + (i < w.nq ? i : 0) * a.qs[1] + hq * a.qs[2]);
 #pragma unroll
     for (int s = 0; s < KS; ++s) q[n][s] = load8<DIRECT>(p, 2 * s + half, a.D, i < w.nq);
@@ -385,6 +398,7 @@ __global__ __launch_bounds__(256, NQ == 1 ? 2 : 1) void k_attn_fwd(AttnArgs a) {
       lk.begin(to, kr, j0 + 64, a.D);
       lv.begin(to + kTile<KS>, vr, j0 + 64, a.D);
     }
+    if (!__any(j0 < furthest)) continue;   // none of the wave's rows sees this tile
     f32x16 x[NQ][2] = {};
 #pragma unroll
     for (int u = 0; u < 2; ++u)
@@ -475,15 +489,19 @@ __global__ __launch_bounds__(256) void k_attn_vmax(AttnArgs a) {
   __shared__ float tops[4];
   const int parts = (a.Lk + 255) / 256, part = blockIdx.x % parts;
   const int hk = blockIdx.x / parts % a.Hk, b = blockIdx.x / parts / a.Hk;
-  const int key = part * 256 + threadIdx.x;
+  // sixteen lanes a row, a piece each
+  const int last = min(part * 256 + 256, length(a.len_k, b, a.Lk)), d = threadIdx.x % 16 * 8;
+  const f16* v = (const f16*)a.v + b * a.vs[0] + hk * a.vs[2] + d;
   float s = 0.0f;
-  if (key < length(a.len_k, b, a.Lk)) {
-    const f16* v = (const f16*)a.v + b * a.vs[0] + key * a.vs[1] + hk * a.vs[2];
-    for (int d = 0; d < a.D; d += 8) {
-      const Pack<f16> x = load_pack(v + d, a.D - d);
+#pragma unroll 4
+  for (int key = part * 256 + threadIdx.x / 16; key < last; key += 16) {
+    const Pack<f16> x = load_pack(v + key * a.vs[1], a.D - d);
+    float n = 0.0f;
 #pragma unroll
-      for (int e = 0; e < 8; ++e) s = __builtin_fmaf((float)x.v[e], (float)x.v[e], s);
-    }
+    for (int e = 0; e < 8; ++e) n = __builtin_fmaf((float)x.v[e], (float)x.v[e], n);
+#pragma unroll
+    for (int i = 8; i; i >>= 1) n += __shfl_xor(n, i);
+    s = fmaxf(s, n);
   }
 #pragma unroll
   for (int d = 32; d; d >>= 1) s = fmaxf(s, __shfl_xor(s, d));
@@ -572,6 +590,7 @@ __global__ __launch_bounds__(256, 2) void k_attn_dq(AttnArgs a) {
         lk.begin(to, kr, j0 + 64, a.D);
         lv.begin(to + kTile<KS>, vr, j0 + 64, a.D);
       }
+      if (!__any(j0 < sees)) continue;
       const bool whole = __all(j0 + 64 <= sees);
       const float shift = delta * up;
 #pragma unroll
@@ -631,10 +650,9 @@ __global__ __launch_bounds__(256, 2) void k_attn_dkv(AttnArgs a) {
   lds_char* const buffers = (lds_char*)lds;
   __shared__ __attribute__((aligned(16))) float sRow[2][2][64];   // level, delta
   const int heads = a.Hk * a.B;
-  int id = blockIdx.x / heads;
-  const int part = id % a.parts, tile = id / a.parts;   // the keys that most rows see first
-  id = dealt(blockIdx.x % heads, heads);
-  const int hk = id % a.Hk, b = id / a.Hk;
+  const Deal deal(heads, (a.Lk + 127) / 128 * a.parts, a.near);
+  const int part = deal.unit % a.parts, tile = deal.unit / a.parts;   // the keys that most rows see first
+  const int hk = deal.head % a.Hk, b = deal.head / a.Hk;
   const int nq = length(a.len_q, b, a.Lq), nk = length(a.len_k, b, a.Lk);
   const int l = threadIdx.x % 64, half = l / 32, key0 = tile * 128 + (threadIdx.x / 64) * 32;
   const int key = key0 + l % 32;
@@ -689,6 +707,7 @@ __global__ __launch_bounds__(256, 2) void k_attn_dkv(AttnArgs a) {
     if constexpr (!DIRECT) __builtin_amdgcn_s_waitcnt(0x0f70);   // sRow
     __syncthreads();
     if (r0 + 64 < end) begin_all(buf ^ 1, r0 + 64);
+    if (!__any(r0 + 64 > first)) continue;   // none of these rows sees a key of the wave
     const bool whole = __all(r0 >= first);
 #pragma unroll 1
     for (int u = 0; u < 2; ++u, tq += Reader<KS>::down(32), tg += Reader<KS>::down(32)) {
@@ -853,6 +872,10 @@ AttnArgs args_of(const gbmw_attention_problem* p) {
   a.D4 = (p->D + 3) / 4 * 4, a.parts = 1;
   a.causal = p->causal, a.scale = p->scale;
   a.magic = (unsigned)(((1ull << 32) + a.share - 1) / a.share);
+  // Without a causal mask units are alike, and four heads at a time (keys and values of a few MB)
+  // suit a die's cache: 5 x 32 heads x 2048 x 128 forward 377 us, all at a time 384.  With one the
+  // order of their lengths counts more: 2 x 40 heads, all at a time 113 us, four 125; backward 411, 456.
+  a.near = p->causal ? INT_MAX : 4;
   // not 0: a hidden key's -inf has to stay -inf when it is scaled
   a.c = std::max(p->scale * kLog2e, 1e-30f);
   return a;
