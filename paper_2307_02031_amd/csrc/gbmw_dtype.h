@@ -44,11 +44,34 @@ __device__ __forceinline__ void store_pack(T* p, const Pack<T>& r, int n) {
   }
 }
 
-template <typename V>
-__device__ __forceinline__ V wave_sum(V x) {   // the same bits in every lane
+__device__ __forceinline__ double wave_sum(double x) {   // the same bits in every lane
 #pragma unroll
   for (int d = 32; d; d >>= 1) x += __shfl_xor(x, d);
   return x;
+}
+
+// x of this lane and of the lane across: halves of 32 (or 16 of each 32) exchanged between two copies
+__device__ __forceinline__ float sum_across32(float x) {
+  const unsigned u = __builtin_bit_cast(unsigned, x);
+  const auto r = __builtin_amdgcn_permlane32_swap(u, u, false, false);
+  return __builtin_bit_cast(float, (unsigned)r[0]) + __builtin_bit_cast(float, (unsigned)r[1]);
+}
+__device__ __forceinline__ float sum_across16(float x) {
+  const unsigned u = __builtin_bit_cast(unsigned, x);
+  const auto r = __builtin_amdgcn_permlane16_swap(u, u, false, false);
+  return __builtin_bit_cast(float, (unsigned)r[0]) + __builtin_bit_cast(float, (unsigned)r[1]);
+}
+template <int CTRL>
+__device__ __forceinline__ float sum_dpp(float x) {
+  const int y = __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, x), CTRL, 0xf, 0xf, true);
+  return x + __builtin_bit_cast(float, y);
+}
+__device__ __forceinline__ float wave_sum(float x) {   // the same bits in every lane
+  x = sum_dpp<0xB1>(x);    // lane ^ 1
+  x = sum_dpp<0x4E>(x);    // lane ^ 2
+  x = sum_dpp<0x141>(x);   // the other half of eight
+  x = sum_dpp<0x140>(x);   // the other half of sixteen
+  return sum_across32(sum_across16(x));
 }
 
 }  // namespace gbmw

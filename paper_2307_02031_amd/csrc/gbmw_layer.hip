@@ -20,6 +20,10 @@ namespace {
 // ... (NJ of them), so the row is read once: the mean first, then the sum of the squared
 // distances from it, which does not cancel where the mean is large.
 //
+// Where the row is no whole number of pieces, its last piece starts early enough to be whole:
+// it shares its first columns with the piece before it, which count there (Span::from).
+// Every load is then one unconditional instruction, and all of a row's are in flight at once.
+//
 // Bound by HBM; one pass over x (and dy) is its floor.
 
 struct NormArgs {
@@ -27,6 +31,7 @@ struct NormArgs {
   int cols;
   float eps;
   const void *x, *dy, *w, *b;
+  bool wide;       // weight and bias are fp32, whatever x is
   void *y, *dx;
   int64_t xs, ys, dys, dxs;
   float *mean, *rstd;
@@ -34,14 +39,13 @@ struct NormArgs {
 };
 
 // Sums of N values over the NT threads of a row.  `scratch`: N * (NT / 64) floats of the
-// row's own.  Every thread of the workgroup calls it.
+// row's own, others than at the last call.  Every thread of the workgroup calls it.
 template <int NT, int N>
 __device__ __forceinline__ void row_sum(float (&s)[N], float* scratch) {
 #pragma unroll
   for (int i = 0; i < N; ++i) s[i] = wave_sum(s[i]);
   if constexpr (NT > 64) {
     const int t = threadIdx.x % NT;
-    __syncthreads();   // the last call's values are read
     if (t % 64 == 0)
 #pragma unroll
       for (int i = 0; i < N; ++i) scratch[i * (NT / 64) + t / 64] = s[i];
@@ -55,108 +59,186 @@ __device__ __forceinline__ void row_sum(float (&s)[N], float* scratch) {
   }
 }
 
-template <typename T, typename W, int NT, int NJ>
-__global__ __launch_bounds__(NT < 256 ? 256 : NT) void k_norm_fwd(NormArgs a) {
-  constexpr int V = kVec<T>, G = (NT < 256 ? 256 : NT) / NT;
-  __shared__ float scratch[G][NT / 64];
-  const int t = threadIdx.x % NT, g = threadIdx.x / NT;
-  const int64_t row = (int64_t)blockIdx.x * G + g;
-  const bool live = row < a.rows;
-  const T* x = (const T*)a.x + (live ? row : 0) * a.xs;
-  Pack<T> px[NJ];
-  float s[1] = {0.0f};
+// V elements of a row from column c on, of which those before column `from` are another piece's.
+// Rows of fewer than V columns have one piece, of n columns.
+template <int V, bool WHOLE>
+struct Span {
+  int c, from, n, row;
+  Span() = default;
+  __device__ __forceinline__ Span(int piece, int cols) : row(cols) {
+    from = piece * V;
+    const bool there = from < cols;
+    c = there ? (WHOLE ? from : max(0, min(from, cols - V))) : 0;
+    n = there ? min(V, cols) : 0;
+  }
+  __device__ __forceinline__ bool has(int i) const { return WHOLE ? n > 0 : c + i >= from && i < n; }
+  template <typename W>
+  __device__ __forceinline__ void load(float (&x)[V], const W* row) const {   // what it does not have may be anything
+    if (WHOLE || this->row >= V) {
+      Pack<W> r[V / kVec<W>];
+      __builtin_memcpy(r, row + c, V * sizeof(W));
 #pragma unroll
-  for (int j = 0; j < NJ; ++j) px[j] = load_pack(x + (t + j * NT) * V, live ? a.cols - (t + j * NT) * V : 0);
+      for (int i = 0; i < V; ++i) x[i] = (float)r[i / kVec<W>].v[i % kVec<W>];
+    } else {
 #pragma unroll
-  for (int j = 0; j < NJ; ++j)
-#pragma unroll
-    for (int i = 0; i < V; ++i) s[0] += (float)px[j].v[i];
-  row_sum<NT>(s, scratch[g]);
-  const float mean = s[0] / (float)a.cols;
-  s[0] = 0.0f;
-#pragma unroll
-  for (int j = 0; j < NJ; ++j)
-#pragma unroll
-    for (int i = 0; i < V; ++i) {
-      const float d = (t + j * NT) * V + i < a.cols ? (float)px[j].v[i] - mean : 0.0f;
-      s[0] = __builtin_fmaf(d, d, s[0]);
+      for (int i = 0; i < V; ++i) x[i] = i < n ? (float)row[i] : 0.0f;
     }
-  row_sum<NT>(s, scratch[g]);
-  const float rstd = 1.0f / __builtin_sqrtf(s[0] / (float)a.cols + a.eps);
-  if (!live) return;
-  if (t == 0) a.mean[row] = mean, a.rstd[row] = rstd;
-  T* y = (T*)a.y + row * a.ys;
-  const W *w = (const W*)a.w, *b = (const W*)a.b;
+  }
+  template <typename T>
+  __device__ __forceinline__ void store(T* row, const float (&y)[V]) const {
+    Pack<T> r;
+    static_assert(V == kVec<T>, "");
+#pragma unroll
+    for (int i = 0; i < V; ++i) r.v[i] = (T)y[i];
+    if (n == V) __builtin_memcpy(row + c, &r, 16);   // shared columns are written twice, the same
+    else store_pack(row, r, n);
+  }
+};
+
+// The raw bytes of a thread's pieces: loaded early, looked at late.
+template <typename T, int NJ, bool WHOLE>
+struct Held {
+  Pack<T> p[NJ];
+  template <typename S>
+  __device__ __forceinline__ void load(const S (&span)[NJ], const T* row, int cols) {
+#pragma unroll
+    for (int j = 0; j < NJ; ++j) {
+      if (WHOLE || cols >= kVec<T>) __builtin_memcpy(&p[j], row + span[j].c, 16);
+      else p[j] = load_pack(row, span[j].n);
+    }
+  }
+};
+
+constexpr int kNormFwdThreads = 256, kNormBwdThreads = 512;
+
+// Workgroups of G rows at a time, rows blockIdx.x * G + g, then gridDim.x * G further on: a thread
+// reads its columns of weight and bias once, and the next row is on its way while one is worked on
+// (not with 1024 threads, which have half the registers).
+template <typename T, int NT, int NJ, bool WHOLE>
+__global__ __launch_bounds__(NT < kNormFwdThreads ? kNormFwdThreads : NT) void k_norm_fwd(NormArgs a) {
+  constexpr int V = kVec<T>, G = (NT < kNormFwdThreads ? kNormFwdThreads : NT) / NT;
+  constexpr bool kAhead = NT < 1024;
+  __shared__ float scratch[2][G][NT / 64];
+  const int t = threadIdx.x % NT, g = threadIdx.x / NT;
+  Span<V, WHOLE> span[NJ];
+#pragma unroll
+  for (int j = 0; j < NJ; ++j) span[j] = Span<V, WHOLE>(t + j * NT, a.cols);
+  Held<T, NJ, WHOLE> x, next;
+  auto fetch = [&](int64_t row) { next.load(span, (const T*)a.x + (row < a.rows ? row : 0) * a.xs, a.cols); };
+  const int64_t step = (int64_t)gridDim.x * G;
+  fetch((int64_t)blockIdx.x * G + g);
+  float w[NJ][V], b[NJ][V];
 #pragma unroll
   for (int j = 0; j < NJ; ++j) {
-    const int c = (t + j * NT) * V, n = a.cols - c;
-    if (n <= 0) break;
 #pragma unroll
-    for (int i = 0; i < V; ++i) {
-      const float xhat = ((float)px[j].v[i] - mean) * rstd;
-      const float wi = w && i < n ? (float)w[c + i] : 1.0f, bi = b && i < n ? (float)b[c + i] : 0.0f;
-      px[j].v[i] = (T)__builtin_fmaf(xhat, wi, bi);
+    for (int i = 0; i < V; ++i) w[j][i] = 1.0f, b[j][i] = 0.0f;
+    if (a.w) a.wide ? span[j].load(w[j], (const float*)a.w) : span[j].load(w[j], (const T*)a.w);
+    if (a.b) a.wide ? span[j].load(b[j], (const float*)a.b) : span[j].load(b[j], (const T*)a.b);
+  }
+  for (int64_t first = (int64_t)blockIdx.x * G; first < a.rows; first += step) {
+    const int64_t row = first + g;
+    x = next;
+    if constexpr (kAhead) fetch(row + step);
+    float s[1] = {0.0f};
+#pragma unroll
+    for (int j = 0; j < NJ; ++j)
+#pragma unroll
+      for (int i = 0; i < V; ++i) s[0] += span[j].has(i) ? (float)x.p[j].v[i] : 0.0f;
+    row_sum<NT>(s, scratch[0][g]);
+    const float mean = s[0] / (float)a.cols;
+    s[0] = 0.0f;
+#pragma unroll
+    for (int j = 0; j < NJ; ++j)
+#pragma unroll
+      for (int i = 0; i < V; ++i) {
+        const float d = span[j].has(i) ? (float)x.p[j].v[i] - mean : 0.0f;
+        s[0] = __builtin_fmaf(d, d, s[0]);
+      }
+    row_sum<NT>(s, scratch[1][g]);
+    const float rstd = 1.0f / __builtin_sqrtf(s[0] / (float)a.cols + a.eps);
+    if (row < a.rows) {
+      if (t == 0) a.mean[row] = mean, a.rstd[row] = rstd;
+      T* y = (T*)a.y + row * a.ys;
+#pragma unroll
+      for (int j = 0; j < NJ; ++j) {
+        if (span[j].n == 0) continue;
+        float out[V];
+#pragma unroll
+        for (int i = 0; i < V; ++i) out[i] = __builtin_fmaf(((float)x.p[j].v[i] - mean) * rstd, w[j][i], b[j][i]);
+        span[j].store(y, out);
+      }
     }
-    store_pack(y + c, px[j], n);
+    if constexpr (!kAhead) fetch(row + step);
   }
 }
 
-constexpr int kNormBwdThreads = 512;
-
-// G rows at a time per workgroup, rows blockIdx.x * G + g, then gridDim.x * G further on.  A
-// thread keeps its columns' share of dweight and dbias in registers over all its rows; the
-// workgroup's shares go to `partial` and k_norm_join adds them up in a fixed order, so the
-// result does not depend on which workgroup ends first.
-template <typename T, typename W, int NT, int NJ>
+// The same walk over the rows.  A thread keeps its columns' share of dweight and dbias in
+// registers over all its rows; the workgroup's shares go to `partial` and k_norm_join adds them
+// up in a fixed order, so the result does not depend on which workgroup ends first.  weight waits
+// in LDS: the registers are taken.
+template <typename T, int NT, int NJ, bool WHOLE>
 __global__ __launch_bounds__(NT < kNormBwdThreads ? kNormBwdThreads : NT) void k_norm_bwd(NormArgs a) {
   constexpr int V = kVec<T>, G = (NT < kNormBwdThreads ? kNormBwdThreads : NT) / NT;
-  __shared__ float scratch[G][2 * (NT / 64)];
-  extern __shared__ float joined[];   // [cols], where dweight or dbias is wanted
+  constexpr bool kAhead = NT < 1024;
+  __shared__ float scratch[2][G][2 * (NT / 64)];
+  extern __shared__ __attribute__((aligned(16))) float columns[];   // [cols] weight, then the shares
   const int t = threadIdx.x % NT, g = threadIdx.x / NT;
-  const W* w = (const W*)a.w;
+  Span<V, WHOLE> span[NJ];
+#pragma unroll
+  for (int j = 0; j < NJ; ++j) span[j] = Span<V, WHOLE>(t + j * NT, a.cols);
+  Held<T, NJ, WHOLE> x, dy, next_x, next_dy;
+  float mean, rstd, next_mean, next_rstd;
+  auto fetch = [&](int64_t row) {
+    const int64_t at = row < a.rows ? row : 0;
+    next_x.load(span, (const T*)a.x + at * a.xs, a.cols);
+    next_dy.load(span, (const T*)a.dy + at * a.dys, a.cols);
+    next_mean = a.mean[at], next_rstd = a.rstd[at];
+  };
+  const int64_t step = (int64_t)gridDim.x * G;
+  fetch((int64_t)blockIdx.x * G + g);
+  for (int c = threadIdx.x; c < a.cols; c += blockDim.x)
+    columns[c] = !a.w ? 1.0f : a.wide ? ((const float*)a.w)[c] : (float)((const T*)a.w)[c];
+  __syncthreads();
   float dw[NJ][V] = {}, db[NJ][V] = {};
-  for (int64_t first = (int64_t)blockIdx.x * G; first < a.rows; first += (int64_t)gridDim.x * G) {
+  int turn = 0;
+  for (int64_t first = (int64_t)blockIdx.x * G; first < a.rows; first += step, turn ^= 1) {
     const int64_t row = first + g;
     const bool live = row < a.rows;
-    const T *x = (const T*)a.x + (live ? row : 0) * a.xs, *dy = (const T*)a.dy + (live ? row : 0) * a.dys;
-    Pack<T> px[NJ], pg[NJ];
-#pragma unroll
-    for (int j = 0; j < NJ; ++j) {
-      const int c = (t + j * NT) * V, n = live ? a.cols - c : 0;
-      px[j] = load_pack(x + c, n);
-      pg[j] = load_pack(dy + c, n);
-    }
-    const float mean = live ? a.mean[row] : 0.0f, rstd = live ? a.rstd[row] : 0.0f;
+    x = next_x, dy = next_dy, mean = next_mean, rstd = next_rstd;
+    if constexpr (kAhead) fetch(row + step);
     float s[2] = {0.0f, 0.0f};
 #pragma unroll
     for (int j = 0; j < NJ; ++j) {
-      const int c = (t + j * NT) * V;
+      float w[V];
+      span[j].load(w, columns);
 #pragma unroll
       for (int i = 0; i < V; ++i) {
-        const bool in = c + i < a.cols;   // beyond the row dy is 0, and xhat must not be large
-        const float xhat = in ? ((float)px[j].v[i] - mean) * rstd : 0.0f, d = (float)pg[j].v[i];
-        const float wi = w && in ? (float)w[c + i] : 1.0f;
+        const bool has = live && span[j].has(i);
+        const float xhat = has ? ((float)x.p[j].v[i] - mean) * rstd : 0.0f, d = has ? (float)dy.p[j].v[i] : 0.0f;
         dw[j][i] = __builtin_fmaf(d, xhat, dw[j][i]);
         db[j][i] += d;
-        s[0] = __builtin_fmaf(d, wi, s[0]);
-        s[1] = __builtin_fmaf(d * wi, xhat, s[1]);
+        s[0] = __builtin_fmaf(d, w[i], s[0]);
+        s[1] = __builtin_fmaf(d * w[i], xhat, s[1]);
       }
     }
-    row_sum<NT>(s, scratch[g]);
+    row_sum<NT>(s, scratch[turn][g]);
     const float c1 = s[0] / (float)a.cols, c2 = s[1] / (float)a.cols;
-    T* dx = (T*)a.dx + row * a.dxs;
+    if (live) {
+      T* dx = (T*)a.dx + row * a.dxs;
 #pragma unroll
-    for (int j = 0; j < NJ; ++j) {
-      const int c = (t + j * NT) * V, n = live ? a.cols - c : 0;
-      if (n <= 0) continue;
+      for (int j = 0; j < NJ; ++j) {
+        if (span[j].n == 0) continue;
+        float w[V], out[V];
+        span[j].load(w, columns);
 #pragma unroll
-      for (int i = 0; i < V; ++i) {
-        const float xhat = ((float)px[j].v[i] - mean) * rstd;
-        const float wi = w && i < n ? (float)w[c + i] : 1.0f;
-        pg[j].v[i] = (T)(__builtin_fmaf(-xhat, c2, __builtin_fmaf((float)pg[j].v[i], wi, -c1)) * rstd);
+        for (int i = 0; i < V; ++i) {
+          const float xhat = ((float)x.p[j].v[i] - mean) * rstd;
+          out[i] = __builtin_fmaf(-xhat, c2, __builtin_fmaf((float)dy.p[j].v[i], w[i], -c1)) * rstd;
+        }
+        span[j].store(dx, out);
       }
-      store_pack(dx + c, pg[j], n);
     }
+    if constexpr (!kAhead) fetch(row + step);
   }
   if (!a.partial) return;
 #pragma unroll
@@ -168,34 +250,34 @@ __global__ __launch_bounds__(NT < kNormBwdThreads ? kNormBwdThreads : NT) void k
         for (int j = 0; j < NJ; ++j)
 #pragma unroll
           for (int i = 0; i < V; ++i) {
-            const int c = (t + j * NT) * V + i;
+            const int c = span[j].c + i;
             const float v = which ? db[j][i] : dw[j][i];
-            if (c < a.cols) joined[c] = k ? joined[c] + v : v;
+            if (span[j].has(i)) columns[c] = k ? columns[c] + v : v;
           }
     }
     __syncthreads();
     float* out = a.partial + ((int64_t)blockIdx.x * 2 + which) * a.cols;
-    for (int c = threadIdx.x; c < a.cols; c += blockDim.x) out[c] = joined[c];
+    for (int c = threadIdx.x; c < a.cols; c += blockDim.x) out[c] = columns[c];
   }
 }
 
-// dweight and dbias from `parts` shares: 64 columns a workgroup, its 16 waves every 16th share.
+// dweight and dbias from `parts` shares: 16 columns a workgroup, every 64th share a thread.
 template <typename W>
 __global__ __launch_bounds__(1024) void k_norm_join(const float* partial, int parts, int cols, W* dw, W* db) {
-  __shared__ float sums[16][64];
-  const int lane = threadIdx.x % 64, wave = threadIdx.x / 64;
-  const int c = blockIdx.x * 64 + lane;
+  __shared__ float sums[64][17];
+  const int col = threadIdx.x % 16, k0 = threadIdx.x / 16, c = blockIdx.x * 16 + col;
   W* out = blockIdx.y ? db : dw;
   if (!out) return;
   float s = 0.0f;
   if (c < cols)
-    for (int k = wave; k < parts; k += 16) s += partial[((int64_t)k * 2 + blockIdx.y) * cols + c];
-  sums[wave][lane] = s;
-  __syncthreads();
-  if (wave == 0 && c < cols) {
-    for (int k = 1; k < 16; ++k) s += sums[k][lane];
-    out[c] = (W)s;
+#pragma unroll 8
+    for (int k = k0; k < parts; k += 64) s += partial[((int64_t)k * 2 + blockIdx.y) * cols + c];
+  sums[k0][col] = s;
+  for (int n = 32; n; n /= 2) {
+    __syncthreads();
+    if (k0 < n) sums[k0][col] += sums[k0 + n][col];
   }
+  if (k0 == 0 && c < cols) out[c] = (W)sums[0][col];
 }
 
 // ---- gradient norm and clipping -----------------------------------------------------------
@@ -207,6 +289,7 @@ struct Piece {   // a run of at most kPiece elements of one tensor
 };
 constexpr int64_t kPiece = 32768;
 constexpr int kNormGroups = 2048;   // at most so many partial sums
+constexpr int kUnroll = 4;          // loads in flight of a thread
 
 struct Clip {   // device memory of a list, in front of the partial sums
   float factor;
@@ -218,20 +301,31 @@ __global__ __launch_bounds__(256) void k_clip_norm(const Piece* pieces, int coun
                                                    double max_norm, double scale, float* norm_out) {
   __shared__ double sums[4];
   __shared__ bool last;
-  constexpr int V = kVec<T>;
-  double s = 0.0;
+  constexpr int V = kVec<T>, U = kUnroll;
+  double part[V] = {};
   for (int k = blockIdx.x; k < count; k += gridDim.x) {
     const Piece pc = pieces[k];
     const T* in = (const T*)pc.in;
-    for (int i = threadIdx.x * V; i < pc.n; i += 256 * V) {
-      const Pack<T> x = load_pack(in + i, (int)pc.n - i);
+    auto add = [&](const Pack<T>& x) {
 #pragma unroll
       for (int e = 0; e < V; ++e) {
         const double d = (double)(float)x.v[e];
-        s = __builtin_fma(d, d, s);
+        part[e] = __builtin_fma(d, d, part[e]);
       }
+    };
+    int i = threadIdx.x * V;
+    for (; i + ((U - 1) * 256 + 1) * V <= pc.n; i += U * 256 * V) {
+      Pack<T> x[U];
+#pragma unroll
+      for (int u = 0; u < U; ++u) __builtin_memcpy(&x[u], in + i + u * 256 * V, 16);
+#pragma unroll
+      for (int u = 0; u < U; ++u) add(x[u]);
     }
+    for (; i < pc.n; i += 256 * V) add(load_pack(in + i, (int)pc.n - i));
   }
+  double s = 0.0;
+#pragma unroll
+  for (int e = 0; e < V; ++e) s += part[e];
   s = wave_sum(s);
   if (threadIdx.x % 64 == 0) sums[threadIdx.x / 64] = s;
   __syncthreads();
@@ -258,26 +352,34 @@ __global__ __launch_bounds__(256) void k_clip_norm(const Piece* pieces, int coun
   }
 }
 
+// The pieces last read by the norm come first: they may still be in the cache.
 template <typename T, typename O>
 __global__ __launch_bounds__(256) void k_clip_scale(const Piece* pieces, int count, const Clip* clip) {
-  constexpr int V = kVec<T>;
+  constexpr int V = kVec<T>, U = kUnroll;
   const float factor = clip->factor;
-  for (int k = blockIdx.x; k < count; k += gridDim.x) {
+  for (int k = count - 1 - (int)blockIdx.x; k >= 0; k -= gridDim.x) {
     const Piece pc = pieces[k];
     if (factor == 1.0f && pc.in == pc.out) continue;   // the values are there
     const T* in = (const T*)pc.in;
     O* out = (O*)pc.out;
-    for (int i = threadIdx.x * V; i < pc.n; i += 256 * V) {
-      const int n = (int)pc.n - i;
-      const Pack<T> x = load_pack(in + i, n);
+    auto put = [&](const Pack<T>& x, int at, int n) {
       Pack<O> y;
 #pragma unroll
       for (int h = 0; h < V; h += kVec<O>) {
 #pragma unroll
         for (int e = 0; e < kVec<O>; ++e) y.v[e] = (O)((float)x.v[h + e] * factor);
-        store_pack(out + i + h, y, n - h);
+        store_pack(out + at + h, y, n - h);
       }
+    };
+    int i = threadIdx.x * V;
+    for (; i + ((U - 1) * 256 + 1) * V <= pc.n; i += U * 256 * V) {
+      Pack<T> x[U];
+#pragma unroll
+      for (int u = 0; u < U; ++u) __builtin_memcpy(&x[u], in + i + u * 256 * V, 16);
+#pragma unroll
+      for (int u = 0; u < U; ++u) put(x[u], i + u * 256 * V, V);
     }
+    for (; i < pc.n; i += 256 * V) put(load_pack(in + i, (int)pc.n - i), i, (int)pc.n - i);
   }
 }
 
@@ -297,75 +399,78 @@ gbmw_status check_norm(const gbmw_layer_norm_problem* p) {
 }
 
 // Threads of a row and 16-byte pieces of each: few threads for short rows, so that the sums
-// stay inside a wave, and at most four pieces a thread, so that they stay in registers.
+// stay inside a wave, and few pieces a thread, so that they stay in registers (three of 16-bit
+// values in the backward pass take 220; with four it spills).
 struct Shape {
   int nt, nj;
 };
 Shape shape_of(const gbmw_layer_norm_problem* p) {
   const int vec = 16 / element_size(p->dtype), n = (p->cols + vec - 1) / vec;
-  if (n <= 4 * 64) return {64, (n + 63) / 64};
-  if (n <= 4 * 256) return {256, (n + 255) / 256};
+  if (n <= 3 * 64) return {64, (n + 63) / 64};
+  if (n <= 3 * 256) return {256, (n + 255) / 256};
   const int nj = (n + 1023) / 1024;
-  return {1024, nj <= 2 ? 2 : nj <= 4 ? 4 : 8};
+  return {1024, nj <= 2 ? nj : nj <= 4 ? 4 : 8};
 }
 
-int norm_groups(const gbmw_layer_norm_problem* p) {   // workgroups of the backward pass
+// Workgroups: enough to fill the chip, each with several rows where there are many.
+int norm_groups(const gbmw_layer_norm_problem* p, bool backward) {
   const Shape s = shape_of(p);
-  const int per = std::max(1, kNormBwdThreads / s.nt);
-  return (int)std::min<int64_t>(512, (p->rows + per - 1) / per);
+  const int per = std::max(1, (backward ? kNormBwdThreads : kNormFwdThreads) / s.nt);
+  const int most = s.nt == 1024 ? 256 : backward ? 512 : 2048;
+  return (int)std::min<int64_t>(most, (p->rows + per - 1) / per);
 }
 
-template <typename T, typename W, int NT, int NJ>
+template <typename T, int NT, int NJ, bool WHOLE>
 gbmw_status launch_norm(const NormArgs& a, bool backward, int groups, hipStream_t st) {
   if (!backward) {
-    constexpr int threads = NT < 256 ? 256 : NT;
-    const int64_t grid = (a.rows + threads / NT - 1) / (threads / NT);
-    hipLaunchKernelGGL((k_norm_fwd<T, W, NT, NJ>), dim3((unsigned)grid), dim3(threads), 0, st, a);
+    hipLaunchKernelGGL((k_norm_fwd<T, NT, NJ, WHOLE>), dim3(groups), dim3(std::max(NT, kNormFwdThreads)), 0, st, a);
   } else {
-    constexpr int threads = NT < kNormBwdThreads ? kNormBwdThreads : NT;
-    const size_t lds = a.partial ? 4 * (size_t)a.cols : 0;
+    const size_t lds = 4 * (size_t)a.cols;
     if (lds > 60 * 1024) {
-      const hipError_t e = hipFuncSetAttribute((const void*)&k_norm_bwd<T, W, NT, NJ>,
+      const hipError_t e = hipFuncSetAttribute((const void*)&k_norm_bwd<T, NT, NJ, WHOLE>,
                                                hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
       if (e != hipSuccess) {
         (void)hipGetLastError();
         return fail(GBMW_ERR_DEVICE, "%zu bytes of shared memory: %s", lds, hipGetErrorString(e));
       }
     }
-    hipLaunchKernelGGL((k_norm_bwd<T, W, NT, NJ>), dim3(groups), dim3(threads), lds, st, a);
+    hipLaunchKernelGGL((k_norm_bwd<T, NT, NJ, WHOLE>), dim3(groups), dim3(std::max(NT, kNormBwdThreads)), lds, st, a);
   }
   HIP_TRY(hipGetLastError());
   return GBMW_OK;
 }
 
-template <typename T, typename W>
+template <typename T, int NT, int NJ>
+gbmw_status launch_norm(const NormArgs& a, bool backward, int groups, hipStream_t st) {
+  return a.cols % kVec<T> ? launch_norm<T, NT, NJ, false>(a, backward, groups, st)
+                          : launch_norm<T, NT, NJ, true>(a, backward, groups, st);
+}
+
+template <typename T>
 gbmw_status launch_norm(const NormArgs& a, Shape s, bool backward, int groups, hipStream_t st) {
   if (s.nt == 64) switch (s.nj) {
-    case 1: return launch_norm<T, W, 64, 1>(a, backward, groups, st);
-    case 2: return launch_norm<T, W, 64, 2>(a, backward, groups, st);
-    case 3: return launch_norm<T, W, 64, 3>(a, backward, groups, st);
-    default: return launch_norm<T, W, 64, 4>(a, backward, groups, st);
+    case 1: return launch_norm<T, 64, 1>(a, backward, groups, st);
+    case 2: return launch_norm<T, 64, 2>(a, backward, groups, st);
+    default: return launch_norm<T, 64, 3>(a, backward, groups, st);
   }
   if (s.nt == 256) switch (s.nj) {
-    case 2: return launch_norm<T, W, 256, 2>(a, backward, groups, st);
-    case 3: return launch_norm<T, W, 256, 3>(a, backward, groups, st);
-    default: return launch_norm<T, W, 256, 4>(a, backward, groups, st);
+    case 1: return launch_norm<T, 256, 1>(a, backward, groups, st);
+    case 2: return launch_norm<T, 256, 2>(a, backward, groups, st);
+    default: return launch_norm<T, 256, 3>(a, backward, groups, st);
   }
-  if (s.nj == 2) return launch_norm<T, W, 1024, 2>(a, backward, groups, st);
-  if (s.nj == 4) return launch_norm<T, W, 1024, 4>(a, backward, groups, st);
-  if constexpr (sizeof(T) == 4) return launch_norm<T, W, 1024, 8>(a, backward, groups, st);
+  if (s.nj == 1) return launch_norm<T, 1024, 1>(a, backward, groups, st);
+  if (s.nj == 2) return launch_norm<T, 1024, 2>(a, backward, groups, st);
+  if (s.nj == 4) return launch_norm<T, 1024, 4>(a, backward, groups, st);
+  if constexpr (sizeof(T) == 4) return launch_norm<T, 1024, 8>(a, backward, groups, st);
   return fail(GBMW_ERR_UNSUPPORTED, "no kernel for %d columns", a.cols);
 }
 
 gbmw_status launch_norm(const gbmw_layer_norm_problem* p, const NormArgs& a, bool backward, int groups) {
   const Shape s = shape_of(p);
   hipStream_t st = (hipStream_t)p->stream;
-  const bool same = p->wdtype == p->dtype;
-  if (p->dtype == GBMW_F32) return launch_norm<float, float>(a, s, backward, groups, st);
-  if (p->dtype == GBMW_F16)
-    return same ? launch_norm<f16, f16>(a, s, backward, groups, st) : launch_norm<f16, float>(a, s, backward, groups, st);
-  return same ? launch_norm<bf16, bf16>(a, s, backward, groups, st)
-              : launch_norm<bf16, float>(a, s, backward, groups, st);
+  if (p->dtype == GBMW_F32) return launch_norm<float>(a, s, backward, groups, st);
+  if (p->dtype == GBMW_F16) return launch_norm<f16>(a, s, backward, groups, st);
+  return launch_norm<bf16>(a, s, backward, groups, st);
 }
 
 gbmw_status check_array(const char* name, const void* ptr, int size, int64_t stride, int64_t least) {
@@ -390,7 +495,7 @@ using namespace gbmw;
 extern "C" int64_t gbmw_layer_norm_workspace(const gbmw_layer_norm_problem* p) {
   gbmw_detail::clear_error();
   if (check_norm(p) != GBMW_OK) return -1;
-  return (int64_t)norm_groups(p) * 2 * p->cols * 4;
+  return (int64_t)norm_groups(p, true) * 2 * p->cols * 4;
 }
 
 extern "C" gbmw_status gbmw_layer_norm_forward(const gbmw_layer_norm_problem* p) {
@@ -409,9 +514,9 @@ extern "C" gbmw_status gbmw_layer_norm_forward(const gbmw_layer_norm_problem* p)
     return fail(GBMW_ERR_INVALID_ARG, "y is x, with another row stride");
   NormArgs a{};
   a.rows = p->rows, a.cols = p->cols, a.eps = p->eps;
-  a.x = p->x, a.w = p->weight, a.b = p->bias, a.y = p->y;
+  a.x = p->x, a.w = p->weight, a.b = p->bias, a.y = p->y, a.wide = p->wdtype == GBMW_F32;
   a.xs = p->x_stride, a.ys = p->y_stride, a.mean = p->mean, a.rstd = p->rstd;
-  return launch_norm(p, a, false, 0);
+  return launch_norm(p, a, false, norm_groups(p, false));
 }
 
 extern "C" gbmw_status gbmw_layer_norm_backward(const gbmw_layer_norm_problem* p) {
@@ -431,7 +536,7 @@ extern "C" gbmw_status gbmw_layer_norm_backward(const gbmw_layer_norm_problem* p
     if (p->dx == p->dy && p->dx_stride != p->dy_stride)
       return fail(GBMW_ERR_INVALID_ARG, "dx is dy, with another row stride");
   }
-  const int groups = norm_groups(p);
+  const int groups = norm_groups(p, true);
   if (wanted && p->rows > 0) {
     const int64_t need = (int64_t)groups * 2 * p->cols * 4;
     if (!p->workspace || p->workspace_bytes < need || (uintptr_t)p->workspace % 16)
@@ -440,13 +545,13 @@ extern "C" gbmw_status gbmw_layer_norm_backward(const gbmw_layer_norm_problem* p
   if (p->rows > 0) {
     NormArgs a{};
     a.rows = p->rows, a.cols = p->cols;
-    a.x = p->x, a.dy = p->dy, a.w = p->weight, a.dx = p->dx;
+    a.x = p->x, a.dy = p->dy, a.w = p->weight, a.dx = p->dx, a.wide = p->wdtype == GBMW_F32;
     a.xs = p->x_stride, a.dys = p->dy_stride, a.dxs = p->dx_stride, a.mean = p->mean, a.rstd = p->rstd;
     a.partial = wanted ? (float*)p->workspace : nullptr;
     CHECK(launch_norm(p, a, true, groups));
   }
   if (wanted) {   // without rows: zeros
-    const dim3 grid((p->cols + 63) / 64, 2);
+    const dim3 grid((p->cols + 15) / 16, 2);
     hipStream_t st = (hipStream_t)p->stream;
     const float* part = (const float*)p->workspace;
     if (p->wdtype == GBMW_F32)
