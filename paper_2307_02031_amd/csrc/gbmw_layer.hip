@@ -291,16 +291,17 @@ constexpr int64_t kPiece = 32768;
 constexpr int kNormGroups = 2048;   // at most so many partial sums
 constexpr int kUnroll = 4;          // loads in flight of a thread
 
-struct Clip {   // device memory of a list, in front of the partial sums
-  float factor;
-  unsigned arrived;
-};
+// Sum over the 256 threads of a workgroup, the same bits in each of them.
+__device__ __forceinline__ double group_sum(double s, double (&sums)[4]) {
+  s = wave_sum(s);
+  if (threadIdx.x % 64 == 0) sums[threadIdx.x / 64] = s;
+  __syncthreads();
+  return (sums[0] + sums[1]) + (sums[2] + sums[3]);
+}
 
 template <typename T>
-__global__ __launch_bounds__(256) void k_clip_norm(const Piece* pieces, int count, double* partial, Clip* clip,
-                                                   double max_norm, double scale, float* norm_out) {
+__global__ __launch_bounds__(256) void k_clip_norm(const Piece* pieces, int count, double* partial) {
   __shared__ double sums[4];
-  __shared__ bool last;
   constexpr int V = kVec<T>, U = kUnroll;
   double part[V] = {};
   for (int k = blockIdx.x; k < count; k += gridDim.x) {
@@ -326,37 +327,26 @@ __global__ __launch_bounds__(256) void k_clip_norm(const Piece* pieces, int coun
   double s = 0.0;
 #pragma unroll
   for (int e = 0; e < V; ++e) s += part[e];
-  s = wave_sum(s);
-  if (threadIdx.x % 64 == 0) sums[threadIdx.x / 64] = s;
-  __syncthreads();
-  if (threadIdx.x == 0) {
-    partial[blockIdx.x] = (sums[0] + sums[1]) + (sums[2] + sums[3]);
-    // the sum is visible to whoever sees the count
-    last = __hip_atomic_fetch_add(&clip->arrived, 1u, __ATOMIC_ACQ_REL, __HIP_MEMORY_SCOPE_AGENT) == gridDim.x - 1;
-  }
-  __syncthreads();
-  if (!last) return;
-  // the workgroup that ends last adds the partial sums, in an order of their own
-  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "agent");
-  s = 0.0;
-  for (int k = threadIdx.x; k < (int)gridDim.x; k += 256) s += partial[k];
-  s = wave_sum(s);
-  if (threadIdx.x % 64 == 0) sums[threadIdx.x / 64] = s;
-  __syncthreads();
-  if (threadIdx.x == 0) {
-    const double norm = __builtin_sqrt((sums[0] + sums[1]) + (sums[2] + sums[3])) * scale;
-    const bool clips = norm > max_norm && norm < __builtin_inf();
-    clip->factor = (float)(clips ? scale * (max_norm / norm) : scale);
-    clip->arrived = 0;   // for the next call
-    if (norm_out) *norm_out = (float)norm;
-  }
+  s = group_sum(s, sums);
+  if (threadIdx.x == 0) partial[blockIdx.x] = s;
 }
 
+// Every workgroup adds the `parts` partial sums itself, in one order: 16 KB from the cache at
+// most, and no workgroup has to wait for another or to make its sum visible to others before its
+// kernel ends (which costs each of them a pass over its die's cache).
 // The pieces last read by the norm come first: they may still be in the cache.
 template <typename T, typename O>
-__global__ __launch_bounds__(256) void k_clip_scale(const Piece* pieces, int count, const Clip* clip) {
+__global__ __launch_bounds__(256) void k_clip_scale(const Piece* pieces, int count, const double* partial, int parts,
+                                                    double max_norm, double scale, float* norm_out) {
   constexpr int V = kVec<T>, U = kUnroll;
-  const float factor = clip->factor;
+  __shared__ double sums[4];
+  double s = 0.0;
+#pragma unroll 8
+  for (int k = threadIdx.x; k < parts; k += 256) s += partial[k];
+  const double norm = __builtin_sqrt(group_sum(s, sums)) * scale;
+  const bool clips = norm > max_norm && norm < __builtin_inf();
+  const float factor = (float)(clips ? scale * (max_norm / norm) : scale);
+  if (blockIdx.x == 0 && threadIdx.x == 0 && norm_out) *norm_out = (float)norm;
   for (int k = count - 1 - (int)blockIdx.x; k >= 0; k -= gridDim.x) {
     const Piece pc = pieces[k];
     if (factor == 1.0f && pc.in == pc.out) continue;   // the values are there
@@ -569,11 +559,10 @@ extern "C" gbmw_status gbmw_layer_norm_backward(const gbmw_layer_norm_problem* p
 }
 
 struct gbmw_gradient_list {
-  gbmw_detail::DevBuf buf;   // Clip (padded to 256 bytes) | partial sums | pieces
+  gbmw_detail::DevBuf buf;   // partial sums | pieces
   int count = 0, in_dtype = 0, out_dtype = 0, device = 0;
-  Clip* clip() const { return (Clip*)buf.p; }
-  double* partial() const { return (double*)((char*)buf.p + 256); }
-  Piece* pieces() const { return (Piece*)((char*)buf.p + 256 + 8 * kNormGroups); }
+  double* partial() const { return (double*)buf.p; }
+  Piece* pieces() const { return (Piece*)((char*)buf.p + 8 * kNormGroups); }
 };
 
 extern "C" gbmw_status gbmw_gradient_list_create(int32_t n, const void* const* in, void* const* out,
@@ -606,12 +595,10 @@ extern "C" gbmw_status gbmw_gradient_list_create(int32_t n, const void* const* i
         pieces.push_back({(const char*)in[i] + at * isize, (char*)out[i] + at * osize, std::min(kPiece, numel[i] - at)});
     gbmw_gradient_list* l = new gbmw_gradient_list;
     l->count = (int)count, l->in_dtype = in_dtype, l->out_dtype = out_dtype;
-    const size_t head = 256 + 8 * kNormGroups;
+    const size_t head = 8 * kNormGroups;
     gbmw_status st = l->buf.reserve(head + sizeof(Piece) * (size_t)count);
     if (st == GBMW_OK) {
       hipError_t e = hipGetDevice(&l->device);
-      const Clip zero{1.0f, 0u};
-      if (e == hipSuccess) e = hipMemcpy(l->clip(), &zero, sizeof zero, hipMemcpyHostToDevice);
       if (e == hipSuccess && count)
         e = hipMemcpy(l->pieces(), pieces.data(), sizeof(Piece) * (size_t)count, hipMemcpyHostToDevice);
       if (e != hipSuccess) {
@@ -643,22 +630,20 @@ extern "C" gbmw_status gbmw_clip_gradients(gbmw_gradient_list* l, float max_norm
   if (dev != l->device) return fail(GBMW_ERR_INVALID_ARG, "the list is on device %d, device %d is current", l->device, dev);
   hipStream_t st = (hipStream_t)stream;
   const dim3 grid(std::max(1, std::min(l->count, kNormGroups))), block(256);
-#define NORM(T) \
-  hipLaunchKernelGGL(k_clip_norm<T>, grid, block, 0, st, l->pieces(), l->count, l->partial(), l->clip(), (double)max_norm, \
-                     (double)scale, norm)
-#define SCALE(T, O) hipLaunchKernelGGL((k_clip_scale<T, O>), grid, block, 0, st, l->pieces(), l->count, l->clip())
+#define NORM(T) hipLaunchKernelGGL(k_clip_norm<T>, grid, block, 0, st, l->pieces(), l->count, l->partial())
+#define SCALE(T, O)                                                                                              \
+  hipLaunchKernelGGL((k_clip_scale<T, O>), grid, block, 0, st, l->pieces(), l->count, l->partial(), (int)grid.x, \
+                     (double)max_norm, (double)scale, norm)
   if (l->in_dtype == GBMW_F32) NORM(float);
   else if (l->in_dtype == GBMW_F16) NORM(f16);
   else NORM(bf16);
   HIP_TRY(hipGetLastError());
-  if (l->count) {
-    if (l->in_dtype == GBMW_F32) SCALE(float, float);
-    else if (l->in_dtype == GBMW_F16 && l->out_dtype == GBMW_F16) SCALE(f16, f16);
-    else if (l->in_dtype == GBMW_F16) SCALE(f16, float);
-    else if (l->out_dtype == GBMW_BF16) SCALE(bf16, bf16);
-    else SCALE(bf16, float);
-    HIP_TRY(hipGetLastError());
-  }
+  if (l->in_dtype == GBMW_F32) SCALE(float, float);
+  else if (l->in_dtype == GBMW_F16 && l->out_dtype == GBMW_F16) SCALE(f16, f16);
+  else if (l->in_dtype == GBMW_F16) SCALE(f16, float);
+  else if (l->out_dtype == GBMW_BF16) SCALE(bf16, bf16);
+  else SCALE(bf16, float);
+  HIP_TRY(hipGetLastError());
 #undef NORM
 #undef SCALE
   return GBMW_OK;
