@@ -13,6 +13,7 @@ enqueued on ``torch.cuda.current_stream()`` unless a stream is given.
 from __future__ import annotations
 
 import ctypes as ct
+import functools
 import os
 
 import numpy as np
@@ -409,85 +410,97 @@ def _refuse(message: str):
     raise GbmwError(GBMW_ERR_INVALID_ARG, message)
 
 
-def _device_tensor(name: str, t, dtype=None, shape=None):
+_LAYER_TYPES = {**_DTYPE, torch.int32: -1}
+# the current stream's handle without an object around it, where torch has it
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", lambda device: torch.cuda.current_stream(device).cuda_stream)
+
+
+def _device_tensor(name: str, t, device: int, dtype=None, shape=None):
     """t, or an error: the kernels take plain addresses, so type and shape are checked here."""
     if not isinstance(t, torch.Tensor) or not t.is_cuda:
         _refuse(f"{name} is not a tensor on the GPU")
-    if t.device.index != torch.cuda.current_device():
-        _refuse(f"{name} is on {t.device}, device {torch.cuda.current_device()} is current")
-    if t.dtype not in _DTYPE and t.dtype != torch.int32:
-        _refuse(f"{name} has type {t.dtype}")
-    if dtype is not None and t.dtype != dtype:
-        _refuse(f"{name} has type {t.dtype}, not {dtype}")
-    if shape is not None and tuple(t.shape) != tuple(shape):
+    if t.get_device() != device:
+        _refuse(f"{name} is on {t.device}, device {device} is current")
+    if t.dtype != dtype and (dtype is not None or t.dtype not in _LAYER_TYPES):
+        _refuse(f"{name} has type {t.dtype}" + ("" if dtype is None else f", not {dtype}"))
+    if shape is not None and t.shape != shape:
         _refuse(f"{name} has shape {tuple(t.shape)}, not {tuple(shape)}")
     return t
 
 
-class _on_stream:
-    """Outputs and scratch memory that a call makes belong to the stream its kernels run on, so that the memory
-    is not handed to anybody else before they have run.  Inputs on another stream than that are the caller's to
-    keep until the stream has got to the call, as with any work on a second stream."""
-
-    def __init__(self, stream):
-        current = torch.cuda.current_stream()
-        self.handle = current.cuda_stream if stream is None else int(getattr(stream, "cuda_stream", stream))
-        other = self.handle != current.cuda_stream
-        self.guard = torch.cuda.stream(torch.cuda.ExternalStream(self.handle)) if other else None
-
-    def __enter__(self):
-        if self.guard is not None:
-            self.guard.__enter__()
-        return self.handle
-
-    def __exit__(self, *exc):
-        if self.guard is not None:
-            self.guard.__exit__(*exc)
+def _on_stream(call):
+    """Runs call(..., _at=(device, stream handle)) on the `stream` argument (a torch stream or a handle), or on the
+    current one.  Outputs and scratch memory that a call makes belong to the stream its kernels run on, so that the
+    memory is not handed to anybody else before they have run.  Inputs on another stream than that are the caller's
+    to keep until the stream has got to the call, as with any work on a second stream."""
+    @functools.wraps(call)
+    def on_stream(*args, stream=None, **kw):
+        ready = torch.cuda.is_initialized()     # without, there is no tensor on a GPU either
+        device = torch.cuda.current_device() if ready else 0
+        if stream is None:
+            return call(*args, _at=(device, _raw_stream(device) if ready else 0), **kw)
+        handle = int(getattr(stream, "cuda_stream", stream))
+        with torch.cuda.stream(torch.cuda.ExternalStream(handle)):
+            return call(*args, _at=(device, handle), **kw)
+    return on_stream
 
 
-def _workspace(p, given, need: int):
+def _workspace(p, given, need: int, device: int):
     """Sets p's workspace: the caller's uint8 tensor, or a new one.  Returns what has to live until the call is made."""
     if need < 0:
         raise GbmwError(GBMW_ERR_INVALID_ARG, gbmw_last_error())
     if given is None:
         given = torch.empty(max(16, need), dtype=torch.uint8, device="cuda")
-    elif not given.is_cuda or given.dtype != torch.uint8 or not given.is_contiguous():
-        _refuse("workspace is not a contiguous uint8 tensor on the GPU")
+    elif _device_tensor("workspace", given, device, torch.uint8) is None or not given.is_contiguous():
+        _refuse("workspace is not contiguous")
     p.workspace, p.workspace_bytes = given.data_ptr(), given.numel()
     return given
 
 
-def _attention_problem(q, k, v, causal, scale, len_q, len_k) -> gbmw_attention_problem:
-    _device_tensor("q", q)
-    if q.dim() != 4:
-        _refuse(f"q has {q.dim()} dimensions, not [B][Lq][Hq][D]")
-    B, Lq, Hq, D = q.shape
-    if not isinstance(k, torch.Tensor) or k.dim() != 4:
-        _refuse("k is not a tensor [B][Lk][Hk][D]")
-    Lk, Hk = k.shape[1], k.shape[2]
-    _device_tensor("k", k, q.dtype, (B, Lk, Hk, D))
-    _device_tensor("v", v, q.dtype, (B, Lk, Hk, D))
-    p = gbmw_attention_problem()
-    if q.dtype not in _DTYPE:
-        _refuse(f"q has type {q.dtype}")
-    p.dtype, p.B, p.Hq, p.Hk, p.Lq, p.Lk, p.D = _DTYPE[q.dtype], B, Hq, Hk, Lq, Lk, D
-    p.causal, p.scale = int(bool(causal)), (1.0 / D ** 0.5 if D else 1.0) if scale is None else float(scale)
-    for name, t in (("q", q), ("k", k), ("v", v)):
-        _set_array(p, name, t)
-    for name, t in (("len_q", len_q), ("len_k", len_k)):
-        if t is not None:
-            if not _device_tensor(name, t, torch.int32, (B,)).is_contiguous():
-                _refuse(f"{name} is not contiguous")
-            setattr(p, name, t.data_ptr())
-    return p
+_Strides = ct.c_int64 * 3
 
 
 def _set_array(p, name: str, t) -> None:
-    s = t.stride()
-    if s[3] != 1 and t.shape[3] > 1:
+    s0, s1, s2, s3 = t.stride()
+    if s3 != 1 and t.shape[3] > 1:
         _refuse(f"{name}: the values of one head are not next to each other")
     setattr(p, name, t.data_ptr())
-    setattr(p, name + "_stride", (ct.c_int64 * 3)(s[0], s[1], s[2]))
+    setattr(p, name + "_stride", _Strides(s0, s1, s2))
+
+
+def _attention_problem(q, k, v, causal, scale, len_q, len_k, at) -> gbmw_attention_problem:
+    device, stream = at
+    _device_tensor("q", q, device)
+    if q.dim() != 4:
+        _refuse(f"q has {q.dim()} dimensions, not [B][Lq][Hq][D]")
+    if not isinstance(k, torch.Tensor) or k.dim() != 4:
+        _refuse("k is not a tensor [B][Lk][Hk][D]")
+    B, Lq, Hq, D = q.shape
+    _, Lk, Hk, _ = k.shape
+    dtype = q.dtype
+    _device_tensor("k", k, device, dtype, (B, Lk, Hk, D))
+    _device_tensor("v", v, device, dtype, (B, Lk, Hk, D))
+    p = gbmw_attention_problem(_DTYPE.get(dtype, -1), B, Hq, Hk, Lq, Lk, D, 1 if causal else 0,
+                               (1.0 / D ** 0.5 if D else 1.0) if scale is None else scale)
+    p.stream = stream
+    _set_array(p, "q", q), _set_array(p, "k", k), _set_array(p, "v", v)
+    if len_q is not None:
+        p.len_q = _length("len_q", len_q, device, B)
+    if len_k is not None:
+        p.len_k = _length("len_k", len_k, device, B)
+    return p
+
+
+def _length(name: str, t, device: int, B: int) -> int:
+    if not _device_tensor(name, t, device, torch.int32, (B,)).is_contiguous():
+        _refuse(f"{name} is not contiguous")
+    return t.data_ptr()
+
+
+def _lse(p, lse, device: int) -> None:
+    p.lse = _device_tensor("lse", lse, device, torch.float32, (p.B, p.Hq, p.Lq)).data_ptr()
+    if not lse.is_contiguous():
+        _refuse("lse is not contiguous")
 
 
 def gbmw_attention_workspace(q, k, backward: bool) -> int:
@@ -500,54 +513,54 @@ def gbmw_attention_workspace(q, k, backward: bool) -> int:
     return n
 
 
+@_on_stream
 def gbmw_attention_forward(q, k, v, causal: bool = False, scale: float | None = None, len_q=None, len_k=None,
-                           out=None, lse=None, workspace=None, stream=None):
+                           out=None, lse=None, workspace=None, *, _at=None):
     """out [B][Lq][Hq][D] and lse [B][Hq][Lq] (float32) of q [B][Lq][Hq][D], k and v [B][Lk][Hk][D]: float16 or
     bfloat16 GPU tensors with any strides whose last one is 1.  scale: 1 / sqrt(D) by default.  len_q, len_k:
-    int32 [B], the samples' lengths.  out, lse, workspace (uint8): made here unless given."""
-    p = _attention_problem(q, k, v, causal, scale, len_q, len_k)
-    with _on_stream(stream) as p.stream:
-        if out is None:
-            out = torch.empty((p.B, p.Lq, p.Hq, p.D), dtype=q.dtype, device="cuda")
-        if lse is None:
-            lse = torch.empty((p.B, p.Hq, p.Lq), dtype=torch.float32, device="cuda")
-        _set_array(p, "out", _device_tensor("out", out, q.dtype, q.shape))
-        p.lse = _device_tensor("lse", lse, torch.float32, (p.B, p.Hq, p.Lq)).data_ptr()
-        if not lse.is_contiguous():
-            _refuse("lse is not contiguous")
-        need = _lib.gbmw_attention_workspace(ct.byref(p), 0)
-        keep = _workspace(p, workspace, need) if need else None
-        _check(_lib.gbmw_attention_forward(ct.byref(p)))
+    int32 [B], the samples' lengths.  out, lse, workspace (uint8): made here unless given.  stream=: as everywhere."""
+    p = _attention_problem(q, k, v, causal, scale, len_q, len_k, _at)
+    if out is None:
+        out = torch.empty(q.shape, dtype=q.dtype, device="cuda")
+    else:
+        _device_tensor("out", out, _at[0], q.dtype, q.shape)
+    if lse is None:
+        lse = torch.empty((p.B, p.Hq, p.Lq), dtype=torch.float32, device="cuda")
+    _set_array(p, "out", out), _lse(p, lse, _at[0])
+    need = _lib.gbmw_attention_workspace(ct.byref(p), 0)
+    keep = _workspace(p, workspace, need, _at[0]) if need else None
+    _check(_lib.gbmw_attention_forward(ct.byref(p)))
     return out, lse
 
 
+@_on_stream
 def gbmw_attention_backward(dout, q, k, v, out, lse, causal: bool = False, scale: float | None = None, len_q=None,
-                            len_k=None, dq=None, dk=None, dv=None, workspace=None, stream=None):
-    """dq, dk, dv from dout and the forward call's arguments and results."""
-    p = _attention_problem(q, k, v, causal, scale, len_q, len_k)
-    with _on_stream(stream) as p.stream:
-        if dq is None:
-            dq = torch.empty((p.B, p.Lq, p.Hq, p.D), dtype=q.dtype, device="cuda")
-        if dk is None:
-            dk = torch.empty((p.B, p.Lk, p.Hk, p.D), dtype=q.dtype, device="cuda")
-        if dv is None:
-            dv = torch.empty((p.B, p.Lk, p.Hk, p.D), dtype=q.dtype, device="cuda")
-        for name, t, like in (("dout", dout, q), ("out", out, q), ("dq", dq, q), ("dk", dk, k), ("dv", dv, k)):
-            _set_array(p, name, _device_tensor(name, t, q.dtype, like.shape))
-        p.lse = _device_tensor("lse", lse, torch.float32, (p.B, p.Hq, p.Lq)).data_ptr()
-        if not lse.is_contiguous():
-            _refuse("lse is not contiguous")
-        keep = _workspace(p, workspace, _lib.gbmw_attention_workspace(ct.byref(p), 1))
-        _check(_lib.gbmw_attention_backward(ct.byref(p)))
+                            len_k=None, dq=None, dk=None, dv=None, workspace=None, *, _at=None):
+    """dq, dk, dv from dout and the forward call's arguments and results.  stream=: as everywhere."""
+    p = _attention_problem(q, k, v, causal, scale, len_q, len_k, _at)
+    dq = torch.empty(q.shape, dtype=q.dtype, device="cuda") if dq is None else dq
+    dk = torch.empty(k.shape, dtype=q.dtype, device="cuda") if dk is None else dk
+    dv = torch.empty(k.shape, dtype=q.dtype, device="cuda") if dv is None else dv
+    for name, t, like in (("dout", dout, q), ("out", out, q), ("dq", dq, q), ("dk", dk, k), ("dv", dv, k)):
+        _set_array(p, name, _device_tensor(name, t, _at[0], q.dtype, like.shape))
+    _lse(p, lse, _at[0])
+    keep = _workspace(p, workspace, _lib.gbmw_attention_workspace(ct.byref(p), 1), _at[0])
+    _check(_lib.gbmw_attention_backward(ct.byref(p)))
     return dq, dk, dv
 
 
-def _norm_rows(name: str, t, like=None):
+def _norm_rows(name: str, t, device: int, like=None):
     """(rows, cols, row stride) of a tensor whose last axis is normed; the axes before it have to be one stride."""
-    _device_tensor(name, t, None if like is None else like.dtype, None if like is None else like.shape)
+    if like is None:
+        _device_tensor(name, t, device)
+    else:
+        _device_tensor(name, t, device, like.dtype, like.shape)
     if t.dim() < 1:
         _refuse(f"{name} has no axis")
-    cols, rows = t.shape[-1], t.numel() // max(1, t.shape[-1])
+    cols = t.shape[-1]
+    rows = t.numel() // max(1, cols)
+    if t.is_contiguous():
+        return rows, cols, cols
     if t.stride(-1) != 1 and cols > 1:
         _refuse(f"{name}: the values of a row are not next to each other")
     stride = cols
@@ -560,68 +573,73 @@ def _norm_rows(name: str, t, like=None):
     return rows, cols, stride
 
 
-def _norm_problem(x, weight, bias) -> gbmw_layer_norm_problem:
+def _norm_problem(x, weight, bias, at) -> gbmw_layer_norm_problem:
     p = gbmw_layer_norm_problem()
-    p.rows, p.cols, p.x_stride = _norm_rows("x", x)
-    if x.dtype not in _DTYPE:
-        _refuse(f"x has type {x.dtype}")
-    p.x, p.dtype = x.data_ptr(), _DTYPE[x.dtype]
+    p.rows, p.cols, p.x_stride = _norm_rows("x", x, at[0])
     wdtype = x.dtype if weight is None and bias is None else (bias if weight is None else weight).dtype
-    p.wdtype = _DTYPE.get(wdtype, -1)
+    p.x, p.dtype, p.wdtype, p.stream = x.data_ptr(), _DTYPE.get(x.dtype, -1), _DTYPE.get(wdtype, -1), at[1]
     for name, t in (("weight", weight), ("bias", bias)):
         if t is not None:
-            if not _device_tensor(name, t, wdtype, (p.cols,)).is_contiguous():
+            if not _device_tensor(name, t, at[0], wdtype, (p.cols,)).is_contiguous():
                 _refuse(f"{name} is not contiguous")
             setattr(p, name, t.data_ptr())
     return p
 
 
-def gbmw_layer_norm_workspace(x, weight=None) -> int:
+@_on_stream
+def gbmw_layer_norm_workspace(x, weight=None, *, _at=None) -> int:
     """Bytes of workspace of the backward call."""
-    n = _lib.gbmw_layer_norm_workspace(ct.byref(_norm_problem(x, weight, None)))
+    n = _lib.gbmw_layer_norm_workspace(ct.byref(_norm_problem(x, weight, None, _at)))
     if n < 0:
         raise GbmwError(GBMW_ERR_INVALID_ARG, gbmw_last_error())
     return n
 
 
-def gbmw_layer_norm_forward(x, weight=None, bias=None, eps: float = 1e-5, y=None, stream=None):
+def _new_rows(x):
+    """A dense tensor like x."""
+    return torch.empty_like(x) if x.is_contiguous() else torch.empty(x.shape, dtype=x.dtype, device="cuda")
+
+
+@_on_stream
+def gbmw_layer_norm_forward(x, weight=None, bias=None, eps: float = 1e-5, y=None, *, _at=None):
     """y like x, mean and rstd float32 of x's shape without its last axis.  x: float32, float16 or bfloat16 GPU
-    tensor; weight, bias: of x's type or float32.  y: made here unless given (it may be x)."""
-    p = _norm_problem(x, weight, bias)
+    tensor; weight, bias: of x's type or float32.  y: made here unless given (it may be x).  stream=: as everywhere."""
+    p = _norm_problem(x, weight, bias, _at)
     p.eps = eps
-    with _on_stream(stream) as p.stream:
-        if y is None:
-            y = torch.empty(x.shape, dtype=x.dtype, device="cuda")
-        _, _, p.y_stride = _norm_rows("y", y, x)
-        mean = torch.empty(x.shape[:-1], dtype=torch.float32, device="cuda")
-        rstd = torch.empty(x.shape[:-1], dtype=torch.float32, device="cuda")
-        p.y, p.mean, p.rstd = y.data_ptr(), mean.data_ptr(), rstd.data_ptr()
-        _check(_lib.gbmw_layer_norm_forward(ct.byref(p)))
+    if y is None:
+        y, p.y_stride = _new_rows(x), p.cols
+    else:
+        _, _, p.y_stride = _norm_rows("y", y, _at[0], x)
+    mean = torch.empty(x.shape[:-1], dtype=torch.float32, device="cuda")
+    rstd = torch.empty_like(mean)
+    p.y, p.mean, p.rstd = y.data_ptr(), mean.data_ptr(), rstd.data_ptr()
+    _check(_lib.gbmw_layer_norm_forward(ct.byref(p)))
     return y, mean, rstd
 
 
-def gbmw_layer_norm_backward(dy, x, weight, mean, rstd, bias: bool = True, dx=None, workspace=None, stream=None):
+@_on_stream
+def gbmw_layer_norm_backward(dy, x, weight, mean, rstd, bias: bool = True, dx=None, workspace=None, *, _at=None):
     """dx, dweight, dbias from dy and the forward call's x, weight, mean and rstd.  weight None: no dweight; bias
-    False: no dbias.  Both are of weight's type (x's without one)."""
-    p = _norm_problem(x, weight, None)
-    with _on_stream(stream) as p.stream:
-        if dx is None:
-            dx = torch.empty(x.shape, dtype=x.dtype, device="cuda")
-        _, _, p.dx_stride = _norm_rows("dx", dx, x)
-        _, _, p.dy_stride = _norm_rows("dy", dy, x)
-        p.dx, p.dy = dx.data_ptr(), dy.data_ptr()
-        for name, t in (("mean", mean), ("rstd", rstd)):
-            if not _device_tensor(name, t, torch.float32, x.shape[:-1]).is_contiguous():
-                _refuse(f"{name} is not contiguous")
-            setattr(p, name, t.data_ptr())
-        wdtype = x.dtype if weight is None else weight.dtype
-        dweight = None if weight is None else torch.empty(p.cols, dtype=wdtype, device="cuda")
-        dbias = torch.empty(p.cols, dtype=wdtype, device="cuda") if bias else None
-        keep = None
-        if dweight is not None or dbias is not None:
-            p.dweight, p.dbias = (None if t is None else t.data_ptr() for t in (dweight, dbias))
-            keep = _workspace(p, workspace, _lib.gbmw_layer_norm_workspace(ct.byref(p)))
-        _check(_lib.gbmw_layer_norm_backward(ct.byref(p)))
+    False: no dbias.  Both are of weight's type (x's without one).  stream=: as everywhere."""
+    p = _norm_problem(x, weight, None, _at)
+    if dx is None:
+        dx, p.dx_stride = _new_rows(x), p.cols
+    else:
+        _, _, p.dx_stride = _norm_rows("dx", dx, _at[0], x)
+    _, _, p.dy_stride = _norm_rows("dy", dy, _at[0], x)
+    p.dx, p.dy = dx.data_ptr(), dy.data_ptr()
+    for name, t in (("mean", mean), ("rstd", rstd)):
+        if not _device_tensor(name, t, _at[0], torch.float32, x.shape[:-1]).is_contiguous():
+            _refuse(f"{name} is not contiguous")
+        setattr(p, name, t.data_ptr())
+    wdtype = x.dtype if weight is None else weight.dtype
+    dweight = None if weight is None else torch.empty(p.cols, dtype=wdtype, device="cuda")
+    dbias = torch.empty(p.cols, dtype=wdtype, device="cuda") if bias else None
+    keep = None
+    if dweight is not None or dbias is not None:
+        p.dweight, p.dbias = (None if t is None else t.data_ptr() for t in (dweight, dbias))
+        keep = _workspace(p, workspace, _lib.gbmw_layer_norm_workspace(ct.byref(p)), _at[0])
+    _check(_lib.gbmw_layer_norm_backward(ct.byref(p)))
     return dx, dweight, dbias
 
 
@@ -648,9 +666,10 @@ def gbmw_gradient_list_create(grads, outs=None) -> GradientList:
         _refuse(f"{len(grads)} gradients, {len(outs)} outputs")
     dtype = grads[0].dtype if grads else torch.float32
     odtype = outs[0].dtype if outs else torch.float32
+    device = torch.cuda.current_device() if torch.cuda.is_initialized() else 0
     for i, (g, o) in enumerate(zip(grads, outs)):
-        _device_tensor(f"gradient {i}", g, dtype)
-        _device_tensor(f"output {i}", o, odtype)
+        _device_tensor(f"gradient {i}", g, device, dtype)
+        _device_tensor(f"output {i}", o, device, odtype)
         if o.numel() != g.numel() or not g.is_contiguous() or not o.is_contiguous():
             _refuse(f"tensor {i}: sizes {g.numel()} and {o.numel()}, or not contiguous")
     n = len(grads)
@@ -663,15 +682,15 @@ def gbmw_gradient_list_create(grads, outs=None) -> GradientList:
     return lst
 
 
-def gbmw_clip_gradients(lst: GradientList, max_norm: float, scale: float = 1.0, norm=None, stream=None):
-    """Writes the list's outputs; returns the norm before clipping, a float32 GPU tensor [1] (norm, if given)."""
-    with _on_stream(stream) as handle:
-        if norm is None:
-            norm = torch.empty(1, dtype=torch.float32, device="cuda")
-        _device_tensor("norm", norm, torch.float32)
-        if norm.numel() < 1:
-            _refuse("norm is empty")
-        _check(_lib.gbmw_clip_gradients(lst.handle, float(max_norm), float(scale), norm.data_ptr(), handle))
+@_on_stream
+def gbmw_clip_gradients(lst: GradientList, max_norm: float, scale: float = 1.0, norm=None, *, _at=None):
+    """Writes the list's outputs; returns the norm before clipping, a float32 GPU tensor [1] (norm, if given).
+    stream=: as everywhere."""
+    if norm is None:
+        norm = torch.empty(1, dtype=torch.float32, device="cuda")
+    elif _device_tensor("norm", norm, _at[0], torch.float32).numel() < 1:
+        _refuse("norm is empty")
+    _check(_lib.gbmw_clip_gradients(lst.handle, max_norm, scale, norm.data_ptr(), _at[1]))
     return norm
 
 
