@@ -24,10 +24,6 @@ using gbmw_detail::fail;
 namespace gbmw {
 namespace {
 
-#ifndef GBMW_FILL
-#define GBMW_FILL 1024
-#define GBMW_LEAST 512
-#endif
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 constexpr float kInf = __builtin_inff();
 
@@ -48,7 +44,9 @@ struct AttnArgs {
   const int *len_q, *len_k;
   float* partial;   // [parts][2][B][Hk][Lk][D4]: shares of dk and dv
   int B, Hq, Hk, Lq, Lk, D, share, causal;
-  int parts, D4;    // D rounded up to 4
+  float *shares, *tops;   // [kparts][B][Hk][rows][D4] and [kparts][B][Hk][rows]: of out (or dq) and of what goes with it
+  int parts, kparts;      // workgroups that share a tile of keys, or a tile of rows
+  int D4;                 // D rounded up to 4
   int near;         // heads that a die works on at a time
   unsigned magic;   // 2^32 / share, rounded up
   float c;       // scale * log2(e): probabilities are powers of two
@@ -166,9 +164,11 @@ struct Rows {
 // A wave brings N runs of kRowsOf rows.  Its lanes' offsets inside a run are the same for all of
 // them where rows have 16 pieces; with SPARE every run gets bounds of its own and the lanes keep
 // one offset, otherwise N (for the kernel that is short of registers, and those that are not).
-template <int KS, bool DIRECT, bool SPARE = false>
+// ALONE: a wave brings 32 rows for itself, and nobody else waits for them.
+template <int KS, bool DIRECT, bool SPARE = false, bool ALONE = false>
 struct Loader {
-  static constexpr int CH = kChunks<KS>, N = DIRECT ? CH / 4 : (64 * 2 * KS + 255) / 256;
+  static constexpr int CH = kChunks<KS>, ROWS = ALONE ? 32 : 64, THREADS = ALONE ? 64 : 256;
+  static constexpr int N = DIRECT ? ROWS * CH / THREADS : (ROWS * 2 * KS + THREADS - 1) / THREADS;
   static constexpr int kRowsOf = 64 / CH;
   static constexpr bool kOne = SPARE && CH == 16;
   static constexpr int NA = kOne ? 1 : N;
@@ -176,7 +176,8 @@ struct Loader {
   s16x8 x[DIRECT ? 1 : N];
   unsigned at[DIRECT ? NA : 1];
 
-  __device__ __forceinline__ static int wave() { return __builtin_amdgcn_readfirstlane(threadIdx.x / 64); }
+  __device__ __forceinline__ static int wave() { return ALONE ? 0 : __builtin_amdgcn_readfirstlane(threadIdx.x / 64); }
+  __device__ __forceinline__ static int thread() { return ALONE ? threadIdx.x % 64 : threadIdx.x; }
   __device__ __forceinline__ static int row_of(int i) {   // of this lane, in the tile
     return (wave() * N + i) * kRowsOf + (int)(threadIdx.x % 64) / CH;
   }
@@ -217,8 +218,8 @@ struct Loader {
     } else {
 #pragma unroll
       for (int i = 0; i < N; ++i) {
-        const int n = threadIdx.x + 256 * i, r = first + n / (2 * KS);
-        const bool there = n < 64 * 2 * KS && r < rows.count;
+        const int n = thread() + THREADS * i, r = first + n / (2 * KS);
+        const bool there = n < ROWS * 2 * KS && r < rows.count;
         const int q = there ? r : first, h = rows.of(q);
         x[i] = load8<false>(rows.base + h * rows.stride + (q - h * rows.share) * rows.head, n % (2 * KS), D, there);
       }
@@ -235,8 +236,8 @@ struct Loader {
       typedef __attribute__((address_space(3))) s16x8 lds8;
 #pragma unroll
       for (int i = 0; i < N; ++i) {
-        const int n = threadIdx.x + 256 * i, r = n / (2 * KS);
-        if (r < 64) *(lds8*)(tile + place_of<CH>(r, n % (2 * KS))) = x[i];
+        const int n = thread() + THREADS * i, r = n / (2 * KS);
+        if (r < ROWS) *(lds8*)(tile + place_of<CH>(r, n % (2 * KS))) = x[i];
       }
     }
   }
@@ -280,6 +281,33 @@ __device__ __forceinline__ void store4(char* row, int d, int D, const f32x16& x,
   }
 }
 
+// Four values of a row from d on (a multiple of four).
+template <typename T>
+__device__ __forceinline__ void store_quad(T* row, int d, int D, f32x4 x) {
+  typedef T Tx4 __attribute__((ext_vector_type(4)));
+  const Tx4 y = {(T)x[0], (T)x[1], (T)x[2], (T)x[3]};
+  if (d + 4 <= D) {
+    __builtin_memcpy(row + d, &y, 8);
+  } else {
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      if (d + i < D) row[d + i] = y[i];
+  }
+}
+
+// A lane's part of a result's rows, times f, as a share in 32 bits.
+template <int DB>
+__device__ __forceinline__ void store_share(float* row, int D4, const f32x16 (&x)[DB], float f) {
+  const int half = threadIdx.x % 64 / 32;
+#pragma unroll
+  for (int d = 0; d < DB; ++d)
+#pragma unroll
+    for (int r = 0; r < 16; r += 4) {
+      const int at = 32 * d + 8 * (r / 4) + 4 * half;
+      if (at < D4) *(f32x4*)(row + at) = f32x4{x[d][r] * f, x[d][r + 1] * f, x[d][r + 2] * f, x[d][r + 3] * f};
+    }
+}
+
 // Which head and which of its `units` pieces of work a workgroup takes.  Workgroups are dealt to
 // the eight dies in turn.  A die works on its own heads, `near` of them at a time, so that what
 // their units read alike stays in its cache; of those the first units (the longest under a
@@ -301,23 +329,29 @@ struct Deal {
   }
 };
 
-// Where a workgroup of the rows' kernels works, and how many keys a row sees.
+// Where a workgroup of the rows' kernels works: `per` rows of one (sample, key head), and of the
+// keys that any of them sees its part of `kparts`.
 struct Place {
-  int tile, tiles, hk, b, nq, nk, rows;
+  int tile, tiles, part, hk, b, nq, nk, rows, most, begin, end;
   __device__ __forceinline__ Place(const AttnArgs& a, int per) {
     rows = a.Lq * a.share;
     tiles = (rows + per - 1) / per;
-    const Deal d(a.Hk * a.B, tiles, a.near);
-    tile = tiles - 1 - d.unit;   // the longest rows of a causal mask first
+    const Deal d(a.Hk * a.B, tiles * a.kparts, a.near);
+    tile = tiles - 1 - d.unit / a.kparts;   // the longest rows of a causal mask first
+    part = d.unit % a.kparts;
     hk = d.head % a.Hk, b = d.head / a.Hk;
     nq = length(a.len_q, b, a.Lq), nk = length(a.len_k, b, a.Lk);
+    const int first = tile * per / a.share, last = min((min(tile * per + per, rows) - 1) / a.share, nq - 1);
+    most = first >= nq ? 0 : sees(a, last);
+    const int run = ((most + 63) / 64 + a.kparts - 1) / a.kparts * 64;
+    begin = min(part * run, most), end = min(begin + run, most);
   }
   __device__ __forceinline__ int sees(const AttnArgs& a, int i) const {   // keys j < sees
     return i >= nq ? 0 : a.causal ? max(0, min(nk, i + nk - nq + 1)) : nk;
   }
-  __device__ __forceinline__ int most(const AttnArgs& a, int per) const {   // of any row of the tile
-    const int first = tile * per / a.share, last = min((min(tile * per + per, rows) - 1) / a.share, nq - 1);
-    return first >= nq ? 0 : sees(a, last);
+  // of a row in `shares` and `tops`
+  __device__ __forceinline__ int64_t share_of(const AttnArgs& a, int row) const {
+    return (((int64_t)part * a.B + b) * a.Hk + hk) * rows + row;
   }
 };
 
@@ -353,134 +387,267 @@ __device__ __forceinline__ float max_of(const float* x, int n) {   // n values, 
 // when that is more than 2^kLag ahead, so they are seldom rescaled.
 constexpr float kLag = 6.0f;
 
-template <typename T, int KS, int NQ, bool DIRECT>
-__global__ __launch_bounds__(256, NQ == 1 ? 2 : 1) void k_attn_fwd(AttnArgs a) {
+// One row's running maximum (in units of x / scale), sum, and out^T: what a wave has of 32 rows.
+template <int DB>
+struct Running {
+  f32x16 o[DB] = {};
+  float m = -kInf, sum = 0.0f;
+};
+
+// Takes N runs of 32 keys in: x holds their scores, and leaves with their probabilities.
+template <typename T, int DB, int N>
+__device__ __forceinline__ void take_scores(Running<DB>& w, f32x16 (&x)[N], float c) {
+  // the matrix results are waited for where the compiler sees them read, before max3
+  float top = w.m;
+#pragma unroll
+  for (int u = 0; u < N; ++u) top = fmaxf(top, x[u][15]);
+#pragma unroll
+  for (int u = 0; u < N; ++u)
+#pragma unroll
+    for (int r = 0; r < 16; r += 2) top = max3(top, x[u][r], x[u][r + 1]);
+  float low;
+  const float high = other_half(top, &low);
+  top = fmaxf(low, high);
+  const bool ahead = (top - w.m) * c > kLag;
+  if (__any(ahead)) {
+    const float f = ahead ? __builtin_amdgcn_exp2f((w.m - top) * c) : 1.0f;
+    if (ahead) w.m = top;
+    w.sum *= f;
+#pragma unroll
+    for (int d = 0; d < DB; ++d)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) w.o[d][r] *= f;
+  }
+  const float off = (w.m == -kInf ? 0.0f : w.m * c) - kUp<T>;
+#pragma unroll
+  for (int u = 0; u < N; ++u)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) {
+      x[u][r] = __builtin_amdgcn_exp2f(__builtin_fmaf(x[u][r], c, -off));
+      w.sum += x[u][r];
+    }
+}
+
+// log2 of a row's sum of 2^(c x): -inf without keys.
+template <typename T>
+__device__ __forceinline__ float level_of(float m, float sum, float c) {
+  const bool empty = m == -kInf && !(sum != sum);
+  return empty ? -kInf : m * c - kUp<T> + __builtin_amdgcn_logf(sum);
+}
+
+template <typename T, int KS, bool DIRECT>
+__global__ __launch_bounds__(256, 2) void k_attn_fwd(AttnArgs a) {
   constexpr int DB = (KS + 1) / 2;
   __shared__ __attribute__((aligned(16))) char lds[4 * kTile<KS>];
   lds_char* const tiles = (lds_char*)lds;
-  const Place w(a, 128 * NQ);
-  const int l = threadIdx.x % 64, half = l / 32;
-  const int most = w.most(a, 128 * NQ);
+  const Place w(a, 128);
+  const int l = threadIdx.x % 64, half = l / 32, row = w.tile * 128 + (threadIdx.x / 64) * 32 + l % 32;
+  const int i = row / a.share, hq = w.hk * a.share + row % a.share;
+  const int sees = w.sees(a, i);
   const Rows kr{a.k + 2 * (w.b * a.ks[0] + w.hk * a.ks[2]), 2 * a.ks[1], 0, 1, w.nk, 0};
   const Rows vr{a.v + 2 * (w.b * a.vs[0] + w.hk * a.vs[2]), 2 * a.vs[1], 0, 1, w.nk, 0};
 
-  s16x8 q[NQ][KS];
-  int sees[NQ];
-  int fewest = INT_MAX, furthest = 0;
+  s16x8 q[KS];
+  const char* qrow = a.q + 2 * (w.b * a.qs[0] + (i < w.nq ? i : 0) * a.qs[1] + hq * a.qs[2]);
 #pragma unroll
-  for (int n = 0; n < NQ; ++n) {
-    const int row = w.tile * 128 * NQ + ((int)(threadIdx.x / 64) * NQ + n) * 32 + l % 32;
-    const int i = row / a.share, hq = w.hk * a.share + row % a.share;
-    sees[n] = w.sees(a, i);
-    fewest = min(fewest, sees[n]), furthest = max(furthest, sees[n]);
-    const char* p = a.q + 2 * (w.b * a.qs[0] + (i < w.nq ? i : 0) * a.qs[1] + hq * a.qs[2]);
-#pragma unroll
-    for (int s = 0; s < KS; ++s) q[n][s] = load8<DIRECT>(p, 2 * s + half, a.D, i < w.nq);
-  }
-  f32x16 o[NQ][DB] = {};
-  float m[NQ], sum[NQ];   // m in units of x / scale
-#pragma unroll
-  for (int n = 0; n < NQ; ++n) m[n] = -kInf, sum[n] = 0.0f;
-
+  for (int s = 0; s < KS; ++s) q[s] = load8<DIRECT>(qrow, 2 * s + half, a.D, i < w.nq);
+  Running<DB> run;
   const Reader<KS> rd;
   Loader<KS, DIRECT> lk, lv;
   lk.init(kr, a.D), lv.init(vr, a.D);
-  if (most > 0) {
-    lk.begin(tiles, kr, 0, a.D);
-    lv.begin(tiles + kTile<KS>, vr, 0, a.D);
+  if (w.begin < w.end) {
+    lk.begin(tiles, kr, w.begin, a.D);
+    lv.begin(tiles + kTile<KS>, vr, w.begin, a.D);
   }
-  for (int j0 = 0, buf = 0; j0 < most; j0 += 64, buf ^= 1) {
+  for (int j0 = w.begin, buf = 0; j0 < w.end; j0 += 64, buf ^= 1) {
     lds_char *tk = tiles + 2 * buf * kTile<KS>, *tv = tk + kTile<KS>;
     lk.end(tk), lv.end(tv);
     __syncthreads();   // this tile is whole, and nobody reads the other buffer any more
-    if (j0 + 64 < most) {
+    if (j0 + 64 < w.end) {
       lds_char* to = tiles + 2 * (buf ^ 1) * kTile<KS>;
       lk.begin(to, kr, j0 + 64, a.D);
       lv.begin(to + kTile<KS>, vr, j0 + 64, a.D);
     }
-    if (!__any(j0 < furthest)) continue;   // none of the wave's rows sees this tile
-    f32x16 x[NQ][2] = {};
+    if (!__any(j0 < sees)) continue;   // none of the wave's rows sees this tile
+    f32x16 x[2] = {};
 #pragma unroll
     for (int u = 0; u < 2; ++u)
 #pragma unroll
-      for (int s = 0; s < KS; ++s) {
-        const s16x8 k = rd.rows(tk, 32 * u, s);
-#pragma unroll
-        for (int n = 0; n < NQ; ++n) x[n][u] = mma<T>(k, q[n][s], x[n][u]);
-      }
-    if (!__all(j0 + 64 <= fewest)) {
-#pragma unroll
-      for (int n = 0; n < NQ; ++n)
-#pragma unroll
-        for (int u = 0; u < 2; ++u)
-#pragma unroll
-          for (int r = 0; r < 16; ++r)
-            if (j0 + 32 * u + 8 * (r / 4) + 4 * half + r % 4 >= sees[n]) x[n][u][r] = -kInf;
-    }
-#pragma unroll
-    for (int n = 0; n < NQ; ++n) {
-      // the matrix results are waited for where the compiler sees them read, before max3
-      float top = fmaxf(fmaxf(m[n], x[n][0][15]), x[n][1][15]);
+      for (int s = 0; s < KS; ++s) x[u] = mma<T>(rd.rows(tk, 32 * u, s), q[s], x[u]);
+    if (!__all(j0 + 64 <= sees)) {
 #pragma unroll
       for (int u = 0; u < 2; ++u)
 #pragma unroll
-        for (int r = 0; r < 16; r += 2) top = max3(top, x[n][u][r], x[n][u][r + 1]);
-      float low;
-      const float high = other_half(top, &low);
-      top = fmaxf(low, high);
-      const bool ahead = (top - m[n]) * a.c > kLag;
-      if (__any(ahead)) {
-        const float f = ahead ? __builtin_amdgcn_exp2f((m[n] - top) * a.c) : 1.0f;
-        if (ahead) m[n] = top;
-        sum[n] *= f;
-#pragma unroll
-        for (int d = 0; d < DB; ++d)
-#pragma unroll
-          for (int r = 0; r < 16; ++r) o[n][d][r] *= f;
-      }
-      const float off = (m[n] == -kInf ? 0.0f : m[n] * a.c) - kUp<T>;
-#pragma unroll
-      for (int u = 0; u < 2; ++u)
-#pragma unroll
-        for (int r = 0; r < 16; ++r) {
-          x[n][u][r] = __builtin_amdgcn_exp2f(__builtin_fmaf(x[n][u][r], a.c, -off));
-          sum[n] += x[n][u][r];
-        }
+        for (int r = 0; r < 16; ++r)
+          if (j0 + 32 * u + 8 * (r / 4) + 4 * half + r % 4 >= sees) x[u][r] = -kInf;
     }
+    take_scores<T>(run, x, a.c);
 #pragma unroll
     for (int u = 0; u < 2; ++u)
 #pragma unroll
       for (int t = 0; t < 2; ++t) {
-        s16x8 p[NQ];
+        const s16x8 p = round8<T>(x[u], t);
 #pragma unroll
-        for (int n = 0; n < NQ; ++n) p[n] = round8<T>(x[n][u], t);
-#pragma unroll
-        for (int d = 0; d < DB; ++d) {
-          const s16x8 v = rd.cols(tv, 32 * u + 16 * t, d);
-#pragma unroll
-          for (int n = 0; n < NQ; ++n) o[n][d] = mma<T>(v, p[n], o[n][d]);
-        }
+        for (int d = 0; d < DB; ++d) run.o[d] = mma<T>(rd.cols(tv, 32 * u + 16 * t, d), p, run.o[d]);
       }
   }
-#pragma unroll
-  for (int n = 0; n < NQ; ++n) {
-    const int row = w.tile * 128 * NQ + ((int)(threadIdx.x / 64) * NQ + n) * 32 + l % 32;
-    const int i = row / a.share, hq = w.hk * a.share + row % a.share;
-    sum[n] += __shfl_xor(sum[n], 32);
-    if (row >= w.rows) continue;
-    const bool empty = m[n] == -kInf && !(sum[n] != sum[n]);
-    const float f = empty ? 0.0f : 1.0f / sum[n];
-    if (half == 0)
-      a.lse[((int64_t)w.b * a.Hq + hq) * a.Lq + i] =
-          empty ? -kInf : (m[n] * a.c - kUp<T> + __builtin_amdgcn_logf(sum[n])) * kLn2;
+  run.sum += __shfl_xor(run.sum, 32);
+  if (row >= w.rows) return;
+  const float level = level_of<T>(run.m, run.sum, a.c), f = level == -kInf ? 0.0f : 1.0f / run.sum;
+  if (a.kparts == 1) {
+    if (half == 0) a.lse[((int64_t)w.b * a.Hq + hq) * a.Lq + i] = level * kLn2;
     char* out = a.out + 2 * (w.b * a.os[0] + i * a.os[1] + hq * a.os[2]);
 #pragma unroll
     for (int d = 0; d < DB; ++d)
 #pragma unroll
       for (int r = 0; r < 16; r += 4) {
         const int at = 32 * d + 8 * (r / 4) + 4 * half;
-        if (at < a.D) store4<T, DIRECT>(out, at, a.D, o[n][d], r, f);
+        if (at < a.D) store4<T, DIRECT>(out, at, a.D, run.o[d], r, f);
       }
+  } else {
+    const int64_t at = w.share_of(a, row);
+    if (half == 0) a.tops[at] = level;
+    store_share(a.shares + at * a.D4, a.D4, run.o, f);
+  }
+}
+
+// Forward where a key head has at most 32 rows (one token, a few of them, few heads that share):
+// there the keys are what has to be read, and every wave of a workgroup walks tiles of 32 keys
+// of its own, without waiting for the others; at the end their sums are put together.
+template <typename T, int KS, bool DIRECT>
+__global__ __launch_bounds__(256, 1) void k_attn_few(AttnArgs a) {
+  constexpr int DB = (KS + 1) / 2, kHalf = Reader<KS>::down(32), kWave = 4 * kHalf, DP = 32 * DB + 4;
+  static_assert(32 * DP * 4 <= kWave, "a wave's sums fit where its tiles were");
+  __shared__ __attribute__((aligned(16))) char lds[4 * kWave];
+  __shared__ float sTop[4][32], sSum[4][32];
+  const Place w(a, 32);
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
+  lds_char* const tiles = (lds_char*)lds + wave * kWave;
+  const int l = threadIdx.x % 64, half = l / 32, row = l % 32;
+  const int i = row / a.share, hq = w.hk * a.share + row % a.share;
+  const int sees = row < w.rows ? w.sees(a, i) : INT_MAX;   // rows that are not there need no mask
+  const Rows kr{a.k + 2 * (w.b * a.ks[0] + w.hk * a.ks[2]), 2 * a.ks[1], 0, 1, w.nk, 0};
+  const Rows vr{a.v + 2 * (w.b * a.vs[0] + w.hk * a.vs[2]), 2 * a.vs[1], 0, 1, w.nk, 0};
+
+  s16x8 q[KS];
+  const bool there = row < w.rows && i < w.nq;
+  const char* qrow = a.q + 2 * (w.b * a.qs[0] + (there ? i * a.qs[1] + hq * a.qs[2] : 0));
+#pragma unroll
+  for (int s = 0; s < KS; ++s) q[s] = load8<DIRECT>(qrow, 2 * s + half, a.D, there);
+  Running<DB> run;
+  const Reader<KS> rd;
+  Loader<KS, DIRECT, false, true> lk, lv;
+  lk.init(kr, a.D), lv.init(vr, a.D);
+  auto begin = [&](int buf, int j0) {
+    lk.begin(tiles + 2 * buf * kHalf, kr, j0, a.D);
+    lv.begin(tiles + (2 * buf + 1) * kHalf, vr, j0, a.D);
+  };
+  int j0 = w.begin + 32 * wave;
+  if (j0 < w.end) begin(0, j0);
+  for (int buf = 0; j0 < w.end; j0 += 128, buf ^= 1) {
+    lds_char *tk = tiles + 2 * buf * kHalf, *tv = tk + kHalf;
+    lk.end(tk), lv.end(tv);
+    __builtin_amdgcn_s_waitcnt(0xc07f);   // the last tile's reads are done: its place is loaded next
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    f32x16 x[1] = {};
+    if (j0 + 128 < w.end) begin(buf ^ 1, j0 + 128);
+#pragma unroll
+    for (int s = 0; s < KS; ++s) x[0] = mma<T>(rd.rows(tk, 0, s), q[s], x[0]);
+    if (!__all(j0 + 32 <= sees)) {
+#pragma unroll
+      for (int r = 0; r < 16; ++r)
+        if (j0 + 8 * (r / 4) + 4 * half + r % 4 >= sees) x[0][r] = -kInf;
+    }
+    take_scores<T>(run, x, a.c);
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+      const s16x8 p = round8<T>(x[0], t);
+#pragma unroll
+      for (int d = 0; d < DB; ++d) run.o[d] = mma<T>(rd.cols(tv, 16 * t, d), p, run.o[d]);
+    }
+  }
+  run.sum += __shfl_xor(run.sum, 32);
+  {
+    const float level = level_of<T>(run.m, run.sum, a.c);
+    if (half == 0) sTop[wave][row] = level, sSum[wave][row] = run.sum;
+    __builtin_amdgcn_s_waitcnt(0);   // every read of this wave's tiles is done
+    float* o = (float*)(lds + wave * kWave) + row * DP;
+#pragma unroll
+    for (int d = 0; d < DB; ++d)
+#pragma unroll
+      for (int r = 0; r < 16; r += 4)
+        *(f32x4*)(o + 32 * d + 8 * (r / 4) + 4 * half) = f32x4{run.o[d][r], run.o[d][r + 1], run.o[d][r + 2], run.o[d][r + 3]};
+  }
+  __syncthreads();
+  // eight threads a row, quads of values
+  const int out_row = threadIdx.x / 8;
+  if (out_row >= w.rows) return;
+  float top = -kInf, sum = 0.0f, f[4];
+#pragma unroll
+  for (int k = 0; k < 4; ++k) top = fmaxf(top, sTop[k][out_row]);
+#pragma unroll
+  for (int k = 0; k < 4; ++k) {
+    const float level = sTop[k][out_row];
+    const float share = level == -kInf ? 0.0f : __builtin_amdgcn_exp2f(level - (top == -kInf ? 0.0f : top));
+    sum += share;
+    f[k] = level == -kInf ? 0.0f : share / sSum[k][out_row];
+  }
+  const bool empty = top == -kInf && !(sum != sum);
+  const float level = empty ? -kInf : top + __builtin_amdgcn_logf(sum), inv = empty ? 0.0f : 1.0f / sum;
+  const int oi = out_row / a.share, oh = w.hk * a.share + out_row % a.share;
+  const int64_t at = w.share_of(a, out_row);
+  if (threadIdx.x % 8 == 0) {
+    if (a.kparts == 1) a.lse[((int64_t)w.b * a.Hq + oh) * a.Lq + oi] = level * kLn2;
+    else a.tops[at] = level;
+  }
+  for (int d = threadIdx.x % 8 * 4; d < a.D4; d += 32) {
+    f32x4 o = {};
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      const f32x4 y = *(const f32x4*)((const float*)(lds + k * kWave) + out_row * DP + d);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) o[e] = __builtin_fmaf(y[e], f[k], o[e]);
+    }
+#pragma unroll
+    for (int e = 0; e < 4; ++e) o[e] *= inv;
+    if (a.kparts == 1) store_quad<T>((T*)a.out + w.b * a.os[0] + oi * a.os[1] + oh * a.os[2], d, a.D, o);
+    else *(f32x4*)(a.shares + at * a.D4 + d) = o;
+  }
+}
+
+// out and lse, or dq and delta, from the parts' shares: four values a thread, in the parts' order.
+template <typename T, bool BACKWARD>
+__global__ __launch_bounds__(256) void k_attn_merge(AttnArgs a) {
+  const int64_t rows = (int64_t)a.Lq * a.share, all = rows * a.Hk * a.B;
+  const int64_t n = (int64_t)blockIdx.x * 256 + threadIdx.x, at = n / (a.D4 / 4);
+  if (at >= all) return;
+  const int d = (int)(n % (a.D4 / 4)) * 4;
+  const int64_t head = at / rows;
+  const int row = (int)(at - head * rows), i = row / a.share, hk = (int)(head % a.Hk), b = (int)(head / a.Hk);
+  const int hq = hk * a.share + row - i * a.share;
+  f32x4 o = {};
+  float top = -kInf, sum = 0.0f;
+  if constexpr (!BACKWARD)
+    for (int k = 0; k < a.kparts; ++k) top = fmaxf(top, a.tops[k * all + at]);
+  for (int k = 0; k < a.kparts; ++k) {
+    const float t = a.tops[k * all + at];
+    float f = 1.0f;
+    if constexpr (!BACKWARD) f = t == -kInf ? 0.0f : __builtin_amdgcn_exp2f(t - (top == -kInf ? 0.0f : top));
+    sum += BACKWARD ? t : f;
+    const f32x4 y = *(const f32x4*)(a.shares + (k * all + at) * a.D4 + d);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) o[e] = __builtin_fmaf(y[e], f, o[e]);
+  }
+  if constexpr (BACKWARD) {
+    if (d == 0) a.delta[at] += sum;
+    store_quad<T>((T*)a.dq + b * a.dqs[0] + i * a.dqs[1] + hq * a.dqs[2], d, a.D, o);
+  } else {
+    const bool empty = top == -kInf && !(sum != sum);
+    const float inv = empty ? 0.0f : 1.0f / sum;
+    if (d == 0) a.lse[((int64_t)b * a.Hq + hq) * a.Lq + i] = empty ? -kInf : (top + __builtin_amdgcn_logf(sum)) * kLn2;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) o[e] *= inv;
+    store_quad<T>((T*)a.out + b * a.os[0] + i * a.os[1] + hq * a.os[2], d, a.D, o);
   }
 }
 
@@ -525,7 +692,7 @@ __global__ __launch_bounds__(256, 2) void k_attn_dq(AttnArgs a) {
   const int l = threadIdx.x % 64, half = l / 32, row = w.tile * 128 + (threadIdx.x / 64) * 32 + l % 32;
   const int i = row / a.share, hq = w.hk * a.share + row % a.share;
   const int b = w.b, hk = w.hk, nq = w.nq, nk = w.nk, rows = w.rows;
-  const int sees = w.sees(a, i), most = w.most(a, 128);
+  const int sees = w.sees(a, i);
   const Rows kr{a.k + 2 * (b * a.ks[0] + hk * a.ks[2]), 2 * a.ks[1], 0, 1, nk, 0};
   const Rows vr{a.v + 2 * (b * a.vs[0] + hk * a.vs[2]), 2 * a.vs[1], 0, 1, nk, 0};
 
@@ -565,7 +732,7 @@ __global__ __launch_bounds__(256, 2) void k_attn_dq(AttnArgs a) {
     float top = norm;
 #pragma unroll
     for (int d = 32; d; d >>= 1) top = fmaxf(top, __shfl_xor(top, d));
-    if (l == 0) a.gmax[(((int64_t)b * a.Hk + hk) * w.tiles + w.tile) * 4 + threadIdx.x / 64] = top;
+    if (l == 0 && w.part == 0) a.gmax[(((int64_t)b * a.Hk + hk) * w.tiles + w.tile) * 4 + threadIdx.x / 64] = top;
   }
   f32x16 o[DB] = {};
   float left = 0.0f;
@@ -575,17 +742,17 @@ __global__ __launch_bounds__(256, 2) void k_attn_dq(AttnArgs a) {
   // The score gradients of a row add up to 0: what their sum leaves over is delta's error, the
   // rounding of `out`.  The other kernel gets the corrected delta.  Here it matters where few
   // keys share a row, and there (one tile) a first pass finds it.
-  for (int pass = most > 64; pass < 2; ++pass) {
+  for (int pass = w.most > 64; pass < 2; ++pass) {
     left = 0.0f;
-    if (most > 0) {
-      lk.begin(tiles, kr, 0, a.D);
-      lv.begin(tiles + kTile<KS>, vr, 0, a.D);
+    if (w.begin < w.end) {
+      lk.begin(tiles, kr, w.begin, a.D);
+      lv.begin(tiles + kTile<KS>, vr, w.begin, a.D);
     }
-    for (int j0 = 0, buf = 0; j0 < most; j0 += 64, buf ^= 1) {
+    for (int j0 = w.begin, buf = 0; j0 < w.end; j0 += 64, buf ^= 1) {
       lds_char *tk = tiles + 2 * buf * kTile<KS>, *tv = tk + kTile<KS>;
       lk.end(tk), lv.end(tv);
       __syncthreads();
-      if (j0 + 64 < most) {
+      if (j0 + 64 < w.end) {
         lds_char* to = tiles + 2 * (buf ^ 1) * kTile<KS>;
         lk.begin(to, kr, j0 + 64, a.D);
         lv.begin(to + kTile<KS>, vr, j0 + 64, a.D);
@@ -620,22 +787,27 @@ __global__ __launch_bounds__(256, 2) void k_attn_dq(AttnArgs a) {
       }
     }
     left += __shfl_xor(left, 32);
-    delta = __builtin_fmaf(left, down, delta);
+    left *= down;
+    if (pass == 0) delta += left;
     __syncthreads();   // the next pass begins with the first buffer again
   }
-  if (row < rows && half == 0) {
-    const int64_t at = ((int64_t)b * a.Hk + hk) * rows + row;
-    a.delta[at] = delta, a.level[at] = lse - kUp<T>;
-  }
   if (row >= rows) return;
-  char* out = a.dq + 2 * (b * a.dqs[0] + i * a.dqs[1] + hq * a.dqs[2]);
+  const int64_t at = ((int64_t)b * a.Hk + hk) * rows + row;
+  if (half == 0 && w.part == 0) a.delta[at] = a.kparts == 1 ? delta + left : delta, a.level[at] = lse - kUp<T>;
+  if (a.kparts == 1) {
+    char* out = a.dq + 2 * (b * a.dqs[0] + i * a.dqs[1] + hq * a.dqs[2]);
 #pragma unroll
-  for (int d = 0; d < DB; ++d)
+    for (int d = 0; d < DB; ++d)
 #pragma unroll
-    for (int r = 0; r < 16; r += 4) {
-      const int at = 32 * d + 8 * (r / 4) + 4 * half;
-      if (at < a.D) store4<T, DIRECT>(out, at, a.D, o[d], r, a.scale * down);
-    }
+      for (int r = 0; r < 16; r += 4) {
+        const int to = 32 * d + 8 * (r / 4) + 4 * half;
+        if (to < a.D) store4<T, DIRECT>(out, to, a.D, o[d], r, a.scale * down);
+      }
+  } else {
+    const int64_t to = w.share_of(a, row);
+    if (half == 0) a.tops[to] = left;
+    store_share(a.shares + to * a.D4, a.D4, o, a.scale * down);
+  }
 }
 
 // ---- backward, dk and dv ----------------------------------------------------------------------
@@ -775,23 +947,14 @@ __global__ __launch_bounds__(256, 2) void k_attn_dkv(AttnArgs a) {
   } else {
     const int64_t all = (int64_t)heads * a.Lk * a.D4;
     float* o = a.partial + part * 2 * all + (((int64_t)b * a.Hk + hk) * a.Lk + key) * a.D4;
-#pragma unroll
-    for (int d = 0; d < DB; ++d)
-#pragma unroll
-      for (int r = 0; r < 16; r += 4) {
-        const int at = 32 * d + 8 * (r / 4) + 4 * half;
-        if (at < a.D4) {
-          *(f32x4*)(o + at) = f32x4{dk[d][r] * fk, dk[d][r + 1] * fk, dk[d][r + 2] * fk, dk[d][r + 3] * fk};
-          *(f32x4*)(o + all + at) = f32x4{dv[d][r] * fv, dv[d][r + 1] * fv, dv[d][r + 2] * fv, dv[d][r + 3] * fv};
-        }
-      }
+    store_share(o, a.D4, dk, fk);
+    store_share(o + all, a.D4, dv, fv);
   }
 }
 
 // dk and dv from their shares, four values a thread, in the shares' order.
 template <typename T>
 __global__ __launch_bounds__(256) void k_attn_join(AttnArgs a) {
-  typedef T Tx4 __attribute__((ext_vector_type(4)));
   const int64_t quads = (int64_t)a.B * a.Hk * a.Lk * (a.D4 / 4);
   const int64_t n = (int64_t)blockIdx.x * 256 + threadIdx.x;
   if (n >= quads) return;
@@ -801,15 +964,7 @@ __global__ __launch_bounds__(256) void k_attn_join(AttnArgs a) {
   int64_t at = n / (a.D4 / 4);
   const int64_t key = at % a.Lk, hk = at / a.Lk % a.Hk, b = at / a.Lk / a.Hk;
   const int64_t* st = blockIdx.y ? a.dvs : a.dks;
-  T* o = (T*)(blockIdx.y ? a.dv : a.dk) + b * st[0] + key * st[1] + hk * st[2] + d;
-  const Tx4 y = {(T)s[0], (T)s[1], (T)s[2], (T)s[3]};
-  if (d + 4 <= a.D) {
-    __builtin_memcpy(o, &y, 8);
-  } else {
-#pragma unroll
-    for (int i = 0; i < 4; ++i)
-      if (d + i < a.D) o[i] = y[i];
-  }
+  store_quad<T>((T*)(blockIdx.y ? a.dv : a.dk) + b * st[0] + key * st[1] + hk * st[2], d, a.D, s);
 }
 
 // ---- host ---------------------------------------------------------------------------------------
@@ -825,8 +980,9 @@ gbmw_status check_sizes(const gbmw_attention_problem* p) {
   if (p->D < 1 || p->D > 128) return fail(GBMW_ERR_INVALID_ARG, "D=%d not in 1..128", p->D);
   const int64_t rows = (int64_t)p->Lq * (p->Hq / p->Hk);
   if (rows > INT_MAX - 256 || p->Lk > INT_MAX - 256) return fail(GBMW_ERR_INVALID_ARG, "too many rows");
+  // a launch has fewer than 2^32 threads, 2^24 workgroups of 256 (few tiles are shared by up to 64 of them)
   const int64_t groups = std::max((rows + 127) / 128, ((int64_t)p->Lk + 127) / 128) * p->Hk;
-  if (groups > INT_MAX || groups * p->B > INT_MAX) return fail(GBMW_ERR_INVALID_ARG, "too many rows in all");
+  if (groups >= 1 << 24 || groups * p->B >= 1 << 24) return fail(GBMW_ERR_INVALID_ARG, "too many rows in all");
   if (p->causal != 0 && p->causal != 1) return fail(GBMW_ERR_INVALID_ARG, "causal=%d", p->causal);
   if (!(p->scale >= 0.0f) || !std::isfinite(p->scale)) return fail(GBMW_ERR_INVALID_ARG, "scale=%g", (double)p->scale);
   return GBMW_OK;
@@ -869,7 +1025,7 @@ AttnArgs args_of(const gbmw_attention_problem* p) {
   }
   a.len_q = p->len_q, a.len_k = p->len_k;
   a.B = p->B, a.Hq = p->Hq, a.Hk = p->Hk, a.Lq = p->Lq, a.Lk = p->Lk, a.D = p->D, a.share = p->Hq / p->Hk;
-  a.D4 = (p->D + 3) / 4 * 4, a.parts = 1;
+  a.D4 = (p->D + 3) / 4 * 4;
   a.causal = p->causal, a.scale = p->scale;
   a.magic = (unsigned)(((1ull << 32) + a.share - 1) / a.share);
   // Without a causal mask units are alike, and four heads at a time (keys and values of a few MB)
@@ -881,53 +1037,84 @@ AttnArgs args_of(const gbmw_attention_problem* p) {
   return a;
 }
 
-// Shares that dk and dv are summed from: where the tiles of keys do not fill the chip a few times
-// over (under a causal mask they differ much in length), each tile's rows are dealt to several
-// workgroups, as long as each gets enough of them.
+constexpr int kSlots = 512;   // workgroups that the chip holds at a time (two a compute unit)
+
+// Workgroups that share a tile of keys in dk and dv: where the tiles do not fill the chip twice
+// over (under a causal mask they differ much in length), each tile's rows are dealt to several,
+// as long as each gets 512 of them.  2 x 40 heads x 2048 causal (1280 tiles): 405 us, in two parts
+// 287 + 77 to join them; 8 heads x 8192 (512 tiles of up to 32768 rows): 4.3 ms, in two parts 1.3.
 int parts_of(const gbmw_attention_problem* p) {
   const int64_t groups = (int64_t)p->B * p->Hk * ((p->Lk + 127) / 128), rows = (int64_t)p->Lq * (p->Hq / p->Hk);
   int parts = 1;
-  while (parts < 16 && groups * parts < GBMW_FILL && rows / (2 * parts) >= GBMW_LEAST) parts *= 2;
+  while (parts < 16 && groups * parts < 2 * kSlots && rows / (2 * parts) >= 512) parts *= 2;
   return parts;
 }
 
-// level and delta [B][Hk][rows], and for float16 gmax [B][Hk][tiles][4] and vmax [B][Hk][parts of 256 keys]
-struct Scratch {
-  int64_t rows, gmax, vmax, partial;   // floats
-  int parts;
-  int64_t bytes() const { return 4 * (2 * rows + gmax + vmax + partial); }
-};
-Scratch scratch_of(const gbmw_attention_problem* p) {
-  const int64_t groups = (int64_t)p->B * p->Hk, rows = (int64_t)p->Lq * (p->Hq / p->Hk);
-  const bool lift = p->dtype == GBMW_F16;
-  const int parts = parts_of(p);
-  auto padded = [](int64_t n) { return (n + 3) / 4 * 4; };
-  return {padded(groups * rows), padded(lift ? groups * ((rows + 127) / 128) * 4 : 0),
-          padded(lift ? groups * (((int64_t)p->Lk + 255) / 256) : 0),
-          parts > 1 ? parts * 2 * groups * p->Lk * ((p->D + 3) / 4 * 4) : 0, parts};
+bool few(const gbmw_attention_problem* p) { return (int64_t)p->Lq * (p->Hq / p->Hk) <= 32; }
+
+// Workgroups that share a tile of rows: as many as fill the chip, each with enough keys that
+// writing its share and reading it back (as much as two tiles of keys per 32 rows) is the less.
+int kparts_of(const gbmw_attention_problem* p, bool backward) {
+  const int64_t rows = (int64_t)p->Lq * (p->Hq / p->Hk), groups = (int64_t)p->B * p->Hk * ((rows + 127) / 128);
+  if (groups == 0) return 1;
+  const int64_t tiles = ((int64_t)p->Lk + 63) / 64, least = few(p) && !backward ? 8 : std::max<int64_t>(2, std::min<int64_t>(rows, 128) / 16);
+  const int64_t fill = few(p) && !backward ? kSlots / 2 : kSlots;
+  return (int)std::max<int64_t>(1, std::min({(fill + groups - 1) / groups, tiles / least, (int64_t)64}));
 }
 
-#ifndef GBMW_NQ
-#define GBMW_NQ 1
-#endif
+// The forward call's workspace: shares and tops.  The backward call's: level and delta
+// [B][Hk][rows], for float16 gmax [B][Hk][tiles][4] and vmax [B][Hk][parts of 256 keys], and
+// shares and tops, or the shares of dk and dv after them.
+struct Scratch {
+  int64_t rows, gmax, vmax, shares, tops, partial;   // floats
+  int parts, kparts;
+  int64_t bytes() const { return 4 * (2 * rows + gmax + vmax + std::max(shares + tops, partial)); }
+};
+Scratch scratch_of(const gbmw_attention_problem* p, bool backward) {
+  const int64_t groups = (int64_t)p->B * p->Hk, rows = (int64_t)p->Lq * (p->Hq / p->Hk), D4 = (p->D + 3) / 4 * 4;
+  const bool lift = backward && p->dtype == GBMW_F16;
+  auto padded = [](int64_t n) { return (n + 3) / 4 * 4; };
+  Scratch s{};
+  s.kparts = kparts_of(p, backward), s.parts = backward ? parts_of(p) : 1;
+  s.rows = backward ? padded(groups * rows) : 0;
+  s.gmax = padded(lift ? groups * ((rows + 127) / 128) * 4 : 0);
+  s.vmax = padded(lift ? groups * (((int64_t)p->Lk + 255) / 256) : 0);
+  if (s.kparts > 1) s.shares = s.kparts * groups * rows * D4, s.tops = padded(s.kparts * groups * rows);
+  if (s.parts > 1) s.partial = s.parts * 2 * groups * p->Lk * D4;
+  return s;
+}
+
+void place_scratch(AttnArgs& a, const Scratch& s, void* workspace) {
+  a.level = (float*)workspace, a.delta = a.level + s.rows, a.gmax = a.delta + s.rows, a.vmax = a.gmax + s.gmax;
+  a.shares = a.partial = a.vmax + s.vmax, a.tops = a.shares + s.shares;
+  a.parts = s.parts, a.kparts = s.kparts;
+}
+
 template <typename T, int KS, bool DIRECT>
 void launch(const AttnArgs& a, bool backward, hipStream_t st) {
   const int64_t rows = (int64_t)a.Lq * a.share, groups = (int64_t)a.Hk * a.B;
-  const dim3 grid_q((unsigned)((rows + 127) / 128 * groups)), grid_k((unsigned)(((int64_t)a.Lk + 127) / 128 * groups));
+  auto grid = [&](int64_t n, int per) { return dim3((unsigned)((n + per - 1) / per * groups)); };
+  auto times = [](dim3 g, int n) { return dim3(g.x * n); };
+  const dim3 block(256), merge = dim3((unsigned)((rows * groups * (a.D4 / 4) + 255) / 256));
   if (!backward) {
-    constexpr int NQ = GBMW_NQ;
-    hipLaunchKernelGGL((k_attn_fwd<T, KS, NQ, DIRECT>), dim3((unsigned)((rows + 128 * NQ - 1) / (128 * NQ) * groups)),
-                       dim3(256), 0, st, a);
+    if (rows <= 32)
+      hipLaunchKernelGGL((k_attn_few<T, KS, DIRECT>), times(grid(rows, 32), a.kparts), block, 0, st, a);
+    else
+      hipLaunchKernelGGL((k_attn_fwd<T, KS, DIRECT>), times(grid(rows, 128), a.kparts), block, 0, st, a);
+    if (a.kparts > 1) hipLaunchKernelGGL((k_attn_merge<T, false>), merge, block, 0, st, a);
     return;
   }
   if constexpr (__is_same(T, f16))
-    if (a.Lk) hipLaunchKernelGGL(k_attn_vmax, dim3((unsigned)(((int64_t)a.Lk + 255) / 256 * groups)), dim3(256), 0, st, a);
-  if (grid_q.x) hipLaunchKernelGGL((k_attn_dq<T, KS, DIRECT>), grid_q, dim3(256), 0, st, a);
-  if (!grid_k.x) return;
-  hipLaunchKernelGGL((k_attn_dkv<T, KS, DIRECT>), dim3(grid_k.x * a.parts), dim3(256), 0, st, a);
+    if (a.Lk) hipLaunchKernelGGL(k_attn_vmax, grid(a.Lk, 256), block, 0, st, a);
+  if (rows) {
+    hipLaunchKernelGGL((k_attn_dq<T, KS, DIRECT>), times(grid(rows, 128), a.kparts), block, 0, st, a);
+    if (a.kparts > 1) hipLaunchKernelGGL((k_attn_merge<T, true>), merge, block, 0, st, a);
+  }
+  if (!a.Lk) return;
+  hipLaunchKernelGGL((k_attn_dkv<T, KS, DIRECT>), times(grid(a.Lk, 128), a.parts), block, 0, st, a);
   if (a.parts > 1) {
     const int64_t quads = groups * a.Lk * (a.D4 / 4);
-    hipLaunchKernelGGL(k_attn_join<T>, dim3((unsigned)((quads + 255) / 256), 2), dim3(256), 0, st, a);
+    hipLaunchKernelGGL(k_attn_join<T>, dim3((unsigned)((quads + 255) / 256), 2), block, 0, st, a);
   }
 }
 
@@ -960,10 +1147,23 @@ void launch(const AttnArgs& a, bool backward, hipStream_t st) {
 
 using namespace gbmw;
 
+static gbmw_status run(const gbmw_attention_problem* p, bool backward) {
+  const Scratch sc = scratch_of(p, backward);
+  const int64_t need = sc.bytes();
+  if (need && (!p->workspace || p->workspace_bytes < need || (uintptr_t)p->workspace % 16))
+    return fail(GBMW_ERR_INVALID_ARG, "workspace of %lld bytes, 16-byte aligned, is needed", (long long)need);
+  AttnArgs a = args_of(p);
+  place_scratch(a, sc, p->workspace);
+  if (p->dtype == GBMW_F16) launch<f16>(a, backward, (hipStream_t)p->stream);
+  else launch<bf16>(a, backward, (hipStream_t)p->stream);
+  HIP_TRY(hipGetLastError());
+  return GBMW_OK;
+}
+
 extern "C" int64_t gbmw_attention_workspace(const gbmw_attention_problem* p, int32_t backward) {
   gbmw_detail::clear_error();
   if (check_sizes(p) != GBMW_OK) return -1;
-  return backward ? scratch_of(p).bytes() : 0;
+  return scratch_of(p, backward != 0).bytes();
 }
 
 extern "C" gbmw_status gbmw_attention_forward(const gbmw_attention_problem* p) {
@@ -971,11 +1171,7 @@ extern "C" gbmw_status gbmw_attention_forward(const gbmw_attention_problem* p) {
   const gbmw_status st = check_common(p, false);
   if (st != GBMW_OK) return st;
   if (p->B == 0 || p->Lq == 0) return GBMW_OK;
-  const AttnArgs a = args_of(p);
-  if (p->dtype == GBMW_F16) launch<f16>(a, false, (hipStream_t)p->stream);
-  else launch<bf16>(a, false, (hipStream_t)p->stream);
-  HIP_TRY(hipGetLastError());
-  return GBMW_OK;
+  return run(p, false);
 }
 
 extern "C" gbmw_status gbmw_attention_backward(const gbmw_attention_problem* p) {
@@ -987,15 +1183,5 @@ extern "C" gbmw_status gbmw_attention_backward(const gbmw_attention_problem* p) 
   if (st == GBMW_OK) st = check_array("dv", p->dv, p->dv_stride, p->Lk, true, p, p->Hk);
   if (st != GBMW_OK) return st;
   if (p->B == 0 || (p->Lq == 0 && p->Lk == 0)) return GBMW_OK;
-  const Scratch sc = scratch_of(p);
-  const int64_t need = sc.bytes();
-  if (need && (!p->workspace || p->workspace_bytes < need || (uintptr_t)p->workspace % 16))
-    return fail(GBMW_ERR_INVALID_ARG, "workspace of %lld bytes, 16-byte aligned, is needed", (long long)need);
-  AttnArgs a = args_of(p);
-  a.level = (float*)p->workspace, a.delta = a.level + sc.rows, a.gmax = a.delta + sc.rows, a.vmax = a.gmax + sc.gmax;
-  a.partial = a.vmax + sc.vmax, a.parts = sc.parts;
-  if (p->dtype == GBMW_F16) launch<f16>(a, true, (hipStream_t)p->stream);
-  else launch<bf16>(a, true, (hipStream_t)p->stream);
-  HIP_TRY(hipGetLastError());
-  return GBMW_OK;
+  return run(p, true);
 }

@@ -277,3 +277,24 @@ def test_small_gradients_keep_their_digits(dtype):
         # two roundings of half an ulp at most, and the outputs' own steps (dk in float16 is below its normal numbers)
         steps = ref.TINY[dtype] * value.numel() ** 0.5 / value.norm()
         assert off <= 2 * ref.U[dtype] + steps, (n, float(off))
+
+
+@pytest.mark.parametrize("dtype", [torch.float16, torch.bfloat16], ids=["f16", "bf16"])
+@pytest.mark.parametrize("B,Lq,Lk,Hq,Hk,D", [(1, 1, 5000, 8, 2, 128), (2, 1, 4097, 4, 4, 64), (1, 8, 3001, 8, 2, 80), (3, 5, 700, 6, 6, 40),
+                                             (1, 33, 2500, 2, 2, 96), (1, 200, 1700, 2, 1, 64), (1, 1, 1100, 3, 1, 17),
+                                             (1, 32, 6000, 1, 1, 128), (1, 40, 1300, 1, 1, 127)])
+def test_few_rows_and_many_keys(B, Lq, Lk, Hq, Hk, D, dtype):
+    """Where several workgroups, and several waves of one, share the keys of a row."""
+    q, k, v, dout = _inputs(B, Lq, Lk, Hq, Hk, D, dtype, seed=Lk)
+    _check(q, k, v, dout)
+    _check(q, k, v, dout, causal=True)
+    nk = torch.tensor([Lk - 70, 3, 0][:B], dtype=torch.int32, device="cuda")
+    nq = torch.tensor([Lq, max(1, Lq - 1), Lq][:B], dtype=torch.int32, device="cuda")
+    _check(q, k, v, dout, causal=True, len_q=nq, len_k=nk)
+
+
+@pytest.mark.parametrize("causal", [False, True], ids=["full", "causal"])
+def test_few_keys_and_many_rows(causal):
+    """Where several workgroups share the rows that see a key."""
+    _check(*_inputs(1, 2100, 130, 2, 1, 64, torch.bfloat16, seed=91), causal=causal)
+    _check(*_inputs(1, 1500, 1500, 4, 1, 40, torch.float16, seed=92), causal=causal)
