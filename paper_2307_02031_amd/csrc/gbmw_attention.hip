@@ -39,7 +39,7 @@ struct AttnArgs {
   char *out, *dq, *dk, *dv;
   float *lse;
   float *level, *delta;   // [B][Hk][rows]: log2(e) lse - kUp, inf for rows without keys; <dout, out>
-  float *vmax, *gmax;   // f16: the largest norms of a value and of a row of dout, for parts of 256 keys and 128 rows
+  float *vmax, *gmax;   // f16: the largest norms of a value and of a row of dout, for parts of 64 keys and 32 rows
   int64_t qs[3], ks[3], vs[3], os[3], dos[3], dqs[3], dks[3], dvs[3];
   const int *len_q, *len_k;
   float* partial;   // [parts][2][B][Hk][Lk][D4]: shares of dk and dv
@@ -343,7 +343,8 @@ struct Place {
     nq = length(a.len_q, b, a.Lq), nk = length(a.len_k, b, a.Lk);
     const int first = tile * per / a.share, last = min((min(tile * per + per, rows) - 1) / a.share, nq - 1);
     most = first >= nq ? 0 : sees(a, last);
-    const int run = ((most + 63) / 64 + a.kparts - 1) / a.kparts * 64;
+    // up to two tiles stay together
+    const int run = most <= 128 ? 128 : ((most + 63) / 64 + a.kparts - 1) / a.kparts * 64;
     begin = min(part * run, most), end = min(begin + run, most);
   }
   __device__ __forceinline__ int sees(const AttnArgs& a, int i) const {   // keys j < sees
@@ -651,17 +652,17 @@ __global__ __launch_bounds__(256) void k_attn_merge(AttnArgs a) {
   }
 }
 
-// The largest norm of a value among 256 keys of a (sample, key head), for float16's lift.
+// The largest norm of a value among 64 keys of a (sample, key head), for float16's lift.
 __global__ __launch_bounds__(256) void k_attn_vmax(AttnArgs a) {
   __shared__ float tops[4];
-  const int parts = (a.Lk + 255) / 256, part = blockIdx.x % parts;
+  const int parts = (a.Lk + 63) / 64, part = blockIdx.x % parts;
   const int hk = blockIdx.x / parts % a.Hk, b = blockIdx.x / parts / a.Hk;
   // sixteen lanes a row, a piece each
-  const int last = min(part * 256 + 256, length(a.len_k, b, a.Lk)), d = threadIdx.x % 16 * 8;
+  const int last = min(part * 64 + 64, length(a.len_k, b, a.Lk)), d = threadIdx.x % 16 * 8;
   const f16* v = (const f16*)a.v + b * a.vs[0] + hk * a.vs[2] + d;
   float s = 0.0f;
 #pragma unroll 4
-  for (int key = part * 256 + threadIdx.x / 16; key < last; key += 16) {
+  for (int key = part * 64 + threadIdx.x / 16; key < last; key += 16) {
     const Pack<f16> x = load_pack(v + key * a.vs[1], a.D - d);
     float n = 0.0f;
 #pragma unroll
@@ -726,8 +727,8 @@ __global__ __launch_bounds__(256, 2) void k_attn_dq(AttnArgs a) {
   float up = 1.0f, down = 1.0f;   // powers of two
   if constexpr (kLift) {
     norm = __builtin_sqrtf(norm + __shfl_xor(norm, 32));
-    const int parts = (a.Lk + 255) / 256;
-    const int k = lift_of(norm * max_of(a.vmax + ((int64_t)b * a.Hk + hk) * parts, (nk + 255) / 256));
+    const int parts = (a.Lk + 63) / 64;
+    const int k = lift_of(norm * max_of(a.vmax + ((int64_t)b * a.Hk + hk) * parts, (nk + 63) / 64));
     up = __builtin_ldexpf(1.0f, k), down = __builtin_ldexpf(1.0f, -k);
     float top = norm;
 #pragma unroll
@@ -741,8 +742,9 @@ __global__ __launch_bounds__(256, 2) void k_attn_dq(AttnArgs a) {
   lk.init(kr, a.D), lv.init(vr, a.D);
   // The score gradients of a row add up to 0: what their sum leaves over is delta's error, the
   // rounding of `out`.  The other kernel gets the corrected delta.  Here it matters where few
-  // keys share a row, and there (one tile) a first pass finds it.
-  for (int pass = w.most > 64; pass < 2; ++pass) {
+  // keys share a row, and there (one tile, or the first rows of a causal mask) a first pass finds it.
+  const bool small = w.most <= (a.causal ? 128 : 64);
+  for (int pass = !small; pass < 2; ++pass) {
     left = 0.0f;
     if (w.begin < w.end) {
       lk.begin(tiles, kr, w.begin, a.D);
@@ -852,9 +854,9 @@ __global__ __launch_bounds__(256, 2) void k_attn_dkv(AttnArgs a) {
 
   float up = 1.0f, down = 1.0f;   // of score gradients, beyond kUp
   if constexpr (__is_same(T, f16)) {
-    const int parts = (a.Lk + 255) / 256, gparts = (a.Lq * a.share + 127) / 128 * 4;
+    const int parts = (a.Lk + 63) / 64, gparts = (a.Lq * a.share + 127) / 128 * 4;
     const int lift = lift_of(max_of(a.gmax + ((int64_t)b * a.Hk + hk) * gparts, gparts) *
-                             max_of(a.vmax + ((int64_t)b * a.Hk + hk) * parts, (nk + 255) / 256));
+                             max_of(a.vmax + ((int64_t)b * a.Hk + hk) * parts, (nk + 63) / 64));
     up = __builtin_ldexpf(1.0f, lift - (int)kUp<T>), down = __builtin_ldexpf(1.0f, -lift);
   }
   const Reader<KS> rd;
@@ -1063,7 +1065,7 @@ int kparts_of(const gbmw_attention_problem* p, bool backward) {
 }
 
 // The forward call's workspace: shares and tops.  The backward call's: level and delta
-// [B][Hk][rows], for float16 gmax [B][Hk][tiles][4] and vmax [B][Hk][parts of 256 keys], and
+// [B][Hk][rows], for float16 gmax [B][Hk][tiles][4] and vmax [B][Hk][parts of 64 keys], and
 // shares and tops, or the shares of dk and dv after them.
 struct Scratch {
   int64_t rows, gmax, vmax, shares, tops, partial;   // floats
@@ -1078,7 +1080,7 @@ Scratch scratch_of(const gbmw_attention_problem* p, bool backward) {
   s.kparts = kparts_of(p, backward), s.parts = backward ? parts_of(p) : 1;
   s.rows = backward ? padded(groups * rows) : 0;
   s.gmax = padded(lift ? groups * ((rows + 127) / 128) * 4 : 0);
-  s.vmax = padded(lift ? groups * (((int64_t)p->Lk + 255) / 256) : 0);
+  s.vmax = padded(lift ? groups * (((int64_t)p->Lk + 63) / 64) : 0);
   if (s.kparts > 1) s.shares = s.kparts * groups * rows * D4, s.tops = padded(s.kparts * groups * rows);
   if (s.parts > 1) s.partial = s.parts * 2 * groups * p->Lk * D4;
   return s;
@@ -1105,7 +1107,7 @@ void launch(const AttnArgs& a, bool backward, hipStream_t st) {
     return;
   }
   if constexpr (__is_same(T, f16))
-    if (a.Lk) hipLaunchKernelGGL(k_attn_vmax, grid(a.Lk, 256), block, 0, st, a);
+    if (a.Lk) hipLaunchKernelGGL(k_attn_vmax, grid(a.Lk, 64), block, 0, st, a);
   if (rows) {
     hipLaunchKernelGGL((k_attn_dq<T, KS, DIRECT>), times(grid(rows, 128), a.kparts), block, 0, st, a);
     if (a.kparts > 1) hipLaunchKernelGGL((k_attn_merge<T, true>), merge, block, 0, st, a);
