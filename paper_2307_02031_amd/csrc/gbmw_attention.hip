@@ -34,6 +34,25 @@ typedef short s16x8 __attribute__((ext_vector_type(8)));
 typedef f16 f16x8 __attribute__((ext_vector_type(8)));
 typedef bf16 bf16x8 __attribute__((ext_vector_type(8)));
 
+// Division of 0 <= n < 2^31 by a number the host knows, without the dozens of instructions that a
+// division is.
+struct Divisor {
+  int d;
+  unsigned magic;   // 2^32 / d, rounded up (0 for 1)
+  __device__ __forceinline__ int of(int n) const {
+    if (d == 1) return n;
+    const unsigned x = __umulhi((unsigned)n, magic);   // at most one too large
+    return (int)(x * (unsigned)d > (unsigned)n ? x - 1 : x);
+  }
+};
+Divisor divisor(int64_t d) { return {(int)d, (unsigned)(((1ull << 32) + d - 1) / d)}; }
+
+// Which head and which of its `units` pieces of work a workgroup takes: see Deal.
+struct Plan {
+  int per, units, near, last;   // heads of a die, units of a head, heads at a time, the first of the last heads
+  Divisor of_near, near_units, of_last, of_rest;
+};
+
 struct AttnArgs {
   const char *q, *k, *v, *dout;
   char *out, *dq, *dk, *dv;
@@ -43,12 +62,12 @@ struct AttnArgs {
   int64_t qs[3], ks[3], vs[3], os[3], dos[3], dqs[3], dks[3], dvs[3];
   const int *len_q, *len_k;
   float* partial;   // [parts][2][B][Hk][Lk][D4]: shares of dk and dv
-  int B, Hq, Hk, Lq, Lk, D, share, causal;
+  Plan by_rows, by_keys;
+  Divisor share, heads_k, parts_d, kparts_d;   // query heads of a key head; Hk, parts, kparts
+  int B, Hq, Hk, Lq, Lk, D, causal;
   float *shares, *tops;   // [kparts][B][Hk][rows][D4] and [kparts][B][Hk][rows]: of out (or dq) and of what goes with it
   int parts, kparts;      // workgroups that share a tile of keys, or a tile of rows
   int D4;                 // D rounded up to 4
-  int near;         // heads that a die works on at a time
-  unsigned magic;   // 2^32 / share, rounded up
   float c;       // scale * log2(e): probabilities are powers of two
   float scale;
 };
@@ -145,13 +164,8 @@ __device__ __forceinline__ s16x8 load8(const char* row, int piece, int D, bool t
 struct Rows {
   const char* base;
   int64_t stride, head;   // bytes
-  int share, count;       // rows beyond count read as zeros
-  unsigned magic;         // 2^32 / share, rounded up
-  __device__ __forceinline__ int of(int r) const {   // r / share
-    if (share == 1) return r;
-    int x = (int)__umulhi((unsigned)r, magic);   // at most one too large for r < 2^31
-    return x * share > r ? x - 1 : x;
-  }
+  Divisor share;
+  int count;              // rows beyond count read as zeros
 };
 
 // Brings 64 rows into a tile, in two halves: begin() before the tile before it is worked on,
@@ -187,14 +201,14 @@ struct Loader {
       for (int i = 0; i < NA; ++i) {
         const int piece = ((int)threadIdx.x % CH) ^ swap_of<CH>(row_of(i));
         const int down = kOne ? (int)(threadIdx.x % 64) / CH : row_of(i);
-        at[i] = 8 * piece >= D ? kOut : 16 * piece + (rows.share == 1 ? down * (unsigned)rows.stride : 0u);
+        at[i] = 8 * piece >= D ? kOut : 16 * piece + (rows.share.d == 1 ? down * (unsigned)rows.stride : 0u);
       }
     }
   }
 
   __device__ __forceinline__ void begin(lds_char* tile, const Rows& rows, int first, int D) {
     if constexpr (DIRECT) {
-      if (rows.share == 1) {   // rows beyond the last one are beyond the bounds
+      if (rows.share.d == 1) {   // rows beyond the last one are beyond the bounds
         const int64_t length = (int64_t)(rows.count - first) * rows.stride;
         const int left = (int)min(length, (int64_t)0x7fffffff), run = kRowsOf * (int)rows.stride;
         const char* base = rows.base + first * rows.stride;
@@ -205,14 +219,14 @@ struct Loader {
           load(tile, __builtin_amdgcn_make_buffer_rsrc((void*)(base + off), 0, max(left - off, 0), 0x00020000), i, at[i % NA]);
         }
       } else {
-        const int x0 = rows.of(first);
+        const int x0 = rows.share.of(first);
         __amdgpu_buffer_rsrc_t from =
             __builtin_amdgcn_make_buffer_rsrc((void*)(rows.base + x0 * rows.stride), 0, 0x7fffffff, 0x00020000);
 #pragma unroll
         for (int i = 0; i < N; ++i) {
-          const int r = first + row_of(i), x = rows.of(r);
+          const int r = first + row_of(i), x = rows.share.of(r);
           load(tile, from, i, (r >= rows.count) | (at[i % NA] == kOut) ? kOut
-                                  : at[i % NA] + (unsigned)(x - x0) * (unsigned)rows.stride + (unsigned)(r - x * rows.share) * (unsigned)rows.head);
+                                  : at[i % NA] + (unsigned)(x - x0) * (unsigned)rows.stride + (unsigned)(r - x * rows.share.d) * (unsigned)rows.head);
         }
       }
     } else {
@@ -220,8 +234,8 @@ struct Loader {
       for (int i = 0; i < N; ++i) {
         const int n = thread() + THREADS * i, r = first + n / (2 * KS);
         const bool there = n < ROWS * 2 * KS && r < rows.count;
-        const int q = there ? r : first, h = rows.of(q);
-        x[i] = load8<false>(rows.base + h * rows.stride + (q - h * rows.share) * rows.head, n % (2 * KS), D, there);
+        const int q = there ? r : first, h = rows.share.of(q);
+        x[i] = load8<false>(rows.base + h * rows.stride + (q - h * rows.share.d) * rows.head, n % (2 * KS), D, there);
       }
     }
   }
@@ -308,23 +322,31 @@ __device__ __forceinline__ void store_share(float* row, int D4, const f32x16 (&x
     }
 }
 
-// Which head and which of its `units` pieces of work a workgroup takes.  Workgroups are dealt to
-// the eight dies in turn.  A die works on its own heads, `near` of them at a time, so that what
-// their units read alike stays in its cache; of those the first units (the longest under a
-// causal mask) come first.  Heads that eight does not divide are dealt to all dies at the end.
+// Which head and which of its units a workgroup takes.  Workgroups are dealt to the eight dies in
+// turn.  A die works on its own heads, `near` of them at a time, so that what their units read
+// alike stays in its cache; of those the first units (the longest under a causal mask) come first.
+// Heads that eight does not divide are dealt to all dies at the end.
 struct Deal {
   int head, unit;
-  __device__ __forceinline__ Deal(int heads, int units, int near) {
-    const int per = heads / 8, id = blockIdx.x;
-    near = min(near, max(per, 1));
-    if (id < 8 * per * units) {
-      const int at = id / 8, first = at / (near * units) * near, n = min(near, per - first);
-      unit = (at - first * units) / n;
-      head = id % 8 * per + first + (at - first * units) % n;
+  __device__ __forceinline__ Deal(const Plan& p) {
+    const int id = blockIdx.x;
+    if (id < 8 * p.per * p.units) {
+      const int at = id / 8;
+      int first = p.last, in = at - p.last * p.units;
+      if (in >= 0) {
+        unit = p.of_last.of(in);
+        in -= unit * p.of_last.d;
+      } else {
+        first = p.near_units.of(at) * p.near;
+        in = at - first * p.units;
+        unit = p.of_near.of(in);
+        in -= unit * p.near;
+      }
+      head = id % 8 * p.per + first + in;
     } else {
-      const int n = heads - 8 * per, at = id - 8 * per * units;
-      unit = at / n;
-      head = 8 * per + at % n;
+      const int at = id - 8 * p.per * p.units;
+      unit = p.of_rest.of(at);
+      head = 8 * p.per + at - unit * p.of_rest.d;
     }
   }
 };
@@ -334,17 +356,18 @@ struct Deal {
 struct Place {
   int tile, tiles, part, hk, b, nq, nk, rows, most, begin, end;
   __device__ __forceinline__ Place(const AttnArgs& a, int per) {
-    rows = a.Lq * a.share;
+    rows = a.Lq * a.share.d;
     tiles = (rows + per - 1) / per;
-    const Deal d(a.Hk * a.B, tiles * a.kparts, a.near);
-    tile = tiles - 1 - d.unit / a.kparts;   // the longest rows of a causal mask first
-    part = d.unit % a.kparts;
-    hk = d.head % a.Hk, b = d.head / a.Hk;
+    const Deal d(a.by_rows);
+    const int at = a.kparts_d.of(d.unit);
+    tile = tiles - 1 - at;   // the longest rows of a causal mask first
+    part = d.unit - at * a.kparts;
+    b = a.heads_k.of(d.head), hk = d.head - b * a.Hk;
     nq = length(a.len_q, b, a.Lq), nk = length(a.len_k, b, a.Lk);
-    const int first = tile * per / a.share, last = min((min(tile * per + per, rows) - 1) / a.share, nq - 1);
+    const int first = a.share.of(tile * per), last = min(a.share.of(min(tile * per + per, rows) - 1), nq - 1);
     most = first >= nq ? 0 : sees(a, last);
     // up to two tiles stay together
-    const int run = most <= 128 ? 128 : ((most + 63) / 64 + a.kparts - 1) / a.kparts * 64;
+    const int run = most <= 128 ? 128 : a.kparts_d.of((most + 63) / 64 + a.kparts - 1) * 64;
     begin = min(part * run, most), end = min(begin + run, most);
   }
   __device__ __forceinline__ int sees(const AttnArgs& a, int i) const {   // keys j < sees
@@ -443,10 +466,10 @@ __global__ __launch_bounds__(256, 2) void k_attn_fwd(AttnArgs a) {
   lds_char* const tiles = (lds_char*)lds;
   const Place w(a, 128);
   const int l = threadIdx.x % 64, half = l / 32, row = w.tile * 128 + (threadIdx.x / 64) * 32 + l % 32;
-  const int i = row / a.share, hq = w.hk * a.share + row % a.share;
+  const int i = a.share.of(row), hq = (w.hk - i) * a.share.d + row;
   const int sees = w.sees(a, i);
-  const Rows kr{a.k + 2 * (w.b * a.ks[0] + w.hk * a.ks[2]), 2 * a.ks[1], 0, 1, w.nk, 0};
-  const Rows vr{a.v + 2 * (w.b * a.vs[0] + w.hk * a.vs[2]), 2 * a.vs[1], 0, 1, w.nk, 0};
+  const Rows kr{a.k + 2 * (w.b * a.ks[0] + w.hk * a.ks[2]), 2 * a.ks[1], 0, {1, 0}, w.nk};
+  const Rows vr{a.v + 2 * (w.b * a.vs[0] + w.hk * a.vs[2]), 2 * a.vs[1], 0, {1, 0}, w.nk};
 
   s16x8 q[KS];
   const char* qrow = a.q + 2 * (w.b * a.qs[0] + (i < w.nq ? i : 0) * a.qs[1] + hq * a.qs[2]);
@@ -525,10 +548,10 @@ __global__ __launch_bounds__(256, 1) void k_attn_few(AttnArgs a) {
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
   lds_char* const tiles = (lds_char*)lds + wave * kWave;
   const int l = threadIdx.x % 64, half = l / 32, row = l % 32;
-  const int i = row / a.share, hq = w.hk * a.share + row % a.share;
+  const int i = a.share.of(row), hq = (w.hk - i) * a.share.d + row;
   const int sees = row < w.rows ? w.sees(a, i) : INT_MAX;   // rows that are not there need no mask
-  const Rows kr{a.k + 2 * (w.b * a.ks[0] + w.hk * a.ks[2]), 2 * a.ks[1], 0, 1, w.nk, 0};
-  const Rows vr{a.v + 2 * (w.b * a.vs[0] + w.hk * a.vs[2]), 2 * a.vs[1], 0, 1, w.nk, 0};
+  const Rows kr{a.k + 2 * (w.b * a.ks[0] + w.hk * a.ks[2]), 2 * a.ks[1], 0, {1, 0}, w.nk};
+  const Rows vr{a.v + 2 * (w.b * a.vs[0] + w.hk * a.vs[2]), 2 * a.vs[1], 0, {1, 0}, w.nk};
 
   s16x8 q[KS];
   const bool there = row < w.rows && i < w.nq;
@@ -595,7 +618,7 @@ __global__ __launch_bounds__(256, 1) void k_attn_few(AttnArgs a) {
   }
   const bool empty = top == -kInf && !(sum != sum);
   const float level = empty ? -kInf : top + __builtin_amdgcn_logf(sum), inv = empty ? 0.0f : 1.0f / sum;
-  const int oi = out_row / a.share, oh = w.hk * a.share + out_row % a.share;
+  const int oi = a.share.of(out_row), oh = (w.hk - oi) * a.share.d + out_row;
   const int64_t at = w.share_of(a, out_row);
   if (threadIdx.x % 8 == 0) {
     if (a.kparts == 1) a.lse[((int64_t)w.b * a.Hq + oh) * a.Lq + oi] = level * kLn2;
@@ -619,13 +642,13 @@ __global__ __launch_bounds__(256, 1) void k_attn_few(AttnArgs a) {
 // out and lse, or dq and delta, from the parts' shares: four values a thread, in the parts' order.
 template <typename T, bool BACKWARD>
 __global__ __launch_bounds__(256) void k_attn_merge(AttnArgs a) {
-  const int64_t rows = (int64_t)a.Lq * a.share, all = rows * a.Hk * a.B;
+  const int64_t rows = (int64_t)a.Lq * a.share.d, all = rows * a.Hk * a.B;
   const int64_t n = (int64_t)blockIdx.x * 256 + threadIdx.x, at = n / (a.D4 / 4);
   if (at >= all) return;
   const int d = (int)(n % (a.D4 / 4)) * 4;
   const int64_t head = at / rows;
-  const int row = (int)(at - head * rows), i = row / a.share, hk = (int)(head % a.Hk), b = (int)(head / a.Hk);
-  const int hq = hk * a.share + row - i * a.share;
+  const int row = (int)(at - head * rows), i = a.share.of(row), hk = (int)(head % a.Hk), b = (int)(head / a.Hk);
+  const int hq = (hk - i) * a.share.d + row;
   f32x4 o = {};
   float top = -kInf, sum = 0.0f;
   if constexpr (!BACKWARD)
@@ -691,11 +714,11 @@ __global__ __launch_bounds__(256, 2) void k_attn_dq(AttnArgs a) {
   lds_char* const tiles = (lds_char*)lds;
   const Place w(a, 128);
   const int l = threadIdx.x % 64, half = l / 32, row = w.tile * 128 + (threadIdx.x / 64) * 32 + l % 32;
-  const int i = row / a.share, hq = w.hk * a.share + row % a.share;
+  const int i = a.share.of(row), hq = (w.hk - i) * a.share.d + row;
   const int b = w.b, hk = w.hk, nq = w.nq, nk = w.nk, rows = w.rows;
   const int sees = w.sees(a, i);
-  const Rows kr{a.k + 2 * (b * a.ks[0] + hk * a.ks[2]), 2 * a.ks[1], 0, 1, nk, 0};
-  const Rows vr{a.v + 2 * (b * a.vs[0] + hk * a.vs[2]), 2 * a.vs[1], 0, 1, nk, 0};
+  const Rows kr{a.k + 2 * (b * a.ks[0] + hk * a.ks[2]), 2 * a.ks[1], 0, {1, 0}, nk};
+  const Rows vr{a.v + 2 * (b * a.vs[0] + hk * a.vs[2]), 2 * a.vs[1], 0, {1, 0}, nk};
 
   s16x8 q[KS], g[KS];
   float delta = 0.0f, lse = kInf, norm = 0.0f;
@@ -824,24 +847,24 @@ __global__ __launch_bounds__(256, 2) void k_attn_dkv(AttnArgs a) {
   lds_char* const buffers = (lds_char*)lds;
   __shared__ __attribute__((aligned(16))) float sRow[2][2][64];   // level, delta
   const int heads = a.Hk * a.B;
-  const Deal deal(heads, (a.Lk + 127) / 128 * a.parts, a.near);
-  const int part = deal.unit % a.parts, tile = deal.unit / a.parts;   // the keys that most rows see first
-  const int hk = deal.head % a.Hk, b = deal.head / a.Hk;
+  const Deal deal(a.by_keys);
+  const int tile = a.parts_d.of(deal.unit), part = deal.unit - tile * a.parts;   // the keys that most rows see first
+  const int b = a.heads_k.of(deal.head), hk = deal.head - b * a.Hk;
   const int nq = length(a.len_q, b, a.Lq), nk = length(a.len_k, b, a.Lk);
   const int l = threadIdx.x % 64, half = l / 32, key0 = tile * 128 + (threadIdx.x / 64) * 32;
   const int key = key0 + l % 32;
-  const int rows = nq * a.share;
+  const int rows = nq * a.share.d;
   // the first row that sees key j
-  auto first_of = [&](int j) { return a.causal ? max(0, j - (nk - nq)) * a.share : 0; };
+  auto first_of = [&](int j) { return a.causal ? max(0, j - (nk - nq)) * a.share.d : 0; };
   const int first = first_of(key);
   // the rows that see a key of the tile, in `parts` runs of whole tiles
   int begin = tile * 128 < nk ? min(first_of(tile * 128) / 64 * 64, rows) : rows;
-  const int run = ((rows - begin + 63) / 64 + a.parts - 1) / a.parts * 64;
+  const int run = a.parts_d.of((rows - begin + 63) / 64 + a.parts - 1) * 64;
   begin = min((int64_t)begin + (int64_t)part * run, (int64_t)rows);
   const int end = min((int64_t)begin + run, (int64_t)rows);
-  const Rows qr{a.q + 2 * (b * a.qs[0] + (int64_t)hk * a.share * a.qs[2]), 2 * a.qs[1], 2 * a.qs[2], a.share, rows, a.magic};
-  const Rows gr{a.dout + 2 * (b * a.dos[0] + (int64_t)hk * a.share * a.dos[2]), 2 * a.dos[1], 2 * a.dos[2], a.share, rows, a.magic};
-  const int64_t row0 = ((int64_t)b * a.Hk + hk) * a.Lq * a.share;
+  const Rows qr{a.q + 2 * (b * a.qs[0] + (int64_t)hk * a.share.d * a.qs[2]), 2 * a.qs[1], 2 * a.qs[2], a.share, rows};
+  const Rows gr{a.dout + 2 * (b * a.dos[0] + (int64_t)hk * a.share.d * a.dos[2]), 2 * a.dos[1], 2 * a.dos[2], a.share, rows};
+  const int64_t row0 = ((int64_t)b * a.Hk + hk) * a.Lq * a.share.d;
 
   s16x8 k[KS], v[KS];
 #pragma unroll
@@ -854,7 +877,7 @@ __global__ __launch_bounds__(256, 2) void k_attn_dkv(AttnArgs a) {
 
   float up = 1.0f, down = 1.0f;   // of score gradients, beyond kUp
   if constexpr (__is_same(T, f16)) {
-    const int parts = (a.Lk + 63) / 64, gparts = (a.Lq * a.share + 127) / 128 * 4;
+    const int parts = (a.Lk + 63) / 64, gparts = (a.Lq * a.share.d + 127) / 128 * 4;
     const int lift = lift_of(max_of(a.gmax + ((int64_t)b * a.Hk + hk) * gparts, gparts) *
                              max_of(a.vmax + ((int64_t)b * a.Hk + hk) * parts, (nk + 63) / 64));
     up = __builtin_ldexpf(1.0f, lift - (int)kUp<T>), down = __builtin_ldexpf(1.0f, -lift);
@@ -1026,14 +1049,10 @@ AttnArgs args_of(const gbmw_attention_problem* p) {
     a.dos[i] = p->dout_stride[i], a.dqs[i] = p->dq_stride[i], a.dks[i] = p->dk_stride[i], a.dvs[i] = p->dv_stride[i];
   }
   a.len_q = p->len_q, a.len_k = p->len_k;
-  a.B = p->B, a.Hq = p->Hq, a.Hk = p->Hk, a.Lq = p->Lq, a.Lk = p->Lk, a.D = p->D, a.share = p->Hq / p->Hk;
+  a.B = p->B, a.Hq = p->Hq, a.Hk = p->Hk, a.Lq = p->Lq, a.Lk = p->Lk, a.D = p->D;
+  a.share = divisor(p->Hq / p->Hk), a.heads_k = divisor(p->Hk);
   a.D4 = (p->D + 3) / 4 * 4;
   a.causal = p->causal, a.scale = p->scale;
-  a.magic = (unsigned)(((1ull << 32) + a.share - 1) / a.share);
-  // Without a causal mask units are alike, and four heads at a time (keys and values of a few MB)
-  // suit a die's cache: 5 x 32 heads x 2048 x 128 forward 377 us, all at a time 384.  With one the
-  // order of their lengths counts more: 2 x 40 heads, all at a time 113 us, four 125; backward 411, 456.
-  a.near = p->causal ? INT_MAX : 4;
   // not 0: a hidden key's -inf has to stay -inf when it is scaled
   a.c = std::max(p->scale * kLog2e, 1e-30f);
   return a;
@@ -1086,15 +1105,28 @@ Scratch scratch_of(const gbmw_attention_problem* p, bool backward) {
   return s;
 }
 
+// Without a causal mask units are alike, and four heads at a time (keys and values of a few MB)
+// suit a die's cache: 5 x 32 heads x 2048 x 128 forward 377 us, all at a time 384.  With one the
+// order of their lengths counts more: 2 x 40 heads, all at a time 113 us, four 125; backward 411, 456.
+Plan plan(int64_t heads, int64_t units, bool causal) {
+  const int64_t per = heads / 8, near = std::max<int64_t>(1, causal ? per : std::min<int64_t>(per, 4));
+  const int64_t rest = per % near, last = rest ? per - rest : std::max<int64_t>(0, per - near);
+  return {(int)per, (int)units, (int)near, (int)last, divisor(near), divisor(std::max<int64_t>(1, near * units)),
+          divisor(std::max<int64_t>(1, per - last)), divisor(std::max<int64_t>(1, heads - 8 * per))};
+}
+
 void place_scratch(AttnArgs& a, const Scratch& s, void* workspace) {
   a.level = (float*)workspace, a.delta = a.level + s.rows, a.gmax = a.delta + s.rows, a.vmax = a.gmax + s.gmax;
   a.shares = a.partial = a.vmax + s.vmax, a.tops = a.shares + s.shares;
-  a.parts = s.parts, a.kparts = s.kparts;
+  a.parts = s.parts, a.kparts = s.kparts, a.parts_d = divisor(s.parts), a.kparts_d = divisor(s.kparts);
+  const int64_t heads = (int64_t)a.Hk * a.B, rows = (int64_t)a.Lq * a.share.d;
+  a.by_rows = plan(heads, (rows + 127) / 128 * a.kparts, a.causal);
+  a.by_keys = plan(heads, ((int64_t)a.Lk + 127) / 128 * a.parts, a.causal);
 }
 
 template <typename T, int KS, bool DIRECT>
 void launch(const AttnArgs& a, bool backward, hipStream_t st) {
-  const int64_t rows = (int64_t)a.Lq * a.share, groups = (int64_t)a.Hk * a.B;
+  const int64_t rows = (int64_t)a.Lq * a.share.d, groups = (int64_t)a.Hk * a.B;
   auto grid = [&](int64_t n, int per) { return dim3((unsigned)((n + per - 1) / per * groups)); };
   auto times = [](dim3 g, int n) { return dim3(g.x * n); };
   const dim3 block(256), merge = dim3((unsigned)((rows * groups * (a.D4 / 4) + 255) / 256));
@@ -1132,7 +1164,7 @@ bool direct(const void* ptr, const int64_t* stride, int L, int share, int D) {
 template <typename T>
 void launch(const AttnArgs& a, bool backward, hipStream_t st) {
   const bool fast = a.D % 8 == 0 && direct(a.k, a.ks, a.Lk, 1, a.D) && direct(a.v, a.vs, a.Lk, 1, a.D) &&
-                    (!backward || (direct(a.q, a.qs, a.Lq, a.share, a.D) && direct(a.dout, a.dos, a.Lq, a.share, a.D)));
+                    (!backward || (direct(a.q, a.qs, a.Lq, a.share.d, a.D) && direct(a.dout, a.dos, a.Lq, a.share.d, a.D)));
   if (!fast) {
     if (a.D <= 64) launch<T, 4, false>(a, backward, st);
     else launch<T, 8, false>(a, backward, st);
