@@ -577,15 +577,15 @@ int64_t gbmw_layer_norm_workspace(const gbmw_layer_norm_problem* p);
  *
  * A list is made once for tensors that stay where they are: it copies the addresses and
  * sizes to the device and owns a workspace for the sums.  It holds no tensor alive.
- * numel[i] >= 0 elements of type in_dtype at in[i]; out_dtype is in_dtype or GBMW_F32;
- * out[i] may be in[i] if the types are the same.  Making a list allocates and waits;
+ * numel[i] >= 0 elements of type in_dtype[i] at in[i]; out_dtype[i] is in_dtype[i] or
+ * GBMW_F32; out[i] may be in[i] if the types are the same.  Making a list allocates and waits;
  * gbmw_clip_gradients does neither.  One list serves one stream at a time.
  */
 typedef struct gbmw_gradient_list gbmw_gradient_list;
 
 gbmw_status gbmw_gradient_list_create(int32_t n, const void* const* in, void* const* out,
-                                      const int64_t* numel, int32_t in_dtype, int32_t out_dtype,
-                                      gbmw_gradient_list** list);
+                                      const int64_t* numel, const int32_t* in_dtype,
+                                      const int32_t* out_dtype, gbmw_gradient_list** list);
 /* norm: DEVICE pointer to one float, or NULL.  max_norm > 0 (may be +inf), scale > 0. */
 gbmw_status gbmw_clip_gradients(gbmw_gradient_list* list, float max_norm, float scale, float* norm,
                                 void* stream);

@@ -145,7 +145,7 @@ for _name in ("gbmw_layer_norm_forward", "gbmw_layer_norm_backward"):
     getattr(_lib, _name).restype = ct.c_int
 _lib.gbmw_layer_norm_workspace.argtypes = [ct.POINTER(gbmw_layer_norm_problem)]
 _lib.gbmw_layer_norm_workspace.restype = ct.c_int64
-_lib.gbmw_gradient_list_create.argtypes = [ct.c_int32] + [ct.c_void_p] * 3 + [ct.c_int32] * 2 + [ct.POINTER(ct.c_void_p)]
+_lib.gbmw_gradient_list_create.argtypes = [ct.c_int32] + [ct.c_void_p] * 5 + [ct.POINTER(ct.c_void_p)]
 _lib.gbmw_gradient_list_create.restype = ct.c_int
 _lib.gbmw_clip_gradients.argtypes = [ct.c_void_p, ct.c_float, ct.c_float, ct.c_void_p, ct.c_void_p]
 _lib.gbmw_clip_gradients.restype = ct.c_int
@@ -658,26 +658,25 @@ class GradientList:
 
 
 def gbmw_gradient_list_create(grads, outs=None) -> GradientList:
-    """A list of gradients (GPU tensors of one type, contiguous) and of the tensors that their clipped values go to:
-    of the same type or float32; by default the gradients themselves.  The tensors have to stay where they are."""
+    """A list of gradients (contiguous GPU tensors) and of the tensors that their clipped values go to, of the same
+    types or float32; by default the gradients themselves.  The tensors have to stay where they are."""
     grads = list(grads)
     outs = grads if outs is None else list(outs)
     if len(outs) != len(grads):
         _refuse(f"{len(grads)} gradients, {len(outs)} outputs")
-    dtype = grads[0].dtype if grads else torch.float32
-    odtype = outs[0].dtype if outs else torch.float32
     device = torch.cuda.current_device() if torch.cuda.is_initialized() else 0
     for i, (g, o) in enumerate(zip(grads, outs)):
-        _device_tensor(f"gradient {i}", g, device, dtype)
-        _device_tensor(f"output {i}", o, device, odtype)
+        _device_tensor(f"gradient {i}", g, device)
+        _device_tensor(f"output {i}", o, device)
         if o.numel() != g.numel() or not g.is_contiguous() or not o.is_contiguous():
             _refuse(f"tensor {i}: sizes {g.numel()} and {o.numel()}, or not contiguous")
     n = len(grads)
-    arr = lambda ts: (ct.c_void_p * max(1, n))(*[t.data_ptr() or None for t in ts])
+    pointers = lambda ts: (ct.c_void_p * max(1, n))(*[t.data_ptr() or None for t in ts])
+    types = lambda ts: (ct.c_int32 * max(1, n))(*[_DTYPE.get(t.dtype, -1) for t in ts])
     numel = (ct.c_int64 * max(1, n))(*[g.numel() for g in grads])
     lst = GradientList()
-    _check(_lib.gbmw_gradient_list_create(n, arr(grads), arr(outs), numel, _DTYPE.get(dtype, -1),
-                                          _DTYPE.get(odtype, -1), ct.byref(lst.handle)))
+    _check(_lib.gbmw_gradient_list_create(n, pointers(grads), pointers(outs), numel, types(grads), types(outs),
+                                          ct.byref(lst.handle)))
     lst._keep = (grads, outs)
     return lst
 

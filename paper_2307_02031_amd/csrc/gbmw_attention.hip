@@ -225,7 +225,7 @@ struct Loader {
 #pragma unroll
         for (int i = 0; i < N; ++i) {
           const int r = first + row_of(i), x = rows.share.of(r);
-          load(tile, from, i, (r >= rows.count) | (at[i % NA] == kOut) ? kOut
+          load(tile, from, i, ((r >= rows.count) | (at[i % NA] == kOut)) ? kOut
                                   : at[i % NA] + (unsigned)(x - x0) * (unsigned)rows.stride + (unsigned)(r - x * rows.share.d) * (unsigned)rows.head);
         }
       }
@@ -684,7 +684,6 @@ __global__ __launch_bounds__(256) void k_attn_vmax(AttnArgs a) {
   const int last = min(part * 64 + 64, length(a.len_k, b, a.Lk)), d = threadIdx.x % 16 * 8;
   const f16* v = (const f16*)a.v + b * a.vs[0] + hk * a.vs[2] + d;
   float s = 0.0f;
-#pragma unroll 4
   for (int key = part * 64 + threadIdx.x / 16; key < last; key += 16) {
     const Pack<f16> x = load_pack(v + key * a.vs[1], a.D - d);
     float n = 0.0f;

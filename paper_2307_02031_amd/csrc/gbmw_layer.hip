@@ -285,7 +285,7 @@ __global__ __launch_bounds__(1024) void k_norm_join(const float* partial, int pa
 struct Piece {   // a run of at most kPiece elements of one tensor
   const void* in;
   void* out;
-  int64_t n;
+  int32_t n, in_dtype, out_dtype, unused;
 };
 constexpr int64_t kPiece = 32768;
 constexpr int kNormGroups = 2048;   // at most so many partial sums
@@ -300,45 +300,75 @@ __device__ __forceinline__ double group_sum(double s, double (&sums)[4]) {
 }
 
 template <typename T>
+__device__ __forceinline__ void add_squares(const Piece& pc, double (&part)[8]) {
+  constexpr int V = kVec<T>, U = kUnroll;
+  const T* in = (const T*)pc.in;
+  auto add = [&](const Pack<T>& x) {
+#pragma unroll
+    for (int e = 0; e < V; ++e) {
+      const double d = (double)(float)x.v[e];
+      part[e] = __builtin_fma(d, d, part[e]);
+    }
+  };
+  int i = threadIdx.x * V;
+  for (; i + ((U - 1) * 256 + 1) * V <= pc.n; i += U * 256 * V) {
+    Pack<T> x[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) __builtin_memcpy(&x[u], in + i + u * 256 * V, 16);
+#pragma unroll
+    for (int u = 0; u < U; ++u) add(x[u]);
+  }
+  for (; i < pc.n; i += 256 * V) add(load_pack(in + i, pc.n - i));
+}
+
+// Tensors of several types may be in one list: which, is the same for a whole workgroup.
 __global__ __launch_bounds__(256) void k_clip_norm(const Piece* pieces, int count, double* partial) {
   __shared__ double sums[4];
-  constexpr int V = kVec<T>, U = kUnroll;
-  double part[V] = {};
+  double part[8] = {};
   for (int k = blockIdx.x; k < count; k += gridDim.x) {
     const Piece pc = pieces[k];
-    const T* in = (const T*)pc.in;
-    auto add = [&](const Pack<T>& x) {
-#pragma unroll
-      for (int e = 0; e < V; ++e) {
-        const double d = (double)(float)x.v[e];
-        part[e] = __builtin_fma(d, d, part[e]);
-      }
-    };
-    int i = threadIdx.x * V;
-    for (; i + ((U - 1) * 256 + 1) * V <= pc.n; i += U * 256 * V) {
-      Pack<T> x[U];
-#pragma unroll
-      for (int u = 0; u < U; ++u) __builtin_memcpy(&x[u], in + i + u * 256 * V, 16);
-#pragma unroll
-      for (int u = 0; u < U; ++u) add(x[u]);
-    }
-    for (; i < pc.n; i += 256 * V) add(load_pack(in + i, (int)pc.n - i));
+    if (pc.in_dtype == GBMW_F32) add_squares<float>(pc, part);
+    else if (pc.in_dtype == GBMW_F16) add_squares<f16>(pc, part);
+    else add_squares<bf16>(pc, part);
   }
   double s = 0.0;
 #pragma unroll
-  for (int e = 0; e < V; ++e) s += part[e];
+  for (int e = 0; e < 8; ++e) s += part[e];
   s = group_sum(s, sums);
   if (threadIdx.x == 0) partial[blockIdx.x] = s;
+}
+
+template <typename T, typename O>
+__device__ __forceinline__ void scale_piece(const Piece& pc, float factor) {
+  constexpr int V = kVec<T>, U = kUnroll;
+  const T* in = (const T*)pc.in;
+  O* out = (O*)pc.out;
+  auto put = [&](const Pack<T>& x, int at, int n) {
+    Pack<O> y;
+#pragma unroll
+    for (int h = 0; h < V; h += kVec<O>) {
+#pragma unroll
+      for (int e = 0; e < kVec<O>; ++e) y.v[e] = (O)((float)x.v[h + e] * factor);
+      store_pack(out + at + h, y, n - h);
+    }
+  };
+  int i = threadIdx.x * V;
+  for (; i + ((U - 1) * 256 + 1) * V <= pc.n; i += U * 256 * V) {
+    Pack<T> x[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) __builtin_memcpy(&x[u], in + i + u * 256 * V, 16);
+#pragma unroll
+    for (int u = 0; u < U; ++u) put(x[u], i + u * 256 * V, V);
+  }
+  for (; i < pc.n; i += 256 * V) put(load_pack(in + i, pc.n - i), i, pc.n - i);
 }
 
 // Every workgroup adds the `parts` partial sums itself, in one order: 16 KB from the cache at
 // most, and no workgroup has to wait for another or to make its sum visible to others before its
 // kernel ends (which costs each of them a pass over its die's cache).
 // The pieces last read by the norm come first: they may still be in the cache.
-template <typename T, typename O>
 __global__ __launch_bounds__(256) void k_clip_scale(const Piece* pieces, int count, const double* partial, int parts,
                                                     double max_norm, double scale, float* norm_out) {
-  constexpr int V = kVec<T>, U = kUnroll;
   __shared__ double sums[4];
   double s = 0.0;
 #pragma unroll 8
@@ -350,26 +380,11 @@ __global__ __launch_bounds__(256) void k_clip_scale(const Piece* pieces, int cou
   for (int k = count - 1 - (int)blockIdx.x; k >= 0; k -= gridDim.x) {
     const Piece pc = pieces[k];
     if (factor == 1.0f && pc.in == pc.out) continue;   // the values are there
-    const T* in = (const T*)pc.in;
-    O* out = (O*)pc.out;
-    auto put = [&](const Pack<T>& x, int at, int n) {
-      Pack<O> y;
-#pragma unroll
-      for (int h = 0; h < V; h += kVec<O>) {
-#pragma unroll
-        for (int e = 0; e < kVec<O>; ++e) y.v[e] = (O)((float)x.v[h + e] * factor);
-        store_pack(out + at + h, y, n - h);
-      }
-    };
-    int i = threadIdx.x * V;
-    for (; i + ((U - 1) * 256 + 1) * V <= pc.n; i += U * 256 * V) {
-      Pack<T> x[U];
-#pragma unroll
-      for (int u = 0; u < U; ++u) __builtin_memcpy(&x[u], in + i + u * 256 * V, 16);
-#pragma unroll
-      for (int u = 0; u < U; ++u) put(x[u], i + u * 256 * V, V);
-    }
-    for (; i < pc.n; i += 256 * V) put(load_pack(in + i, (int)pc.n - i), i, (int)pc.n - i);
+    if (pc.in_dtype == GBMW_F32) scale_piece<float, float>(pc, factor);
+    else if (pc.in_dtype == GBMW_F16 && pc.out_dtype == GBMW_F16) scale_piece<f16, f16>(pc, factor);
+    else if (pc.in_dtype == GBMW_F16) scale_piece<f16, float>(pc, factor);
+    else if (pc.out_dtype == GBMW_BF16) scale_piece<bf16, bf16>(pc, factor);
+    else scale_piece<bf16, float>(pc, factor);
   }
 }
 
@@ -560,25 +575,26 @@ extern "C" gbmw_status gbmw_layer_norm_backward(const gbmw_layer_norm_problem* p
 
 struct gbmw_gradient_list {
   gbmw_detail::DevBuf buf;   // partial sums | pieces
-  int count = 0, in_dtype = 0, out_dtype = 0, device = 0;
+  int count = 0, device = 0;
   double* partial() const { return (double*)buf.p; }
   Piece* pieces() const { return (Piece*)((char*)buf.p + 8 * kNormGroups); }
 };
 
 extern "C" gbmw_status gbmw_gradient_list_create(int32_t n, const void* const* in, void* const* out,
-                                                 const int64_t* numel, int32_t in_dtype, int32_t out_dtype,
-                                                 gbmw_gradient_list** list) {
+                                                 const int64_t* numel, const int32_t* in_dtype,
+                                                 const int32_t* out_dtype, gbmw_gradient_list** list) {
   gbmw_detail::clear_error();
   if (!list) return fail(GBMW_ERR_INVALID_ARG, "null list");
   *list = nullptr;
-  if (n < 0 || (n > 0 && (!in || !out || !numel))) return fail(GBMW_ERR_INVALID_ARG, "n=%d, or a null array", n);
-  if (!known_dtype(in_dtype)) return fail(GBMW_ERR_INVALID_ARG, "in_dtype=%d", in_dtype);
-  if (out_dtype != in_dtype && out_dtype != GBMW_F32)
-    return fail(GBMW_ERR_INVALID_ARG, "out_dtype=%d is neither in_dtype nor GBMW_F32", out_dtype);
-  const int isize = element_size(in_dtype), osize = element_size(out_dtype);
+  if (n < 0 || (n > 0 && (!in || !out || !numel || !in_dtype || !out_dtype)))
+    return fail(GBMW_ERR_INVALID_ARG, "n=%d, or a null array", n);
   int64_t count = 0;
   for (int i = 0; i < n; ++i) {
-    if (numel[i] < 0 || numel[i] > (1ll << 44)) return fail(GBMW_ERR_INVALID_ARG, "numel[%d]=%lld", i, (long long)numel[i]);
+    if (!known_dtype(in_dtype[i])) return fail(GBMW_ERR_INVALID_ARG, "in_dtype[%d]=%d", i, in_dtype[i]);
+    if (out_dtype[i] != in_dtype[i] && out_dtype[i] != GBMW_F32)
+      return fail(GBMW_ERR_INVALID_ARG, "out_dtype[%d]=%d is neither the gradient's nor GBMW_F32", i, out_dtype[i]);
+    const int isize = element_size(in_dtype[i]), osize = element_size(out_dtype[i]);
+    if (numel[i] < 0 || numel[i] > (1ll << 41)) return fail(GBMW_ERR_INVALID_ARG, "numel[%d]=%lld", i, (long long)numel[i]);
     if (numel[i] == 0) continue;
     if (!in[i] || !out[i]) return fail(GBMW_ERR_INVALID_ARG, "tensor %d is null", i);
     if ((uintptr_t)in[i] % (unsigned)isize || (uintptr_t)out[i] % (unsigned)osize)
@@ -592,9 +608,10 @@ extern "C" gbmw_status gbmw_gradient_list_create(int32_t n, const void* const* i
     pieces.reserve((size_t)count);
     for (int i = 0; i < n; ++i)
       for (int64_t at = 0; at < numel[i]; at += kPiece)
-        pieces.push_back({(const char*)in[i] + at * isize, (char*)out[i] + at * osize, std::min(kPiece, numel[i] - at)});
+        pieces.push_back({(const char*)in[i] + at * element_size(in_dtype[i]), (char*)out[i] + at * element_size(out_dtype[i]),
+                          (int32_t)std::min(kPiece, numel[i] - at), in_dtype[i], out_dtype[i], 0});
     gbmw_gradient_list* l = new gbmw_gradient_list;
-    l->count = (int)count, l->in_dtype = in_dtype, l->out_dtype = out_dtype;
+    l->count = (int)count;
     const size_t head = 8 * kNormGroups;
     gbmw_status st = l->buf.reserve(head + sizeof(Piece) * (size_t)count);
     if (st == GBMW_OK) {
@@ -630,22 +647,10 @@ extern "C" gbmw_status gbmw_clip_gradients(gbmw_gradient_list* l, float max_norm
   if (dev != l->device) return fail(GBMW_ERR_INVALID_ARG, "the list is on device %d, device %d is current", l->device, dev);
   hipStream_t st = (hipStream_t)stream;
   const dim3 grid(std::max(1, std::min(l->count, kNormGroups))), block(256);
-#define NORM(T) hipLaunchKernelGGL(k_clip_norm<T>, grid, block, 0, st, l->pieces(), l->count, l->partial())
-#define SCALE(T, O)                                                                                              \
-  hipLaunchKernelGGL((k_clip_scale<T, O>), grid, block, 0, st, l->pieces(), l->count, l->partial(), (int)grid.x, \
-                     (double)max_norm, (double)scale, norm)
-  if (l->in_dtype == GBMW_F32) NORM(float);
-  else if (l->in_dtype == GBMW_F16) NORM(f16);
-  else NORM(bf16);
+  hipLaunchKernelGGL(k_clip_norm, grid, block, 0, st, l->pieces(), l->count, l->partial());
+  hipLaunchKernelGGL(k_clip_scale, grid, block, 0, st, l->pieces(), l->count, l->partial(), (int)grid.x, (double)max_norm,
+                     (double)scale, norm);
   HIP_TRY(hipGetLastError());
-  if (l->in_dtype == GBMW_F32) SCALE(float, float);
-  else if (l->in_dtype == GBMW_F16 && l->out_dtype == GBMW_F16) SCALE(f16, f16);
-  else if (l->in_dtype == GBMW_F16) SCALE(f16, float);
-  else if (l->out_dtype == GBMW_BF16) SCALE(bf16, bf16);
-  else SCALE(bf16, float);
-  HIP_TRY(hipGetLastError());
-#undef NORM
-#undef SCALE
   return GBMW_OK;
 }
 

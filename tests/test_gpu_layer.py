@@ -190,6 +190,14 @@ def test_clip(dtype, odtype):
             _check_clip(grads, None, max_norm, scale)
 
 
+def test_clip_of_several_types():
+    """One norm over tensors of every type, each to an output of its own type or float32, some in place."""
+    types = [torch.float32, torch.float16, torch.bfloat16]
+    grads = [_normal(n, dtype=types[i % 3], seed=200 + i, spread=10.0 ** -(i % 4)) for i, n in enumerate(SIZES)]
+    outs = [t if i % 4 == 0 else torch.empty_like(t, dtype=torch.float32 if i % 4 == 1 else t.dtype) for i, t in enumerate(grads)]
+    _check_clip(grads, outs, 0.7, 0.5)
+
+
 def test_clip_again_and_on_odd_addresses():
     """A list is used step after step, and its tensors may start at any element."""
     import paper_2307_02031_amd as g

@@ -96,14 +96,16 @@ def test_clip_refuses():
 
     def status(n=1, ins=(1 << 20,), outs=(1 << 20,), numel=(5,), it=g.GBMW_F32, ot=g.GBMW_F32, null=()):
         a, b, c = (ct.c_void_p * 1)(*ins), (ct.c_void_p * 1)(*outs), (ct.c_int64 * 1)(*numel)
-        return make(n, None if "in" in null else a, None if "out" in null else b, None if "numel" in null else c, it, ot, ct.byref(h))
+        t, o = (ct.c_int32 * 1)(it), (ct.c_int32 * 1)(ot)
+        return make(n, None if "in" in null else a, None if "out" in null else b, None if "numel" in null else c,
+                    None if "types" in null else t, o, ct.byref(h))
 
-    for kw, word in [(dict(n=-1), "n=-1"), (dict(null=("in",)), "null"), (dict(null=("numel",)), "null"), (dict(it=9), "in_dtype"),
+    for kw, word in [(dict(n=-1), "n=-1"), (dict(null=("in",)), "null"), (dict(null=("numel",)), "null"), (dict(null=("types",)), "null"), (dict(it=9), "in_dtype"),
                      (dict(ot=g.GBMW_F16), "out_dtype"), (dict(numel=(-1,)), "numel"), (dict(ins=(None,)), "null"),
                      (dict(ins=((1 << 20) + 2,)), "aligned"), (dict(it=g.GBMW_F16), "in place")]:
         assert status(**kw) == g.GBMW_ERR_INVALID_ARG and word in g.gbmw_last_error(), (kw, g.gbmw_last_error())
         assert h.value is None
-    assert make(0, None, None, None, 0, 0, None) == g.GBMW_ERR_INVALID_ARG
+    assert make(0, None, None, None, None, None, None) == g.GBMW_ERR_INVALID_ARG
     assert g._lib.gbmw_clip_gradients(None, 1.0, 1.0, None, None) == g.GBMW_ERR_INVALID_ARG
     g._lib.gbmw_gradient_list_destroy(None)
 
