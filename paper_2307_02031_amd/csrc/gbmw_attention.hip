@@ -865,6 +865,10 @@ __global__ __launch_bounds__(256, 2) void k_attn_dkv(AttnArgs a) {
   const Rows gr{a.dout + 2 * (b * a.dos[0] + (int64_t)hk * a.share.d * a.dos[2]), 2 * a.dos[1], 2 * a.dos[2], a.share, rows};
   const int64_t row0 = ((int64_t)b * a.Hk + hk) * a.Lq * a.share.d;
 
+  // With heads of 128 not all of a lane's keys and values fit in its registers beside the sums:
+  // the last pieces of them wait in LDS, each lane's for itself.
+  constexpr int PK = KS == 8 ? 2 : 0, PV = KS == 8 ? 1 : 0;
+  __shared__ s16x8 parked[PK + PV > 0 ? PK + PV : 1][PK + PV > 0 ? 256 : 1];
   s16x8 k[KS], v[KS];
 #pragma unroll
   for (int s = 0; s < KS; ++s) {
@@ -872,6 +876,13 @@ __global__ __launch_bounds__(256, 2) void k_attn_dkv(AttnArgs a) {
     k[s] = load8<DIRECT>(a.k + 2 * (b * a.ks[0] + j * a.ks[1] + hk * a.ks[2]), 2 * s + half, a.D, key < nk);
     v[s] = load8<DIRECT>(a.v + 2 * (b * a.vs[0] + j * a.vs[1] + hk * a.vs[2]), 2 * s + half, a.D, key < nk);
   }
+#pragma unroll
+  for (int s = 0; s < PK; ++s) parked[s][threadIdx.x] = k[KS - PK + s];
+#pragma unroll
+  for (int s = 0; s < PV; ++s) parked[PK + s][threadIdx.x] = v[KS - PV + s];
+  int mine = threadIdx.x;
+  auto key_of = [&](int s) { return s < KS - PK ? k[s] : parked[s - (KS - PK)][mine]; };
+  auto value_of = [&](int s) { return s < KS - PV ? v[s] : parked[PK + s - (KS - PV)][mine]; };
   f32x16 dk[DB] = {}, dv[DB] = {};
 
   float up = 1.0f, down = 1.0f;   // of score gradients, beyond kUp
@@ -907,9 +918,10 @@ __global__ __launch_bounds__(256, 2) void k_attn_dkv(AttnArgs a) {
     const bool whole = __all(r0 >= first);
 #pragma unroll 1
     for (int u = 0; u < 2; ++u, tq += Reader<KS>::down(32), tg += Reader<KS>::down(32)) {
+      asm("" : "+v"(mine));   // read again, not kept
       f32x16 x = {}, dp = {};
 #pragma unroll
-      for (int s = 0; s < KS; ++s) x = mma<T>(rd.rows(tq, 0, s), k[s], x);
+      for (int s = 0; s < KS; ++s) x = mma<T>(rd.rows(tq, 0, s), key_of(s), x);
 #pragma unroll
       for (int r = 0; r < 16; r += 4) {
         const f32x4 lse = *(const f32x4*)&sRow[buf][0][32 * u + 2 * r + 4 * half];
@@ -928,7 +940,7 @@ __global__ __launch_bounds__(256, 2) void k_attn_dkv(AttnArgs a) {
         for (int d = 0; d < DB; ++d) dv[d] = mma<T>(rd.cols(tg, 16 * t, d), p, dv[d]);
       }
 #pragma unroll
-      for (int s = 0; s < KS; ++s) dp = mma<T>(rd.rows(tg, 0, s), v[s], dp);
+      for (int s = 0; s < KS; ++s) dp = mma<T>(rd.rows(tg, 0, s), value_of(s), dp);
 #pragma unroll
       for (int r = 0; r < 16; r += 4) {
         const f32x4 delta = *(const f32x4*)&sRow[buf][1][32 * u + 2 * r + 4 * half];
