@@ -417,11 +417,16 @@ Shape shape_of(const gbmw_layer_norm_problem* p) {
   return {1024, nj <= 2 ? nj : nj <= 4 ? 4 : 8};
 }
 
-// Workgroups: enough to fill the chip, each with several rows where there are many.
+// Workgroups: as many as the chip holds at a time, each with several rows where there are many.
+// Backward, every one more costs a row of shares to write and read: with two or three 16-byte
+// pieces of 16-bit values a thread only one of 512 threads fits a compute unit's registers
+// (16384 x 5120: 101 us and 7 to join them, with twice as many 106 and 10); else two do (6304 x
+// 1283 in 32 bits: 24 us, with half as many 34).
 int norm_groups(const gbmw_layer_norm_problem* p, bool backward) {
   const Shape s = shape_of(p);
   const int per = std::max(1, (backward ? kNormBwdThreads : kNormFwdThreads) / s.nt);
-  const int most = s.nt == 1024 ? 256 : backward ? 512 : 2048;
+  const bool one = s.nt == 1024 || (s.nj > 1 && p->dtype != GBMW_F32);
+  const int most = !backward && s.nt < 1024 ? 2048 : one ? 256 : 512;
   return (int)std::min<int64_t>(most, (p->rows + per - 1) / per);
 }
 
