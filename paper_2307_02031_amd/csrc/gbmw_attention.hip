@@ -11,7 +11,7 @@
 // 8t .. 8t+7, rounded to 16 bits, ARE a B operand whose terms are the rows
 //   16 t + 8 (i / 4) + 4 (l / 32) + i % 4,  i = 0..7:
 // probabilities go from one product into the next without leaving their lanes, and the
-// other operand is read in the same order (read_cols).
+// other operand is read in the same order (Reader::cols).
 #include <algorithm>
 #include <climits>
 #include <cmath>
@@ -56,19 +56,19 @@ struct Plan {
 struct AttnArgs {
   const char *q, *k, *v, *dout;
   char *out, *dq, *dk, *dv;
-  float *lse;
+  float* lse;
   float *level, *delta;   // [B][Hk][rows]: log2(e) lse - kUp, inf for rows without keys; <dout, out>
-  float *vmax, *gmax;   // f16: the largest norms of a value and of a row of dout, for parts of 64 keys and 32 rows
+  float *vmax, *gmax;     // f16: the largest norms of a value and of a row of dout, for parts of 64 keys and 32 rows
   int64_t qs[3], ks[3], vs[3], os[3], dos[3], dqs[3], dks[3], dvs[3];
   const int *len_q, *len_k;
-  float* partial;   // [parts][2][B][Hk][Lk][D4]: shares of dk and dv
+  float* partial;         // [parts][2][B][Hk][Lk][D4]: shares of dk and dv
   Plan by_rows, by_keys;
   Divisor share, heads_k, parts_d, kparts_d;   // query heads of a key head; Hk, parts, kparts
   int B, Hq, Hk, Lq, Lk, D, causal;
   float *shares, *tops;   // [kparts][B][Hk][rows][D4] and [kparts][B][Hk][rows]: of out (or dq) and of what goes with it
   int parts, kparts;      // workgroups that share a tile of keys, or a tile of rows
   int D4;                 // D rounded up to 4
-  float c;       // scale * log2(e): probabilities are powers of two
+  float c;                // scale * log2(e): probabilities are powers of two
   float scale;
 };
 
@@ -850,8 +850,7 @@ __global__ __launch_bounds__(256, 2) void k_attn_dkv(AttnArgs a) {
   const int tile = a.parts_d.of(deal.unit), part = deal.unit - tile * a.parts;   // the keys that most rows see first
   const int b = a.heads_k.of(deal.head), hk = deal.head - b * a.Hk;
   const int nq = length(a.len_q, b, a.Lq), nk = length(a.len_k, b, a.Lk);
-  const int l = threadIdx.x % 64, half = l / 32, key0 = tile * 128 + (threadIdx.x / 64) * 32;
-  const int key = key0 + l % 32;
+  const int l = threadIdx.x % 64, half = l / 32, key = tile * 128 + (threadIdx.x / 64) * 32 + l % 32;
   const int rows = nq * a.share.d;
   // the first row that sees key j
   auto first_of = [&](int j) { return a.causal ? max(0, j - (nk - nq)) * a.share.d : 0; };
@@ -1031,7 +1030,7 @@ gbmw_status check_array(const char* name, const void* ptr, const int64_t* stride
   if ((uintptr_t)ptr % 2) return fail(GBMW_ERR_INVALID_ARG, "%s is not aligned to its elements", name);
   const int64_t extent[3] = {p->B, L, H};
   for (int i = 0; i < 3; ++i) {
-    if (stride[i] < 0 || stride[i] > (1ll << 40)) return fail(GBMW_ERR_INVALID_ARG, "%s: stride %lld", name, (long long)stride[i]);
+    if (extent[i] > 1 && (stride[i] < 0 || stride[i] > (1ll << 40))) return fail(GBMW_ERR_INVALID_ARG, "%s: stride %lld", name, (long long)stride[i]);
     if (written && extent[i] > 1 && stride[i] < p->D)
       return fail(GBMW_ERR_INVALID_ARG, "%s: stride %lld lets rows overlap", name, (long long)stride[i]);
   }
@@ -1055,10 +1054,16 @@ AttnArgs args_of(const gbmw_attention_problem* p) {
   a.q = (const char*)p->q, a.k = (const char*)p->k, a.v = (const char*)p->v, a.dout = (const char*)p->dout;
   a.out = (char*)p->out, a.dq = (char*)p->dq, a.dk = (char*)p->dk, a.dv = (char*)p->dv;
   a.lse = p->lse;
-  for (int i = 0; i < 3; ++i) {
-    a.qs[i] = p->q_stride[i], a.ks[i] = p->k_stride[i], a.vs[i] = p->v_stride[i], a.os[i] = p->out_stride[i];
-    a.dos[i] = p->dout_stride[i], a.dqs[i] = p->dq_stride[i], a.dks[i] = p->dk_stride[i], a.dvs[i] = p->dv_stride[i];
-  }
+  // the stride of an extent of one says nothing
+  auto take = [&](int64_t (&to)[3], const int64_t* stride, int L, int H) {
+    to[0] = p->B > 1 ? stride[0] : 0;
+    to[1] = L > 1 ? stride[1] : (p->D + 7) / 8 * 8;
+    to[2] = H > 1 ? stride[2] : 0;
+  };
+  take(a.qs, p->q_stride, p->Lq, p->Hq), take(a.os, p->out_stride, p->Lq, p->Hq);
+  take(a.dos, p->dout_stride, p->Lq, p->Hq), take(a.dqs, p->dq_stride, p->Lq, p->Hq);
+  take(a.ks, p->k_stride, p->Lk, p->Hk), take(a.vs, p->v_stride, p->Lk, p->Hk);
+  take(a.dks, p->dk_stride, p->Lk, p->Hk), take(a.dvs, p->dv_stride, p->Lk, p->Hk);
   a.len_q = p->len_q, a.len_k = p->len_k;
   a.B = p->B, a.Hq = p->Hq, a.Hk = p->Hk, a.Lq = p->Lq, a.Lk = p->Lk, a.D = p->D;
   a.share = divisor(p->Hq / p->Hk), a.heads_k = divisor(p->Hk);

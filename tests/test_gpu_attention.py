@@ -298,3 +298,15 @@ def test_few_keys_and_many_rows(causal):
     """Where several workgroups share the rows that see a key."""
     _check(*_inputs(1, 2100, 130, 2, 1, 64, torch.bfloat16, seed=91), causal=causal)
     _check(*_inputs(1, 1500, 1500, 4, 1, 40, torch.float16, seed=92), causal=causal)
+
+
+def test_strides_of_extents_of_one():
+    """They may hold anything, and count for nothing."""
+    import paper_2307_02031_amd as g
+    q, k, v, dout = _inputs(1, 1, 1, 1, 1, 64, torch.bfloat16, seed=95)
+    base = g.gbmw_attention_forward(q, k, v)
+    odd = [torch.as_strided(t, t.shape, (1 << 50, 7, 3, 1)) for t in (q, k, v, dout)]
+    got = g.gbmw_attention_forward(*odd[:3])
+    assert torch.equal(base[0], got[0]) and torch.equal(base[1], got[1]) and torch.equal(base[0], v)
+    for x, y in zip(g.gbmw_attention_backward(dout, q, k, v, *base), g.gbmw_attention_backward(odd[3], *odd[:3], *got)):
+        assert torch.equal(x, y)
