@@ -840,7 +840,7 @@ __global__ __launch_bounds__(256, 2) void k_attn_dq(AttnArgs a) {
 // of 64: x = Q K^T (lane: one key, 16 rows), dv^T += dout^T p, dk^T += Q^T ds.  No sums are
 // shared between workgroups, so there is nothing to add atomically.
 template <typename T, int KS, bool DIRECT>
-__global__ __launch_bounds__(256, 2) void k_attn_dkv(AttnArgs a) {
+__global__ __launch_bounds__(256, KS <= 4 ? 3 : 2) void k_attn_dkv(AttnArgs a) {
   constexpr int DB = (KS + 1) / 2;
   __shared__ __attribute__((aligned(16))) char lds[4 * kTile<KS>];
   lds_char* const buffers = (lds_char*)lds;
