@@ -93,18 +93,18 @@ __device__ __forceinline__ s16x8 round8(const f32x16& x, int t) {
 
 // ---- tiles in LDS ---------------------------------------------------------------------------
 //
-// A tile is 64 rows of CH 16-byte pieces, stored so that the two kinds of reads, a piece of
-// each of 32 rows and (transposing) 64 bytes of each of four rows, touch all 64 banks evenly:
-// piece p of row r lies at place p ^ swap_of(r) of its row, and rows of 16 pieces have 16 bytes
-// between groups of four.  A lane then needs four addresses for each kind (Reader);
-// everything else is a constant offset.
+// A tile is 64 rows of CH 16-byte pieces (8, 12 or 16, by the head size), stored so that the two
+// kinds of reads, a piece of each of 32 rows and (transposing) 64 bytes of each of four rows,
+// touch all 64 banks evenly: piece p of row r lies at place p ^ swap_of(r) of its row, and rows of
+// 16 pieces have 16 bytes between groups of four.  A lane then needs two or four addresses for
+// each kind (Reader); everything else is a constant offset.
 typedef __attribute__((address_space(3))) char lds_char;
 
 template <int KS>
-constexpr int kChunks = KS <= 4 ? 8 : 16;
+constexpr int kChunks = KS <= 4 ? 8 : KS <= 6 ? 12 : 16;
 template <int CH>
 __device__ __forceinline__ constexpr int swap_of(int row) {
-  return CH == 16 ? (row & 3) << 2 : ((row & 2) << 1) | ((row >> 2) & 3);
+  return CH == 16 ? (row & 3) << 2 : CH == 12 ? (row >> 2) & 3 : ((row & 2) << 1) | ((row >> 2) & 3);
 }
 template <int CH>
 __device__ __forceinline__ constexpr int place_of(int row, int piece) {   // bytes
@@ -115,24 +115,28 @@ constexpr int kTile = 64 * 16 * kChunks<KS> + (kChunks<KS> == 16 ? 256 : 0);   /
 
 template <int KS>
 struct Reader {
-  static constexpr int CH = kChunks<KS>;
-  int row[4], col[4];
+  static constexpr int CH = kChunks<KS>, kSteps = CH == 16 ? 2 : 1;   // steps that share an address
+  int row[CH == 12 ? 2 : 4], col[CH == 12 ? 2 : 4];
   __device__ __forceinline__ Reader() {
     const int l = threadIdx.x % 64, i = l % 16, half = l / 32;
 #pragma unroll
-    for (int s = 0; s < 4; ++s) row[s] = place_of<CH>(l % 32, (CH == 16 ? 4 * s : 2 * s) + half);
+    for (int n = 0; n < (CH == 12 ? 2 : 4); ++n) row[n] = place_of<CH>(l % 32, 2 * kSteps * n + half);
     // lanes 4u..4u+3 of sixteen name the quarters of run u of sixteen elements; lane i gets
     // element i of each of the four runs
     const int r = 4 * half + i / 4, c = 16 * ((l / 16) % 2) + 4 * (i % 4);
 #pragma unroll
-    for (int n = 0; n < 4; ++n)   // of 32 columns each, or of two times 32 columns eight rows apart
-      col[n] = (CH == 16 ? place_of<CH>(r, 4 * n + c / 8) : place_of<CH>(r + 8 * (n / 2), 4 * (n % 2) + c / 8)) + (c % 8) * 2;
+    for (int n = 0; n < (CH == 12 ? 2 : 4); ++n)   // of 32 columns each, of eight rows each, or of both
+      col[n] = (CH == 16   ? place_of<CH>(r, 4 * n + c / 8)
+                : CH == 12 ? place_of<CH>(r + 8 * n, c / 8)
+                           : place_of<CH>(r + 8 * (n / 2), 4 * (n % 2) + c / 8)) + (c % 8) * 2;
   }
   static constexpr int down(int r) { return r * CH * 16 + (CH == 16 ? r / 4 * 16 : 0); }   // r a multiple of 16, or of 8 for CH = 16
   // A operand: rows r .. r+31 of the tile (r = 0 or 32), terms 16 step .. 16 step + 15
   __device__ __forceinline__ s16x8 rows(lds_char* tile, int r, int step) const {
     typedef __attribute__((address_space(3))) s16x8 lds8;
-    return *(lds8*)(tile + (CH == 16 ? row[step / 2] + (step % 2) * 32 : row[step]) + down(r));
+    return *(lds8*)(tile + (CH == 16   ? row[step / 2] + (step % 2) * 32
+                            : CH == 12 ? row[step % 2] + (step / 2) * 64
+                                       : row[step]) + down(r));
   }
   // A operand: rows = columns 32 d .. 32 d + 31 of the tile, terms = its rows r .. r+15 in the
   // order of a result's registers
@@ -141,7 +145,9 @@ struct Reader {
     s16x4 x[2];
 #pragma unroll
     for (int u = 0; u < 2; ++u)
-      x[u] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4*)(tile + (CH == 16 ? col[d] + down(r + 8 * u) : col[d + 2 * u] + down(r))));
+      x[u] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4*)(tile + (CH == 16   ? col[d] + down(r + 8 * u)
+                                                                     : CH == 12 ? col[u] + d * 64 + down(r)
+                                                                                : col[d + 2 * u] + down(r))));
     return __builtin_shufflevector(x[0], x[1], 0, 1, 2, 3, 4, 5, 6, 7);
   }
 };
@@ -175,7 +181,7 @@ struct Rows {
 // that belong in their places, and what is beyond the buffer's bounds arrives as zeros.  Needs
 // 16-byte aligned rows and offsets inside a tile below 2^31.  Otherwise through registers.
 //
-// A wave brings N runs of kRowsOf rows.  Its lanes' offsets inside a run are the same for all of
+// A wave brings N runs of 64 pieces.  Its lanes' offsets inside a run are the same for all of
 // them where rows have 16 pieces; with SPARE every run gets bounds of its own and the lanes keep
 // one offset, otherwise N (for the kernel that is short of registers, and those that are not).
 // ALONE: a wave brings 32 rows for itself, and nobody else waits for them.
@@ -183,7 +189,6 @@ template <int KS, bool DIRECT, bool SPARE = false, bool ALONE = false>
 struct Loader {
   static constexpr int CH = kChunks<KS>, ROWS = ALONE ? 32 : 64, THREADS = ALONE ? 64 : 256;
   static constexpr int N = DIRECT ? ROWS * CH / THREADS : (ROWS * 2 * KS + THREADS - 1) / THREADS;
-  static constexpr int kRowsOf = 64 / CH;
   static constexpr bool kOne = SPARE && CH == 16;
   static constexpr int NA = kOne ? 1 : N;
   static constexpr unsigned kOut = 0x80000000u;
@@ -192,15 +197,13 @@ struct Loader {
 
   __device__ __forceinline__ static int wave() { return ALONE ? 0 : __builtin_amdgcn_readfirstlane(threadIdx.x / 64); }
   __device__ __forceinline__ static int thread() { return ALONE ? threadIdx.x % 64 : threadIdx.x; }
-  __device__ __forceinline__ static int row_of(int i) {   // of this lane, in the tile
-    return (wave() * N + i) * kRowsOf + (int)(threadIdx.x % 64) / CH;
-  }
+  __device__ __forceinline__ static int row_of(int i) { return ((wave() * N + i) * 64 + (int)threadIdx.x % 64) / CH; }
   __device__ __forceinline__ void init(const Rows& rows, int D) {
     if constexpr (DIRECT) {
 #pragma unroll
       for (int i = 0; i < NA; ++i) {
-        const int piece = ((int)threadIdx.x % CH) ^ swap_of<CH>(row_of(i));
-        const int down = kOne ? (int)(threadIdx.x % 64) / CH : row_of(i);
+        const int piece = ((wave() * N + i) * 64 + (int)threadIdx.x % 64) % CH ^ swap_of<CH>(row_of(i));
+        const int down = kOne ? (int)(threadIdx.x % 64) / CH : row_of(i);   // of its run, or of the tile
         at[i] = 8 * piece >= D ? kOut : 16 * piece + (rows.share.d == 1 ? down * (unsigned)rows.stride : 0u);
       }
     }
@@ -210,7 +213,7 @@ struct Loader {
     if constexpr (DIRECT) {
       if (rows.share.d == 1) {   // rows beyond the last one are beyond the bounds
         const int64_t length = (int64_t)(rows.count - first) * rows.stride;
-        const int left = (int)min(length, (int64_t)0x7fffffff), run = kRowsOf * (int)rows.stride;
+        const int left = (int)min(length, (int64_t)0x7fffffff), run = 64 / CH * (int)rows.stride;
         const char* base = rows.base + first * rows.stride;
         const int skip = kOne ? wave() * N * run : 0;
 #pragma unroll
