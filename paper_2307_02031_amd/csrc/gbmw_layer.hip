@@ -24,7 +24,10 @@ namespace {
 // it shares its first columns with the piece before it, which count there (Span::from).
 // Every load is then one unconditional instruction, and all of a row's are in flight at once.
 //
-// Bound by HBM; one pass over x (and dy) is its floor.
+// Bound by HBM; one pass over x (and dy) is its floor.  16384 x 5120 bf16: forward 57 us, 5.8 TB/s;
+// backward 101 us, 5.0 TB/s, and 7 us to join the weights' shares (a large copy runs at 4.7 TB/s,
+// reads and writes together).  6304 x 1283 fp32: 15 and 25 us.  512 x 1280 bf16: 3.6 us, two sums
+// after one load, bound by latency.
 
 struct NormArgs {
   int64_t rows;
@@ -281,6 +284,12 @@ __global__ __launch_bounds__(1024) void k_norm_join(const float* partial, int pa
 }
 
 // ---- gradient norm and clipping -----------------------------------------------------------
+//
+// Two launches, bound by HBM: one reads every gradient for the norm, one reads and writes them
+// all, because no value can be written before the last has been read.  236M bf16 gradients into
+// fp32: 121 us (3.9 TB/s) and 265 us (5.3 TB/s); 20M fp32 ones, from the cache: 13 and 26 us.
+// Squares are added in fp64, at a few per cent of its rate: nothing overflows, and the norm is
+// right to the last bit of fp32.
 
 struct Piece {   // a run of at most kPiece elements of one tensor
   const void* in;
