@@ -589,7 +589,7 @@ gbmw_status gbmw_gradient_list_create(int32_t n, const void* const* in, void* co
 /* norm: DEVICE pointer to one float, or NULL.  max_norm > 0 (may be +inf), scale > 0. */
 gbmw_status gbmw_clip_gradients(gbmw_gradient_list* list, float max_norm, float scale, float* norm,
                                 void* stream);
-/* Waits for the device.  NULL is allowed. */
+/* Waits for the list's device.  NULL is allowed. */
 void gbmw_gradient_list_destroy(gbmw_gradient_list* list);
 
 /* Lmax of the last solve (row length of `plan` above); 0 if none. */

@@ -669,7 +669,9 @@ __global__ __launch_bounds__(256) void k_attn_merge(AttnArgs a) {
   f32x4 o = {};
   float top = -kInf, sum = 0.0f;
   if constexpr (!BACKWARD)
+#pragma unroll 8
     for (int k = 0; k < a.kparts; ++k) top = fmaxf(top, a.tops[k * all + at]);
+#pragma unroll 8
   for (int k = 0; k < a.kparts; ++k) {
     const float t = a.tops[k * all + at];
     float f = 1.0f;

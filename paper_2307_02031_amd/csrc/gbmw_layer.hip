@@ -287,7 +287,7 @@ __global__ __launch_bounds__(1024) void k_norm_join(const float* partial, int pa
 //
 // Two launches, bound by HBM: one reads every gradient for the norm, one reads and writes them
 // all, because no value can be written before the last has been read.  236M bf16 gradients into
-// fp32: 121 us (3.9 TB/s) and 265 us (5.3 TB/s); 20M fp32 ones, from the cache: 13 and 26 us.
+// fp32: together 342 us (387 with ordinary stores), 1.9 GB at 5.5 TB/s; 20M fp32 ones: 39 us (49).
 // Squares are added in fp64, at a few per cent of its rate: nothing overflows, and the norm is
 // right to the last bit of fp32.
 
@@ -347,29 +347,38 @@ __global__ __launch_bounds__(256) void k_clip_norm(const Piece* pieces, int coun
   if (threadIdx.x == 0) partial[blockIdx.x] = s;
 }
 
-template <typename T, typename O>
+// STREAM: the stores pass the cache by (a wave's are whole lines of it), so that what is still to
+// be read stays there.
+template <typename T, typename O, bool STREAM>
 __device__ __forceinline__ void scale_piece(const Piece& pc, float factor) {
-  constexpr int V = kVec<T>, U = kUnroll;
+  constexpr int V = kVec<O>, U = kUnroll;   // as many elements as a store of 16 bytes takes
+  typedef float f32x4 __attribute__((ext_vector_type(4)));
   const T* in = (const T*)pc.in;
   O* out = (O*)pc.out;
-  auto put = [&](const Pack<T>& x, int at, int n) {
-    Pack<O> y;
-#pragma unroll
-    for (int h = 0; h < V; h += kVec<O>) {
-#pragma unroll
-      for (int e = 0; e < kVec<O>; ++e) y.v[e] = (O)((float)x.v[h + e] * factor);
-      store_pack(out + at + h, y, n - h);
-    }
-  };
   int i = threadIdx.x * V;
   for (; i + ((U - 1) * 256 + 1) * V <= pc.n; i += U * 256 * V) {
-    Pack<T> x[U];
+    T x[U][V];
 #pragma unroll
-    for (int u = 0; u < U; ++u) __builtin_memcpy(&x[u], in + i + u * 256 * V, 16);
+    for (int u = 0; u < U; ++u) __builtin_memcpy(&x[u], in + i + u * 256 * V, V * sizeof(T));
 #pragma unroll
-    for (int u = 0; u < U; ++u) put(x[u], i + u * 256 * V, V);
+    for (int u = 0; u < U; ++u) {
+      Pack<O> y;
+#pragma unroll
+      for (int e = 0; e < V; ++e) y.v[e] = (O)((float)x[u][e] * factor);
+      if constexpr (STREAM) __builtin_nontemporal_store(__builtin_bit_cast(f32x4, y), (f32x4*)(out + i + u * 256 * V));
+      else __builtin_memcpy(out + i + u * 256 * V, &y, 16);
+    }
   }
-  for (; i < pc.n; i += 256 * V) put(load_pack(in + i, pc.n - i), i, pc.n - i);
+  for (; i < pc.n; i += 256 * V)
+#pragma unroll
+    for (int e = 0; e < V; ++e)
+      if (i + e < pc.n) out[i + e] = (O)((float)in[i + e] * factor);
+}
+
+template <typename T, typename O>
+__device__ __forceinline__ void scale_piece(const Piece& pc, float factor) {
+  if ((uintptr_t)pc.out % 128 == 0) scale_piece<T, O, true>(pc, factor);
+  else scale_piece<T, O, false>(pc, factor);
 }
 
 // Every workgroup adds the `parts` partial sums itself, in one order: 16 KB from the cache at
@@ -670,7 +679,11 @@ extern "C" gbmw_status gbmw_clip_gradients(gbmw_gradient_list* l, float max_norm
 
 extern "C" void gbmw_gradient_list_destroy(gbmw_gradient_list* l) {
   if (!l) return;
+  int current = l->device;
+  (void)hipGetDevice(&current);
+  if (current != l->device) (void)hipSetDevice(l->device);
   (void)hipDeviceSynchronize();
   l->buf.release();
+  if (current != l->device) (void)hipSetDevice(current);
   delete l;
 }
