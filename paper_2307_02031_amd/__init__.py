@@ -410,38 +410,49 @@ def _refuse(message: str):
     raise GbmwError(GBMW_ERR_INVALID_ARG, message)
 
 
-_LAYER_TYPES = {**_DTYPE, torch.int32: -1}
 # the current stream's handle without an object around it, where torch has it
 _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", lambda device: torch.cuda.current_stream(device).cuda_stream)
 
 
-def _device_tensor(name: str, t, device: int, dtype=None, shape=None):
-    """t, or an error: the kernels take plain addresses, so type and shape are checked here."""
+def _refuse_tensor(name: str, t, device: int, dtype, shape):
+    """Says what is wrong with t: the kernels take plain addresses, so type, place and shape are checked here."""
     if not isinstance(t, torch.Tensor) or not t.is_cuda:
         _refuse(f"{name} is not a tensor on the GPU")
     if t.get_device() != device:
         _refuse(f"{name} is on {t.device}, device {device} is current")
-    if t.dtype != dtype and (dtype is not None or t.dtype not in _LAYER_TYPES):
-        _refuse(f"{name} has type {t.dtype}" + ("" if dtype is None else f", not {dtype}"))
-    if shape is not None and t.shape != shape:
-        _refuse(f"{name} has shape {tuple(t.shape)}, not {tuple(shape)}")
-    return t
+    if t.dtype != dtype:
+        _refuse(f"{name} has type {t.dtype}, not {dtype}")
+    _refuse(f"{name} has shape {tuple(t.shape)}, not {tuple(shape)}")
+
+
+def _check_tensor(name: str, t, device: int, dtype, shape) -> None:
+    if not isinstance(t, torch.Tensor) or t.get_device() != device or t.dtype != dtype or t.shape != shape:
+        _refuse_tensor(name, t, device, dtype, shape)
+
+
+def _device_of(name: str, t, types) -> int:
+    """The current device, which the first argument has to be on, with one of the types."""
+    if not isinstance(t, torch.Tensor) or not t.is_cuda:
+        _refuse(f"{name} is not a tensor on the GPU")
+    device = torch.cuda.current_device()
+    if t.get_device() != device:
+        _refuse(f"{name} is on {t.device}, device {device} is current")
+    if t.dtype not in types:
+        _refuse(f"{name} has type {t.dtype}")
+    return device
 
 
 def _on_stream(call):
-    """Runs call(..., _at=(device, stream handle)) on the `stream` argument (a torch stream or a handle), or on the
-    current one.  Outputs and scratch memory that a call makes belong to the stream its kernels run on, so that the
-    memory is not handed to anybody else before they have run.  Inputs on another stream than that are the caller's
-    to keep until the stream has got to the call, as with any work on a second stream."""
+    """call with one more argument: `stream`, a torch stream or a handle, by default the current one.  Outputs and
+    scratch memory that a call makes belong to the stream its kernels run on, so that the memory is not handed to
+    anybody else before they have run.  Inputs on another stream than that are the caller's to keep until the stream
+    has got to the call, as with any work on a second stream."""
     @functools.wraps(call)
     def on_stream(*args, stream=None, **kw):
-        ready = torch.cuda.is_initialized()     # without, there is no tensor on a GPU either
-        device = torch.cuda.current_device() if ready else 0
         if stream is None:
-            return call(*args, _at=(device, _raw_stream(device) if ready else 0), **kw)
-        handle = int(getattr(stream, "cuda_stream", stream))
-        with torch.cuda.stream(torch.cuda.ExternalStream(handle)):
-            return call(*args, _at=(device, handle), **kw)
+            return call(*args, **kw)
+        with torch.cuda.stream(torch.cuda.ExternalStream(int(getattr(stream, "cuda_stream", stream)))):
+            return call(*args, **kw)
     return on_stream
 
 
@@ -451,56 +462,64 @@ def _workspace(p, given, need: int, device: int):
         raise GbmwError(GBMW_ERR_INVALID_ARG, gbmw_last_error())
     if given is None:
         given = torch.empty(max(16, need), dtype=torch.uint8, device="cuda")
-    elif _device_tensor("workspace", given, device, torch.uint8) is None or not given.is_contiguous():
-        _refuse("workspace is not contiguous")
+    elif not isinstance(given, torch.Tensor) or given.get_device() != device or given.dtype != torch.uint8 \
+            or not given.is_contiguous():
+        _refuse("workspace is not a contiguous uint8 tensor on the current GPU")
     p.workspace, p.workspace_bytes = given.data_ptr(), given.numel()
     return given
 
 
-_Strides = ct.c_int64 * 3
-
-
-def _set_array(p, name: str, t) -> None:
+def _strides(name: str, t) -> tuple:
     s0, s1, s2, s3 = t.stride()
     if s3 != 1 and t.shape[3] > 1:
         _refuse(f"{name}: the values of one head are not next to each other")
+    return s0, s1, s2
+
+
+def _set_array(p, name: str, t) -> None:
     setattr(p, name, t.data_ptr())
-    setattr(p, name + "_stride", _Strides(s0, s1, s2))
+    setattr(p, name + "_stride", _strides(name, t))
 
 
-def _attention_problem(q, k, v, causal, scale, len_q, len_k, at) -> gbmw_attention_problem:
-    device, stream = at
-    _device_tensor("q", q, device)
-    if q.dim() != 4:
+_HALF_TYPES = (torch.bfloat16, torch.float16, torch.float32)      # float32: the library says that it is not supported
+
+
+def _attention_problem(q, k, v, causal, scale, len_q, len_k):
+    device = _device_of("q", q, _HALF_TYPES)
+    shape, dtype = q.shape, q.dtype
+    if len(shape) != 4:
         _refuse(f"q has {q.dim()} dimensions, not [B][Lq][Hq][D]")
     if not isinstance(k, torch.Tensor) or k.dim() != 4:
         _refuse("k is not a tensor [B][Lk][Hk][D]")
-    B, Lq, Hq, D = q.shape
-    _, Lk, Hk, _ = k.shape
-    dtype = q.dtype
-    _device_tensor("k", k, device, dtype, (B, Lk, Hk, D))
-    _device_tensor("v", v, device, dtype, (B, Lk, Hk, D))
-    p = gbmw_attention_problem(_DTYPE.get(dtype, -1), B, Hq, Hk, Lq, Lk, D, 1 if causal else 0,
-                               (1.0 / D ** 0.5 if D else 1.0) if scale is None else scale)
-    p.stream = stream
-    _set_array(p, "q", q), _set_array(p, "k", k), _set_array(p, "v", v)
+    B, Lq, Hq, D = shape
+    kshape = k.shape
+    if kshape[0] != B or kshape[3] != D or k.dtype != dtype or k.get_device() != device:
+        _refuse_tensor("k", k, device, dtype, (B, kshape[1], kshape[2], D))
+    _check_tensor("v", v, device, dtype, kshape)
     if len_q is not None:
-        p.len_q = _length("len_q", len_q, device, B)
+        len_q = _length("len_q", len_q, device, B)
     if len_k is not None:
-        p.len_k = _length("len_k", len_k, device, B)
-    return p
+        len_k = _length("len_k", len_k, device, B)
+    p = gbmw_attention_problem(_DTYPE[dtype], B, Hq, kshape[2], Lq, kshape[1], D, 1 if causal else 0,
+                               (1.0 / D ** 0.5 if D else 1.0) if scale is None else scale, len_q, len_k,
+                               q.data_ptr(), k.data_ptr(), v.data_ptr(),
+                               _strides("q", q), _strides("k", k), _strides("v", v))
+    p.stream = _raw_stream(device)
+    return p, device
 
 
 def _length(name: str, t, device: int, B: int) -> int:
-    if not _device_tensor(name, t, device, torch.int32, (B,)).is_contiguous():
+    _check_tensor(name, t, device, torch.int32, (B,))
+    if not t.is_contiguous():
         _refuse(f"{name} is not contiguous")
     return t.data_ptr()
 
 
 def _lse(p, lse, device: int) -> None:
-    p.lse = _device_tensor("lse", lse, device, torch.float32, (p.B, p.Hq, p.Lq)).data_ptr()
+    _check_tensor("lse", lse, device, torch.float32, (p.B, p.Hq, p.Lq))
     if not lse.is_contiguous():
         _refuse("lse is not contiguous")
+    p.lse = lse.data_ptr()
 
 
 def gbmw_attention_workspace(q, k, backward: bool) -> int:
@@ -513,133 +532,162 @@ def gbmw_attention_workspace(q, k, backward: bool) -> int:
     return n
 
 
+def _new_like(t):
+    """A dense tensor like t."""
+    return torch.empty_like(t) if t.is_contiguous() else torch.empty(t.shape, dtype=t.dtype, device="cuda")
+
+
 @_on_stream
 def gbmw_attention_forward(q, k, v, causal: bool = False, scale: float | None = None, len_q=None, len_k=None,
-                           out=None, lse=None, workspace=None, *, _at=None):
+                           out=None, lse=None, workspace=None):
     """out [B][Lq][Hq][D] and lse [B][Hq][Lq] (float32) of q [B][Lq][Hq][D], k and v [B][Lk][Hk][D]: float16 or
     bfloat16 GPU tensors with any strides whose last one is 1.  scale: 1 / sqrt(D) by default.  len_q, len_k:
     int32 [B], the samples' lengths.  out, lse, workspace (uint8): made here unless given.  stream=: as everywhere."""
-    p = _attention_problem(q, k, v, causal, scale, len_q, len_k, _at)
+    p, device = _attention_problem(q, k, v, causal, scale, len_q, len_k)
     if out is None:
-        out = torch.empty(q.shape, dtype=q.dtype, device="cuda")
+        out = _new_like(q)
     else:
-        _device_tensor("out", out, _at[0], q.dtype, q.shape)
+        _check_tensor("out", out, device, q.dtype, q.shape)
     if lse is None:
         lse = torch.empty((p.B, p.Hq, p.Lq), dtype=torch.float32, device="cuda")
-    _set_array(p, "out", out), _lse(p, lse, _at[0])
-    need = _lib.gbmw_attention_workspace(ct.byref(p), 0)
-    keep = _workspace(p, workspace, need, _at[0]) if need else None
-    _check(_lib.gbmw_attention_forward(ct.byref(p)))
+        p.lse = lse.data_ptr()
+    else:
+        _lse(p, lse, device)
+    _set_array(p, "out", out)
+    ref = ct.byref(p)
+    need = _lib.gbmw_attention_workspace(ref, 0)
+    keep = _workspace(p, workspace, need, device) if need else None
+    _check(_lib.gbmw_attention_forward(ref))
     return out, lse
 
 
 @_on_stream
 def gbmw_attention_backward(dout, q, k, v, out, lse, causal: bool = False, scale: float | None = None, len_q=None,
-                            len_k=None, dq=None, dk=None, dv=None, workspace=None, *, _at=None):
+                            len_k=None, dq=None, dk=None, dv=None, workspace=None):
     """dq, dk, dv from dout and the forward call's arguments and results.  stream=: as everywhere."""
-    p = _attention_problem(q, k, v, causal, scale, len_q, len_k, _at)
-    dq = torch.empty(q.shape, dtype=q.dtype, device="cuda") if dq is None else dq
-    dk = torch.empty(k.shape, dtype=q.dtype, device="cuda") if dk is None else dk
-    dv = torch.empty(k.shape, dtype=q.dtype, device="cuda") if dv is None else dv
-    for name, t, like in (("dout", dout, q), ("out", out, q), ("dq", dq, q), ("dk", dk, k), ("dv", dv, k)):
-        _set_array(p, name, _device_tensor(name, t, _at[0], q.dtype, like.shape))
-    _lse(p, lse, _at[0])
-    keep = _workspace(p, workspace, _lib.gbmw_attention_workspace(ct.byref(p), 1), _at[0])
-    _check(_lib.gbmw_attention_backward(ct.byref(p)))
+    p, device = _attention_problem(q, k, v, causal, scale, len_q, len_k)
+    dtype, qshape, kshape = q.dtype, q.shape, k.shape
+    _check_tensor("dout", dout, device, dtype, qshape)
+    _check_tensor("out", out, device, dtype, qshape)
+    _lse(p, lse, device)
+    if dq is None:
+        dq = _new_like(q)
+    else:
+        _check_tensor("dq", dq, device, dtype, qshape)
+    if dk is None:
+        dk = _new_like(k)
+    else:
+        _check_tensor("dk", dk, device, dtype, kshape)
+    if dv is None:
+        dv = torch.empty_like(dk) if dk.is_contiguous() else _new_like(k)
+    else:
+        _check_tensor("dv", dv, device, dtype, kshape)
+    _set_array(p, "dout", dout), _set_array(p, "out", out)
+    _set_array(p, "dq", dq), _set_array(p, "dk", dk), _set_array(p, "dv", dv)
+    ref = ct.byref(p)
+    keep = _workspace(p, workspace, _lib.gbmw_attention_workspace(ref, 1), device)
+    _check(_lib.gbmw_attention_backward(ref))
     return dq, dk, dv
 
 
-def _norm_rows(name: str, t, device: int, like=None):
-    """(rows, cols, row stride) of a tensor whose last axis is normed; the axes before it have to be one stride."""
-    if like is None:
-        _device_tensor(name, t, device)
-    else:
-        _device_tensor(name, t, device, like.dtype, like.shape)
-    if t.dim() < 1:
-        _refuse(f"{name} has no axis")
+def _row_stride(name: str, t) -> int:
+    """Row stride of a tensor whose last axis is normed; the axes before it have to be one stride."""
     cols = t.shape[-1]
-    rows = t.numel() // max(1, cols)
     if t.is_contiguous():
-        return rows, cols, cols
+        return cols
     if t.stride(-1) != 1 and cols > 1:
         _refuse(f"{name}: the values of a row are not next to each other")
-    stride = cols
-    if rows > 1:
-        axes = [(n, s) for n, s in zip(t.shape[:-1], t.stride()[:-1]) if n > 1]
-        stride = axes[-1][1]
-        for (n, s), (n1, s1) in zip(axes, axes[1:]):
-            if s != n1 * s1:
-                _refuse(f"{name}: its rows are not one stride apart")
-    return rows, cols, stride
+    axes = [(n, s) for n, s in zip(t.shape[:-1], t.stride()[:-1]) if n > 1]
+    if not axes or not t.numel():
+        return cols
+    for (n, s), (n1, s1) in zip(axes, axes[1:]):
+        if s != n1 * s1:
+            _refuse(f"{name}: its rows are not one stride apart")
+    return axes[-1][1]
 
 
-def _norm_problem(x, weight, bias, at) -> gbmw_layer_norm_problem:
-    p = gbmw_layer_norm_problem()
-    p.rows, p.cols, p.x_stride = _norm_rows("x", x, at[0])
-    wdtype = x.dtype if weight is None and bias is None else (bias if weight is None else weight).dtype
-    p.x, p.dtype, p.wdtype, p.stream = x.data_ptr(), _DTYPE.get(x.dtype, -1), _DTYPE.get(wdtype, -1), at[1]
-    for name, t in (("weight", weight), ("bias", bias)):
-        if t is not None:
-            if not _device_tensor(name, t, at[0], wdtype, (p.cols,)).is_contiguous():
-                _refuse(f"{name} is not contiguous")
-            setattr(p, name, t.data_ptr())
-    return p
+def _norm_problem(x, weight, bias):
+    device = _device_of("x", x, _DTYPE)
+    shape, dtype = x.shape, x.dtype
+    if len(shape) < 1:
+        _refuse("x has no axis")
+    p, cols = gbmw_layer_norm_problem(), shape[-1]
+    p.dtype = p.wdtype = _DTYPE[dtype]
+    p.rows, p.cols, p.x_stride = x.numel() // max(1, cols), cols, _row_stride("x", x)
+    p.x, p.stream = x.data_ptr(), _raw_stream(device)
+    if weight is not None or bias is not None:
+        wdtype = getattr(bias if weight is None else weight, "dtype", None)
+        p.wdtype = _DTYPE.get(wdtype, -1)
+        if weight is not None:
+            p.weight = _column("weight", weight, device, wdtype, cols)
+        if bias is not None:
+            p.bias = _column("bias", bias, device, wdtype, cols)
+    return p, device
+
+
+def _column(name: str, t, device: int, dtype, cols: int) -> int:
+    _check_tensor(name, t, device, dtype, (cols,))
+    if not t.is_contiguous():
+        _refuse(f"{name} is not contiguous")
+    return t.data_ptr()
 
 
 @_on_stream
-def gbmw_layer_norm_workspace(x, weight=None, *, _at=None) -> int:
+def gbmw_layer_norm_workspace(x, weight=None) -> int:
     """Bytes of workspace of the backward call."""
-    n = _lib.gbmw_layer_norm_workspace(ct.byref(_norm_problem(x, weight, None, _at)))
+    n = _lib.gbmw_layer_norm_workspace(ct.byref(_norm_problem(x, weight, None)[0]))
     if n < 0:
         raise GbmwError(GBMW_ERR_INVALID_ARG, gbmw_last_error())
     return n
 
 
-def _new_rows(x):
-    """A dense tensor like x."""
-    return torch.empty_like(x) if x.is_contiguous() else torch.empty(x.shape, dtype=x.dtype, device="cuda")
-
-
 @_on_stream
-def gbmw_layer_norm_forward(x, weight=None, bias=None, eps: float = 1e-5, y=None, *, _at=None):
+def gbmw_layer_norm_forward(x, weight=None, bias=None, eps: float = 1e-5, y=None):
     """y like x, mean and rstd float32 of x's shape without its last axis.  x: float32, float16 or bfloat16 GPU
     tensor; weight, bias: of x's type or float32.  y: made here unless given (it may be x).  stream=: as everywhere."""
-    p = _norm_problem(x, weight, bias, _at)
-    p.eps = eps
+    p, device = _norm_problem(x, weight, bias)
     if y is None:
-        y, p.y_stride = _new_rows(x), p.cols
+        y, p.y_stride = _new_like(x), p.cols
     else:
-        _, _, p.y_stride = _norm_rows("y", y, _at[0], x)
+        _check_tensor("y", y, device, x.dtype, x.shape)
+        p.y_stride = _row_stride("y", y)
     mean = torch.empty(x.shape[:-1], dtype=torch.float32, device="cuda")
     rstd = torch.empty_like(mean)
-    p.y, p.mean, p.rstd = y.data_ptr(), mean.data_ptr(), rstd.data_ptr()
+    p.eps, p.y, p.mean, p.rstd = eps, y.data_ptr(), mean.data_ptr(), rstd.data_ptr()
     _check(_lib.gbmw_layer_norm_forward(ct.byref(p)))
     return y, mean, rstd
 
 
 @_on_stream
-def gbmw_layer_norm_backward(dy, x, weight, mean, rstd, bias: bool = True, dx=None, workspace=None, *, _at=None):
+def gbmw_layer_norm_backward(dy, x, weight, mean, rstd, bias: bool = True, dx=None, workspace=None):
     """dx, dweight, dbias from dy and the forward call's x, weight, mean and rstd.  weight None: no dweight; bias
     False: no dbias.  Both are of weight's type (x's without one).  stream=: as everywhere."""
-    p = _norm_problem(x, weight, None, _at)
+    p, device = _norm_problem(x, weight, None)
     if dx is None:
-        dx, p.dx_stride = _new_rows(x), p.cols
+        dx, p.dx_stride = _new_like(x), p.cols
     else:
-        _, _, p.dx_stride = _norm_rows("dx", dx, _at[0], x)
-    _, _, p.dy_stride = _norm_rows("dy", dy, _at[0], x)
+        _check_tensor("dx", dx, device, x.dtype, x.shape)
+        p.dx_stride = _row_stride("dx", dx)
+    _check_tensor("dy", dy, device, x.dtype, x.shape)
+    p.dy_stride = _row_stride("dy", dy)
     p.dx, p.dy = dx.data_ptr(), dy.data_ptr()
     for name, t in (("mean", mean), ("rstd", rstd)):
-        if not _device_tensor(name, t, _at[0], torch.float32, x.shape[:-1]).is_contiguous():
+        _check_tensor(name, t, device, torch.float32, x.shape[:-1])
+        if not t.is_contiguous():
             _refuse(f"{name} is not contiguous")
-        setattr(p, name, t.data_ptr())
+    p.mean, p.rstd = mean.data_ptr(), rstd.data_ptr()
     wdtype = x.dtype if weight is None else weight.dtype
-    dweight = None if weight is None else torch.empty(p.cols, dtype=wdtype, device="cuda")
-    dbias = torch.empty(p.cols, dtype=wdtype, device="cuda") if bias else None
-    keep = None
-    if dweight is not None or dbias is not None:
-        p.dweight, p.dbias = (None if t is None else t.data_ptr() for t in (dweight, dbias))
-        keep = _workspace(p, workspace, _lib.gbmw_layer_norm_workspace(ct.byref(p)), _at[0])
-    _check(_lib.gbmw_layer_norm_backward(ct.byref(p)))
+    dweight = dbias = keep = None
+    if weight is not None:
+        dweight = torch.empty(p.cols, dtype=wdtype, device="cuda")
+        p.dweight = dweight.data_ptr()
+    if bias:
+        dbias = torch.empty(p.cols, dtype=wdtype, device="cuda")
+        p.dbias = dbias.data_ptr()
+    ref = ct.byref(p)
+    if weight is not None or bias:
+        keep = _workspace(p, workspace, _lib.gbmw_layer_norm_workspace(ref), device)
+    _check(_lib.gbmw_layer_norm_backward(ref))
     return dx, dweight, dbias
 
 
@@ -664,10 +712,8 @@ def gbmw_gradient_list_create(grads, outs=None) -> GradientList:
     outs = grads if outs is None else list(outs)
     if len(outs) != len(grads):
         _refuse(f"{len(grads)} gradients, {len(outs)} outputs")
-    device = torch.cuda.current_device() if torch.cuda.is_initialized() else 0
     for i, (g, o) in enumerate(zip(grads, outs)):
-        _device_tensor(f"gradient {i}", g, device)
-        _device_tensor(f"output {i}", o, device)
+        _device_of(f"gradient {i}", g, _DTYPE), _device_of(f"output {i}", o, _DTYPE)
         if o.numel() != g.numel() or not g.is_contiguous() or not o.is_contiguous():
             _refuse(f"tensor {i}: sizes {g.numel()} and {o.numel()}, or not contiguous")
     n = len(grads)
@@ -682,14 +728,14 @@ def gbmw_gradient_list_create(grads, outs=None) -> GradientList:
 
 
 @_on_stream
-def gbmw_clip_gradients(lst: GradientList, max_norm: float, scale: float = 1.0, norm=None, *, _at=None):
+def gbmw_clip_gradients(lst: GradientList, max_norm: float, scale: float = 1.0, norm=None):
     """Writes the list's outputs; returns the norm before clipping, a float32 GPU tensor [1] (norm, if given).
     stream=: as everywhere."""
     if norm is None:
         norm = torch.empty(1, dtype=torch.float32, device="cuda")
-    elif _device_tensor("norm", norm, _at[0], torch.float32).numel() < 1:
+    elif _device_of("norm", norm, (torch.float32,)) < 0 or norm.numel() < 1:
         _refuse("norm is empty")
-    _check(_lib.gbmw_clip_gradients(lst.handle, max_norm, scale, norm.data_ptr(), _at[1]))
+    _check(_lib.gbmw_clip_gradients(lst.handle, max_norm, scale, norm.data_ptr(), _raw_stream(norm.get_device())))
     return norm
 
 
