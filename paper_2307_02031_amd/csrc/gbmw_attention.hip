@@ -1107,27 +1107,35 @@ AttnArgs args_of(const gbmw_attention_problem* p) {
 
 constexpr int kSlots = 512;   // workgroups that the chip holds at a time (two a compute unit)
 
-// Workgroups that share a tile of keys in dk and dv: where the tiles do not fill the chip twice
-// over (under a causal mask they differ much in length), each tile's rows are dealt to several,
-// as long as each gets 512 of them.  2 x 40 heads x 2048 causal (1280 tiles): 405 us, in two parts
-// 287 + 77 to join them; 8 heads x 8192 (512 tiles of up to 32768 rows): 4.3 ms, in two parts 1.3.
+// Workgroups that share a tile of keys in dk and dv.  Two reasons: tiles that do not fill half the
+// chip, as long as each part gets 192 rows (28 heads, 484 rows, 56 tiles: backward 111 us, in four parts
+// 67; 456 tiles of 395 rows in two: 68, in one 47), and a causal mask, under which they differ much in
+// length, as long as each part gets 1024 (8 heads x 8192, 512 tiles of up to 8192 rows: 646 us, in two
+// parts 557; 500 tiles of 1213 rows in two: 108, in one 92).
 int parts_of(const gbmw_attention_problem* p) {
   const int64_t groups = (int64_t)p->B * p->Hk * ((p->Lk + 127) / 128), rows = (int64_t)p->Lq * (p->Hq / p->Hk);
   int parts = 1;
-  while (parts < 16 && groups * parts < 2 * kSlots && rows / (2 * parts) >= 512) parts *= 2;
+  while (parts < 16 && ((groups * parts < 2 * kSlots && rows / (2 * parts) >= 1024) ||
+                        (groups * parts <= kSlots / 2 && rows / (2 * parts) >= 192)))
+    parts *= 2;
   return parts;
 }
 
 bool few(const gbmw_attention_problem* p) { return (int64_t)p->Lq * (p->Hq / p->Hk) <= 32; }
 
-// Workgroups that share a tile of rows: as many as fill the chip, each with enough keys that
-// writing its share and reading it back (as much as two tiles of keys per 32 rows) is the less.
+// Workgroups that share a tile of rows: as many as fit the chip, each with enough keys that
+// writing its share and reading it back (as much as two tiles of keys per 32 rows) is the less; under
+// a causal mask up to twice as many, as long as each gets 1024 keys (388 tiles of up to 6171 keys
+// forward: 105 us, in two parts 79; 500 of 1213: 30 us, in two 40).
 int kparts_of(const gbmw_attention_problem* p, bool backward) {
   const int64_t rows = (int64_t)p->Lq * (p->Hq / p->Hk), groups = (int64_t)p->B * p->Hk * ((rows + 127) / 128);
   if (groups == 0) return 1;
-  const int64_t tiles = ((int64_t)p->Lk + 63) / 64, least = few(p) && !backward ? 8 : std::max<int64_t>(2, std::min<int64_t>(rows, 128) / 16);
-  const int64_t fill = few(p) && !backward ? kSlots / 2 : kSlots;
-  return (int)std::max<int64_t>(1, std::min({(fill + groups - 1) / groups, tiles / least, (int64_t)64}));
+  const int64_t tiles = ((int64_t)p->Lk + 63) / 64;
+  if (few(p) && !backward) return (int)std::max<int64_t>(1, std::min({kSlots / 2 / groups, tiles / 8, (int64_t)64}));
+  const int64_t least = std::max<int64_t>(2, std::min<int64_t>(rows, 128) / 16);
+  int64_t parts = std::min({kSlots / groups, tiles / least, (int64_t)64});
+  if (p->causal) parts = std::max(parts, std::min(2 * kSlots / groups, tiles / 16));
+  return (int)std::max<int64_t>(1, parts);
 }
 
 // The forward call's workspace: shares and tops.  The backward call's: level and delta
