@@ -25,9 +25,12 @@ namespace {
 // Every load is then one unconditional instruction, and all of a row's are in flight at once.
 //
 // Bound by HBM; one pass over x (and dy) is its floor.  16384 x 5120 bf16: forward 57 us, 5.8 TB/s;
-// backward 101 us, 5.0 TB/s, and 7 us to join the weights' shares (a large copy runs at 4.7 TB/s,
-// reads and writes together).  6304 x 1283 fp32: 15 and 25 us.  512 x 1280 bf16: 3.6 us, two sums
+// backward 103 us, 4.9 TB/s, and 5 us to join the weights' shares (a large copy runs at 4.7 TB/s,
+// reads and writes together).  6304 x 1283 fp32: 14 and 20 us.  512 x 1280 bf16: 3.6 us, two sums
 // after one load, bound by latency.
+
+// Floats from one share of dweight or dbias to the next: each starts at 16 bytes.
+__host__ __device__ constexpr int share_stride(int cols) { return (cols + 3) / 4 * 4; }
 
 struct NormArgs {
   int64_t rows;
@@ -38,7 +41,7 @@ struct NormArgs {
   void *y, *dx;
   int64_t xs, ys, dys, dxs;
   float *mean, *rstd;
-  float* partial;  // [gridDim.x][2][cols]
+  float* partial;  // [gridDim.x][2][share_stride(cols)]
 };
 
 // Sums of N values over the NT threads of a row.  `scratch`: N * (NT / 64) floats of the
@@ -63,8 +66,8 @@ __device__ __forceinline__ void row_sum(float (&s)[N], float* scratch) {
 }
 
 // V elements of a row from column c on, of which those before column `from` are another piece's.
-// Rows of fewer than V columns have one piece, of n columns.
-template <int V, bool WHOLE>
+// Rows of fewer than V columns (TINY: there may be such) have one piece, of n columns.
+template <int V, bool WHOLE, bool TINY>
 struct Span {
   int c, from, n, row;
   Span() = default;
@@ -72,12 +75,12 @@ struct Span {
     from = piece * V;
     const bool there = from < cols;
     c = there ? (WHOLE ? from : max(0, min(from, cols - V))) : 0;
-    n = there ? min(V, cols) : 0;
+    n = there ? (TINY ? min(V, cols) : V) : 0;
   }
   __device__ __forceinline__ bool has(int i) const { return WHOLE ? n > 0 : c + i >= from && i < n; }
   template <typename W>
   __device__ __forceinline__ void load(float (&x)[V], const W* row) const {   // what it does not have may be anything
-    if (WHOLE || this->row >= V) {
+    if (!TINY || this->row >= V) {
       Pack<W> r[V / kVec<W>];
       __builtin_memcpy(r, row + c, V * sizeof(W));
 #pragma unroll
@@ -93,20 +96,20 @@ struct Span {
     static_assert(V == kVec<T>, "");
 #pragma unroll
     for (int i = 0; i < V; ++i) r.v[i] = (T)y[i];
-    if (n == V) __builtin_memcpy(row + c, &r, 16);   // shared columns are written twice, the same
+    if (!TINY || n == V) __builtin_memcpy(row + c, &r, 16);   // shared columns are written twice, the same
     else store_pack(row, r, n);
   }
 };
 
 // The raw bytes of a thread's pieces: loaded early, looked at late.
-template <typename T, int NJ, bool WHOLE>
+template <typename T, int NJ, bool TINY>
 struct Held {
   Pack<T> p[NJ];
   template <typename S>
   __device__ __forceinline__ void load(const S (&span)[NJ], const T* row, int cols) {
 #pragma unroll
     for (int j = 0; j < NJ; ++j) {
-      if (WHOLE || cols >= kVec<T>) __builtin_memcpy(&p[j], row + span[j].c, 16);
+      if (!TINY || cols >= kVec<T>) __builtin_memcpy(&p[j], row + span[j].c, 16);
       else p[j] = load_pack(row, span[j].n);
     }
   }
@@ -114,19 +117,28 @@ struct Held {
 
 constexpr int kNormFwdThreads = 256, kNormBwdThreads = 512;
 
+// Of a thread's NJ pieces the first so many are whole and there, whatever the row's length
+// (1024 threads have kernels of 1, 2, 4 and 8 pieces, so more than half are).
+template <int NT, int NJ>
+constexpr int kSure = NT < 1024 || NJ <= 2 ? NJ - 1 : NJ / 2;
+
+template <int NT, int NJ>
+constexpr bool kRunsAhead = NT < 1024 || NJ == 1;
+
 // Workgroups of G rows at a time, rows blockIdx.x * G + g, then gridDim.x * G further on: a thread
 // reads its columns of weight and bias once, and the next row is on its way while one is worked on
-// (not with 1024 threads, which have half the registers).
+// (not with several pieces for each of 1024 threads, which have half the registers).
 template <typename T, int NT, int NJ, bool WHOLE>
 __global__ __launch_bounds__(NT < kNormFwdThreads ? kNormFwdThreads : NT) void k_norm_fwd(NormArgs a) {
   constexpr int V = kVec<T>, G = (NT < kNormFwdThreads ? kNormFwdThreads : NT) / NT;
-  constexpr bool kAhead = NT < 1024;
+  constexpr bool kAhead = kRunsAhead<NT, NJ>;
   __shared__ float scratch[2][G][NT / 64];
   const int t = threadIdx.x % NT, g = threadIdx.x / NT;
-  Span<V, WHOLE> span[NJ];
+  constexpr bool kTiny = !WHOLE && NT * NJ == 64;
+  Span<V, WHOLE, kTiny> span[NJ];
 #pragma unroll
-  for (int j = 0; j < NJ; ++j) span[j] = Span<V, WHOLE>(t + j * NT, a.cols);
-  Held<T, NJ, WHOLE> x, next;
+  for (int j = 0; j < NJ; ++j) span[j] = Span<V, WHOLE, kTiny>(t + j * NT, a.cols);
+  Held<T, NJ, kTiny> x, next;
   auto fetch = [&](int64_t row) { next.load(span, (const T*)a.x + (row < a.rows ? row : 0) * a.xs, a.cols); };
   const int64_t step = (int64_t)gridDim.x * G;
   fetch((int64_t)blockIdx.x * G + g);
@@ -146,7 +158,7 @@ __global__ __launch_bounds__(NT < kNormFwdThreads ? kNormFwdThreads : NT) void k
 #pragma unroll
     for (int j = 0; j < NJ; ++j)
 #pragma unroll
-      for (int i = 0; i < V; ++i) s[0] += span[j].has(i) ? (float)x.p[j].v[i] : 0.0f;
+      for (int i = 0; i < V; ++i) s[0] += j < kSure<NT, NJ> || span[j].has(i) ? (float)x.p[j].v[i] : 0.0f;
     row_sum<NT>(s, scratch[0][g]);
     const float mean = s[0] / (float)a.cols;
     s[0] = 0.0f;
@@ -154,7 +166,7 @@ __global__ __launch_bounds__(NT < kNormFwdThreads ? kNormFwdThreads : NT) void k
     for (int j = 0; j < NJ; ++j)
 #pragma unroll
       for (int i = 0; i < V; ++i) {
-        const float d = span[j].has(i) ? (float)x.p[j].v[i] - mean : 0.0f;
+        const float d = j < kSure<NT, NJ> || span[j].has(i) ? (float)x.p[j].v[i] - mean : 0.0f;
         s[0] = __builtin_fmaf(d, d, s[0]);
       }
     row_sum<NT>(s, scratch[1][g]);
@@ -175,21 +187,34 @@ __global__ __launch_bounds__(NT < kNormFwdThreads ? kNormFwdThreads : NT) void k
   }
 }
 
+// Whether one workgroup of k_norm_bwd has a compute unit to itself.
+template <typename T, int NT, int NJ>
+constexpr bool kOne = NT == 1024 || (sizeof(T) == 2 && NJ == 3);
+
 // The same walk over the rows.  A thread keeps its columns' share of dweight and dbias in
 // registers over all its rows; the workgroup's shares go to `partial` and k_norm_join adds them
 // up in a fixed order, so the result does not depend on which workgroup ends first.  weight waits
-// in LDS: the registers are taken.
+// in LDS (the registers are taken) by pieces, four columns of each after the other, so that a wave
+// reads 16 bytes a lane one after the other.  13673 x 4574 bf16, whose last piece starts early:
+// 75 us; with weight read by columns, every column masked and rows shorter than a piece allowed
+// for where there are none, 176.
+//
+// Rows that are not there are masked (kOne) or branched around.  A mask lets the compiler keep all
+// converted values from the sums to dx, in 200 registers: better where only one workgroup fits
+// anyway (16384 x 5120 bf16: 103 us, with a branch 108), worse where it makes one of two (20000 x
+// 768 in 32 bits: 38 us, with a branch 34).
 template <typename T, int NT, int NJ, bool WHOLE>
 __global__ __launch_bounds__(NT < kNormBwdThreads ? kNormBwdThreads : NT) void k_norm_bwd(NormArgs a) {
   constexpr int V = kVec<T>, G = (NT < kNormBwdThreads ? kNormBwdThreads : NT) / NT;
-  constexpr bool kAhead = NT < 1024;
+  constexpr bool kAhead = kRunsAhead<NT, NJ>;
   __shared__ float scratch[2][G][2 * (NT / 64)];
-  extern __shared__ __attribute__((aligned(16))) float columns[];   // [cols] weight, then the shares
+  extern __shared__ __attribute__((aligned(16))) float columns[];   // [V/4][pieces][4] weight, then [cols] shares
   const int t = threadIdx.x % NT, g = threadIdx.x / NT;
-  Span<V, WHOLE> span[NJ];
+  constexpr bool kTiny = !WHOLE && NT * NJ == 64;
+  Span<V, WHOLE, kTiny> span[NJ];
 #pragma unroll
-  for (int j = 0; j < NJ; ++j) span[j] = Span<V, WHOLE>(t + j * NT, a.cols);
-  Held<T, NJ, WHOLE> x, dy, next_x, next_dy;
+  for (int j = 0; j < NJ; ++j) span[j] = Span<V, WHOLE, kTiny>(t + j * NT, a.cols);
+  Held<T, NJ, kTiny> x, dy, next_x, next_dy;
   float mean, rstd, next_mean, next_rstd;
   auto fetch = [&](int64_t row) {
     const int64_t at = row < a.rows ? row : 0;
@@ -199,9 +224,28 @@ __global__ __launch_bounds__(NT < kNormBwdThreads ? kNormBwdThreads : NT) void k
   };
   const int64_t step = (int64_t)gridDim.x * G;
   fetch((int64_t)blockIdx.x * G + g);
-  for (int c = threadIdx.x; c < a.cols; c += blockDim.x)
-    columns[c] = !a.w ? 1.0f : a.wide ? ((const float*)a.w)[c] : (float)((const T*)a.w)[c];
+  typedef float f32x4 __attribute__((ext_vector_type(4)));
+  const int pieces = (a.cols + V - 1) / V;
+  f32x4* weight = (f32x4*)columns;
+  for (int k = threadIdx.x; k < pieces; k += blockDim.x) {
+    const Span<V, WHOLE, kTiny> s(k, a.cols);
+    float w[V];
+#pragma unroll
+    for (int i = 0; i < V; ++i) w[i] = 1.0f;
+    if (a.w) a.wide ? s.load(w, (const float*)a.w) : s.load(w, (const T*)a.w);
+#pragma unroll
+    for (int q = 0; q < V / 4; ++q) weight[q * pieces + k] = f32x4{w[4 * q], w[4 * q + 1], w[4 * q + 2], w[4 * q + 3]};
+  }
   __syncthreads();
+  auto weight_of = [&](int j, float (&w)[V]) {
+    const int k = span[j].from / V;
+#pragma unroll
+    for (int q = 0; q < V / 4; ++q) {
+      const f32x4 r = weight[q * pieces + (j < kSure<NT, NJ> || k < pieces ? k : 0)];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) w[4 * q + i] = r[i];
+    }
+  };
   float dw[NJ][V] = {}, db[NJ][V] = {};
   int turn = 0;
   for (int64_t first = (int64_t)blockIdx.x * G; first < a.rows; first += step, turn ^= 1) {
@@ -210,18 +254,20 @@ __global__ __launch_bounds__(NT < kNormBwdThreads ? kNormBwdThreads : NT) void k
     x = next_x, dy = next_dy, mean = next_mean, rstd = next_rstd;
     if constexpr (kAhead) fetch(row + step);
     float s[2] = {0.0f, 0.0f};
+    if (kOne<T, NT, NJ> || live) {
 #pragma unroll
-    for (int j = 0; j < NJ; ++j) {
-      float w[V];
-      span[j].load(w, columns);
+      for (int j = 0; j < NJ; ++j) {
+        float w[V];
+        weight_of(j, w);
 #pragma unroll
-      for (int i = 0; i < V; ++i) {
-        const bool has = live && span[j].has(i);
-        const float xhat = has ? ((float)x.p[j].v[i] - mean) * rstd : 0.0f, d = has ? (float)dy.p[j].v[i] : 0.0f;
-        dw[j][i] = __builtin_fmaf(d, xhat, dw[j][i]);
-        db[j][i] += d;
-        s[0] = __builtin_fmaf(d, w[i], s[0]);
-        s[1] = __builtin_fmaf(d * w[i], xhat, s[1]);
+        for (int i = 0; i < V; ++i) {
+          const bool has = (live || !kOne<T, NT, NJ>) && (j < kSure<NT, NJ> || span[j].has(i));
+          const float xhat = has ? ((float)x.p[j].v[i] - mean) * rstd : 0.0f, d = has ? (float)dy.p[j].v[i] : 0.0f;
+          dw[j][i] = __builtin_fmaf(d, xhat, dw[j][i]);
+          db[j][i] += d;
+          s[0] = __builtin_fmaf(d, w[i], s[0]);
+          s[1] = __builtin_fmaf(d * w[i], xhat, s[1]);
+        }
       }
     }
     row_sum<NT>(s, scratch[turn][g]);
@@ -232,7 +278,7 @@ __global__ __launch_bounds__(NT < kNormBwdThreads ? kNormBwdThreads : NT) void k
       for (int j = 0; j < NJ; ++j) {
         if (span[j].n == 0) continue;
         float w[V], out[V];
-        span[j].load(w, columns);
+        weight_of(j, w);
 #pragma unroll
         for (int i = 0; i < V; ++i) {
           const float xhat = ((float)x.p[j].v[i] - mean) * rstd;
@@ -259,28 +305,36 @@ __global__ __launch_bounds__(NT < kNormBwdThreads ? kNormBwdThreads : NT) void k
           }
     }
     __syncthreads();
-    float* out = a.partial + ((int64_t)blockIdx.x * 2 + which) * a.cols;
+    float* out = a.partial + ((int64_t)blockIdx.x * 2 + which) * share_stride(a.cols);
     for (int c = threadIdx.x; c < a.cols; c += blockDim.x) out[c] = columns[c];
   }
 }
 
-// dweight and dbias from `parts` shares: 16 columns a workgroup, every 64th share a thread.
+// dweight and dbias from `parts` shares: 32 columns a workgroup, four of every 128th share a thread
+// (8 threads read a line of the cache).  256 shares of 4574 columns: 4.8 us, 1.9 TB/s from the cache
+// (one column a thread and half a line at a time: 7.4); 146 of 9714: 7.
 template <typename W>
 __global__ __launch_bounds__(1024) void k_norm_join(const float* partial, int parts, int cols, W* dw, W* db) {
-  __shared__ float sums[64][17];
-  const int col = threadIdx.x % 16, k0 = threadIdx.x / 16, c = blockIdx.x * 16 + col;
+  typedef float f32x4 __attribute__((ext_vector_type(4)));
+  __shared__ f32x4 sums[16][8];
+  const int quad = threadIdx.x % 8, c = blockIdx.x * 32 + quad * 4, stride = share_stride(cols);
   W* out = blockIdx.y ? db : dw;
   if (!out) return;
-  float s = 0.0f;
+  f32x4 s = {};
   if (c < cols)
-#pragma unroll 8
-    for (int k = k0; k < parts; k += 64) s += partial[((int64_t)k * 2 + blockIdx.y) * cols + c];
-  sums[k0][col] = s;
-  for (int n = 32; n; n /= 2) {
-    __syncthreads();
-    if (k0 < n) sums[k0][col] += sums[k0 + n][col];
-  }
-  if (k0 == 0 && c < cols) out[c] = (W)sums[0][col];
+#pragma unroll 4
+    for (int k = threadIdx.x / 8; k < parts; k += 128)
+      s += *(const f32x4*)(partial + ((int64_t)k * 2 + blockIdx.y) * stride + c);
+#pragma unroll
+  for (int e = 0; e < 4; ++e) s[e] = sum_across32(sum_across16(sum_dpp<0x128>(s[e])));   // lanes 8, 16 and 32 apart
+  if (threadIdx.x % 64 < 8) sums[threadIdx.x / 64][quad] = s;
+  __syncthreads();
+  if (threadIdx.x >= 32) return;
+  const int col = blockIdx.x * 32 + (int)threadIdx.x;
+  float total = 0.0f;
+#pragma unroll
+  for (int w = 0; w < 16; ++w) total += sums[w][threadIdx.x / 4][threadIdx.x % 4];
+  if (col < cols) out[col] = (W)total;
 }
 
 // ---- gradient norm and clipping -----------------------------------------------------------
@@ -423,7 +477,7 @@ gbmw_status check_norm(const gbmw_layer_norm_problem* p) {
 
 // Threads of a row and 16-byte pieces of each: few threads for short rows, so that the sums
 // stay inside a wave, and few pieces a thread, so that they stay in registers (three of 16-bit
-// values in the backward pass take 220; with four it spills).
+// values in the backward pass take 208; with four it spills).
 struct Shape {
   int nt, nj;
 };
@@ -435,17 +489,20 @@ Shape shape_of(const gbmw_layer_norm_problem* p) {
   return {1024, nj <= 2 ? nj : nj <= 4 ? 4 : 8};
 }
 
-// Workgroups: as many as the chip holds at a time, each with several rows where there are many.
-// Backward, every one more costs a row of shares to write and read: with two or three 16-byte
-// pieces of 16-bit values a thread only one of 512 threads fits a compute unit's registers
-// (16384 x 5120: 101 us and 7 to join them, with twice as many 106 and 10); else two do (6304 x
-// 1283 in 32 bits: 24 us, with half as many 34).
+// Workgroups: as many as the chip holds at a time, each with several rows where there are many, and
+// no more than it takes for the most that one of them has.  Forward, two of 1024 threads with a
+// piece each fit (4000 x 8192 bf16: 25 us, with one 30), of more pieces one does.  Backward, every one more costs a row of
+// shares to write and read: with 16-bit values and three pieces a thread, or with 1024 threads, only
+// one fits a compute unit's registers (16384 x 5120: 103 us and 5 to join them); else two do (6304 x
+// 1283 in 32 bits: 20 us, with half as many 34).
 int norm_groups(const gbmw_layer_norm_problem* p, bool backward) {
   const Shape s = shape_of(p);
   const int per = std::max(1, (backward ? kNormBwdThreads : kNormFwdThreads) / s.nt);
-  const bool one = s.nt == 1024 || (s.nj > 1 && p->dtype != GBMW_F32);
-  const int most = !backward && s.nt < 1024 ? 2048 : one ? 256 : 512;
-  return (int)std::min<int64_t>(most, (p->rows + per - 1) / per);
+  const bool one = s.nt == 1024 || (s.nj == 3 && p->dtype != GBMW_F32);   // kOne
+  const int64_t most = !backward ? s.nt < 1024 ? 2048 : s.nj == 1 ? 512 : 256 : one ? 256 : 512, all = (p->rows + per - 1) / per;
+  if (all <= most) return (int)all;
+  const int64_t turns = (all + most - 1) / most;   // of the one that has most rows: no more workgroups than that takes
+  return (int)((all + turns - 1) / turns);
 }
 
 template <typename T, int NT, int NJ, bool WHOLE>
@@ -453,7 +510,7 @@ gbmw_status launch_norm(const NormArgs& a, bool backward, int groups, hipStream_
   if (!backward) {
     hipLaunchKernelGGL((k_norm_fwd<T, NT, NJ, WHOLE>), dim3(groups), dim3(std::max(NT, kNormFwdThreads)), 0, st, a);
   } else {
-    const size_t lds = 4 * (size_t)a.cols;
+    const size_t lds = 16 * (size_t)((a.cols + kVec<T> - 1) / kVec<T>) * (kVec<T> / 4);
     if (lds > 60 * 1024) {
       const hipError_t e = hipFuncSetAttribute((const void*)&k_norm_bwd<T, NT, NJ, WHOLE>,
                                                hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
@@ -523,7 +580,7 @@ using namespace gbmw;
 extern "C" int64_t gbmw_layer_norm_workspace(const gbmw_layer_norm_problem* p) {
   gbmw_detail::clear_error();
   if (check_norm(p) != GBMW_OK) return -1;
-  return (int64_t)norm_groups(p, true) * 2 * p->cols * 4;
+  return (int64_t)norm_groups(p, true) * 2 * share_stride(p->cols) * 4;
 }
 
 extern "C" gbmw_status gbmw_layer_norm_forward(const gbmw_layer_norm_problem* p) {
@@ -566,7 +623,7 @@ extern "C" gbmw_status gbmw_layer_norm_backward(const gbmw_layer_norm_problem* p
   }
   const int groups = norm_groups(p, true);
   if (wanted && p->rows > 0) {
-    const int64_t need = (int64_t)groups * 2 * p->cols * 4;
+    const int64_t need = (int64_t)groups * 2 * share_stride(p->cols) * 4;
     if (!p->workspace || p->workspace_bytes < need || (uintptr_t)p->workspace % 16)
       return fail(GBMW_ERR_INVALID_ARG, "workspace of %lld bytes, 16-byte aligned, is needed", (long long)need);
   }
@@ -579,7 +636,7 @@ extern "C" gbmw_status gbmw_layer_norm_backward(const gbmw_layer_norm_problem* p
     CHECK(launch_norm(p, a, true, groups));
   }
   if (wanted) {   // without rows: zeros
-    const dim3 grid((p->cols + 15) / 16, 2);
+    const dim3 grid((p->cols + 31) / 32, 2);
     hipStream_t st = (hipStream_t)p->stream;
     const float* part = (const float*)p->workspace;
     if (p->wdtype == GBMW_F32)
