@@ -26,7 +26,7 @@ namespace {
 //
 // Bound by HBM; one pass over x (and dy) is its floor.  16384 x 5120 bf16: forward 57 us, 5.8 TB/s;
 // backward 103 us, 4.9 TB/s, and 5 us to join the weights' shares (a large copy runs at 4.7 TB/s,
-// reads and writes together).  6304 x 1283 fp32: 14 and 20 us.  512 x 1280 bf16: 3.6 us, two sums
+// reads and writes together).  6304 x 1283 fp32: 12 and 20 us.  512 x 1280 bf16: 3.6 us, two sums
 // after one load, bound by latency.
 
 // Floats from one share of dweight or dbias to the next: each starts at 16 bytes.
