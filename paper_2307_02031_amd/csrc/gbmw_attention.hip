@@ -50,6 +50,7 @@ Divisor divisor(int64_t d) { return {(int)d, (unsigned)(((1ull << 32) + d - 1) /
 // Which head and which of its `units` pieces of work a workgroup takes: see Deal.
 struct Plan {
   int per, units, near, last;   // heads of a die, units of a head, heads at a time, the first of the last heads
+  int lot;                      // 2^lot heads next to each other are one die's
   Divisor of_near, near_units, of_last, of_rest;
 };
 
@@ -328,7 +329,8 @@ __device__ __forceinline__ void store_share(float* row, int D4, const f32x16 (&x
 // Which head and which of its units a workgroup takes.  Workgroups are dealt to the eight dies in
 // turn.  A die works on its own heads, `near` of them at a time, so that what their units read
 // alike stays in its cache; of those the first units (the longest under a causal mask) come first.
-// Heads that eight does not divide are dealt to all dies at the end.
+// Heads are dealt to the dies in lots, so that every die gets a share of every sample: samples have
+// lengths of their own.  Heads that eight does not divide are dealt to all dies at the end.
 struct Deal {
   int head, unit;
   __device__ __forceinline__ Deal(const Plan& p) {
@@ -345,7 +347,8 @@ struct Deal {
         unit = p.of_near.of(in);
         in -= unit * p.near;
       }
-      head = id % 8 * p.per + first + in;
+      const int n = first + in;
+      head = ((((n >> p.lot) * 8 + id % 8) << p.lot) | (n & ((1 << p.lot) - 1)));
     } else {
       const int at = id - 8 * p.per * p.units;
       unit = p.of_rest.of(at);
@@ -1163,10 +1166,16 @@ Scratch scratch_of(const gbmw_attention_problem* p, bool backward) {
 // Without a causal mask units are alike, and four heads at a time (keys and values of a few MB)
 // suit a die's cache: 5 x 32 heads x 2048 x 128 forward 377 us, all at a time 384.  With one the
 // order of their lengths counts more: 2 x 40 heads, all at a time 113 us, four 125; backward 411, 456.
-Plan plan(int64_t heads, int64_t units, bool causal) {
+//
+// A lot is as many heads as fill whole lines of the cache, four at most: 8 x 8 heads, 1024 to 2048
+// keys, 128 forward 247 us, with a die's heads all next to each other (of one sample) 289; 32 x 16
+// heads of 80, 128 to 256 keys, 23 us, one by one 28.
+Plan plan(int64_t heads, int64_t units, int D, bool causal) {
   const int64_t per = heads / 8, near = std::max<int64_t>(1, causal ? per : std::min<int64_t>(per, 4));
   const int64_t rest = per % near, last = rest ? per - rest : std::max<int64_t>(0, per - near);
-  return {(int)per, (int)units, (int)near, (int)last, divisor(near), divisor(std::max<int64_t>(1, near * units)),
+  int lot = 0;
+  while (lot < 2 && (D << lot) % 64 && per % (2 << lot) == 0) ++lot;
+  return {(int)per, (int)units, (int)near, (int)last, lot, divisor(near), divisor(std::max<int64_t>(1, near * units)),
           divisor(std::max<int64_t>(1, per - last)), divisor(std::max<int64_t>(1, heads - 8 * per))};
 }
 
@@ -1175,8 +1184,8 @@ void place_scratch(AttnArgs& a, const Scratch& s, void* workspace) {
   a.shares = a.partial = a.vmax + s.vmax, a.tops = a.shares + s.shares;
   a.parts = s.parts, a.kparts = s.kparts, a.parts_d = divisor(s.parts), a.kparts_d = divisor(s.kparts);
   const int64_t heads = (int64_t)a.Hk * a.B, rows = (int64_t)a.Lq * a.share.d;
-  a.by_rows = plan(heads, (rows + 127) / 128 * a.kparts, a.causal);
-  a.by_keys = plan(heads, ((int64_t)a.Lk + 127) / 128 * a.parts, a.causal);
+  a.by_rows = plan(heads, (rows + 127) / 128 * a.kparts, a.D, a.causal);
+  a.by_keys = plan(heads, ((int64_t)a.Lk + 127) / 128 * a.parts, a.D, a.causal);
 }
 
 template <typename T, int KS, bool DIRECT>
