@@ -1225,6 +1225,8 @@ bool direct(const void* ptr, const int64_t* stride, int L, int share, int D) {
   return 64 * row + share * head < (1ll << 31);
 }
 
+// Head sizes by steps of 16 terms: heads of 40 take dk and dv 830 us with three steps, 1020 with four
+// (14 x 30 on 15 heads, 1576 to 3152 keys, causal; dq 560 and 580, forward 469 and 477).
 template <typename T>
 void launch(const AttnArgs& a, bool backward, hipStream_t st) {
   const bool fast = a.D % 8 == 0 && direct(a.k, a.ks, a.Lk, 1, a.D) && direct(a.v, a.vs, a.Lk, 1, a.D) &&
@@ -1234,6 +1236,7 @@ void launch(const AttnArgs& a, bool backward, hipStream_t st) {
     else launch<T, 8, false>(a, backward, st);
   }
   else if (a.D <= 32) launch<T, 2, true>(a, backward, st);
+  else if (a.D <= 48) launch<T, 3, true>(a, backward, st);
   else if (a.D <= 64) launch<T, 4, true>(a, backward, st);
   else if (a.D <= 80) launch<T, 5, true>(a, backward, st);
   else if (a.D <= 96) launch<T, 6, true>(a, backward, st);

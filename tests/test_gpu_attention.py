@@ -33,7 +33,7 @@ def _check(q, k, v, dout, backward=True, **mask):
 
 
 @pytest.mark.parametrize("dtype", [torch.float16, torch.bfloat16], ids=["f16", "bf16"])
-@pytest.mark.parametrize("D", [1, 8, 17, 32, 40, 64, 72, 80, 96, 100, 128])
+@pytest.mark.parametrize("D", [1, 8, 17, 32, 40, 48, 64, 72, 80, 96, 100, 128])
 def test_head_sizes(D, dtype):
     _check(*_inputs(2, 70, 150, 2, 2, D, dtype, seed=D))
     _check(*_inputs(1, 130, 130, 2, 1, D, dtype, seed=D + 1), causal=True)

@@ -30,7 +30,7 @@ def kernels(tmp_path_factory):
 
 
 def test_every_kernel_is_there(kernels):
-    want = {(k, p, True) for k in ("fwd", "few", "dq", "dkv") for p in (2, 4, 5, 6, 8)}
+    want = {(k, p, True) for k in ("fwd", "few", "dq", "dkv") for p in (2, 3, 4, 5, 6, 8)}
     want |= {(k, p, False) for k in ("fwd", "few", "dq", "dkv") for p in (4, 8)}
     assert set(kernels) == want
 
