@@ -1021,6 +1021,83 @@ __global__ __launch_bounds__(256, KS <= 4 ? 3 : 2) void k_attn_dkv(AttnArgs a) {
   }
 }
 
+// ---- backward of a few rows over a few keys ------------------------------------------------------
+//
+// All of one key head's problem in LDS and in 32 bits, one workgroup, one launch for dq, dk and dv:
+//   P = exp2(c q k - log2(e) lse), dS = P (dout v - sum_j P dout v),
+//   dq = scale dS k, dk = scale dS^T q, dv = P^T dout.
+// Bound by latency: the products are a few thousand terms a column, and matrix instructions would
+// be given tiles that are mostly empty.  With so few terms the roundings of P and dS to 16 bits
+// do not average out either (errors up to 1.55 times those of the result's rounding alone); here
+// there are none.  4 heads, 8 x 8: 15 us the call (17 with the kernels above, two launches); 2560
+// heads of 128, 8 x 16: 67 us (80); of 64, 11 x 11: 49 (bfloat16 42, float16 56); 16 x 32, past
+// the limit: 156 (88).
+constexpr int kFewRows = 16, kFewKeys = 32, kFewTerms = 128;
+
+template <typename T>
+__global__ __launch_bounds__(256) void k_attn_small(AttnArgs a) {
+  constexpr int S = 129;   // floats from row to row: odd, so that neither order of reading meets a bank twice
+  __shared__ float q[kFewRows][S], dout[kFewRows][S], k[kFewKeys][S], v[kFewKeys][S];
+  __shared__ float p[kFewRows][kFewKeys + 1], ds[kFewRows][kFewKeys + 1];
+  const int b = a.heads_k.of(blockIdx.x), hk = blockIdx.x - b * a.Hk, rows = a.Lq * a.share.d;
+  const int nq = length(a.len_q, b, a.Lq), nk = length(a.len_k, b, a.Lk), ahead = nk - nq;
+  const int d = threadIdx.x % 128, part = threadIdx.x / 128;
+  auto sees = [&](int i) { return i >= nq ? 0 : a.causal ? max(0, min(nk, i + ahead + 1)) : nk; };
+  if (d < a.D) {
+#pragma unroll
+    for (int n = 0; n < kFewRows; n += 2) {
+      const int r = n + part, i = a.share.of(r), h = (hk - i) * a.share.d + r;
+      const bool there = r < rows && i < nq;
+      q[r][d] = there ? (float)((const T*)a.q)[b * a.qs[0] + i * a.qs[1] + h * a.qs[2] + d] : 0.0f;
+      dout[r][d] = there ? (float)((const T*)a.dout)[b * a.dos[0] + i * a.dos[1] + h * a.dos[2] + d] : 0.0f;
+    }
+#pragma unroll
+    for (int n = 0; n < kFewKeys; n += 2) {
+      const int j = n + part;
+      k[j][d] = j < nk ? (float)((const T*)a.k)[b * a.ks[0] + j * a.ks[1] + hk * a.ks[2] + d] : 0.0f;
+      v[j][d] = j < nk ? (float)((const T*)a.v)[b * a.vs[0] + j * a.vs[1] + hk * a.vs[2] + d] : 0.0f;
+    }
+  }
+  __syncthreads();
+#pragma unroll
+  for (int n = 0; n < kFewRows; n += 8) {   // 32 lanes a row
+    const int r = n + threadIdx.x / 32, j = threadIdx.x % 32, i = a.share.of(r), h = (hk - i) * a.share.d + r;
+    float x = 0.0f, dp = 0.0f;
+    const bool seen = r < rows && j < sees(i);
+    if (seen) {
+      for (int e = 0; e < a.D; ++e) {
+        x = __builtin_fmaf(q[r][e], k[j][e], x);
+        dp = __builtin_fmaf(dout[r][e], v[j][e], dp);
+      }
+      const float lse = a.lse[((int64_t)b * a.Hq + h) * a.Lq + i];
+      x = lse == -kInf ? 0.0f : __builtin_amdgcn_exp2f(__builtin_fmaf(x, a.c, -kLog2e * lse));
+    }
+    float delta = seen ? x * dp : 0.0f;
+#pragma unroll
+    for (int m = 1; m < 32; m *= 2) delta += __shfl_xor(delta, m);
+    p[r][j] = seen ? x : 0.0f;
+    ds[r][j] = seen ? x * (dp - delta) : 0.0f;
+  }
+  __syncthreads();
+  if (d >= a.D) return;
+  for (int r = part; r < rows; r += 2) {
+    const int i = a.share.of(r), h = (hk - i) * a.share.d + r, end = sees(i);
+    float x = 0.0f;
+    for (int j = 0; j < end; ++j) x = __builtin_fmaf(ds[r][j], k[j][d], x);
+    ((T*)a.dq)[b * a.dqs[0] + i * a.dqs[1] + h * a.dqs[2] + d] = (T)(x * a.scale);
+  }
+  for (int j = part; j < a.Lk; j += 2) {
+    const int first = j >= nk ? rows : a.causal ? max(0, j - ahead) * a.share.d : 0, end = nq * a.share.d;
+    float x = 0.0f, y = 0.0f;
+    for (int r = first; r < end; ++r) {
+      x = __builtin_fmaf(ds[r][j], q[r][d], x);
+      y = __builtin_fmaf(p[r][j], dout[r][d], y);
+    }
+    ((T*)a.dk)[b * a.dks[0] + j * a.dks[1] + hk * a.dks[2] + d] = (T)(x * a.scale);
+    ((T*)a.dv)[b * a.dvs[0] + j * a.dvs[1] + hk * a.dvs[2] + d] = (T)y;
+  }
+}
+
 // dk and dv from their shares, four values a thread, in the shares' order.
 template <typename T>
 __global__ __launch_bounds__(256) void k_attn_join(AttnArgs a) {
@@ -1216,6 +1293,11 @@ void launch(const AttnArgs& a, bool backward, hipStream_t st) {
   }
 }
 
+bool small(const AttnArgs& a) {
+  const int64_t rows = (int64_t)a.Lq * a.share.d;
+  return rows <= kFewRows && a.Lk <= kFewKeys && rows * a.Lk <= kFewTerms;
+}
+
 // Whether 64 rows of an array can be loaded straight to LDS.
 bool direct(const void* ptr, const int64_t* stride, int L, int share, int D) {
   if (L == 0) return true;
@@ -1229,6 +1311,10 @@ bool direct(const void* ptr, const int64_t* stride, int L, int share, int D) {
 // (14 x 30 on 15 heads, 1576 to 3152 keys, causal; dq 560 and 580, forward 469 and 477).
 template <typename T>
 void launch(const AttnArgs& a, bool backward, hipStream_t st) {
+  if (backward && small(a)) {
+    hipLaunchKernelGGL(k_attn_small<T>, dim3((unsigned)(a.B * a.Hk)), dim3(256), 0, st, a);
+    return;
+  }
   const bool fast = a.D % 8 == 0 && direct(a.k, a.ks, a.Lk, 1, a.D) && direct(a.v, a.vs, a.Lk, 1, a.D) &&
                     (!backward || (direct(a.q, a.qs, a.Lq, a.share.d, a.D) && direct(a.dout, a.dos, a.Lq, a.share.d, a.D)));
   if (!fast) {

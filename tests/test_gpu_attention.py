@@ -310,3 +310,47 @@ def test_strides_of_extents_of_one():
     assert torch.equal(base[0], got[0]) and torch.equal(base[1], got[1]) and torch.equal(base[0], v)
     for x, y in zip(g.gbmw_attention_backward(dout, q, k, v, *base), g.gbmw_attention_backward(odd[3], *odd[:3], *got)):
         assert torch.equal(x, y)
+
+
+@pytest.mark.parametrize("dtype", [torch.float16, torch.bfloat16], ids=["f16", "bf16"])
+@pytest.mark.parametrize("B,Lq,Lk,Hq,Hk,D", [(1, 1, 1, 1, 1, 8), (3, 8, 8, 6, 6, 64), (5, 3, 19, 4, 2, 96), (2, 16, 8, 2, 2, 128), (4, 4, 32, 3, 3, 40),
+                                             (2, 2, 7, 8, 1, 17), (3, 0, 9, 2, 2, 64), (9, 11, 11, 2, 1, 80)])
+def test_gradients_of_few_rows_and_keys_are_rounded_once(B, Lq, Lk, Hq, Hk, D, dtype):
+    """Few terms do not average their roundings out.  Bound: the result's rounding; probabilities from a log-sum-exp and
+    an exponential good to 2^-18 (1 + |lse|), |lse| < 7 here, so 2^-15 of each term; up to 11 x 2 rows or 32 keys and
+    256 products in 32 bits, far less.  Past the kernel's sizes (11 x 11 rows of two heads) the usual bound."""
+    import paper_2307_02031_amd as g
+    q, k, v, dout = _inputs(B, Lq, Lk, Hq, Hk, D, dtype, seed=17)
+    wide = torch.full((B, Lk, 2 * Hk, D), float("nan"), dtype=dtype, device="cuda")
+    wide[:, :, :Hk] = k
+    k = wide[:, :, :Hk]                                            # heads of a larger row
+    n = torch.arange(B, dtype=torch.int32, device="cuda")
+    for mask in (dict(), dict(causal=True), dict(causal=True, len_q=(Lq - n).clamp(0), len_k=(Lk - 2 * n).clamp(0)), dict(scale=0.4)):
+        got = _check(q, k, v, dout, **mask)
+        if Lq * Hq // Hk * Lk > 128:
+            continue
+        want = ref.attention(q, k, v, dout=dout, out_given=got["out"], **mask)
+        terms = _terms(q, k, v, dout, **mask)
+        u = ref.U[dtype]
+        for name in ("dq", "dk", "dv"):
+            bound = u * want[name][0].abs() + 2.0 ** -15 * terms[name] + ref.TINY[dtype]
+            ref.assert_close(name, got[name], want[name][0], bound)
+
+
+def _terms(q, k, v, dout, causal=False, scale=None, len_q=None, len_k=None):
+    """The sums of the terms' sizes in dq, dk and dv."""
+    q, k, v, dout = (ref.f64(t) for t in (q, k, v, dout))
+    (B, Lq, Hq, D), (Lk, Hk) = q.shape, k.shape[1:3]
+    scale = D ** -0.5 if scale is None else scale
+    res = dict(dq=torch.zeros_like(q), dk=torch.zeros_like(v), dv=torch.zeros_like(v))
+    for b, h in itertools.product(range(B), range(Hq)):
+        nq, nk = (L if n is None else int(n[b]) for L, n in ((Lq, len_q), (Lk, len_k)))
+        m, kh = ref.sees(Lq, Lk, causal, nq, nk)[:nq, :nk], h * Hk // Hq
+        qq, dd, kk, vv = q[b, :nq, h], dout[b, :nq, h], k[b, :nk, kh], v[b, :nk, kh]
+        p = torch.where(m, torch.softmax(torch.where(m, scale * qq @ kk.T, -1e300), 1), 0.0)
+        dp = dd.abs() @ vv.abs().T
+        ds = p * (dp + (p * dp).sum(1, keepdim=True))
+        res["dq"][b, :nq, h] = scale * ds @ kk.abs()
+        res["dk"][b, :nk, kh] += scale * ds.T @ qq.abs()
+        res["dv"][b, :nk, kh] += p.T @ dd.abs()
+    return res
