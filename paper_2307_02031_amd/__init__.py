@@ -442,6 +442,15 @@ def _device_of(name: str, t, types) -> int:
     return device
 
 
+def _stream_of(stream):
+    """A torch stream for one, or for a handle.  0 is the default stream's: an ExternalStream of it would be a new
+    stream, which waits for nobody."""
+    if isinstance(stream, torch.cuda.Stream):
+        return stream
+    handle = int(getattr(stream, "cuda_stream", stream))
+    return torch.cuda.ExternalStream(handle) if handle else torch.cuda.default_stream()
+
+
 def _on_stream(call):
     """call with one more argument: `stream`, a torch stream or a handle, by default the current one.  Outputs and
     scratch memory that a call makes belong to the stream its kernels run on, so that the memory is not handed to
@@ -451,7 +460,7 @@ def _on_stream(call):
     def on_stream(*args, stream=None, **kw):
         if stream is None:
             return call(*args, **kw)
-        with torch.cuda.stream(torch.cuda.ExternalStream(int(getattr(stream, "cuda_stream", stream)))):
+        with torch.cuda.stream(_stream_of(stream)):
             return call(*args, **kw)
     return on_stream
 
