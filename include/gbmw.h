@@ -527,8 +527,9 @@ typedef struct {
 gbmw_status gbmw_attention_forward(const gbmw_attention_problem* p);
 gbmw_status gbmw_attention_backward(const gbmw_attention_problem* p);
 
-/* Bytes of workspace that a call on this problem needs (the sizes alone are read; may
- * be 0); -1 with a message if the sizes are out of range. */
+/* Bytes of workspace that a call on this problem needs (may be 0); -1 with a message if
+ * they are out of range.  Read: dtype, the sizes, causal and scale.  More or fewer under a
+ * causal mask than without one. */
 int64_t gbmw_attention_workspace(const gbmw_attention_problem* p, int32_t backward);
 
 /*

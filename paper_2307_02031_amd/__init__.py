@@ -531,14 +531,18 @@ def _lse(p, lse, device: int) -> None:
     p.lse = lse.data_ptr()
 
 
-def gbmw_attention_workspace(q, k, backward: bool) -> int:
-    """Bytes of workspace of a call on q [B][Lq][Hq][D] and k [B][Lk][Hk][D]."""
+def gbmw_attention_workspace(q, k, backward: bool, causal: bool | None = None) -> int:
+    """Bytes of workspace of a call on q [B][Lq][Hq][D] and k [B][Lk][Hk][D].  causal: the call's mask; by default as
+    many bytes as either mask needs."""
     p = gbmw_attention_problem()
     p.dtype, (p.B, p.Lq, p.Hq, p.D), (p.Lk, p.Hk) = _DTYPE.get(q.dtype, -1), q.shape, (k.shape[1], k.shape[2])
-    n = _lib.gbmw_attention_workspace(ct.byref(p), int(backward))
-    if n < 0:
-        raise GbmwError(GBMW_ERR_INVALID_ARG, gbmw_last_error())
-    return n
+    need = 0
+    for p.causal in (0, 1) if causal is None else (1 if causal else 0,):
+        n = _lib.gbmw_attention_workspace(ct.byref(p), int(backward))
+        if n < 0:
+            raise GbmwError(GBMW_ERR_INVALID_ARG, gbmw_last_error())
+        need = max(need, n)
+    return need
 
 
 def _new_like(t):
