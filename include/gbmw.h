@@ -493,9 +493,10 @@ enum { GBMW_F32 = 0, GBMW_F16 = 1, GBMW_BF16 = 2 };
  *   dq_i = scale sum_j ds_ij k_j,  dk_j = scale sum_i ds_ij q_i,  dv_j = sum_i p_ij dout_i,
  * dk and dv summed over the query heads that read the key head.  Rows without keys
  * give and get no gradient (0), nor do keys that no row sees.
- * q, k, v, dout beyond the lengths are not used, whatever they hold.  Inside the
- * lengths values should be finite: a NaN or an infinity reaches the rows that see it,
- * and may reach rows from which only the causal mask hides it.
+ * q, k, v, dout beyond the lengths are not used, whatever they hold, nor are q and dout
+ * of rows without keys.  Elsewhere values should be finite: a NaN or an infinity reaches
+ * the rows that see it, and may reach rows that see other keys and from which only the
+ * causal mask hides it.
  *
  * Layout: element (b, row, head, d) of an array X is at X + b * X_stride[0] +
  * row * X_stride[1] + head * X_stride[2] + d, in elements; strides are >= 0, so inputs

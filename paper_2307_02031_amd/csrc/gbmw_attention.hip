@@ -313,6 +313,16 @@ __device__ __forceinline__ void store_quad(T* row, int d, int D, f32x4 x) {
   }
 }
 
+// A row that sees no key has the result 0 by choice, not as a product with 0: the others' keys may
+// hold anything.
+template <int DB>
+__device__ __forceinline__ void clear_unless(bool sees, f32x16 (&x)[DB]) {
+#pragma unroll
+  for (int d = 0; d < DB; ++d)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) x[d][r] = sees ? x[d][r] : 0.0f;
+}
+
 // A lane's part of a result's rows, times f, as a share in 32 bits.
 template <int DB>
 __device__ __forceinline__ void store_share(float* row, int D4, const f32x16 (&x)[DB], float f) {
@@ -535,6 +545,7 @@ __global__ __launch_bounds__(256, 2) void k_attn_fwd(AttnArgs a) {
   run.sum += __shfl_xor(run.sum, 32);
   if (row >= w.rows) return;
   const float level = level_of<T>(run.m, run.sum, a.c), f = level == -kInf ? 0.0f : 1.0f / run.sum;
+  if (!__all(w.begin < sees)) clear_unless(w.begin < sees, run.o);
   if (a.kparts == 1) {
     if (half == 0) a.lse[((int64_t)w.b * a.Hq + hq) * a.Lq + i] = level * kLn2;
     char* out = a.out + 2 * (w.b * a.os[0] + i * a.os[1] + hq * a.os[2]);
@@ -611,6 +622,7 @@ __global__ __launch_bounds__(256, 1) void k_attn_few(AttnArgs a) {
     }
   }
   run.sum += __shfl_xor(run.sum, 32);
+  if (!__all(w.begin < sees)) clear_unless(w.begin < sees, run.o);
   {
     const float level = level_of<T>(run.m, run.sum, a.c);
     if (half == 0) sTop[wave][row] = level, sSum[wave][row] = run.sum;
@@ -778,7 +790,8 @@ __global__ __launch_bounds__(256, 2) void k_attn_dq(AttnArgs a) {
   }
   float up = 1.0f, down = 1.0f;   // powers of two
   if constexpr (kLift) {
-    norm = __builtin_sqrtf(norm + __shfl_xor(norm, 32));
+    norm += __shfl_xor(norm, 32);
+    norm = sees > 0 ? __builtin_sqrtf(norm) : 0.0f;
     const int parts = (a.Lk + 63) / 64;
     const int k = lift_of(norm * max_of(a.vmax + ((int64_t)b * a.Hk + hk) * parts, (nk + 63) / 64));
     up = __builtin_ldexpf(1.0f, k), down = __builtin_ldexpf(1.0f, -k);
@@ -846,6 +859,7 @@ __global__ __launch_bounds__(256, 2) void k_attn_dq(AttnArgs a) {
     __syncthreads();   // the next pass begins with the first buffer again
   }
   if (row >= rows) return;
+  if (!__all(w.begin < sees)) clear_unless(w.begin < sees, o);
   const int64_t at = ((int64_t)b * a.Hk + hk) * rows + row;
   if (half == 0 && w.part == 0) a.delta[at] = a.kparts == 1 ? delta + left : delta, a.level[at] = lse - kUp<T>;
   if (a.kparts == 1) {
@@ -890,7 +904,8 @@ __global__ __launch_bounds__(256, KS <= 4 ? 3 : 2) void k_attn_dkv(AttnArgs a) {
   auto first_of = [&](int j) { return a.causal ? max(0, j - (nk - nq)) * a.share.d : 0; };
   const int first = first_of(key);
   // the rows that see a key of the tile, in `parts` runs of whole tiles
-  int begin = tile * 128 < nk ? min(first_of(tile * 128) / 64 * 64, rows) : rows;
+  // and no row before the first that sees a key at all: dout there may be anything
+  int begin = tile * 128 < nk ? min(max(first_of(tile * 128) / 64 * 64, first_of(0)), rows) : rows;
   const int run = a.parts_d.of((rows - begin + 63) / 64 + a.parts - 1) * 64;
   begin = min((int64_t)begin + (int64_t)part * run, (int64_t)rows);
   const int end = min((int64_t)begin + run, (int64_t)rows);
