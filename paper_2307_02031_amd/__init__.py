@@ -14,6 +14,7 @@ from __future__ import annotations
 
 import ctypes as ct
 import functools
+import operator
 import os
 
 import numpy as np
@@ -430,6 +431,12 @@ def _check_tensor(name: str, t, device: int, dtype, shape) -> None:
         _refuse_tensor(name, t, device, dtype, shape)
 
 
+def _check_counts(name: str, sizes: int) -> None:
+    """sizes: the sizes' bits together.  What the library counts in 32 bits would lose its upper ones without a word."""
+    if sizes >> 31:
+        _refuse(f"{name}: a size of 2^31 or more")
+
+
 def _device_of(name: str, t, types) -> int:
     """The current device, which the first argument has to be on, with one of the types."""
     if not isinstance(t, torch.Tensor) or not t.is_cuda:
@@ -505,6 +512,7 @@ def _attention_problem(q, k, v, causal, scale, len_q, len_k):
     if kshape[0] != B or kshape[3] != D or k.dtype != dtype or k.get_device() != device:
         _refuse_tensor("k", k, device, dtype, (B, kshape[1], kshape[2], D))
     _check_tensor("v", v, device, dtype, kshape)
+    _check_counts("q and k", B | Lq | Hq | D | kshape[1] | kshape[2])
     if len_q is not None:
         len_q = _length("len_q", len_q, device, B)
     if len_k is not None:
@@ -534,6 +542,7 @@ def _lse(p, lse, device: int) -> None:
 def gbmw_attention_workspace(q, k, backward: bool, causal: bool | None = None) -> int:
     """Bytes of workspace of a call on q [B][Lq][Hq][D] and k [B][Lk][Hk][D].  causal: the call's mask; by default as
     many bytes as either mask needs."""
+    _check_counts("q and k", functools.reduce(operator.or_, (*q.shape, *k.shape)))
     p = gbmw_attention_problem()
     p.dtype, (p.B, p.Lq, p.Hq, p.D), (p.Lk, p.Hk) = _DTYPE.get(q.dtype, -1), q.shape, (k.shape[1], k.shape[2])
     need = 0
@@ -625,6 +634,7 @@ def _norm_problem(x, weight, bias):
     if len(shape) < 1:
         _refuse("x has no axis")
     p, cols = gbmw_layer_norm_problem(), shape[-1]
+    _check_counts("x", cols)
     p.dtype = p.wdtype = _DTYPE[dtype]
     p.rows, p.cols, p.x_stride = x.numel() // max(1, cols), cols, _row_stride("x", x)
     p.x, p.stream = x.data_ptr(), _raw_stream(device)
