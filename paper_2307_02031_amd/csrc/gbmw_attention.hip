@@ -709,11 +709,13 @@ __global__ __launch_bounds__(256) void k_attn_merge(AttnArgs a) {
   }
 }
 
-// The largest norm of a value among 64 keys of a (sample, key head), for float16's lift.
+// The largest norm of a value among 64 keys of a (sample, key head), for float16's lift.  Workgroup
+// (x, y) takes half y of x's 128 keys.
 __global__ __launch_bounds__(256) void k_attn_vmax(AttnArgs a) {
   __shared__ float tops[4];
-  const int parts = (a.Lk + 63) / 64, part = blockIdx.x % parts;
-  const int hk = blockIdx.x / parts % a.Hk, b = blockIdx.x / parts / a.Hk;
+  const int parts = (a.Lk + 63) / 64, tiles = (a.Lk + 127) / 128, part = 2 * (blockIdx.x % tiles) + blockIdx.y;
+  if (part >= parts) return;
+  const int head = blockIdx.x / tiles, hk = head % a.Hk, b = head / a.Hk;
   // sixteen lanes a row, a piece each
   const int last = min(part * 64 + 64, length(a.len_k, b, a.Lk)), d = threadIdx.x % 16 * 8;
   const f16* v = (const f16*)a.v + b * a.vs[0] + hk * a.vs[2] + d;
@@ -731,7 +733,7 @@ __global__ __launch_bounds__(256) void k_attn_vmax(AttnArgs a) {
   for (int d = 32; d; d >>= 1) s = fmaxf(s, __shfl_xor(s, d));
   if (threadIdx.x % 64 == 0) tops[threadIdx.x / 64] = s;
   __syncthreads();
-  if (threadIdx.x == 0) a.vmax[blockIdx.x] = __builtin_sqrtf(fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3])));
+  if (threadIdx.x == 0) a.vmax[(int64_t)head * parts + part] = __builtin_sqrtf(fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3])));
 }
 
 // ---- backward, dq -----------------------------------------------------------------------------
@@ -1141,7 +1143,8 @@ gbmw_status check_sizes(const gbmw_attention_problem* p) {
   if (p->D < 1 || p->D > 128) return fail(GBMW_ERR_INVALID_ARG, "D=%d not in 1..128", p->D);
   const int64_t rows = (int64_t)p->Lq * (p->Hq / p->Hk);
   if (rows > INT_MAX - 256 || p->Lk > INT_MAX - 256) return fail(GBMW_ERR_INVALID_ARG, "too many rows");
-  // a launch has fewer than 2^32 threads, 2^24 workgroups of 256 (few tiles are shared by up to 64 of them)
+  // A launch has fewer than 2^32 threads along x, 2^24 workgroups of 256.  Tiles are shared by several
+  // workgroups only where all of them are at most 4 * kSlots.
   const int64_t groups = std::max((rows + 127) / 128, ((int64_t)p->Lk + 127) / 128) * p->Hk;
   if (groups >= 1 << 24 || groups * p->B >= 1 << 24) return fail(GBMW_ERR_INVALID_ARG, "too many rows in all");
   if (p->causal != 0 && p->causal != 1) return fail(GBMW_ERR_INVALID_ARG, "causal=%d", p->causal);
@@ -1295,7 +1298,7 @@ void launch(const AttnArgs& a, bool backward, hipStream_t st) {
     return;
   }
   if constexpr (__is_same(T, f16))
-    if (a.Lk) hipLaunchKernelGGL(k_attn_vmax, grid(a.Lk, 64), block, 0, st, a);
+    if (a.Lk) hipLaunchKernelGGL(k_attn_vmax, dim3(grid(a.Lk, 128).x, 2), block, 0, st, a);
   if (rows) {
     hipLaunchKernelGGL((k_attn_dq<T, KS, DIRECT>), times(grid(rows, 128), a.kparts), block, 0, st, a);
     if (a.kparts > 1) hipLaunchKernelGGL((k_attn_merge<T, true>), merge, block, 0, st, a);
