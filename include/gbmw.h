@@ -575,7 +575,8 @@ int64_t gbmw_layer_norm_workspace(const gbmw_layer_norm_problem* p);
  *   out  = grad * (scale * (norm > max_norm ? max_norm / norm : 1)),
  * scale being the inverse of a loss scale (1 without one).  The sum is kept in fp64, so
  * no square overflows.  A norm that is NaN or infinite (a gradient is) leaves the
- * factor at `scale`: `norm` tells, and the step is the caller's to skip.
+ * factor at `scale`: `norm` tells, and the step is the caller's to skip.  A finite norm
+ * beyond fp32's range clips like any other; `norm` then reads infinity, but no output is.
  *
  * A list is made once for tensors that stay where they are: it copies the addresses and
  * sizes to the device and owns a workspace for the sums.  It holds no tensor alive.

@@ -344,6 +344,18 @@ __global__ __launch_bounds__(1024) void k_norm_join(const float* partial, int pa
 // fp32: together 342 us (387 with ordinary stores), 1.9 GB at 5.5 TB/s; 20M fp32 ones: 39 us (49).
 // Squares are added in fp64, at a few per cent of its rate: nothing overflows, and the norm is
 // right to the last bit of fp32.
+//
+// A factor below fp32's normal numbers (gradients near the largest ones, whose norm fp32 may not
+// hold) would lose its digits, so it is taken with an exponent of its own.
+struct Factor {
+  float value;   // times 2^exponent
+  int exponent = 0;
+  __device__ __forceinline__ explicit Factor(double factor) : value((float)factor) {
+    if (factor < 0x1p-126 && (double)value != factor) value = (float)frexp(factor, &exponent);
+  }
+  __device__ __forceinline__ bool is_one() const { return value == 1.0f && exponent == 0; }
+  __device__ __forceinline__ float of(float x) const { return __builtin_ldexpf(x * value, exponent); }
+};
 
 struct Piece {   // a run of at most kPiece elements of one tensor
   const void* in;
@@ -404,7 +416,7 @@ __global__ __launch_bounds__(256) void k_clip_norm(const Piece* pieces, int coun
 // STREAM: the stores pass the cache by (a wave's are whole lines of it), so that what is still to
 // be read stays there.
 template <typename T, typename O, bool STREAM>
-__device__ __forceinline__ void scale_piece(const Piece& pc, float factor) {
+__device__ __forceinline__ void scale_piece(const Piece& pc, Factor factor) {
   constexpr int V = kVec<O>, U = kUnroll;   // as many elements as a store of 16 bytes takes
   typedef float f32x4 __attribute__((ext_vector_type(4)));
   const T* in = (const T*)pc.in;
@@ -418,7 +430,7 @@ __device__ __forceinline__ void scale_piece(const Piece& pc, float factor) {
     for (int u = 0; u < U; ++u) {
       Pack<O> y;
 #pragma unroll
-      for (int e = 0; e < V; ++e) y.v[e] = (O)((float)x[u][e] * factor);
+      for (int e = 0; e < V; ++e) y.v[e] = (O)factor.of((float)x[u][e]);
       if constexpr (STREAM) __builtin_nontemporal_store(__builtin_bit_cast(f32x4, y), (f32x4*)(out + i + u * 256 * V));
       else __builtin_memcpy(out + i + u * 256 * V, &y, 16);
     }
@@ -426,11 +438,11 @@ __device__ __forceinline__ void scale_piece(const Piece& pc, float factor) {
   for (; i < pc.n; i += 256 * V)
 #pragma unroll
     for (int e = 0; e < V; ++e)
-      if (i + e < pc.n) out[i + e] = (O)((float)in[i + e] * factor);
+      if (i + e < pc.n) out[i + e] = (O)factor.of((float)in[i + e]);
 }
 
 template <typename T, typename O>
-__device__ __forceinline__ void scale_piece(const Piece& pc, float factor) {
+__device__ __forceinline__ void scale_piece(const Piece& pc, Factor factor) {
   if ((uintptr_t)pc.out % 128 == 0) scale_piece<T, O, true>(pc, factor);
   else scale_piece<T, O, false>(pc, factor);
 }
@@ -447,11 +459,11 @@ __global__ __launch_bounds__(256) void k_clip_scale(const Piece* pieces, int cou
   for (int k = threadIdx.x; k < parts; k += 256) s += partial[k];
   const double norm = __builtin_sqrt(group_sum(s, sums)) * scale;
   const bool clips = norm > max_norm && norm < __builtin_inf();
-  const float factor = (float)(clips ? scale * (max_norm / norm) : scale);
+  const Factor factor(clips ? scale * (max_norm / norm) : scale);
   if (blockIdx.x == 0 && threadIdx.x == 0 && norm_out) *norm_out = (float)norm;
   for (int k = count - 1 - (int)blockIdx.x; k >= 0; k -= gridDim.x) {
     const Piece pc = pieces[k];
-    if (factor == 1.0f && pc.in == pc.out) continue;   // the values are there
+    if (factor.is_one() && pc.in == pc.out) continue;   // the values are there
     if (pc.in_dtype == GBMW_F32) scale_piece<float, float>(pc, factor);
     else if (pc.in_dtype == GBMW_F16 && pc.out_dtype == GBMW_F16) scale_piece<f16, f16>(pc, factor);
     else if (pc.in_dtype == GBMW_F16) scale_piece<f16, float>(pc, factor);
