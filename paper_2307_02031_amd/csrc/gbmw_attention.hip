@@ -1045,10 +1045,19 @@ __global__ __launch_bounds__(256, KS <= 4 ? 3 : 2) void k_attn_dkv(AttnArgs a) {
 //   dq = scale dS k, dk = scale dS^T q, dv = P^T dout.
 // Bound by latency: the products are a few thousand terms a column, and matrix instructions would
 // be given tiles that are mostly empty.  With so few terms the roundings of P and dS to 16 bits
-// do not average out either (errors up to 1.55 times those of the result's rounding alone); here
-// there are none.  4 heads, 8 x 8: 15 us the call (17 with the kernels above, two launches); 2560
-// heads of 128, 8 x 16: 67 us (80); of 64, 11 x 11: 49 (bfloat16 42, float16 56); 16 x 32, past
-// the limit: 156 (88).
+// do not average out either: the kernels above are off by 1.42 times the result's own rounding on
+// average, by up to 1.56 where there are few heads.  Here P and dS are not rounded: 1.00.
+//
+// Its time grows with the pairs of rows and keys, theirs hardly does (us of the kernels, here / there):
+//   heads x size   type       8 x 8        8 x 16       4 x 32       16 x 8       12 x 12      16 x 16
+//   64 x 64        bfloat16   9.6 / 12.1   12.1 / 12.1  13.1 / 12.1  14.1 / 11.9  14.8 / 12.1  18.4 / 11.9
+//   64 x 128       bfloat16   11.1 / 15.5  13.4 / 15.5  14.4 / 15.5  16.8 / 15.4  17.2 / 15.5  20.9 / 15.4
+//   64 x 64        float16    9.7 / 17.1   12.3 / 17.1  13.3 / 17.3  14.3 / 17.0  14.9 / 17.0  18.6 / 17.0
+//   2560 x 64      bfloat16   36 / 41      47 / 43      62 / 45      55 / 42      58 / 43      80 / 44
+//   2560 x 128     float16    47 / 89      64 / 91      71 / 96      79 / 91      80 / 91      102 / 92
+// They meet between 64 and 128 pairs with bfloat16, between 144 and 256 with float16; the limit is
+// one in between, 128.  Up to it bfloat16 pays at most 1.37 times the time (2560 heads of 64, 4 x 32)
+// for results that are rounded once.
 constexpr int kFewRows = 16, kFewKeys = 32, kFewTerms = 128;
 
 template <typename T>
