@@ -13,6 +13,7 @@
 // probabilities go from one product into the next without leaving their lanes, and the
 // other operand is read in the same order (Reader::cols).
 #include <algorithm>
+#include <cfloat>
 #include <climits>
 #include <cmath>
 
@@ -1207,8 +1208,8 @@ AttnArgs args_of(const gbmw_attention_problem* p) {
   a.share = divisor(p->Hq / p->Hk), a.heads_k = divisor(p->Hk);
   a.D4 = (p->D + 3) / 4 * 4;
   a.causal = p->causal, a.scale = p->scale;
-  // not 0: a hidden key's -inf has to stay -inf when it is scaled
-  a.c = std::max(p->scale * kLog2e, 1e-30f);
+  // neither 0 nor infinite: a hidden key's -inf has to stay -inf when it is scaled, a score of 0 has to stay 0
+  a.c = std::clamp(p->scale * kLog2e, FLT_MIN, FLT_MAX);
   return a;
 }
 
