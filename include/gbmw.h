@@ -477,7 +477,9 @@ gbmw_status gbmw_cost_model(const gbmw_layer_shape* layers, int32_t L,
  *     faster, not required); outputs must not overlap one another or the inputs
  *     unless a text below says so;
  *   - sums, softmax statistics and products are accumulated in fp32 (sums of squares
- *     of gradients in fp64) and outputs are rounded once, to nearest even;
+ *     of gradients in fp64) and outputs are rounded to nearest even.  They are rounded
+ *     once, but for attention's: there p_ij and ds_ij are rounded to dtype too, where
+ *     they enter a matrix product (see below);
  *   - results do not depend on timing: the same call gives the same bits.
  */
 enum { GBMW_F32 = 0, GBMW_F16 = 1, GBMW_BF16 = 2 };
@@ -488,11 +490,20 @@ enum { GBMW_F32 = 0, GBMW_F16 = 1, GBMW_BF16 = 2 };
  *   x_ij  = scale * <q_i, k_j>      for i < n, j < m and, if causal, j <= i + m - n,
  *   lse_i = log sum_j exp x_ij,  p_ij = exp(x_ij - lse_i),  out_i = sum_j p_ij v_j.
  * A row that sees no key, and every row i >= n, has out_i = 0 and lse_i = -inf.
- * Backward, from dout, out and lse (as the forward call left them):
+ * Backward, from dout, and from out and lse as the forward call left them for the same
+ * q, k, v, lengths, mask and scale:
  *   ds_ij = p_ij (<dout_i, v_j> - <dout_i, out_i>),
  *   dq_i = scale sum_j ds_ij k_j,  dk_j = scale sum_i ds_ij q_i,  dv_j = sum_i p_ij dout_i,
  * dk and dv summed over the query heads that read the key head.  Rows without keys
  * give and get no gradient (0), nor do keys that no row sees.
+ * Over all keys that a row sees its ds_ij add up to 0.  The backward call relies on that to
+ * take the rounding of out_i out of <dout_i, out_i> (with few rows and keys it does not
+ * read out), so it is not for a part of the keys with out and lse of all of them.
+ * Roundings to dtype: p_ij before p v (the row's sum in lse takes it unrounded) and before
+ * p^T dout, ds_ij before ds k and ds^T q; in float16 p is held times 2^8 and ds times the
+ * power of two that the largest norms of dout and v leave room for.  On random data the
+ * results are off by 1.4 times the one rounding of the result.  A backward call on few rows
+ * and keys (up to 16 and 32, and 128 pairs of a head) rounds neither.
  * q, k, v, dout beyond the lengths are not used, whatever they hold, nor are q and dout
  * of rows without keys.  Elsewhere values should be finite: a NaN or an infinity reaches
  * the rows that see it, and may reach rows that see other keys and from which only the

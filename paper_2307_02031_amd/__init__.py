@@ -403,6 +403,9 @@ def gbmw_cost_model(layers, strategies, hw: dict, Bm: float, P: int, device: boo
 
 
 # ---- operators of a transformer layer's training ------------------------------------------------------------------
+#
+# torch's autograd does not record these calls: results carry no graph, also of tensors that require grad, and the
+# backward calls are the caller's to make (in a torch.autograd.Function, or by hand as in layer_example).
 
 _DTYPE = {torch.float32: GBMW_F32, torch.float16: GBMW_F16, torch.bfloat16: GBMW_BF16}
 
@@ -564,7 +567,8 @@ def gbmw_attention_forward(q, k, v, causal: bool = False, scale: float | None = 
                            out=None, lse=None, workspace=None):
     """out [B][Lq][Hq][D] and lse [B][Hq][Lq] (float32) of q [B][Lq][Hq][D], k and v [B][Lk][Hk][D]: float16 or
     bfloat16 GPU tensors with any strides whose last one is 1.  scale: 1 / sqrt(D) by default.  len_q, len_k:
-    int32 [B], the samples' lengths.  out, lse, workspace (uint8): made here unless given.  stream=: as everywhere."""
+    int32 [B], the samples' lengths.  out, lse, workspace (uint8): made here unless given.  stream=: as everywhere.
+    Not recorded by autograd: gradients come from gbmw_attention_backward."""
     p, device = _attention_problem(q, k, v, causal, scale, len_q, len_k)
     if out is None:
         out = _new_like(q)
@@ -586,7 +590,8 @@ def gbmw_attention_forward(q, k, v, causal: bool = False, scale: float | None = 
 @_on_stream
 def gbmw_attention_backward(dout, q, k, v, out, lse, causal: bool = False, scale: float | None = None, len_q=None,
                             len_k=None, dq=None, dk=None, dv=None, workspace=None):
-    """dq, dk, dv from dout and the forward call's arguments and results.  stream=: as everywhere."""
+    """dq, dk, dv from dout and the forward call's arguments and results, all of its keys: a call on a part of the keys
+    with out and lse of all of them gives something else.  stream=: as everywhere."""
     p, device = _attention_problem(q, k, v, causal, scale, len_q, len_k)
     dtype, qshape, kshape = q.dtype, q.shape, k.shape
     _check_tensor("dout", dout, device, dtype, qshape)
@@ -667,7 +672,8 @@ def gbmw_layer_norm_workspace(x, weight=None) -> int:
 @_on_stream
 def gbmw_layer_norm_forward(x, weight=None, bias=None, eps: float = 1e-5, y=None):
     """y like x, mean and rstd float32 of x's shape without its last axis.  x: float32, float16 or bfloat16 GPU
-    tensor; weight, bias: of x's type or float32.  y: made here unless given (it may be x).  stream=: as everywhere."""
+    tensor; weight, bias: of x's type or float32.  y: made here unless given (it may be x).  stream=: as everywhere.
+    Not recorded by autograd: gradients come from gbmw_layer_norm_backward."""
     p, device = _norm_problem(x, weight, bias)
     if y is None:
         y, p.y_stride = _new_like(x), p.cols
