@@ -432,11 +432,12 @@ __device__ __forceinline__ float max_of(const float* x, int n) {   // n values, 
 //
 // Per tile and wave 32 matrix instructions of 32 cycles (heads of 128), about as many cycles of
 // exponentials and other vector instructions and a quarter of them of LDS: two waves a SIMD
-// overlap the first two.  40 heads x 8192 x 128: 1.26 ms, 1090 TFLOP/s, the library's large
-// product of the type reaches 1223; 5 x 32 heads x 2048: 352 us, 977; 4 x 40 heads x 2048
-// causal: 211 us, 814 of the visible half (tiles on the diagonal, and a start and an end per
-// workgroup of 17 tiles).  64 rows a wave (half the LDS reads, one wave a SIMD) took 397 us for
-// the last where 32 took 287.
+// overlap the first two.  Medians: 40 heads x 8192 x 128: 1.28 ms, 1075 TFLOP/s, the library's
+// large product of the type reaches 1223; 5 x 32 heads x 2048: 344 us, 999; 4 x 40 heads x 2048
+// causal: 208 us, 826 of the visible half (tiles on the diagonal, and a start and an end per
+// workgroup of 17 tiles), 214 where q, k and v are parts of one product's rows, and 250 for
+// those repeated without a pause.  64 rows a wave (half the LDS reads, one wave a SIMD) took
+// 397 us for the last where 32 took 287.
 constexpr float kLag = 6.0f;
 
 // One row's running maximum (in units of x / scale), sum, and out^T: what a wave has of 32 rows.
@@ -569,7 +570,8 @@ __global__ __launch_bounds__(256, 2) void k_attn_fwd(AttnArgs a) {
 // of its own, without waiting for the others; at the end their sums are put together.  4 x 32
 // query on 8 key heads, one token, 4500 keys on average: 19 us, 4.2 TB/s of keys and values
 // (128 us with tiles shared by the workgroup, of which one wave has rows); 8 x 16 heads, 4 rows
-// over 384 keys: 7.9 us, bound by the latency of three tiles in sequence (12.6).
+// over 384 keys: 7.9 us (9.5 where keys and values are not in the cache yet), the latency of three
+// tiles in sequence on half of the chip (12.6 with shared tiles).
 template <typename T, int KS, bool DIRECT>
 __global__ __launch_bounds__(256, 1) void k_attn_few(AttnArgs a) {
   constexpr int DB = (KS + 1) / 2, kHalf = Reader<KS>::down(32), kWave = 4 * kHalf, DP = 32 * DB + 4;
@@ -746,9 +748,9 @@ __global__ __launch_bounds__(256) void k_attn_vmax(AttnArgs a) {
 // The backward pass is two kernels that both recompute p and dp (seven products, where one kernel
 // would do with five): each sum then has one owner, nothing is added atomically, and the result
 // does not depend on timing.  One kernel's shares of dq, a row tile's per tile of keys, would be
-// written and read at more than the memory's rate.  Score gradients are rounded to the type once,
-// as operands.  This one's three products: 32 query on 8 key heads x 8192 x 128 causal 733 us, 1125
-// TFLOP/s; 16 x 20 heads x 512 x 64, ragged: 48 us, bound by starts, ends and a last round of
+// written and read at more than the memory's rate (where a head has several tiles of keys).  Score gradients are rounded to the type once,
+// as operands.  This one's three products: 32 query on 8 key heads x 8192 x 128 causal 741 us, 1113
+// TFLOP/s; 16 x 20 heads x 512 x 64, ragged: 47 us, bound by starts, ends and a last round of
 // workgroups that fills a quarter of the chip.
 template <typename T, int KS, bool DIRECT>
 __global__ __launch_bounds__(256, 2) void k_attn_dq(AttnArgs a) {
@@ -889,7 +891,8 @@ __global__ __launch_bounds__(256, 2) void k_attn_dq(AttnArgs a) {
 //
 // Bound by registers (128 sums a lane, and the keys and values it multiplies with): two waves a
 // SIMD that wait for LDS 45 % of their time.  Four products: 32 query on 8 key heads x 8192 x 128
-// causal 1.15 ms, 960 TFLOP/s; 16 x 20 heads x 512 x 64, ragged: 65 us.
+// causal 1.16 ms, 950 TFLOP/s; 16 x 20 heads x 512 x 64, ragged: 55 to 66 us, by which samples are
+// long.  Without direct loads it keeps 96 to 212 bytes a lane in scratch memory.
 template <typename T, int KS, bool DIRECT>
 __global__ __launch_bounds__(256, KS <= 4 ? 3 : 2) void k_attn_dkv(AttnArgs a) {
   constexpr int DB = (KS + 1) / 2;

@@ -48,3 +48,11 @@ def test_workgroups_on_a_compute_unit(kernels):
         least = dict(few=1, fwd=4 if pieces <= 4 else 3 if pieces <= 6 else 2, dq=3 if pieces <= 4 else 2,
                      dkv=3 if pieces <= 4 else 2)[kernel]
         assert together >= least - (not direct and pieces <= 4), (kernel, pieces, direct, waves, lds)
+
+
+def test_scratch_memory_without_direct_loads(kernels):
+    """Rows that come through registers leave the backward kernels too few; forward has enough."""
+    for (kernel, pieces, direct), (scratch, _, _) in kernels.items():
+        if not direct:
+            most = {"dq": {4: 0, 8: 128}, "dkv": {4: 128, 8: 224}}.get(kernel, {}).get(pieces, 0)
+            assert scratch <= most, (kernel, pieces, scratch)
