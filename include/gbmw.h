@@ -606,6 +606,178 @@ gbmw_status gbmw_clip_gradients(gbmw_gradient_list* list, float max_norm, float 
 /* Waits for the list's device.  NULL is allowed. */
 void gbmw_gradient_list_destroy(gbmw_gradient_list* list);
 
+/*
+ * RMS norm over rows of `cols` values, after the addition of a residual:
+ *   h = x + residual, rounded to dtype (h = x without one),
+ *   rstd = 1 / sqrt(sum h^2 / cols + eps),  y = h rstd weight.
+ * The rounded h is what is normed, so the bits are those of an addition and a norm of its
+ * result.  Any of h, y, q and rstd may be NULL (not wanted), but not both y and q; h is
+ * not written without a residual.
+ * q holds y in 8 bits, of the value in fp32 and not of y as rounded to dtype: for each row
+ * and group of `group` columns (the last may have fewer; one group a row if group is 0)
+ *   scale = max(largest |y| / top, 2^-126),  q = y / scale rounded to nearest even,
+ * with top 448 for GBMW_E4M3 and 127 for GBMW_I8 (whose codes are whole numbers from -127
+ * to 127).  A NaN in a group makes its scale NaN, and every value of a row that holds a NaN or
+ * an infinity is one, so its scales are too; GBMW_I8's codes are then without meaning.
+ * Backward, from dy (the gradient of y, or of the values that q stands for), h and rstd as
+ * the forward call left them (x if there was no residual), with g = dy * weight:
+ *   dx = (g - xhat sum(g xhat) / cols) rstd + dres,  xhat = h rstd,
+ *   dweight = sum over rows of dy xhat.
+ * dx is the gradient of x and of the residual; dres (NULL: zeros) is the one that reaches h
+ * past the norm.  weight may be NULL (ones), dweight may be NULL (not wanted).
+ * y or h may be x or residual, and dx may be dy or dres, with the same row stride.
+ * Squares are summed in fp32: rows with values beyond about 1e18 have rstd = 0.
+ */
+enum { GBMW_E4M3 = 3, GBMW_I8 = 4 };
+
+typedef struct {
+  int32_t dtype;             /* of x, residual, h, y, dy, dres, dx                   */
+  int32_t wdtype;            /* of weight, dweight: dtype or GBMW_F32                */
+  int64_t rows;              /* >= 0                                                 */
+  int32_t cols;              /* 1..32768                                             */
+  float eps;                 /* >= 0                                                 */
+  const void* x;             /* backward: h                                          */
+  int64_t x_stride;          /* elements from row to row, >= cols (inputs: >= 0)     */
+  const void* weight;        /* [cols]                                               */
+  float* rstd;               /* [rows]; forward: written, backward: read             */
+  const void* residual;      /* from here on forward only                            */
+  int64_t residual_stride;
+  void* h;
+  int64_t h_stride;
+  void* y;
+  int64_t y_stride;
+  void* q;                   /* bytes                                                */
+  int64_t q_stride;
+  float* scale;              /* [rows][ceil(cols / group)], dense; with q only       */
+  int32_t qtype;             /* GBMW_E4M3 or GBMW_I8                                 */
+  int32_t group;             /* 0, 32, 64 or 128                                     */
+  const void* dy;            /* from here on backward only                           */
+  int64_t dy_stride;
+  const void* dres;
+  int64_t dres_stride;
+  void* dx;
+  int64_t dx_stride;
+  void* dweight;             /* [cols]                                               */
+  void* workspace;           /* at least gbmw_rms_norm_workspace() bytes, 16-byte    */
+  int64_t workspace_bytes;   /* aligned; backward with dweight only                  */
+  void* stream;
+} gbmw_rms_norm_problem;
+
+gbmw_status gbmw_rms_norm_forward(const gbmw_rms_norm_problem* p);
+gbmw_status gbmw_rms_norm_backward(const gbmw_rms_norm_problem* p);
+int64_t gbmw_rms_norm_workspace(const gbmw_rms_norm_problem* p);
+
+/*
+ * Rotary positions, of queries and keys in one call.  Pair i < rot / 2 of a head is its
+ * values (i, i + rot / 2), or (2 i, 2 i + 1) if interleaved; at position t it becomes
+ *   (a, b) -> factor (a cos(t freq_i) - b sin(t freq_i), a sin(t freq_i) + b cos(t freq_i)).
+ * Values from rot on are handed through.  The backward call applies the transpose (sin with
+ * the other sign) to the gradients of the results; it needs no values of the forward call.
+ * Row r of sample b has position positions[b * position_stride + r], or r if positions is
+ * NULL.  Rows from len[b] on are neither read nor written.  Angles are computed and reduced
+ * in fp64, so positions may be any int32.
+ * q_out may be q and k_out may be k, with the same strides (in place); an array given
+ * in place must have all its elements at different places.  k and k_out may be NULL (Hk 0).
+ * Layouts and strides are attention's.
+ */
+typedef struct {
+  int32_t dtype;             /* of all arrays                                        */
+  int32_t B, L;              /* samples and rows, >= 0                               */
+  int32_t Hq, Hk;            /* heads: Hq >= 1, Hk >= 0                              */
+  int32_t D;                 /* head size, 1..512                                    */
+  int32_t rot;               /* even, 0..D                                           */
+  int32_t interleaved;       /* 0 or 1                                               */
+  float factor;              /* finite                                               */
+  const double* freq;        /* [rot / 2] radians per position                       */
+  const int32_t* positions;  /* [B][L] or NULL                                       */
+  int64_t position_stride;   /* from sample to sample, >= 0                          */
+  const int32_t* len;        /* [B] or NULL (all L); values are clamped to 0..L      */
+  const void *q, *k;
+  int64_t q_stride[3], k_stride[3];
+  void *q_out, *k_out;
+  int64_t q_out_stride[3], k_out_stride[3];
+  void* stream;
+} gbmw_rotary_problem;
+
+gbmw_status gbmw_rotary_forward(const gbmw_rotary_problem* p);
+gbmw_status gbmw_rotary_backward(const gbmw_rotary_problem* p);
+
+/*
+ * Frequencies freq[0 .. rot / 2) for the calls above, computed on the host into HOST memory:
+ * f_i = theta^(-2 i / rot), and for contexts `by` times as long as those that f is made for
+ *   GBMW_ROTARY_LINEAR  f_i / by,
+ *   GBMW_ROTARY_BASE    f_i with theta by^(rot / (rot - 2)) in theta's place (rot > 2),
+ *   GBMW_ROTARY_RAMP    f_i where it turns at least `fast` times in `original` positions,
+ *                       f_i / by where it turns at most `slow` times, and in between
+ *                       w f_i + (1 - w) f_i / by, w rising linearly with the turns
+ *                       (original f_i / 2 pi) from 0 at slow to 1 at fast.
+ */
+enum { GBMW_ROTARY_NONE = 0, GBMW_ROTARY_LINEAR = 1, GBMW_ROTARY_BASE = 2, GBMW_ROTARY_RAMP = 3 };
+
+gbmw_status gbmw_rotary_frequencies(int32_t rot, double theta, int32_t scaling, double by, double original, double slow,
+                                    double fast, double* freq);
+
+/*
+ * One AdamW step over many tensors.  For every element, with c1 = 1 - beta1^step and
+ * c2 = 1 - beta2^step,
+ *   g = grad * scale * (norm > max_norm ? max_norm / norm : 1),
+ *   m = beta1 m + (1 - beta1) g,  v = beta2 v + (1 - beta2) g^2,
+ *   param = param (1 - lr weight_decay) - (lr / c1) m / (sqrt(v) / sqrt(c2) + eps),
+ * in fp32 (the factors in fp64, rounded once), param rounded to dtype.  `copy`, if given, gets
+ * the new param (of GBMW_F32) rounded to copy_dtype.  norm is what gbmw_clip_gradients wrote:
+ * with a list whose outputs are its inputs and max_norm +inf that call only computes it, and the
+ * step clips as it reads.  If *norm is NaN or infinite the step is left out: nothing is written.
+ *
+ * States of 32 bits: m and v in fp32.  States of 8 bits: for each block of 256 elements of a
+ * tensor (the last may have fewer) m is held as codes of GBMW_E4M3 with a scale, and so is
+ * r = sqrt(v) in the place of v:
+ *   value = code * scale,  scale = max(largest |value| / 448, 2^-126).
+ * With seed 0 value / scale is rounded to nearest even.  With another seed it goes to one of
+ * its two neighbours at random, with the probabilities that make it right on average, by 16
+ * bits of a hash of seed, step and the element's place in the list (the same call gives the same
+ * bits).  Rounding to nearest leaves a moment unchanged for ever that moves by less than half a
+ * step (up to 6 %) at a time.  r > 0 is never held as 0, which would let m / r grow without bound.
+ * Zeroed codes and scales are states before the first step.  A NaN or an infinity in a
+ * gradient makes its block's states NaN.
+ *
+ * A list is made once for tensors that stay where they are, as a gradient list is: it copies the
+ * addresses to the device, holds no tensor alive and has no state of its own.  What is written
+ * must not overlap anything else in the list (refused).  Making a list allocates and waits; a step
+ * does neither.  One list may be used by one step at a time.
+ */
+typedef struct {
+  int64_t numel;             /* >= 0                                                 */
+  const void* grad;
+  void* param;
+  void* copy;                /* or NULL                                              */
+  void *m, *v;               /* fp32, or codes of 8 bits                             */
+  float *m_scale, *v_scale;  /* [ceil(numel / 256)] with states of 8 bits            */
+  int32_t grad_dtype, dtype, copy_dtype;   /* copy_dtype: GBMW_F16 or GBMW_BF16      */
+  float weight_decay;        /* >= 0                                                 */
+} gbmw_adamw_tensor;
+
+typedef struct {
+  double lr, beta1, beta2;   /* lr >= 0, betas in [0, 1)                             */
+  double eps;                /* > 0                                                  */
+  double scale;              /* > 0: the inverse of a loss scale                     */
+  double max_norm;           /* > 0, may be +inf                                     */
+  int64_t step;              /* >= 1: the number of this step                        */
+  uint32_t seed;             /* states of 8 bits: 0 rounds to nearest                */
+  /* DEVICE pointers, each may be NULL: read when the step runs, for steps in a graph */
+  const float* norm;
+  const float* lr_now;       /* in the place of lr                                   */
+  const int64_t* step_now;   /* in the place of step; below 1 is taken as 1          */
+} gbmw_adamw_options;
+
+typedef struct gbmw_adamw_list gbmw_adamw_list;
+
+/* state_bits: 32 or 8, of all tensors. */
+gbmw_status gbmw_adamw_list_create(int32_t n, const gbmw_adamw_tensor* tensors, int32_t state_bits,
+                                   gbmw_adamw_list** list);
+gbmw_status gbmw_adamw_step(const gbmw_adamw_list* list, const gbmw_adamw_options* options, void* stream);
+/* Waits for the list's device.  NULL is allowed. */
+void gbmw_adamw_list_destroy(gbmw_adamw_list* list);
+
 /* Lmax of the last solve (row length of `plan` above); 0 if none. */
 int32_t gbmw_max_layers(const gbmw_ctx* ctx);
 

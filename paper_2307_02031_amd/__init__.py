@@ -12,6 +12,7 @@ enqueued on ``torch.cuda.current_stream()`` unless a stream is given.
 """
 from __future__ import annotations
 
+import collections
 import ctypes as ct
 import functools
 import operator
@@ -44,6 +45,9 @@ EXPORTS = [
     "gbmw_attention_forward", "gbmw_attention_backward", "gbmw_attention_workspace",
     "gbmw_layer_norm_forward", "gbmw_layer_norm_backward", "gbmw_layer_norm_workspace",
     "gbmw_gradient_list_create", "gbmw_clip_gradients", "gbmw_gradient_list_destroy",
+    "gbmw_rms_norm_forward", "gbmw_rms_norm_backward", "gbmw_rms_norm_workspace",
+    "gbmw_rotary_forward", "gbmw_rotary_backward", "gbmw_rotary_frequencies",
+    "gbmw_adamw_list_create", "gbmw_adamw_step", "gbmw_adamw_list_destroy",
     "gbmw_max_layers", "gbmw_get_best",
     "gbmw_export_tables", "gbmw_synchronize", "gbmw_last_solve_ms", "gbmw_last_solve_work", "gbmw_destroy",
     "gbmw_last_error", "gbmw_version",
@@ -84,6 +88,8 @@ class gbmw_hardware(ct.Structure):
 
 
 GBMW_F32, GBMW_F16, GBMW_BF16 = 0, 1, 2
+GBMW_E4M3, GBMW_I8 = 3, 4
+GBMW_ROTARY_NONE, GBMW_ROTARY_LINEAR, GBMW_ROTARY_BASE, GBMW_ROTARY_RAMP = range(4)
 
 
 class gbmw_attention_problem(ct.Structure):
@@ -105,6 +111,38 @@ class gbmw_layer_norm_problem(ct.Structure):
                 ("rstd", ct.c_void_p), ("dy", ct.c_void_p), ("dy_stride", ct.c_int64), ("dx", ct.c_void_p),
                 ("dx_stride", ct.c_int64), ("dweight", ct.c_void_p), ("dbias", ct.c_void_p),
                 ("workspace", ct.c_void_p), ("workspace_bytes", ct.c_int64), ("stream", ct.c_void_p)]
+
+
+class gbmw_rms_norm_problem(ct.Structure):
+    _fields_ = ([("dtype", ct.c_int32), ("wdtype", ct.c_int32), ("rows", ct.c_int64), ("cols", ct.c_int32),
+                 ("eps", ct.c_float), ("x", ct.c_void_p), ("x_stride", ct.c_int64), ("weight", ct.c_void_p),
+                 ("rstd", ct.c_void_p)] +
+                [f for n in ("residual", "h", "y", "q") for f in ((n, ct.c_void_p), (n + "_stride", ct.c_int64))] +
+                [("scale", ct.c_void_p), ("qtype", ct.c_int32), ("group", ct.c_int32)] +
+                [f for n in ("dy", "dres", "dx") for f in ((n, ct.c_void_p), (n + "_stride", ct.c_int64))] +
+                [("dweight", ct.c_void_p), ("workspace", ct.c_void_p), ("workspace_bytes", ct.c_int64),
+                 ("stream", ct.c_void_p)])
+
+
+class gbmw_rotary_problem(ct.Structure):
+    _fields_ = ([(n, ct.c_int32) for n in ("dtype", "B", "L", "Hq", "Hk", "D", "rot", "interleaved")] +
+                [("factor", ct.c_float), ("freq", ct.c_void_p), ("positions", ct.c_void_p),
+                 ("position_stride", ct.c_int64), ("len", ct.c_void_p), ("q", ct.c_void_p), ("k", ct.c_void_p),
+                 ("q_stride", ct.c_int64 * 3), ("k_stride", ct.c_int64 * 3), ("q_out", ct.c_void_p),
+                 ("k_out", ct.c_void_p), ("q_out_stride", ct.c_int64 * 3), ("k_out_stride", ct.c_int64 * 3),
+                 ("stream", ct.c_void_p)])
+
+
+class gbmw_adamw_tensor(ct.Structure):
+    _fields_ = ([("numel", ct.c_int64)] +
+                [(n, ct.c_void_p) for n in ("grad", "param", "copy", "m", "v", "m_scale", "v_scale")] +
+                [(n, ct.c_int32) for n in ("grad_dtype", "dtype", "copy_dtype")] + [("weight_decay", ct.c_float)])
+
+
+class gbmw_adamw_options(ct.Structure):
+    _fields_ = ([(n, ct.c_double) for n in ("lr", "beta1", "beta2", "eps", "scale", "max_norm")] +
+                [("step", ct.c_int64), ("seed", ct.c_uint32)] +
+                [(n, ct.c_void_p) for n in ("norm", "lr_now", "step_now")])
 
 
 STRATEGY_DTYPE = np.dtype([("n_levels", np.int32), ("kind", np.int32, 3), ("degree", np.int32, 3), ("ckpt", np.int32)])
@@ -152,6 +190,20 @@ _lib.gbmw_clip_gradients.argtypes = [ct.c_void_p, ct.c_float, ct.c_float, ct.c_v
 _lib.gbmw_clip_gradients.restype = ct.c_int
 _lib.gbmw_gradient_list_destroy.argtypes = [ct.c_void_p]
 _lib.gbmw_gradient_list_destroy.restype = None
+for _name in ("gbmw_rms_norm_forward", "gbmw_rms_norm_backward", "gbmw_rms_norm_workspace"):
+    getattr(_lib, _name).argtypes = [ct.POINTER(gbmw_rms_norm_problem)]
+    getattr(_lib, _name).restype = ct.c_int64 if _name.endswith("workspace") else ct.c_int
+for _name in ("gbmw_rotary_forward", "gbmw_rotary_backward"):
+    getattr(_lib, _name).argtypes = [ct.POINTER(gbmw_rotary_problem)]
+    getattr(_lib, _name).restype = ct.c_int
+_lib.gbmw_rotary_frequencies.argtypes = [ct.c_int32, ct.c_double, ct.c_int32] + [ct.c_double] * 4 + [ct.c_void_p]
+_lib.gbmw_rotary_frequencies.restype = ct.c_int
+_lib.gbmw_adamw_list_create.argtypes = [ct.c_int32, ct.POINTER(gbmw_adamw_tensor), ct.c_int32, ct.POINTER(ct.c_void_p)]
+_lib.gbmw_adamw_list_create.restype = ct.c_int
+_lib.gbmw_adamw_step.argtypes = [ct.c_void_p, ct.POINTER(gbmw_adamw_options), ct.c_void_p]
+_lib.gbmw_adamw_step.restype = ct.c_int
+_lib.gbmw_adamw_list_destroy.argtypes = [ct.c_void_p]
+_lib.gbmw_adamw_list_destroy.restype = None
 _lib.gbmw_cost_model.argtypes = [ct.c_void_p, ct.c_int32, ct.c_void_p, ct.c_int32, ct.POINTER(gbmw_hardware),
                                  ct.c_double, ct.c_int32, ct.c_int32] + [ct.c_void_p] * 8
 _lib.gbmw_cost_model.restype = ct.c_int
@@ -771,6 +823,291 @@ def gbmw_clip_gradients(lst: GradientList, max_norm: float, scale: float = 1.0, 
 def gbmw_gradient_list_destroy(lst: GradientList) -> None:
     if lst.handle:
         _lib.gbmw_gradient_list_destroy(lst.handle)
+        lst.handle = ct.c_void_p(None)
+        lst._keep = ()
+
+
+RmsNorm = collections.namedtuple("RmsNorm", "y h rstd q scale")
+_QTYPE = {torch.float8_e4m3fn: GBMW_E4M3, torch.int8: GBMW_I8}
+
+
+def _rms_problem(x, weight):
+    device = _device_of("x", x, _DTYPE)
+    shape, dtype = x.shape, x.dtype
+    if len(shape) < 1:
+        _refuse("x has no axis")
+    p, cols = gbmw_rms_norm_problem(), shape[-1]
+    _check_counts("x", cols)
+    p.dtype = p.wdtype = _DTYPE[dtype]
+    p.rows, p.cols, p.x_stride = x.numel() // max(1, cols), cols, _row_stride("x", x)
+    p.x, p.stream = x.data_ptr(), _raw_stream(device)
+    if weight is not None:
+        wdtype = getattr(weight, "dtype", None)
+        p.wdtype = _DTYPE.get(wdtype, -1)
+        p.weight = _column("weight", weight, device, wdtype, cols)
+    return p, device
+
+
+def _set_rows(p, name: str, t, device: int, dtype, shape) -> None:
+    _check_tensor(name, t, device, dtype, shape)
+    setattr(p, name, t.data_ptr())
+    setattr(p, name + "_stride", _row_stride(name, t))
+
+
+@_on_stream
+def gbmw_rms_norm_workspace(x, weight=None) -> int:
+    """Bytes of workspace of the backward call."""
+    n = _lib.gbmw_rms_norm_workspace(ct.byref(_rms_problem(x, weight)[0]))
+    if n < 0:
+        raise GbmwError(GBMW_ERR_INVALID_ARG, gbmw_last_error())
+    return n
+
+
+@_on_stream
+def gbmw_rms_norm_forward(x, weight=None, eps: float = 1e-5, residual=None, qtype=None, group: int = 0,
+                          want_y: bool = True, y=None, h=None, q=None):
+    """RmsNorm(y, h, rstd, q, scale) of x, a float32, float16 or bfloat16 GPU tensor whose last axis is normed, after
+    the addition of residual, if there is one.  weight: of x's type or float32.  y: like x, None unless want_y.
+    h: x + residual (x itself without a residual).  rstd: float32 of x's shape without its last axis.  qtype
+    (torch.float8_e4m3fn or torch.int8): q holds y in 8 bits, with scale (float32, of x's shape but for the last axis)
+    for each row, or for each `group` (32, 64 or 128) columns; None without a qtype.  y, h, q: made here unless given (y
+    or h may be x or residual).  stream=: as everywhere.  Not recorded by autograd: gradients come from
+    gbmw_rms_norm_backward."""
+    p, device = _rms_problem(x, weight)
+    shape, dtype = x.shape, x.dtype
+    p.eps = eps
+    if y is not None:
+        _set_rows(p, "y", y, device, dtype, shape)
+    elif want_y:
+        y = _new_like(x)
+        p.y, p.y_stride = y.data_ptr(), p.cols
+    if residual is not None:
+        _set_rows(p, "residual", residual, device, dtype, shape)
+        if h is None:
+            h = _new_like(x)
+            p.h, p.h_stride = h.data_ptr(), p.cols
+        else:
+            _set_rows(p, "h", h, device, dtype, shape)
+    elif h is not None:
+        _refuse("h without a residual is x")
+    else:
+        h = x
+    scale = None
+    if qtype is not None:
+        p.qtype, p.group = _QTYPE.get(qtype, -1), group
+        if q is None:
+            q = torch.empty(shape, dtype=qtype, device="cuda")
+            p.q, p.q_stride = q.data_ptr(), p.cols
+        else:
+            _set_rows(p, "q", q, device, qtype, shape)
+        scale = torch.empty((*shape[:-1], -(-p.cols // group) if group > 0 else 1), dtype=torch.float32, device="cuda")
+        p.scale = scale.data_ptr()
+    elif q is not None:
+        _refuse("q without a qtype")
+    rstd = torch.empty(shape[:-1], dtype=torch.float32, device="cuda")
+    p.rstd = rstd.data_ptr()
+    _check(_lib.gbmw_rms_norm_forward(ct.byref(p)))
+    return RmsNorm(y, h, rstd, q, scale)
+
+
+@_on_stream
+def gbmw_rms_norm_backward(dy, h, weight, rstd, dres=None, dx=None, workspace=None):
+    """dx (of x and of the residual) and dweight from dy and the forward call's h, weight and rstd.  dres: the gradient
+    that reaches h past the norm, added to dx.  weight None: no dweight.  dx: made here unless given (it may be dy or
+    dres).  stream=: as everywhere."""
+    p, device = _rms_problem(h, weight)
+    shape, dtype = h.shape, h.dtype
+    _set_rows(p, "dy", dy, device, dtype, shape)
+    if dres is not None:
+        _set_rows(p, "dres", dres, device, dtype, shape)
+    if dx is None:
+        dx = _new_like(h)
+        p.dx, p.dx_stride = dx.data_ptr(), p.cols
+    else:
+        _set_rows(p, "dx", dx, device, dtype, shape)
+    _check_tensor("rstd", rstd, device, torch.float32, shape[:-1])
+    if not rstd.is_contiguous():
+        _refuse("rstd is not contiguous")
+    p.rstd = rstd.data_ptr()
+    ref, dweight, keep = ct.byref(p), None, None
+    if weight is not None:
+        dweight = torch.empty(p.cols, dtype=weight.dtype, device="cuda")
+        p.dweight = dweight.data_ptr()
+        keep = _workspace(p, workspace, _lib.gbmw_rms_norm_workspace(ref), device)
+    _check(_lib.gbmw_rms_norm_backward(ref))
+    return dx, dweight
+
+
+_SCALING = dict(none=GBMW_ROTARY_NONE, linear=GBMW_ROTARY_LINEAR, base=GBMW_ROTARY_BASE, ramp=GBMW_ROTARY_RAMP)
+
+
+@_on_stream
+def gbmw_rotary_frequencies(rot: int, theta: float = 10000.0, scaling: str = "none", by: float = 1.0,
+                            original: float = 0.0, slow: float = 1.0, fast: float = 32.0):
+    """Radians per position of rot / 2 pairs, a float64 GPU tensor.  scaling: "none", "linear", "base" or "ramp", for
+    contexts `by` times as long as those that theta is made for (of `original` positions, with "ramp")."""
+    _check_counts("rot", abs(rot))
+    if scaling not in _SCALING:
+        _refuse(f"scaling {scaling!r} is none of {', '.join(_SCALING)}")
+    freq = np.empty(max(0, rot // 2))
+    _check(_lib.gbmw_rotary_frequencies(rot, theta, _SCALING[scaling], by, original, slow, fast, freq.ctypes.data))
+    return torch.from_numpy(freq).to("cuda")
+
+
+def _rotary(call, q, k, freq, positions, len_x, interleaved, factor, q_out, k_out):
+    device = _device_of("q", q, _DTYPE)
+    shape, dtype = q.shape, q.dtype
+    if len(shape) != 4:
+        _refuse(f"q has {q.dim()} dimensions, not [B][L][Hq][D]")
+    B, L, Hq, D = shape
+    Hk = 0
+    if k is not None:
+        if not isinstance(k, torch.Tensor) or k.dim() != 4:
+            _refuse("k is not a tensor [B][L][Hk][D]")
+        Hk = k.shape[2]
+        _check_tensor("k", k, device, dtype, (B, L, Hk, D))
+    elif k_out is not None:
+        _refuse("k_out without k")
+    _check_counts("q and k", B | L | Hq | Hk | D)
+    if not isinstance(freq, torch.Tensor) or freq.dim() != 1:
+        _refuse("freq is not a tensor [rot / 2]")
+    _check_tensor("freq", freq, device, torch.float64, freq.shape)
+    if not freq.is_contiguous():
+        _refuse("freq is not contiguous")
+    p = gbmw_rotary_problem(_DTYPE[dtype], B, L, Hq, Hk, D, 2 * min(freq.shape[0], 1 << 20), 1 if interleaved else 0, factor,
+                            freq.data_ptr())
+    if positions is not None:
+        if not isinstance(positions, torch.Tensor) or positions.dim() != 2:
+            _refuse("positions is not a tensor [B][L]")
+        _check_tensor("positions", positions, device, torch.int32, (B, L))
+        if L > 1 and positions.stride(1) != 1:
+            _refuse("positions of one sample are not next to each other")
+        p.positions, p.position_stride = positions.data_ptr(), positions.stride(0)
+    if len_x is not None:
+        p.len = _length("len_x", len_x, device, B)
+    if q_out is None:
+        q_out = _new_like(q)
+    else:
+        _check_tensor("q_out", q_out, device, dtype, shape)
+    _set_array(p, "q", q), _set_array(p, "q_out", q_out)
+    if k is not None:
+        if k_out is None:
+            k_out = _new_like(k)
+        else:
+            _check_tensor("k_out", k_out, device, dtype, k.shape)
+        _set_array(p, "k", k), _set_array(p, "k_out", k_out)
+    p.stream = _raw_stream(device)
+    _check(call(ct.byref(p)))
+    return q_out, k_out
+
+
+@_on_stream
+def gbmw_rotary_forward(q, k, freq, positions=None, len_x=None, interleaved: bool = False, factor: float = 1.0,
+                        q_out=None, k_out=None):
+    """q [B][L][Hq][D] and k [B][L][Hk][D] (or None) with the first 2 * len(freq) values of each head turned by their
+    rows' positions: float32, float16 or bfloat16 GPU tensors with any strides whose last one is 1.  freq: float64,
+    radians per position (gbmw_rotary_frequencies).  positions: int32 [B][L]; by default a row's number.  len_x: int32
+    [B]; rows from there on are left as they were.  q_out, k_out: made here unless given (they may be q and k).
+    stream=: as everywhere.  Not recorded by autograd: gradients come from gbmw_rotary_backward."""
+    return _rotary(_lib.gbmw_rotary_forward, q, k, freq, positions, len_x, interleaved, factor, q_out, k_out)
+
+
+@_on_stream
+def gbmw_rotary_backward(dq, dk, freq, positions=None, len_x=None, interleaved: bool = False, factor: float = 1.0,
+                         q_out=None, k_out=None):
+    """The gradients of the forward call's q and k from those of its results, dq and dk (or None), by the same freq,
+    positions, len_x, interleaved and factor.  q_out, k_out: made here unless given (they may be dq and dk)."""
+    return _rotary(_lib.gbmw_rotary_backward, dq, dk, freq, positions, len_x, interleaved, factor, q_out, k_out)
+
+
+class AdamWList:
+    """Owns a gbmw_adamw_list and keeps its tensors; freed by gbmw_adamw_list_destroy or with this object."""
+
+    def __init__(self):
+        self.handle = ct.c_void_p(None)
+        self._keep = ()
+
+    def __del__(self):
+        try:
+            gbmw_adamw_list_destroy(self)
+        except Exception:
+            pass
+
+
+def gbmw_adamw_list_create(params, grads, m, v, m_scales=None, v_scales=None, copies=None, weight_decay=0.0) -> AdamWList:
+    """A list of parameters (contiguous GPU tensors of float32, float16 or bfloat16), their gradients, and their states:
+    m and v in float32, or in float8_e4m3fn (v: of the second moment's square root), then with m_scales and v_scales in
+    float32, one for each 256 elements.  copies: tensors of 16 bits that get the new parameters too (None, or None in
+    the place of one).  weight_decay: a number, or one for each tensor.  The tensors have to stay where they are."""
+    params, grads, m, v = list(params), list(grads), list(m), list(v)
+    n = len(params)
+    wide = torch.float8_e4m3fn if m and getattr(m[0], "dtype", None) == torch.float8_e4m3fn else torch.float32
+    bits = 8 if wide == torch.float8_e4m3fn else 32
+    scales = [list(s) if s is not None else [None] * n for s in (m_scales, v_scales)]
+    copies = [None] * n if copies is None else list(copies)
+    decay = list(weight_decay) if isinstance(weight_decay, (list, tuple)) else [weight_decay] * n
+    for name, ts in (("gradients", grads), ("m", m), ("v", v), ("m_scales", scales[0]), ("v_scales", scales[1]),
+                     ("copies", copies), ("weight_decay", decay)):
+        if len(ts) != n:
+            _refuse(f"{n} parameters, {len(ts)} {name}")
+    if bits == 32 and not (m_scales is None and v_scales is None):
+        _refuse("states of 32 bits have no scales")
+    tensors = (gbmw_adamw_tensor * max(1, n))()
+    for i, t in enumerate(tensors[:n]):
+        device = _device_of(f"parameter {i}", params[i], _DTYPE)
+        shape = params[i].shape
+        _device_of(f"gradient {i}", grads[i], _DTYPE)
+        arrays = [("param", params[i], params[i].dtype, shape), ("grad", grads[i], grads[i].dtype, shape),
+                  ("m", m[i], wide, shape), ("v", v[i], wide, shape)]
+        if bits == 8:
+            blocks = ((params[i].numel() + 255) // 256,)
+            arrays += [("m_scale", scales[0][i], torch.float32, blocks), ("v_scale", scales[1][i], torch.float32, blocks)]
+        if copies[i] is not None:
+            arrays.append(("copy", copies[i], getattr(copies[i], "dtype", None), shape))
+        for name, x, dtype, size in arrays:
+            _check_tensor(f"{name} of tensor {i}", x, device, dtype, size)
+            if not x.is_contiguous():
+                _refuse(f"{name} of tensor {i} is not contiguous")
+            setattr(t, name, x.data_ptr() or None)
+        t.numel, t.grad_dtype, t.dtype = params[i].numel(), _DTYPE[grads[i].dtype], _DTYPE[params[i].dtype]
+        t.copy_dtype, t.weight_decay = -1 if copies[i] is None else _DTYPE.get(copies[i].dtype, -1), decay[i]
+    lst = AdamWList()
+    _check(_lib.gbmw_adamw_list_create(n, tensors, bits, ct.byref(lst.handle)))
+    lst._keep = (params, grads, m, v, scales, copies)
+    return lst
+
+
+def _scalar_now(name: str, t, dtype) -> int:
+    _device_of(name, t, (dtype,))
+    if t.numel() < 1:
+        _refuse(f"{name} is empty")
+    return t.data_ptr()
+
+
+@_on_stream
+def gbmw_adamw_step(lst: AdamWList, lr, step, beta1: float = 0.9, beta2: float = 0.999, eps: float = 1e-8,
+                    scale: float = 1.0, norm=None, max_norm: float = float("inf"), seed: int = 0) -> None:
+    """One step of the list's parameters and states.  lr: a number, or a float32 GPU tensor that is read when the step
+    runs; step: the step's number from 1 on, or an int64 GPU tensor.  norm: what gbmw_clip_gradients returned: the
+    gradients are clipped to max_norm as they are read, and the step is left out where it is not finite.  seed: of the
+    rounding of states of 8 bits, 0 for the nearest.  stream=: as everywhere."""
+    o = gbmw_adamw_options(0.0, beta1, beta2, eps, scale, max_norm, 1, seed & 0xFFFFFFFF)
+    if isinstance(lr, torch.Tensor):
+        o.lr_now = _scalar_now("lr", lr, torch.float32)
+    else:
+        o.lr = lr
+    if isinstance(step, torch.Tensor):
+        o.step_now = _scalar_now("step", step, torch.int64)
+    else:
+        o.step = step
+    if norm is not None:
+        o.norm = _scalar_now("norm", norm, torch.float32)
+    _check(_lib.gbmw_adamw_step(lst.handle, ct.byref(o), _raw_stream(torch.cuda.current_device())))
+
+
+def gbmw_adamw_list_destroy(lst: AdamWList) -> None:
+    if lst.handle:
+        _lib.gbmw_adamw_list_destroy(lst.handle)
         lst.handle = ct.c_void_p(None)
         lst._keep = ()
 

@@ -6,8 +6,7 @@
 #include <new>
 #include <vector>
 
-#include "gbmw_ctx.h"
-#include "gbmw_dtype.h"
+#include "gbmw_rows.h"
 
 using gbmw_detail::fail;
 
@@ -29,9 +28,6 @@ namespace {
 // reads and writes together).  6304 x 1283 fp32: 12 and 20 us.  512 x 1280 bf16: 3.6 us, two sums
 // after one load, bound by latency.
 
-// Floats from one share of dweight or dbias to the next: each starts at 16 bytes.
-__host__ __device__ constexpr int share_stride(int cols) { return (cols + 3) / 4 * 4; }
-
 struct NormArgs {
   int64_t rows;
   int cols;
@@ -44,86 +40,7 @@ struct NormArgs {
   float* partial;  // [gridDim.x][2][share_stride(cols)]
 };
 
-// Sums of N values over the NT threads of a row.  `scratch`: N * (NT / 64) floats of the
-// row's own, others than at the last call.  Every thread of the workgroup calls it.
-template <int NT, int N>
-__device__ __forceinline__ void row_sum(float (&s)[N], float* scratch) {
-#pragma unroll
-  for (int i = 0; i < N; ++i) s[i] = wave_sum(s[i]);
-  if constexpr (NT > 64) {
-    const int t = threadIdx.x % NT;
-    if (t % 64 == 0)
-#pragma unroll
-      for (int i = 0; i < N; ++i) scratch[i * (NT / 64) + t / 64] = s[i];
-    __syncthreads();
-#pragma unroll
-    for (int i = 0; i < N; ++i) {
-      s[i] = 0.0f;
-#pragma unroll
-      for (int w = 0; w < NT / 64; ++w) s[i] += scratch[i * (NT / 64) + w];
-    }
-  }
-}
-
-// V elements of a row from column c on, of which those before column `from` are another piece's.
-// Rows of fewer than V columns (TINY: there may be such) have one piece, of n columns.
-template <int V, bool WHOLE, bool TINY>
-struct Span {
-  int c, from, n, row;
-  Span() = default;
-  __device__ __forceinline__ Span(int piece, int cols) : row(cols) {
-    from = piece * V;
-    const bool there = from < cols;
-    c = there ? (WHOLE ? from : max(0, min(from, cols - V))) : 0;
-    n = there ? (TINY ? min(V, cols) : V) : 0;
-  }
-  __device__ __forceinline__ bool has(int i) const { return WHOLE ? n > 0 : c + i >= from && i < n; }
-  template <typename W>
-  __device__ __forceinline__ void load(float (&x)[V], const W* row) const {   // what it does not have may be anything
-    if (!TINY || this->row >= V) {
-      Pack<W> r[V / kVec<W>];
-      __builtin_memcpy(r, row + c, V * sizeof(W));
-#pragma unroll
-      for (int i = 0; i < V; ++i) x[i] = (float)r[i / kVec<W>].v[i % kVec<W>];
-    } else {
-#pragma unroll
-      for (int i = 0; i < V; ++i) x[i] = i < n ? (float)row[i] : 0.0f;
-    }
-  }
-  template <typename T>
-  __device__ __forceinline__ void store(T* row, const float (&y)[V]) const {
-    Pack<T> r;
-    static_assert(V == kVec<T>, "");
-#pragma unroll
-    for (int i = 0; i < V; ++i) r.v[i] = (T)y[i];
-    if (!TINY || n == V) __builtin_memcpy(row + c, &r, 16);   // shared columns are written twice, the same
-    else store_pack(row, r, n);
-  }
-};
-
-// The raw bytes of a thread's pieces: loaded early, looked at late.
-template <typename T, int NJ, bool TINY>
-struct Held {
-  Pack<T> p[NJ];
-  template <typename S>
-  __device__ __forceinline__ void load(const S (&span)[NJ], const T* row, int cols) {
-#pragma unroll
-    for (int j = 0; j < NJ; ++j) {
-      if (!TINY || cols >= kVec<T>) __builtin_memcpy(&p[j], row + span[j].c, 16);
-      else p[j] = load_pack(row, span[j].n);
-    }
-  }
-};
-
 constexpr int kNormFwdThreads = 256, kNormBwdThreads = 512;
-
-// Of a thread's NJ pieces the first so many are whole and there, whatever the row's length
-// (1024 threads have kernels of 1, 2, 4 and 8 pieces, so more than half are).
-template <int NT, int NJ>
-constexpr int kSure = NT < 1024 || NJ <= 2 ? NJ - 1 : NJ / 2;
-
-template <int NT, int NJ>
-constexpr bool kRunsAhead = NT < 1024 || NJ == 1;
 
 // Workgroups of G rows at a time, rows blockIdx.x * G + g, then gridDim.x * G further on: a thread
 // reads its columns of weight and bias once, and the next row is on its way while one is worked on
@@ -310,33 +227,6 @@ __global__ __launch_bounds__(NT < kNormBwdThreads ? kNormBwdThreads : NT) void k
   }
 }
 
-// dweight and dbias from `parts` shares: 32 columns a workgroup, four of every 128th share a thread
-// (8 threads read a line of the cache).  256 shares of 4574 columns: 4.8 us, 1.9 TB/s from the cache
-// (one column a thread and half a line at a time: 7.4); 146 of 9714: 7.
-template <typename W>
-__global__ __launch_bounds__(1024) void k_norm_join(const float* partial, int parts, int cols, W* dw, W* db) {
-  typedef float f32x4 __attribute__((ext_vector_type(4)));
-  __shared__ f32x4 sums[16][8];
-  const int quad = threadIdx.x % 8, c = blockIdx.x * 32 + quad * 4, stride = share_stride(cols);
-  W* out = blockIdx.y ? db : dw;
-  if (!out) return;
-  f32x4 s = {};
-  if (c < cols)
-#pragma unroll 4
-    for (int k = threadIdx.x / 8; k < parts; k += 128)
-      s += *(const f32x4*)(partial + ((int64_t)k * 2 + blockIdx.y) * stride + c);
-#pragma unroll
-  for (int e = 0; e < 4; ++e) s[e] = sum_across32(sum_across16(sum_dpp<0x128>(s[e])));   // lanes 8, 16 and 32 apart
-  if (threadIdx.x % 64 < 8) sums[threadIdx.x / 64][quad] = s;
-  __syncthreads();
-  if (threadIdx.x >= 32) return;
-  const int col = blockIdx.x * 32 + (int)threadIdx.x;
-  float total = 0.0f;
-#pragma unroll
-  for (int w = 0; w < 16; ++w) total += sums[w][threadIdx.x / 4][threadIdx.x % 4];
-  if (col < cols) out[col] = (W)total;
-}
-
 // ---- gradient norm and clipping -----------------------------------------------------------
 //
 // Two launches, bound by HBM: one reads every gradient for the norm, one reads and writes them
@@ -474,9 +364,6 @@ __global__ __launch_bounds__(256) void k_clip_scale(const Piece* pieces, int cou
 
 // ---- host ---------------------------------------------------------------------------------
 
-int element_size(int dtype) { return dtype == GBMW_F32 ? 4 : 2; }
-bool known_dtype(int dtype) { return dtype == GBMW_F32 || dtype == GBMW_F16 || dtype == GBMW_BF16; }
-
 gbmw_status check_norm(const gbmw_layer_norm_problem* p) {
   if (!p) return fail(GBMW_ERR_INVALID_ARG, "null problem");
   if (!known_dtype(p->dtype)) return fail(GBMW_ERR_INVALID_ARG, "dtype=%d", p->dtype);
@@ -487,20 +374,6 @@ gbmw_status check_norm(const gbmw_layer_norm_problem* p) {
   return GBMW_OK;
 }
 
-// Threads of a row and 16-byte pieces of each: few threads for short rows, so that the sums
-// stay inside a wave, and few pieces a thread, so that they stay in registers (three of 16-bit
-// values in the backward pass take 208; with four it spills).
-struct Shape {
-  int nt, nj;
-};
-Shape shape_of(const gbmw_layer_norm_problem* p) {
-  const int vec = 16 / element_size(p->dtype), n = (p->cols + vec - 1) / vec;
-  if (n <= 3 * 64) return {64, (n + 63) / 64};
-  if (n <= 3 * 256) return {256, (n + 255) / 256};
-  const int nj = (n + 1023) / 1024;
-  return {1024, nj <= 2 ? nj : nj <= 4 ? 4 : 8};
-}
-
 // Workgroups: as many as the chip holds at a time, each with several rows where there are many, and
 // no more than it takes for the most that one of them has.  Forward, two of 1024 threads with a
 // piece each fit (4000 x 8192 bf16: 25 us, with one 30), of more pieces one does.  Backward, every one more costs a row of
@@ -508,7 +381,7 @@ Shape shape_of(const gbmw_layer_norm_problem* p) {
 // one fits a compute unit's registers (16384 x 5120: 103 us and 5 to join them); else two do (6304 x
 // 1283 in 32 bits: 20 us, with half as many 34).
 int norm_groups(const gbmw_layer_norm_problem* p, bool backward) {
-  const Shape s = shape_of(p);
+  const Shape s = shape_of(p->dtype, p->cols);
   const int per = std::max(1, (backward ? kNormBwdThreads : kNormFwdThreads) / s.nt);
   const bool one = s.nt == 1024 || (s.nj == 3 && p->dtype != GBMW_F32);   // kOne
   const int64_t most = !backward ? s.nt < 1024 ? 2048 : s.nj == 1 ? 512 : 256 : one ? 256 : 512, all = (p->rows + per - 1) / per;
@@ -563,31 +436,17 @@ gbmw_status launch_norm(const NormArgs& a, Shape s, bool backward, int groups, h
 }
 
 gbmw_status launch_norm(const gbmw_layer_norm_problem* p, const NormArgs& a, bool backward, int groups) {
-  const Shape s = shape_of(p);
+  const Shape s = shape_of(p->dtype, p->cols);
   hipStream_t st = (hipStream_t)p->stream;
   if (p->dtype == GBMW_F32) return launch_norm<float>(a, s, backward, groups, st);
   if (p->dtype == GBMW_F16) return launch_norm<f16>(a, s, backward, groups, st);
   return launch_norm<bf16>(a, s, backward, groups, st);
 }
 
-gbmw_status check_array(const char* name, const void* ptr, int size, int64_t stride, int64_t least) {
-  if (!ptr) return fail(GBMW_ERR_INVALID_ARG, "%s is null", name);
-  if ((uintptr_t)ptr % (unsigned)size) return fail(GBMW_ERR_INVALID_ARG, "%s is not aligned to its elements", name);
-  if (stride < least || stride > (INT64_MAX >> 34))
-    return fail(GBMW_ERR_INVALID_ARG, "%s: row stride %lld", name, (long long)stride);
-  return GBMW_OK;
-}
-
 }  // namespace
 }  // namespace gbmw
 
 using namespace gbmw;
-
-#define CHECK(expr)                            \
-  do {                                         \
-    const gbmw_status st_ = (expr);            \
-    if (st_ != GBMW_OK) return st_;            \
-  } while (0)
 
 extern "C" int64_t gbmw_layer_norm_workspace(const gbmw_layer_norm_problem* p) {
   gbmw_detail::clear_error();
