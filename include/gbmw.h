@@ -758,7 +758,7 @@ typedef struct {
 
 typedef struct {
   double lr, beta1, beta2;   /* lr >= 0, betas in [0, 1)                             */
-  double eps;                /* > 0                                                  */
+  double eps;                /* >= 2^-126                                            */
   double scale;              /* > 0: the inverse of a loss scale                     */
   double max_norm;           /* > 0, may be +inf                                     */
   int64_t step;              /* >= 1: the number of this step                        */

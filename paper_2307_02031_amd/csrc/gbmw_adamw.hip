@@ -9,11 +9,12 @@ using gbmw_detail::fail;
 namespace gbmw {
 namespace {
 
-constexpr int kBlock = 256;        // elements that share a scale
-constexpr int64_t kRun = 16384;    // at most so many elements of one tensor are a run
+constexpr int kBlock = 256;         // elements that share a scale
+constexpr int kTurn = 2048;         // elements that a workgroup has at a time
+constexpr int kMostTurns = 8;       // of a run
 constexpr int kMostGroups = 2048;
 
-struct Run {
+struct Run {   // elements of one tensor
   const void* grad;
   void *param, *copy, *m, *v;
   float *m_scale, *v_scale;
@@ -23,110 +24,148 @@ struct Run {
   float decay;
 };
 
+// The numbers that all elements share: computed in fp64, rounded once.
+struct Rates {
+  double lr;
+  float grad, b1, a1, b2, a2, eps, lr_c1, root_c2;
+  uint32_t key;   // of the random numbers; 0: round to nearest
+};
+
 struct AdamArgs {
-  double lr, beta1, beta2, scale, max_norm;
-  float eps;
-  int64_t step;
+  Rates r;   // of the numbers that the host knows
+  double beta1, beta2, scale, max_norm, c1;
   uint32_t seed;
   const float *norm, *lr_now;
   const int64_t* step_now;
 };
 
-// The numbers that all elements share: computed in fp64, rounded once.
-struct Rates {
-  float grad, b1, a1, b2, a2, eps, lr_c1, root_c2;
-  double lr;
-  uint32_t key;   // of the random numbers; 0: round to nearest
-  bool skip;
-};
-
-__device__ __forceinline__ uint32_t hash(uint32_t x) {
+__host__ __device__ __forceinline__ uint32_t hash(uint32_t x) {
   x *= 0x9E3779B1u;
   x = (x ^ (x >> 15)) * 0x85EBCA77u;
   return x ^ (x >> 13);
 }
 
-__device__ __forceinline__ Rates rates_of(const AdamArgs& a) {
-  Rates r;
-  double factor = a.scale;
-  r.skip = false;
+__host__ __device__ __forceinline__ uint32_t key_of(uint32_t seed, int64_t step) {
+  return seed ? hash(seed + (uint32_t)step * 0x9E3779B9u) : 0;
+}
+
+__host__ __device__ __forceinline__ double power(double x, int64_t n) {
+  double p = 1.0;
+  for (; n; n >>= 1, x *= x)
+    if (n & 1) p *= x;
+  return p;
+}
+
+// What the device knows alone is read here.  False: the step is left out.
+__device__ __forceinline__ bool rates_now(const AdamArgs& a, Rates& r) {
   if (a.norm) {
     const double norm = (double)*a.norm;
-    r.skip = !(norm < __builtin_inf());   // a NaN too
-    if (norm > a.max_norm) factor *= a.max_norm / norm;
+    if (!(norm < __builtin_inf())) return false;   // a NaN too
+    if (norm > a.max_norm) r.grad = (float)(a.scale * (a.max_norm / norm));
   }
-  r.lr = a.lr_now ? (double)*a.lr_now : a.lr;
-  int64_t step = a.step_now ? *a.step_now : a.step;
-  if (step < 1) step = 1;
-  double p1 = 1.0, p2 = 1.0, q1 = a.beta1, q2 = a.beta2;   // beta^step by squares
-  for (int64_t k = step; k; k >>= 1) {
-    if (k & 1) p1 *= q1, p2 *= q2;
-    q1 *= q1, q2 *= q2;
+  double c1 = a.c1;
+  if (a.step_now) {
+    int64_t step = *a.step_now;
+    if (step < 1) step = 1;
+    c1 = 1.0 - power(a.beta1, step);
+    r.root_c2 = (float)(1.0 / __builtin_sqrt(1.0 - power(a.beta2, step)));
+    r.key = key_of(a.seed, step);
   }
-  r.grad = (float)factor;
-  r.b1 = (float)a.beta1, r.a1 = (float)(1.0 - a.beta1);
-  r.b2 = (float)a.beta2, r.a2 = (float)(1.0 - a.beta2);
-  r.eps = a.eps;
-  r.lr_c1 = (float)(r.lr / (1.0 - p1));
-  r.root_c2 = (float)(1.0 / __builtin_sqrt(1.0 - p2));
-  r.key = a.seed ? hash(a.seed + (uint32_t)step * 0x9E3779B9u) : 0;
+  if (a.lr_now) r.lr = (double)*a.lr_now;
+  if (a.lr_now || a.step_now) r.lr_c1 = (float)(r.lr / c1);
+  return true;
+}
+
+// N elements at p of which n (0..N) are there, loaded or stored at once where all are.
+template <typename T, int N>
+struct alignas(sizeof(T)) Few {
+  T v[N];
+};
+template <typename T, int N>
+__device__ __forceinline__ Few<T, N> load(const void* p, int64_t i, int n) {
+  Few<T, N> r;
+  if (n >= N) {
+    __builtin_memcpy(&r, (const T*)p + i, sizeof(r));
+  } else {
+#pragma unroll
+    for (int e = 0; e < N; ++e) r.v[e] = e < n ? ((const T*)p)[i + e] : (T)0;
+  }
   return r;
 }
-
-// One element's step: m, the second moment before its root is taken, and the parameter.
-__device__ __forceinline__ void step_of(const Rates& r, float keep, float g, float& m, float& v, float& root, float& p) {
-  g *= r.grad;
-  m = m * r.b1 + g * r.a1;
-  v = v * r.b2 + g * g * r.a2;
-  root = __builtin_sqrtf(v);
-  p = p * keep - m / (root * r.root_c2 + r.eps) * r.lr_c1;
-}
-
-template <typename G, typename P>
-__device__ __forceinline__ void copy_out(const Run& run, int i, int n, const float (&p)[4]) {
-  if (!run.copy) return;
+template <typename T, int N>
+__device__ __forceinline__ void store(void* p, int64_t i, const Few<T, N>& x, int n) {
+  if (n >= N) {
+    __builtin_memcpy((T*)p + i, &x, sizeof(x));
+  } else {
 #pragma unroll
-  for (int e = 0; e < 4; ++e)
-    if (e < n) {
-      if (run.copy_dtype == GBMW_F16) ((f16*)run.copy)[i + e] = (f16)p[e];
-      else ((bf16*)run.copy)[i + e] = (bf16)p[e];
-    }
+    for (int e = 0; e < N; ++e)
+      if (e < n) ((T*)p)[i + e] = x.v[e];
+  }
 }
 
+template <int N>
+__device__ __forceinline__ void store_copy(const Run& run, int i, const float (&p)[N], int n) {
+  if (!run.copy) return;
+  if (run.copy_dtype == GBMW_F16) {
+    Few<f16, N> c;
+#pragma unroll
+    for (int e = 0; e < N; ++e) c.v[e] = (f16)p[e];
+    store(run.copy, i, c, n);
+  } else {
+    Few<bf16, N> c;
+#pragma unroll
+    for (int e = 0; e < N; ++e) c.v[e] = (bf16)p[e];
+    store(run.copy, i, c, n);
+  }
+}
+
+// States in 32 bits: a thread has four elements here and four 1024 further on, all loads on their way at once.
 template <typename G, typename P>
 __device__ __forceinline__ void run_of_32(const Run& run, const Rates& r) {
+  constexpr int N = 4, U = kTurn / (256 * N);
   const float keep = (float)(1.0 - r.lr * (double)run.decay);
-  for (int i = threadIdx.x * 4; i < run.n; i += 256 * 4) {
-    const int n = min(4, run.n - i);
-    float p[4], m[4], v[4], g[4], root;
+  for (int first = threadIdx.x * N; first < run.n; first += kTurn) {
+    Few<P, N> p[U];
+    Few<G, N> g[U];
+    Few<float, N> m[U], v[U];
 #pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      const int at = i + min(e, n - 1);
-      p[e] = (float)((const P*)run.param)[at], g[e] = (float)((const G*)run.grad)[at];
-      m[e] = ((const float*)run.m)[at], v[e] = ((const float*)run.v)[at];
+    for (int u = 0; u < U; ++u) {
+      const int i = first + u * 256 * N, n = run.n - i;
+      g[u] = load<G, N>(run.grad, i, n), p[u] = load<P, N>(run.param, i, n);
+      m[u] = load<float, N>(run.m, i, n), v[u] = load<float, N>(run.v, i, n);
     }
 #pragma unroll
-    for (int e = 0; e < 4; ++e) step_of(r, keep, g[e], m[e], v[e], root, p[e]);
+    for (int u = 0; u < U; ++u) {
+      const int i = first + u * 256 * N, n = run.n - i;
+      float q[N];
 #pragma unroll
-    for (int e = 0; e < 4; ++e)
-      if (e < n) ((P*)run.param)[i + e] = (P)p[e], ((float*)run.m)[i + e] = m[e], ((float*)run.v)[i + e] = v[e];
-    copy_out<G, P>(run, i, n, p);
+      for (int e = 0; e < N; ++e) {
+        const float d = (float)g[u].v[e] * r.grad;
+        const float me = m[u].v[e] = m[u].v[e] * r.b1 + d * r.a1;
+        const float ve = v[u].v[e] = v[u].v[e] * r.b2 + d * d * r.a2;
+        q[e] = (float)p[u].v[e] * keep - me / (__builtin_sqrtf(ve) * r.root_c2 + r.eps) * r.lr_c1;
+        p[u].v[e] = (P)q[e];
+      }
+      if (n <= 0) continue;
+      store(run.param, i, p[u], n), store(run.m, i, m[u], n), store(run.v, i, v[u], n);
+      store_copy(run, i, q, n);
+    }
   }
 }
 
 __device__ __forceinline__ unsigned magnitude(float x) { return __builtin_bit_cast(unsigned, x) & 0x7fffffffu; }   // a NaN's is the largest
 
-__device__ __forceinline__ float wave_most(unsigned u) {
-#pragma unroll
-  for (int d = 32; d; d >>= 1) u = max(u, (unsigned)__shfl_xor((int)u, d));
-  return __builtin_bit_cast(float, u);
+template <int CTRL>
+__device__ __forceinline__ unsigned max_dpp(unsigned x) {
+  return max(x, (unsigned)__builtin_amdgcn_update_dpp(0, (int)x, CTRL, 0xf, 0xf, true));
 }
-
-// x / scale as one of the 8-bit values beside it: up where the part cut off and `random`, of [0, 1), make a whole step.
-__device__ __forceinline__ float at_random(float x, float random) {
-  const float size = __builtin_fminf(__builtin_fabsf(x), 448.0f);
-  const int exponent = max((int)(__builtin_bit_cast(unsigned, size) >> 23) - 127, -6);
-  return __builtin_copysignf(__builtin_ldexpf(__builtin_floorf(__builtin_ldexpf(size, 3 - exponent) + random), exponent - 3), x);
+__device__ __forceinline__ float most_of_32(unsigned x) {   // over a half of the wave
+  x = max_dpp<0xB1>(x);    // lane ^ 1
+  x = max_dpp<0x4E>(x);    // lane ^ 2
+  x = max_dpp<0x141>(x);   // the other half of eight
+  x = max_dpp<0x140>(x);   // the other half of sixteen
+  const auto r = __builtin_amdgcn_permlane16_swap(x, x, false, false);
+  return __builtin_bit_cast(float, max((unsigned)r[0], (unsigned)r[1]));
 }
 
 __device__ __forceinline__ float scale_of(float most) {
@@ -134,46 +173,90 @@ __device__ __forceinline__ float scale_of(float most) {
   return s < 0x1p-126f ? 0x1p-126f : s;
 }
 
-__device__ __forceinline__ float value_of(uint8_t code) { return __builtin_amdgcn_cvt_f32_fp8((int)code, 0); }
-__device__ __forceinline__ uint8_t code_of(float x) { return (uint8_t)__builtin_amdgcn_cvt_pk_fp8_f32(x, x, 0, false); }
+// Eight values in 8 bits.  By the hash the conversion adds `random` (its upper 20 bits, below the last digit that is
+// kept) and cuts off: sixteen bits of the hash, and a half behind them.
+__device__ __forceinline__ void codes_of(const float (&x)[8], uint32_t key, const uint32_t (&random)[8], Few<uint32_t, 2>& code) {
+#pragma unroll
+  for (int w = 0; w < 2; ++w) {
+    int c = 0;
+    const float* y = x + 4 * w;
+    if (key) {
+      c = __builtin_amdgcn_cvt_sr_fp8_f32(y[0], random[4 * w], c, 0);
+      c = __builtin_amdgcn_cvt_sr_fp8_f32(y[1], random[4 * w + 1], c, 1);
+      c = __builtin_amdgcn_cvt_sr_fp8_f32(y[2], random[4 * w + 2], c, 2);
+      c = __builtin_amdgcn_cvt_sr_fp8_f32(y[3], random[4 * w + 3], c, 3);
+    } else {
+      c = __builtin_amdgcn_cvt_pk_fp8_f32(y[0], y[1], c, false);
+      c = __builtin_amdgcn_cvt_pk_fp8_f32(y[2], y[3], c, true);
+    }
+    code.v[w] = (uint32_t)c;
+  }
+}
 
-// A wave has a block of 256.
+__device__ __forceinline__ void values_of(const Few<uint8_t, 8>& code, float (&x)[8]) {
+  Few<uint32_t, 2> c;
+  __builtin_memcpy(&c, &code, 8);
+#pragma unroll
+  for (int w = 0; w < 2; ++w) {
+    typedef float f32x2 __attribute__((ext_vector_type(2)));
+    const f32x2 lo = __builtin_amdgcn_cvt_pk_f32_fp8((int)c.v[w], false), hi = __builtin_amdgcn_cvt_pk_f32_fp8((int)c.v[w], true);
+    x[4 * w] = lo[0], x[4 * w + 1] = lo[1], x[4 * w + 2] = hi[0], x[4 * w + 3] = hi[1];
+  }
+}
+
+// States in 8 bits: half a wave has a block, a lane eight of its elements.
 template <typename G, typename P>
 __device__ __forceinline__ void run_of_8(const Run& run, const Rates& r) {
+  constexpr int N = 8;
   const float keep = (float)(1.0 - r.lr * (double)run.decay);
-  const int lane = threadIdx.x % 64;
-  for (int k = threadIdx.x / 64; k * kBlock < run.n; k += 4) {
-    const int i = k * kBlock + lane * 4, n = min(4, run.n - i);   // 0 or less behind the last element
+  const int half = threadIdx.x / 32, lane = threadIdx.x % 32;
+  for (int k = half; k * kBlock < run.n; k += 8) {
+    const int i = k * kBlock + lane * N, n = run.n - i;   // 0 or less behind the last element
+    const Few<G, N> g = load<G, N>(run.grad, i, n);
+    const Few<P, N> p = load<P, N>(run.param, i, n);
+    const Few<uint8_t, N> mc = load<uint8_t, N>(run.m, i, n), vc = load<uint8_t, N>(run.v, i, n);
     const float ms = run.m_scale[k], vs = run.v_scale[k];
-    float p[4], m[4], v, g, root[4];
+    float m[N], root[N], q[N];
+    values_of(mc, m), values_of(vc, root);
     unsigned most_m = 0, most_v = 0;
 #pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      m[e] = root[e] = 0.0f;
-      if (e >= n) continue;
-      p[e] = (float)((const P*)run.param)[i + e], g = (float)((const G*)run.grad)[i + e];
-      m[e] = value_of(((const uint8_t*)run.m)[i + e]) * ms;
-      v = value_of(((const uint8_t*)run.v)[i + e]) * vs;
-      v *= v;
-      step_of(r, keep, g, m[e], v, root[e], p[e]);
+    for (int e = 0; e < N; ++e) {
+      const float d = (float)g.v[e] * r.grad, old = root[e] * vs;
+      m[e] = m[e] * ms * r.b1 + d * r.a1;
+      root[e] = __builtin_sqrtf(old * old * r.b2 + d * d * r.a2);
+      q[e] = (float)p.v[e] * keep - m[e] / (root[e] * r.root_c2 + r.eps) * r.lr_c1;
       most_m = max(most_m, magnitude(m[e])), most_v = max(most_v, magnitude(root[e]));
     }
-    const float new_ms = scale_of(wave_most(most_m)), new_vs = scale_of(wave_most(most_v));
-    if (lane == 0) run.m_scale[k] = new_ms, run.v_scale[k] = new_vs;
+    const float new_ms = scale_of(most_of_32(most_m)), new_vs = scale_of(most_of_32(most_v));
+    const float by_m = 1.0f / new_ms, by_v = 1.0f / new_vs;
+    uint32_t word[N] = {}, low[N] = {};
+    if (r.key) {
 #pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      if (e >= n) continue;
-      float cm = m[e] / new_ms, cv = root[e] / new_vs;
-      if (root[e] > 0.0f && cv < 0x1p-9f) cv = 0x1p-9f;
-      if (r.key) {
-        const uint32_t word = hash(((run.block + k) * kBlock + lane * 4 + e) ^ r.key);
-        cm = at_random(cm, ((float)(word >> 16) + 0.5f) * 0x1p-16f);
-        cv = at_random(cv, ((float)(word & 65535) + 0.5f) * 0x1p-16f);
+      for (int e = 0; e < N; ++e) {
+        word[e] = hash(((run.block + k) * kBlock + lane * N + e) ^ r.key);
+        low[e] = word[e] << 16 | 0x8000;
+        word[e] = (word[e] & 0xffff0000u) | 0x8000;
       }
-      ((uint8_t*)run.m)[i + e] = code_of(cm), ((uint8_t*)run.v)[i + e] = code_of(cv);
-      ((P*)run.param)[i + e] = (P)p[e];
     }
-    copy_out<G, P>(run, i, n, p);
+#pragma unroll
+    for (int e = 0; e < N; ++e) {
+      m[e] = __builtin_amdgcn_fmed3f(m[e] * by_m, -448.0f, 448.0f);
+      root[e] = root[e] > 0.0f ? __builtin_amdgcn_fmed3f(root[e] * by_v, 0x1p-9f, 448.0f) : 0.0f;
+    }
+    Few<uint32_t, 2> mw, vw;
+    codes_of(m, r.key, word, mw), codes_of(root, r.key, low, vw);
+    if (n <= 0) continue;
+    Few<uint8_t, N> out;
+    __builtin_memcpy(&out, &mw, N);
+    store(run.m, i, out, n);
+    __builtin_memcpy(&out, &vw, N);
+    store(run.v, i, out, n);
+    Few<P, N> to;
+#pragma unroll
+    for (int e = 0; e < N; ++e) to.v[e] = (P)q[e];
+    store(run.param, i, to, n);
+    store_copy(run, i, q, n);
+    if (lane == 0) run.m_scale[k] = new_ms, run.v_scale[k] = new_vs;
   }
 }
 
@@ -192,8 +275,8 @@ __device__ __forceinline__ void run_of(const Run& run, const Rates& r) {
 
 template <bool BITS8>
 __global__ __launch_bounds__(256) void k_adamw(const Run* runs, int count, AdamArgs a) {
-  const Rates r = rates_of(a);
-  if (r.skip) return;
+  Rates r = a.r;
+  if (!rates_now(a, r)) return;
   for (int k = blockIdx.x; k < count; k += gridDim.x) {
     const Run run = runs[k];
     if (run.grad_dtype == GBMW_F32) run_of<BITS8, float>(run, r);
@@ -274,12 +357,16 @@ extern "C" gbmw_status gbmw_adamw_list_create(int32_t n, const gbmw_adamw_tensor
   if (state_bits != 8 && state_bits != 32) return fail(GBMW_ERR_INVALID_ARG, "state_bits=%d is neither 8 nor 32", state_bits);
   try {
     std::vector<Extent> all;
-    int64_t count = 0;
+    int64_t total = 0, count = 0;
     for (int i = 0; i < n; ++i) {
       CHECK(check_adamw(i, tensors[i], state_bits, all));
-      count += (tensors[i].numel + kRun - 1) / kRun;
+      total += tensors[i].numel;
+      if (total > (1ll << 41)) return fail(GBMW_ERR_INVALID_ARG, "more than 2^41 elements");
     }
-    if (count > (1 << 27)) return fail(GBMW_ERR_INVALID_ARG, "more than 2^41 elements");
+    // runs as long as leave every workgroup one, so that a small list is spread over the chip
+    const int64_t length = kTurn * std::max<int64_t>(1, std::min<int64_t>(kMostTurns, total / ((int64_t)kTurn * kMostGroups)));
+    for (int i = 0; i < n; ++i) count += (tensors[i].numel + length - 1) / length;
+    if (count > INT32_MAX) return fail(GBMW_ERR_INVALID_ARG, "%lld runs", (long long)count);
     const int bad = overlap(all);
     if (bad >= 0) return fail(GBMW_ERR_INVALID_ARG, "tensor %d: an array overlaps another, and one of them is written", bad);
     std::vector<Run> runs;
@@ -288,13 +375,13 @@ extern "C" gbmw_status gbmw_adamw_list_create(int32_t n, const gbmw_adamw_tensor
     for (int i = 0; i < n; ++i) {
       const gbmw_adamw_tensor& t = tensors[i];
       const int gs = element_size(t.grad_dtype), ps = element_size(t.dtype), ss = state_bits == 8 ? 1 : 4;
-      for (int64_t at = 0; at < t.numel; at += kRun) {
+      for (int64_t at = 0; at < t.numel; at += length) {
         Run r{};
         r.grad = (const char*)t.grad + at * gs, r.param = (char*)t.param + at * ps;
         r.copy = t.copy ? (char*)t.copy + at * 2 : nullptr;
         r.m = (char*)t.m + at * ss, r.v = (char*)t.v + at * ss;
         if (state_bits == 8) r.m_scale = t.m_scale + at / kBlock, r.v_scale = t.v_scale + at / kBlock;
-        r.n = (int32_t)std::min(kRun, t.numel - at);
+        r.n = (int32_t)std::min(length, t.numel - at);
         r.block = block + (uint32_t)(at / kBlock);
         r.grad_dtype = t.grad_dtype, r.dtype = t.dtype, r.copy_dtype = t.copy_dtype, r.decay = t.weight_decay;
         runs.push_back(r);
@@ -330,7 +417,7 @@ extern "C" gbmw_status gbmw_adamw_step(const gbmw_adamw_list* l, const gbmw_adam
   if (!(o->lr >= 0.0) || !std::isfinite(o->lr)) return fail(GBMW_ERR_INVALID_ARG, "lr=%g", o->lr);
   if (!(o->beta1 >= 0.0 && o->beta1 < 1.0)) return fail(GBMW_ERR_INVALID_ARG, "beta1=%g", o->beta1);
   if (!(o->beta2 >= 0.0 && o->beta2 < 1.0)) return fail(GBMW_ERR_INVALID_ARG, "beta2=%g", o->beta2);
-  if (!((float)o->eps > 0.0f) || !std::isfinite((float)o->eps)) return fail(GBMW_ERR_INVALID_ARG, "eps=%g", o->eps);
+  if (!((float)o->eps >= 0x1p-126f) || !std::isfinite((float)o->eps)) return fail(GBMW_ERR_INVALID_ARG, "eps=%g", o->eps);
   if (!((float)o->scale > 0.0f) || !std::isfinite((float)o->scale)) return fail(GBMW_ERR_INVALID_ARG, "scale=%g", o->scale);
   if (!(o->max_norm > 0.0)) return fail(GBMW_ERR_INVALID_ARG, "max_norm=%g is not positive", o->max_norm);
   if (!o->step_now && o->step < 1) return fail(GBMW_ERR_INVALID_ARG, "step=%lld is below 1", (long long)o->step);
@@ -340,7 +427,15 @@ extern "C" gbmw_status gbmw_adamw_step(const gbmw_adamw_list* l, const gbmw_adam
   HIP_TRY(hipGetDevice(&dev));
   if (dev != l->device) return fail(GBMW_ERR_INVALID_ARG, "the list is on device %d, device %d is current", l->device, dev);
   if (l->count == 0) return GBMW_OK;
-  const AdamArgs a{o->lr, o->beta1, o->beta2, o->scale, o->max_norm, (float)o->eps, o->step, o->seed, o->norm, o->lr_now, o->step_now};
+  AdamArgs a{};
+  const int64_t step = std::max<int64_t>(1, o->step);   // read on the device if step_now is given
+  a.beta1 = o->beta1, a.beta2 = o->beta2, a.scale = o->scale, a.max_norm = o->max_norm, a.seed = o->seed;
+  a.norm = o->norm, a.lr_now = o->lr_now, a.step_now = o->step_now;
+  a.c1 = 1.0 - power(o->beta1, step);
+  a.r.lr = o->lr, a.r.grad = (float)o->scale, a.r.eps = (float)o->eps;
+  a.r.b1 = (float)o->beta1, a.r.a1 = (float)(1.0 - o->beta1), a.r.b2 = (float)o->beta2, a.r.a2 = (float)(1.0 - o->beta2);
+  a.r.lr_c1 = (float)(o->lr / a.c1), a.r.root_c2 = (float)(1.0 / std::sqrt(1.0 - power(o->beta2, step)));
+  a.r.key = key_of(o->seed, step);
   const dim3 grid(std::min(l->count, kMostGroups)), block(256);
   hipStream_t st = (hipStream_t)stream;
   if (l->bits == 8) hipLaunchKernelGGL(k_adamw<true>, grid, block, 0, st, (const Run*)l->runs.p, l->count, a);
