@@ -738,7 +738,7 @@ gbmw_status gbmw_rotary_frequencies(int32_t rot, double theta, int32_t scaling, 
  * bits).  Rounding to nearest leaves a moment unchanged for ever that moves by less than half a
  * step (up to 6 %) at a time.  r > 0 is never held as 0, which would let m / r grow without bound.
  * Zeroed codes and scales are states before the first step.  A NaN or an infinity in a
- * gradient makes its block's states NaN.
+ * gradient leaves no state of its block finite.
  *
  * A list is made once for tensors that stay where they are, as a gradient list is: it copies the
  * addresses to the device, holds no tensor alive and has no state of its own.  What is written
