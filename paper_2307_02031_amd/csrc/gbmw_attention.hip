@@ -35,19 +35,6 @@ typedef short s16x8 __attribute__((ext_vector_type(8)));
 typedef f16 f16x8 __attribute__((ext_vector_type(8)));
 typedef bf16 bf16x8 __attribute__((ext_vector_type(8)));
 
-// Division of 0 <= n < 2^31 by a number the host knows, without the dozens of instructions that a
-// division is.
-struct Divisor {
-  int d;
-  unsigned magic;   // 2^32 / d, rounded up (0 for 1)
-  __device__ __forceinline__ int of(int n) const {
-    if (d == 1) return n;
-    const unsigned x = __umulhi((unsigned)n, magic);   // at most one too large
-    return (int)(x * (unsigned)d > (unsigned)n ? x - 1 : x);
-  }
-};
-Divisor divisor(int64_t d) { return {(int)d, (unsigned)(((1ull << 32) + d - 1) / d)}; }
-
 // Which head and which of its `units` pieces of work a workgroup takes: see Deal.
 struct Plan {
   int per, units, near, last;   // heads of a die, units of a head, heads at a time, the first of the last heads

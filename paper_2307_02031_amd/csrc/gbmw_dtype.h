@@ -1,5 +1,5 @@
 // Internal: element types of the layer operators, 16-byte pieces of rows, sums over
-// a wave or a workgroup.  Not part of the ABI.
+// a wave or a workgroup, divisions.  Not part of the ABI.
 #pragma once
 #include <hip/hip_runtime.h>
 
@@ -9,6 +9,19 @@ namespace gbmw {
 
 using f16 = _Float16;
 using bf16 = __bf16;
+
+// Division of 0 <= n < 2^31 by a number the host knows, without the dozens of instructions that a
+// division is.
+struct Divisor {
+  int d;
+  unsigned magic;   // 2^32 / d, rounded up (0 for 1)
+  __device__ __forceinline__ int of(int n) const {
+    if (d == 1) return n;
+    const unsigned x = __umulhi((unsigned)n, magic);   // at most one too large
+    return (int)(x * (unsigned)d > (unsigned)n ? x - 1 : x);
+  }
+};
+inline Divisor divisor(int64_t d) { return {(int)d, (unsigned)(((1ull << 32) + d - 1) / d)}; }
 
 // As many elements as 16 bytes hold.
 template <typename T>

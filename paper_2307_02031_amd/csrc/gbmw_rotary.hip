@@ -6,13 +6,16 @@ using gbmw_detail::fail;
 namespace gbmw {
 namespace {
 
+constexpr int kMostPairs = 256;
+constexpr int kTable = 512;    // angles of a wave
+
 struct RotaryArgs {
   int B, L, Hq, H, D, rot;   // H: query and key heads
   int pairs;                 // rot / 2
   int turning, pieces;       // pieces of a head that turn, and those with the ones that are handed through
-  int rounds;                // of 64 / pieces heads that a token's heads take
-  int chunks, per_chunk;     // waves that share a token, rounds of each
-  unsigned units;            // tokens times chunks
+  int tokens, heads, chunks; // of a wave: tokens and heads; waves that share a token's heads
+  unsigned units;            // waves' worth of work
+  Divisor of_chunk, of_head, of_row, of_pairs;
   float factor, sign;
   const double* freq;
   const int32_t *positions, *len;
@@ -38,78 +41,124 @@ template <typename T, int W>
 struct alignas(sizeof(T)) Piece {
   T v[W];
 };
+template <int WORDS>
+using Words = uint32_t __attribute__((ext_vector_type(WORDS), aligned(1)));
 
-constexpr int kMostPairs = 256;
-
-// A wave has one token, or a share of its heads: it computes the token's angles, in turns and in fp64 (a
-// position times a frequency loses the digits of its fraction in fp32), and every lane keeps those of its
-// piece of W values (or of W values and the W that are rot / 2 further on) for all heads.
-template <typename T, int W, bool INTER>
-__global__ __launch_bounds__(256) void k_rotary(RotaryArgs a) {
-  constexpr int P = INTER ? W / 2 : W;   // pairs of a piece
-  __shared__ float table[4][2][kMostPairs];
-  const int lane = threadIdx.x % 64, wave = threadIdx.x / 64;
-  for (unsigned unit = blockIdx.x * 4 + wave; unit < a.units; unit += gridDim.x * 4) {
-  const unsigned token = unit / (unsigned)a.chunks;
-  const int chunk = (int)(unit % (unsigned)a.chunks), b = (int)(token / (unsigned)a.L), row = (int)(token % (unsigned)a.L);
-  if (a.len && row >= a.len[b]) continue;
-  const int position = a.positions ? a.positions[b * a.ps + row] : row;
-  float(*tab)[kMostPairs] = table[wave];
-  for (int i = lane; i < a.pairs; i += 64) {
-    const double t = (double)position * (a.freq[i] * 0.15915494309189533577);
-    float c, s;
-    turn_of((float)(t - __builtin_rint(t)), c, s);
-    tab[0][i] = c * a.factor, tab[1][i] = s * a.factor * a.sign;
+template <bool STREAM, typename T, int W>
+__device__ __forceinline__ void load(Piece<T, W>& r, const T* p) {
+  if constexpr (STREAM && sizeof(r) >= 8) {
+    const auto w = __builtin_nontemporal_load((const Words<sizeof(r) / 4>*)p);
+    __builtin_memcpy(&r, &w, sizeof(r));
+  } else {
+    __builtin_memcpy(&r, p, sizeof(r));
   }
-  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
-  __builtin_amdgcn_wave_barrier();
-  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
-  const int half = a.rot / 2;
+}
+template <bool STREAM, typename T, int W>
+__device__ __forceinline__ void store(T* p, const Piece<T, W>& r) {
+  if constexpr (STREAM && sizeof(r) >= 8) {
+    Words<sizeof(r) / 4> w;
+    __builtin_memcpy(&w, &r, sizeof(r));
+    __builtin_nontemporal_store(w, (Words<sizeof(r) / 4>*)p);
+  } else {
+    __builtin_memcpy(p, &r, sizeof(r));
+  }
+}
+
+// Nothing behind this comes before the piece has been loaded.
+template <typename T, int W>
+__device__ __forceinline__ void arrived(const Piece<T, W>& r) {
+  if constexpr (sizeof(r) >= 4) {
+    uint32_t w[sizeof(r) / 4];
+    __builtin_memcpy(w, &r, sizeof(r));
+#pragma unroll
+    for (unsigned i = 0; i < sizeof(r) / 4; ++i) asm volatile("" ::"v"(w[i]) : "memory");
+  }
+}
+
+template <typename T>
+__device__ __forceinline__ void turn(T& x, T& y, float c, float s) {
+  const float u = (float)x, v = (float)y;
+  x = (T)(u * c - v * s), y = (T)(u * s + v * c);
+}
+
+// A lane has two pieces of W values of a head: one and the one rot / 2 further on, or two of pairs next to each
+// other (INTER), or two that are handed through.  A wave has as many heads as its lanes have pieces for: some of a
+// token's, or all heads of some tokens.  Its loads go out first; then it computes its tokens' angles, in turns and
+// in fp64 (a position times a frequency loses the digits of its fraction in fp32), into LDS, once for all heads.
+//
+// Bound by HBM, and by how much of it is asked for at a time: one load of each piece a lane and many short waves
+// (4 x 2048 x 80 heads of 128 in bf16: 54 us, 6.2 TB/s; two rounds of heads a wave 60, a token a wave 68).
+//
+// Where what turns, or is handed through, is no whole number of pieces, the last piece starts early and shares
+// columns with the one before it.  Both lanes have loaded them, by one instruction, before one of them stores:
+// also in place (the pieces of a head that turn are at most 64).
+template <typename T, int W, bool INTER, bool STREAM, bool ONE>
+__global__ __launch_bounds__(256) void k_rotary(RotaryArgs a) {
+  __shared__ float table[4][2][kTable];
+  const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), half = a.rot / 2;
+  const unsigned unit = blockIdx.x * 4 + wave;
+  if (unit >= a.units) return;
+  const int group = a.of_chunk.of((int)unit), chunk = (int)unit - group * a.chunks;
+  const int first = group * a.tokens, here = min(a.tokens, a.B * a.L - first), first_head = chunk * a.heads;
+  const int items = ONE ? min(a.heads, a.H - first_head) : here * a.H;
+  float(*angles)[kTable] = table[wave];
+  if constexpr (ONE) {
+    const int b = a.of_row.of(first);
+    if (a.len && first - b * a.L >= a.len[b]) return;
+  }
   for (int p0 = 0; p0 < a.pieces; p0 += 64) {
     const int width = min(64, a.pieces - p0), slots = 64 / width, slot = lane / width, piece = p0 + lane % width;
-    if (slot >= slots) continue;
     const bool turns = piece < a.turning;
-    float c[P], s[P];
-    if (turns)
-#pragma unroll
-      for (int i = 0; i < P; ++i) c[i] = tab[0][piece * P + i], s[i] = tab[1][piece * P + i];
-    const int at = turns ? piece * W : a.rot + (piece - a.turning) * W;
-    const int first = chunk * a.per_chunk * slots, last = min(a.H, first + a.per_chunk * slots);
-    for (int head = first + slot; head < last; head += slots) {
-      const bool key = head >= a.Hq;
-      const int64_t in = key ? b * a.ks[0] + row * a.ks[1] + (head - a.Hq) * a.ks[2] : b * a.qs[0] + row * a.qs[1] + head * a.qs[2];
-      const int64_t to = key ? b * a.kos[0] + row * a.kos[1] + (head - a.Hq) * a.kos[2]
-                             : b * a.qos[0] + row * a.qos[1] + head * a.qos[2];
-      const T* src = (const T*)(key ? a.k : a.q) + in + at;
-      T* dst = (T*)(key ? a.ko : a.qo) + to + at;
-      Piece<T, W> x, y;
-      if (!turns && at + W > a.D) {   // the last of those handed through
-        for (int i = 0; at + i < a.D; ++i) dst[i] = src[i];
-        continue;
-      }
-      __builtin_memcpy(&x, src, sizeof(x));
-      if (turns) {
-        if constexpr (INTER) {
-#pragma unroll
-          for (int i = 0; i < P; ++i) {
-            const float u = (float)x.v[2 * i], v = (float)x.v[2 * i + 1];
-            x.v[2 * i] = (T)(u * c[i] - v * s[i]), x.v[2 * i + 1] = (T)(u * s[i] + v * c[i]);
-          }
-        } else {
-          __builtin_memcpy(&y, src + half, sizeof(y));
-#pragma unroll
-          for (int i = 0; i < P; ++i) {
-            const float u = (float)x.v[i], v = (float)y.v[i];
-            x.v[i] = (T)(u * c[i] - v * s[i]), y.v[i] = (T)(u * s[i] + v * c[i]);
-          }
-          __builtin_memcpy(dst + half, &y, sizeof(y));
-        }
-      }
-      __builtin_memcpy(dst, &x, sizeof(x));
+    int at, other;   // the places of its two pieces in a head
+    if (turns) {
+      at = INTER ? piece * W : min(piece * W, half - W);
+      other = INTER ? min(at + a.turning * W, a.rot - W) : at + half;
+    } else {
+      at = a.rot + (piece - a.turning) * W, other = min(at + (a.pieces - a.turning) * W, a.D - W);
     }
-  }
-  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-  __builtin_amdgcn_wave_barrier();
+    const bool few = !turns && a.D - a.rot < W;   // no piece is handed through, but single values
+    const int t = ONE ? 0 : a.of_head.of(slot), head = first_head + slot - t * a.H;
+    const int token = ONE ? first : min(first + t, a.B * a.L - 1), b = a.of_row.of(token), row = token - b * a.L;
+    const bool live = slot < min(slots, items) && (ONE || !(a.len && row >= a.len[b])), key = head >= a.Hq;
+    const T* from = key ? (const T*)a.k + (b * a.ks[0] + row * a.ks[1] + (head - a.Hq) * a.ks[2])
+                        : (const T*)a.q + (b * a.qs[0] + row * a.qs[1] + head * a.qs[2]);
+    T* to = key ? (T*)a.ko + (b * a.kos[0] + row * a.kos[1] + (head - a.Hq) * a.kos[2])
+                : (T*)a.qo + (b * a.qos[0] + row * a.qos[1] + head * a.qos[2]);
+    Piece<T, W> x, y;
+    if (live) load<STREAM>(x, from + min(at, a.D - W)), load<STREAM>(y, from + other);
+    if (p0 == 0) {
+      for (int i = lane; i < here * a.pairs; i += 64) {
+        const int t = ONE ? 0 : a.of_pairs.of(i), token = first + t, b = a.of_row.of(token), row = token - b * a.L;
+        const int position = a.positions ? a.positions[b * a.ps + row] : row;
+        const double angle = (double)position * (a.freq[i - t * a.pairs] * 0.15915494309189533577);
+        float c, s;
+        turn_of((float)(angle - __builtin_rint(angle)), c, s);
+        angles[0][i] = c * a.factor, angles[1][i] = s * a.factor * a.sign;
+      }
+      __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+      __builtin_amdgcn_wave_barrier();
+      __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+    }
+    if (!live) continue;
+    if (turns) {
+      const float *c = angles[0] + t * a.pairs, *s = angles[1] + t * a.pairs;
+      if constexpr (INTER) {
+        arrived(x), arrived(y);
+#pragma unroll
+        for (int i = 0; i < W / 2; ++i) {
+          turn(x.v[2 * i], x.v[2 * i + 1], c[at / 2 + i], s[at / 2 + i]);
+          turn(y.v[2 * i], y.v[2 * i + 1], c[other / 2 + i], s[other / 2 + i]);
+        }
+      } else {
+#pragma unroll
+        for (int i = 0; i < W; ++i) turn(x.v[i], y.v[i], c[at + i], s[at + i]);
+      }
+    }
+    if (few) {
+      for (int i = a.rot; i < a.D; ++i) to[i] = from[i];
+    } else {
+      store<STREAM>(to + at, x), store<STREAM>(to + other, y);
+    }
   }
 }
 
@@ -138,24 +187,29 @@ bool apart(int B, int L, int H, int D, const int64_t (&s)[3]) {
   return true;
 }
 
+template <typename T, int W, bool INTER, bool STREAM>
+void launch_rotary(const RotaryArgs& a, hipStream_t st) {
+  const dim3 grid((a.units + 3) / 4), block(256);
+  if (a.tokens == 1) hipLaunchKernelGGL((k_rotary<T, W, INTER, STREAM, true>), grid, block, 0, st, a);
+  else hipLaunchKernelGGL((k_rotary<T, W, INTER, STREAM, false>), grid, block, 0, st, a);
+}
+
+template <typename T, int W, bool STREAM>
+void launch_rotary(const RotaryArgs& a, bool interleaved, hipStream_t st) {
+  if constexpr (W > 1) {
+    if (interleaved) return launch_rotary<T, W, true, STREAM>(a, st);
+  }
+  launch_rotary<T, W, false, STREAM>(a, st);
+}
+
 template <typename T>
-gbmw_status launch_rotary(const RotaryArgs& a, int W, bool interleaved, int64_t groups, hipStream_t st) {
-  const dim3 grid((unsigned)groups), block(256);
-  if constexpr (sizeof(T) == 2) {
-    if (W == 8) {
-      if (interleaved) hipLaunchKernelGGL((k_rotary<T, 8, true>), grid, block, 0, st, a);
-      else hipLaunchKernelGGL((k_rotary<T, 8, false>), grid, block, 0, st, a);
-    }
-  }
-  if (W == 4) {
-    if (interleaved) hipLaunchKernelGGL((k_rotary<T, 4, true>), grid, block, 0, st, a);
-    else hipLaunchKernelGGL((k_rotary<T, 4, false>), grid, block, 0, st, a);
-  }
-  if (W == 2) {
-    if (interleaved) hipLaunchKernelGGL((k_rotary<T, 2, true>), grid, block, 0, st, a);
-    else hipLaunchKernelGGL((k_rotary<T, 2, false>), grid, block, 0, st, a);
-  }
-  if (W == 1) hipLaunchKernelGGL((k_rotary<T, 1, false>), grid, block, 0, st, a);
+gbmw_status launch_rotary(const RotaryArgs& a, int W, bool interleaved, bool stream, hipStream_t st) {
+  constexpr int V = kVec<T>;
+  if (W == V && stream) launch_rotary<T, V, true>(a, interleaved, st);
+  else if (W == V) launch_rotary<T, V, false>(a, interleaved, st);
+  else if (V == 8 && W == 4) launch_rotary<T, 4, false>(a, interleaved, st);
+  else if (W == 2) launch_rotary<T, 2, false>(a, interleaved, st);
+  else launch_rotary<T, 1, false>(a, interleaved, st);
   HIP_TRY(hipGetLastError());
   return GBMW_OK;
 }
@@ -171,7 +225,7 @@ gbmw_status rotary(const gbmw_rotary_problem* p, float sign) {
   if (p->rot < 0 || p->rot > p->D || p->rot % 2) return fail(GBMW_ERR_INVALID_ARG, "rot=%d is odd or not in 0..D", p->rot);
   if (p->interleaved != 0 && p->interleaved != 1) return fail(GBMW_ERR_INVALID_ARG, "interleaved=%d", p->interleaved);
   if (!std::isfinite(p->factor)) return fail(GBMW_ERR_INVALID_ARG, "factor=%g", (double)p->factor);
-  if ((int64_t)p->B * p->L > INT32_MAX) return fail(GBMW_ERR_INVALID_ARG, "too many rows: B=%d, L=%d", p->B, p->L);
+  if ((int64_t)p->B * p->L > INT32_MAX - 64) return fail(GBMW_ERR_INVALID_ARG, "too many rows: B=%d, L=%d", p->B, p->L);
   if (p->B == 0 || p->L == 0) return GBMW_OK;
   const int size = element_size(p->dtype);
   if (p->rot > 0 && (!p->freq || (uintptr_t)p->freq % 8)) return fail(GBMW_ERR_INVALID_ARG, "freq is null or not aligned to a double");
@@ -200,24 +254,39 @@ gbmw_status rotary(const gbmw_rotary_problem* p, float sign) {
   a.q = p->q, a.k = p->k, a.qo = p->q_out, a.ko = p->k_out;
   std::copy(p->q_stride, p->q_stride + 3, a.qs), std::copy(p->k_stride, p->k_stride + 3, a.ks);
   std::copy(p->q_out_stride, p->q_out_stride + 3, a.qos), std::copy(p->k_out_stride, p->k_out_stride + 3, a.kos);
-  // the widest piece of up to 16 bytes of which what turns is a whole number
+  // the widest piece of up to 16 bytes that what turns has room for
   const int through = in_place ? 0 : p->D - p->rot, unit = p->interleaved ? p->rot : p->rot / 2;
   if (unit == 0 && through == 0) return GBMW_OK;
   int W = 16 / size;
-  while (unit % W) W /= 2;
-  a.turning = unit / W, a.pieces = a.turning + (through + W - 1) / W;
-  const int slots = 64 / std::min(64, a.pieces);
-  a.rounds = (a.H + slots - 1) / slots;
+  while ((unit && W > unit) || W > p->D) W /= 2;
+  a.turning = p->interleaved ? (unit + 2 * W - 1) / (2 * W) : (unit + W - 1) / W;
+  a.pieces = a.turning + (through + 2 * W - 1) / (2 * W);
+  // a wave has as many heads as its lanes have pieces for, of several tokens where one has fewer
   const int64_t tokens = (int64_t)p->B * p->L;
-  a.chunks = (int)std::max<int64_t>(1, std::min<int64_t>(a.rounds, 4096 / tokens));
-  a.per_chunk = (a.rounds + a.chunks - 1) / a.chunks;
-  a.chunks = (a.rounds + a.per_chunk - 1) / a.per_chunk;
-  a.units = (unsigned)(tokens * a.chunks);
-  const int64_t groups = std::min<int64_t>(1 << 20, ((int64_t)a.units + 3) / 4);
+  const int items = 64 / std::min(64, a.pieces);
+  a.tokens = std::max(1, std::min(items / a.H, kTable / std::max(1, a.pairs)));
+  a.heads = a.tokens > 1 ? a.H : std::min(a.H, items);
+  a.chunks = (a.H + a.heads - 1) / a.heads;
+  a.heads = (a.H + a.chunks - 1) / a.chunks;
+  const int64_t units = (tokens + a.tokens - 1) / a.tokens * a.chunks;
+  if (units > (1 << 26) - 8) return fail(GBMW_ERR_UNSUPPORTED, "too many rows and heads: %lld waves", (long long)units);
+  a.units = (unsigned)units;
+  a.of_chunk = divisor(a.chunks), a.of_head = divisor(a.H), a.of_row = divisor(p->L), a.of_pairs = divisor(std::max(1, a.pairs));
+  // Loads and stores pass the cache by where it would not hold the results for who reads them next, and where a wave's
+  // stores are whole lines of it.  With the attention that reads them, bytes read and written, through the cache and past
+  // it: 8192 rows of 40 heads of 128 (168 MB) 212 and 220 us, 12288 (252 MB) 325 and 322, 16384 (336 MB) 431 and 427;
+  // 8192 of 80 heads (336 MB) 359 and 349, the call alone 66 and 55.
+  const int line = 128 / size;
+  auto lines = [line](const void* x, const int64_t (&s)[3]) {
+    return (uintptr_t)x % 128 == 0 && s[0] % line == 0 && s[1] % line == 0 && s[2] % line == 0;
+  };
+  const bool stream = tokens * a.H * (p->rot + through) >= (1ll << 27) / size && p->rot % (2 * line) == 0 &&
+                      through % (2 * line) == 0 && lines(p->q_out, p->q_out_stride) &&
+                      (!p->Hk || lines(p->k_out, p->k_out_stride));
   hipStream_t st = (hipStream_t)p->stream;
-  if (p->dtype == GBMW_F32) return launch_rotary<float>(a, W, p->interleaved && W > 1, groups, st);
-  if (p->dtype == GBMW_F16) return launch_rotary<f16>(a, W, p->interleaved && W > 1, groups, st);
-  return launch_rotary<bf16>(a, W, p->interleaved && W > 1, groups, st);
+  if (p->dtype == GBMW_F32) return launch_rotary<float>(a, W, p->interleaved, stream, st);
+  if (p->dtype == GBMW_F16) return launch_rotary<f16>(a, W, p->interleaved, stream, st);
+  return launch_rotary<bf16>(a, W, p->interleaved, stream, st);
 }
 
 }  // namespace
