@@ -21,9 +21,61 @@ struct RmsArgs {
   int group, groups;    // columns of a scale, or 0; scales of a row
   float *scale, *rstd;
   float* partial;  // [gridDim.x][share_stride(cols)]
+  bool stream;     // past the cache
 };
 
 constexpr int kRmsFwdThreads = 256, kRmsBwdThreads = 512;
+
+template <int WORDS>
+using Words = uint32_t __attribute__((ext_vector_type(WORDS), aligned(1)));
+
+// A thread's pieces of a row, as they are.  STREAM: past the cache.
+template <bool STREAM, typename T, int NJ, typename S>
+__device__ __forceinline__ void load_row(Pack<T> (&p)[NJ], const S (&span)[NJ], const T* row) {
+#pragma unroll
+  for (int j = 0; j < NJ; ++j) {
+    if (!S::kTiny || span[j].row >= kVec<T>) {
+      if constexpr (STREAM) {
+        const auto w = __builtin_nontemporal_load((const Words<4>*)(row + span[j].c));
+        __builtin_memcpy(&p[j], &w, 16);
+      } else {
+        __builtin_memcpy(&p[j], row + span[j].c, 16);
+      }
+    } else {
+      p[j] = load_pack(row, span[j].n);
+    }
+  }
+}
+template <bool STREAM, typename T, typename S, int V>
+__device__ __forceinline__ void store_row(const S& span, T* row, const float (&y)[V]) {
+  if constexpr (STREAM) {
+    if (!S::kTiny || span.n == V) {
+      Pack<T> r;
+#pragma unroll
+      for (int i = 0; i < V; ++i) r.v[i] = (T)y[i];
+      Words<4> w;
+      __builtin_memcpy(&w, &r, 16);
+      __builtin_nontemporal_store(w, (Words<4>*)(row + span.c));
+      return;
+    }
+  }
+  span.store(row, y);
+}
+
+// Sum over the NT threads of a row, of which a wave may have four.  `scratch`: NT / 64 floats of the row's own.
+template <int NT>
+__device__ __forceinline__ float sum_of_row(float x, float* scratch) {
+  if constexpr (NT == 16) {
+    return sum_dpp<0x140>(sum_dpp<0x141>(sum_dpp<0x4E>(sum_dpp<0xB1>(x))));
+  } else {
+    float s[1] = {x};
+    row_sum<NT>(s, scratch);
+    return s[0];
+  }
+}
+
+template <int NT>
+constexpr int kWaves = NT < 64 ? 1 : NT / 64;   // of a row
 
 // Largest of |x| as bits: a NaN is larger than any number, and stays.
 __device__ __forceinline__ unsigned magnitude(float x) { return __builtin_bit_cast(unsigned, x) & 0x7fffffffu; }
@@ -68,171 +120,150 @@ __device__ __forceinline__ void to_codes(const float (&x)[V], float by, bool who
   }
 }
 
-template <typename T, int NT, int NJ, bool WHOLE>
+template <typename T, int NT, int NJ, bool WHOLE, bool STREAM>
 __global__ __launch_bounds__(NT < kRmsFwdThreads ? kRmsFwdThreads : NT) void k_rms_fwd(RmsArgs a) {
   constexpr int V = kVec<T>, G = (NT < kRmsFwdThreads ? kRmsFwdThreads : NT) / NT;
-  constexpr bool kAhead = kRunsAhead<NT, NJ>;
-  __shared__ float scratch[2][G][NT / 64];
-  __shared__ unsigned most_of[G][NT / 64];
+  __shared__ float scratch[2][G][kWaves<NT>];
+  __shared__ unsigned most_of[G][kWaves<NT>];
   const int t = threadIdx.x % NT, g = threadIdx.x / NT;
-  constexpr bool kTiny = !WHOLE && NT * NJ == 64;
-  Span<V, WHOLE, kTiny> span[NJ];
+  Span<V, WHOLE, !WHOLE && NT * NJ == 16> span[NJ];
 #pragma unroll
-  for (int j = 0; j < NJ; ++j) span[j] = Span<V, WHOLE, kTiny>(t + j * NT, a.cols);
-  Held<T, NJ, kTiny> h, r, next, next_r;
-  auto fetch = [&](int64_t row) {
-    const int64_t at = row < a.rows ? row : 0;
-    next.load(span, (const T*)a.x + at * a.xs, a.cols);
-    if (a.res) next_r.load(span, (const T*)a.res + at * a.rs, a.cols);
-  };
-  const int64_t step = (int64_t)gridDim.x * G;
-  fetch((int64_t)blockIdx.x * G + g);
-  float w[NJ][V];
-#pragma unroll
-  for (int j = 0; j < NJ; ++j) {
-#pragma unroll
-    for (int i = 0; i < V; ++i) w[j][i] = 1.0f;
-    if (a.w) a.wide ? span[j].load(w[j], (const float*)a.w) : span[j].load(w[j], (const T*)a.w);
-  }
+  for (int j = 0; j < NJ; ++j) span[j] = {t + j * NT, a.cols};
   int turn = 0;
-  for (int64_t first = (int64_t)blockIdx.x * G; first < a.rows; first += step, turn ^= 1) {
-    const int64_t row = first + g;
-    h = next;
-    if (a.res) r = next_r;
-    if constexpr (kAhead) fetch(row + step);
+  for (int64_t first = (int64_t)blockIdx.x * G; first < a.rows; first += (int64_t)gridDim.x * G, turn ^= 1) {
+    const int64_t row = first + g, at = row < a.rows ? row : 0;
+    Pack<T> h[NJ], r[NJ];
+    load_row<STREAM>(h, span, (const T*)a.x + at * a.xs);
+    if (a.res) load_row<STREAM>(r, span, (const T*)a.res + at * a.rs);
+    float w[NJ][V];
+#pragma unroll
+    for (int j = 0; j < NJ; ++j) {
+#pragma unroll
+      for (int i = 0; i < V; ++i) w[j][i] = 1.0f;
+      if (a.w) a.wide ? span[j].load(w[j], (const float*)a.w) : span[j].load(w[j], (const T*)a.w);
+    }
     if (a.res) {
 #pragma unroll
       for (int j = 0; j < NJ; ++j)
 #pragma unroll
-        for (int i = 0; i < V; ++i) h.p[j].v[i] = (T)((float)h.p[j].v[i] + (float)r.p[j].v[i]);
+        for (int i = 0; i < V; ++i) h[j].v[i] = (T)((float)h[j].v[i] + (float)r[j].v[i]);
     }
-    float s[1] = {0.0f};
+    float s = 0.0f;
 #pragma unroll
     for (int j = 0; j < NJ; ++j)
 #pragma unroll
       for (int i = 0; i < V; ++i) {
-        const float d = j < kSure<NT, NJ> || span[j].has(i) ? (float)h.p[j].v[i] : 0.0f;
-        s[0] = __builtin_fmaf(d, d, s[0]);
+        const float d = j < kSure<NT, NJ> || span[j].has(i) ? (float)h[j].v[i] : 0.0f;
+        s = __builtin_fmaf(d, d, s);
       }
     // stores come after the sum, which has every thread's values of the row: it may be written in place
-    row_sum<NT>(s, scratch[turn][g]);
-    const float rstd = 1.0f / __builtin_sqrtf(s[0] / (float)a.cols + a.eps);
+    s = sum_of_row<NT>(s, scratch[turn][g]);
+    const float rstd = 1.0f / __builtin_sqrtf(s / (float)a.cols + a.eps);
     const bool live = row < a.rows;
     auto normed = [&](int j, float (&y)[V]) {
 #pragma unroll
-      for (int i = 0; i < V; ++i) y[i] = (float)h.p[j].v[i] * rstd * w[j][i];
+      for (int i = 0; i < V; ++i) y[i] = (float)h[j].v[i] * rstd * w[j][i];
     };
     if (live) {
       if (t == 0 && a.rstd) a.rstd[row] = rstd;
-      if (a.h) {
-        T* out = (T*)a.h + row * a.hs;
-#pragma unroll
-        for (int j = 0; j < NJ; ++j) {
-          if (span[j].n == 0) continue;
-          float v[V];
-#pragma unroll
-          for (int i = 0; i < V; ++i) v[i] = (float)h.p[j].v[i];
-          span[j].store(out, v);
-        }
-      }
-      if (a.y) {
-        T* out = (T*)a.y + row * a.ys;
-#pragma unroll
-        for (int j = 0; j < NJ; ++j) {
-          if (span[j].n == 0) continue;
-          float y[V];
-          normed(j, y);
-          span[j].store(out, y);
-        }
-      }
-    }
-    if (a.q) {
-      const float top = a.whole_numbers ? 127.0f : 448.0f;
-      unsigned most[NJ];
 #pragma unroll
       for (int j = 0; j < NJ; ++j) {
+        if (span[j].n == 0) continue;
         float y[V];
-        normed(j, y);
-        most[j] = 0;
+        if (a.h) {
 #pragma unroll
-        for (int i = 0; i < V; ++i)
-          if (j < kSure<NT, NJ> || span[j].has(i)) most[j] = max(most[j], magnitude(y[i]));
-      }
-      if (a.group) {
-#pragma unroll
-        for (int j = 0; j < NJ; ++j) most[j] = lanes_max(most[j], a.group / V);
-      } else {
-        unsigned all = most[0];
-#pragma unroll
-        for (int j = 1; j < NJ; ++j) all = max(all, most[j]);
-        all = lanes_max(all, 64);
-        if constexpr (NT > 64) {
-          if (t % 64 == 0) most_of[g][t / 64] = all;
-          __syncthreads();
-          all = 0;
-#pragma unroll
-          for (int k = 0; k < NT / 64; ++k) all = max(all, most_of[g][k]);
+          for (int i = 0; i < V; ++i) y[i] = (float)h[j].v[i];
+          store_row<STREAM>(span[j], (T*)a.h + row * a.hs, y);
         }
-#pragma unroll
-        for (int j = 0; j < NJ; ++j) most[j] = all;
-      }
-      if (live) {
-        uint8_t* out = a.q + row * a.qs;
-        float* scales = a.scale + row * a.groups;
-#pragma unroll
-        for (int j = 0; j < NJ; ++j) {
-          if (span[j].n == 0) continue;
-          const float most_f = __builtin_bit_cast(float, most[j]) / top;
-          const float scale = most_f < 0x1p-126f ? 0x1p-126f : most_f, by = 1.0f / scale;
-          if (a.group ? span[j].from % a.group == 0 : t == 0 && j == 0)
-            scales[a.group ? span[j].from / a.group : 0] = scale;
-          float y[V];
+        if (a.y) {
           normed(j, y);
-          unsigned code[V / 4];
-          to_codes(y, by, a.whole_numbers, code);
-          // a piece that starts early has columns of another group: those are the piece's before it
-          if (WHOLE || (span[j].n == V && span[j].c == span[j].from)) {
-            __builtin_memcpy(out + span[j].c, code, V);
-          } else {
-#pragma unroll
-            for (int i = 0; i < V; ++i)
-              if (span[j].has(i)) out[span[j].c + i] = (uint8_t)(code[i / 4] >> (8 * (i % 4)));
-          }
+          store_row<STREAM>(span[j], (T*)a.y + row * a.ys, y);
         }
       }
     }
-    if constexpr (!kAhead) fetch(row + step);
+    if (!a.q) continue;
+    const float top = a.whole_numbers ? 127.0f : 448.0f;
+    unsigned most[NJ];
+#pragma unroll
+    for (int j = 0; j < NJ; ++j) {
+      float y[V];
+      normed(j, y);
+      most[j] = 0;
+#pragma unroll
+      for (int i = 0; i < V; ++i)
+        if (j < kSure<NT, NJ> || span[j].has(i)) most[j] = max(most[j], magnitude(y[i]));
+    }
+    if (a.group) {
+#pragma unroll
+      for (int j = 0; j < NJ; ++j) most[j] = lanes_max(most[j], min(a.group / V, NT));
+    } else {
+      unsigned all = most[0];
+#pragma unroll
+      for (int j = 1; j < NJ; ++j) all = max(all, most[j]);
+      all = lanes_max(all, NT < 64 ? NT : 64);
+      if constexpr (NT > 64) {
+        if (t % 64 == 0) most_of[g][t / 64] = all;
+        __syncthreads();
+        all = 0;
+#pragma unroll
+        for (int k = 0; k < NT / 64; ++k) all = max(all, most_of[g][k]);
+      }
+#pragma unroll
+      for (int j = 0; j < NJ; ++j) most[j] = all;
+    }
+    if (!live) continue;
+    uint8_t* out = a.q + row * a.qs;
+    float* scales = a.scale + row * a.groups;
+#pragma unroll
+    for (int j = 0; j < NJ; ++j) {
+      if (span[j].n == 0) continue;
+      const float most_f = __builtin_bit_cast(float, most[j]) / top;
+      const float scale = most_f < 0x1p-126f ? 0x1p-126f : most_f, by = 1.0f / scale;
+      if (a.group ? span[j].from % a.group == 0 : t == 0 && j == 0) scales[a.group ? span[j].from / a.group : 0] = scale;
+      float y[V];
+      normed(j, y);
+      unsigned code[V / 4];
+      to_codes(y, by, a.whole_numbers, code);
+      // a piece that starts early has columns of another group: those are the piece's before it
+      if (WHOLE || (span[j].n == V && span[j].c == span[j].from)) {
+        __builtin_memcpy(out + span[j].c, code, V);
+      } else {
+#pragma unroll
+        for (int i = 0; i < V; ++i)
+          if (span[j].has(i)) out[span[j].c + i] = (uint8_t)(code[i / 4] >> (8 * (i % 4)));
+      }
+    }
   }
 }
 
 // The same walk; a thread keeps its columns' share of dweight over all its rows, as layer norm's does.
-template <typename T, int NT, int NJ, bool WHOLE>
+template <typename T, int NT, int NJ, bool WHOLE, bool STREAM>
 __global__ __launch_bounds__(NT < kRmsBwdThreads ? kRmsBwdThreads : NT) void k_rms_bwd(RmsArgs a) {
   constexpr int V = kVec<T>, G = (NT < kRmsBwdThreads ? kRmsBwdThreads : NT) / NT;
   constexpr bool kAhead = kRunsAhead<NT, NJ>;
-  __shared__ float scratch[2][G][NT / 64];
+  __shared__ float scratch[2][G][kWaves<NT>];
   extern __shared__ __attribute__((aligned(16))) float columns[];   // [V/4][pieces][4] weight, then [cols] shares
   const int t = threadIdx.x % NT, g = threadIdx.x / NT;
-  constexpr bool kTiny = !WHOLE && NT * NJ == 64;
-  Span<V, WHOLE, kTiny> span[NJ];
+  using Piece = Span<V, WHOLE, !WHOLE && NT * NJ == 16>;
+  Piece span[NJ];
 #pragma unroll
-  for (int j = 0; j < NJ; ++j) span[j] = Span<V, WHOLE, kTiny>(t + j * NT, a.cols);
-  Held<T, NJ, kTiny> x, dy, next_x, next_dy, dres, next_dres;
+  for (int j = 0; j < NJ; ++j) span[j] = Piece(t + j * NT, a.cols);
+  Pack<T> x[NJ], dy[NJ], dres[NJ], next_x[NJ], next_dy[NJ], next_dres[NJ];
   float rstd, next_rstd;
   auto fetch = [&](int64_t row) {
     const int64_t at = row < a.rows ? row : 0;
-    next_x.load(span, (const T*)a.x + at * a.xs, a.cols);
-    next_dy.load(span, (const T*)a.dy + at * a.dys, a.cols);
-    if (a.dres) next_dres.load(span, (const T*)a.dres + at * a.drs, a.cols);
+    load_row<STREAM>(next_x, span, (const T*)a.x + at * a.xs);
+    load_row<STREAM>(next_dy, span, (const T*)a.dy + at * a.dys);
+    if (a.dres) load_row<STREAM>(next_dres, span, (const T*)a.dres + at * a.drs);
     next_rstd = a.rstd[at];
   };
-  const int64_t step = (int64_t)gridDim.x * G;
-  fetch((int64_t)blockIdx.x * G + g);
+  const int64_t step = (int64_t)gridDim.x * G, begin = (int64_t)blockIdx.x * G, end = a.rows;
+  fetch(begin + g);
   typedef float f32x4 __attribute__((ext_vector_type(4)));
   const int pieces = (a.cols + V - 1) / V;
   f32x4* weight = (f32x4*)columns;
   for (int k = threadIdx.x; k < pieces; k += blockDim.x) {
-    const Span<V, WHOLE, kTiny> s(k, a.cols);
+    const Piece s(k, a.cols);
     float w[V];
 #pragma unroll
     for (int i = 0; i < V; ++i) w[i] = 1.0f;
@@ -252,13 +283,14 @@ __global__ __launch_bounds__(NT < kRmsBwdThreads ? kRmsBwdThreads : NT) void k_r
   };
   float dw[NJ][V] = {};
   int turn = 0;
-  for (int64_t first = (int64_t)blockIdx.x * G; first < a.rows; first += step, turn ^= 1) {
+  for (int64_t first = begin; first < end; first += step, turn ^= 1) {
     const int64_t row = first + g;
-    const bool live = row < a.rows;
-    x = next_x, dy = next_dy, rstd = next_rstd;
-    if (a.dres) dres = next_dres;
+    const bool live = row < end;
+    rstd = next_rstd;
+#pragma unroll
+    for (int j = 0; j < NJ; ++j) x[j] = next_x[j], dy[j] = next_dy[j], dres[j] = next_dres[j];
     if constexpr (kAhead) fetch(row + step);
-    float s[1] = {0.0f};
+    float s = 0.0f;
     if (live) {
 #pragma unroll
       for (int j = 0; j < NJ; ++j) {
@@ -267,9 +299,9 @@ __global__ __launch_bounds__(NT < kRmsBwdThreads ? kRmsBwdThreads : NT) void k_r
 #pragma unroll
         for (int i = 0; i < V; ++i) {
           const bool has = j < kSure<NT, NJ> || span[j].has(i);
-          const float xhat = has ? (float)x.p[j].v[i] * rstd : 0.0f, d = has ? (float)dy.p[j].v[i] : 0.0f;
+          const float xhat = has ? (float)x[j].v[i] * rstd : 0.0f, d = has ? (float)dy[j].v[i] : 0.0f;
           dw[j][i] = __builtin_fmaf(d, xhat, dw[j][i]);
-          s[0] = __builtin_fmaf(d * w[i], xhat, s[0]);
+          s = __builtin_fmaf(d * w[i], xhat, s);
         }
       }
     }
@@ -277,10 +309,9 @@ __global__ __launch_bounds__(NT < kRmsBwdThreads ? kRmsBwdThreads : NT) void k_r
       typedef int i32x4 __attribute__((ext_vector_type(4)));
       if (a.dres)
 #pragma unroll
-        for (int j = 0; j < NJ; ++j) asm volatile("" ::"v"(__builtin_bit_cast(i32x4, dres.p[j])));
+        for (int j = 0; j < NJ; ++j) asm volatile("" ::"v"(__builtin_bit_cast(i32x4, dres[j])));
     }
-    row_sum<NT>(s, scratch[turn][g]);
-    const float c = s[0] / (float)a.cols;
+    const float c = sum_of_row<NT>(s, scratch[turn][g]) / (float)a.cols;
     if (live) {
       T* dx = (T*)a.dx + row * a.dxs;
 #pragma unroll
@@ -290,30 +321,31 @@ __global__ __launch_bounds__(NT < kRmsBwdThreads ? kRmsBwdThreads : NT) void k_r
         weight_of(j, w);
 #pragma unroll
         for (int i = 0; i < V; ++i) {
-          const float xhat = (float)x.p[j].v[i] * rstd;
-          out[i] = __builtin_fmaf(-xhat, c, (float)dy.p[j].v[i] * w[i]) * rstd;
-          if (a.dres) out[i] += (float)dres.p[j].v[i];
+          const float xhat = (float)x[j].v[i] * rstd;
+          out[i] = __builtin_fmaf(-xhat, c, (float)dy[j].v[i] * w[i]) * rstd;
+          if (a.dres) out[i] += (float)dres[j].v[i];
         }
-        span[j].store(dx, out);
+        store_row<STREAM>(span[j], dx, out);
       }
     }
     if constexpr (!kAhead) fetch(row + step);
   }
   if (!a.partial) return;
-  for (int k = 0; k < G; ++k) {   // one row's threads after the other add their share
-    __syncthreads();
-    if (g == k)
+  // the shares of the G rows' threads side by side, then added in order
+  __syncthreads();
 #pragma unroll
-      for (int j = 0; j < NJ; ++j)
+  for (int j = 0; j < NJ; ++j)
 #pragma unroll
-        for (int i = 0; i < V; ++i) {
-          const int col = span[j].c + i;
-          if (span[j].has(i)) columns[col] = k ? columns[col] + dw[j][i] : dw[j][i];
-        }
-  }
+    for (int i = 0; i < V; ++i)
+      if (span[j].has(i)) columns[g * a.cols + span[j].c + i] = dw[j][i];
   __syncthreads();
   float* out = a.partial + (int64_t)blockIdx.x * share_stride(a.cols);
-  for (int col = threadIdx.x; col < a.cols; col += blockDim.x) out[col] = columns[col];
+  for (int col = threadIdx.x; col < a.cols; col += blockDim.x) {
+    float sum = columns[col];
+#pragma unroll
+    for (int k = 1; k < G; ++k) sum += columns[k * a.cols + col];
+    out[col] = sum;
+  }
 }
 
 // ---- host ---------------------------------------------------------------------------------
@@ -328,31 +360,49 @@ gbmw_status check_rms(const gbmw_rms_norm_problem* p) {
   return GBMW_OK;
 }
 
+// As layer norm's, and: 16 threads where a row of up to 48 pieces fits them (not where a scale has columns of
+// more threads than these), 128 where 256 would leave many without a piece, 512 between the rows of 256 and those of 1024.
+Shape rms_shape(const gbmw_rms_norm_problem* p, bool backward) {
+  const int vec = 16 / element_size(p->dtype), n = (p->cols + vec - 1) / vec;
+  if (n <= 16 || (n <= 3 * 16 && (backward || !p->q || p->group <= 16 * vec))) return {16, (n + 15) / 16};
+  if (n <= 3 * 64) return {64, (n + 63) / 64};
+  if (n > 2 * 128 && n <= 3 * 128) return {128, 3};
+  if (n <= 3 * 256) return {256, (n + 255) / 256};
+  if (n <= 3 * 512) return {512, (n + 511) / 512};
+  const int nj = (n + 1023) / 1024;
+  return {1024, nj <= 4 ? nj : 8};
+}
+
+// Workgroups: forward one for every so many rows (many short ones keep memory busier than some that stay: 16384 x 5120
+// 117 us, with 2048 that walk 129); backward so few that their shares of dweight cost little, one or two for a compute
+// unit.  Two where rows are short enough that one leaves memory idle (16384 x 2560 76 us, with one 91; 65536 x 128 19 and
+// 21) and there are rows for it (8192 x 1280, two turns of two or four of one: 27 and 24).
 int rms_groups(const gbmw_rms_norm_problem* p, bool backward) {
-  const Shape s = shape_of(p->dtype, p->cols);
-  const int per = std::max(1, (backward ? kRmsBwdThreads : kRmsFwdThreads) / s.nt);
-  const int64_t most = !backward ? s.nt < 1024 ? 2048 : s.nj == 1 ? 512 : 256 : s.nt == 1024 ? 256 : 512;
-  const int64_t all = (p->rows + per - 1) / per;
+  const Shape s = rms_shape(p, backward);
+  const int64_t per = std::max(1, (backward ? kRmsBwdThreads : kRmsFwdThreads) / s.nt), all = (p->rows + per - 1) / per;
+  if (!backward) return (int)std::min<int64_t>(all, 1 << 22);
+  const int64_t most = s.nt == 1024 || s.nj == 3 || all < 4 * 512 ? 256 : 512;
   if (all <= most) return (int)all;
-  const int64_t turns = (all + most - 1) / most;
+  const int64_t turns = (all + most - 1) / most;   // of the one that has most rows: no more workgroups than that takes
   return (int)((all + turns - 1) / turns);
 }
 
-template <typename T, int NT, int NJ, bool WHOLE>
+template <typename T, int NT, int NJ, bool WHOLE, bool STREAM>
 gbmw_status launch_rms(const RmsArgs& a, bool backward, int groups, hipStream_t st) {
   if (!backward) {
-    hipLaunchKernelGGL((k_rms_fwd<T, NT, NJ, WHOLE>), dim3(groups), dim3(std::max(NT, kRmsFwdThreads)), 0, st, a);
+    hipLaunchKernelGGL((k_rms_fwd<T, NT, NJ, WHOLE, STREAM>), dim3(groups), dim3(std::max(NT, kRmsFwdThreads)), 0, st, a);
   } else {
-    const size_t lds = 16 * (size_t)((a.cols + kVec<T> - 1) / kVec<T>) * (kVec<T> / 4);
+    const size_t weight = 16 * (size_t)((a.cols + kVec<T> - 1) / kVec<T>) * (kVec<T> / 4);
+    const size_t lds = std::max(weight, 4 * (size_t)a.cols * std::max(1, kRmsBwdThreads / NT));
     if (lds > 60 * 1024) {
-      const hipError_t e = hipFuncSetAttribute((const void*)&k_rms_bwd<T, NT, NJ, WHOLE>,
+      const hipError_t e = hipFuncSetAttribute((const void*)&k_rms_bwd<T, NT, NJ, WHOLE, STREAM>,
                                                hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
       if (e != hipSuccess) {
         (void)hipGetLastError();
         return fail(GBMW_ERR_DEVICE, "%zu bytes of shared memory: %s", lds, hipGetErrorString(e));
       }
     }
-    hipLaunchKernelGGL((k_rms_bwd<T, NT, NJ, WHOLE>), dim3(groups), dim3(std::max(NT, kRmsBwdThreads)), lds, st, a);
+    hipLaunchKernelGGL((k_rms_bwd<T, NT, NJ, WHOLE, STREAM>), dim3(groups), dim3(std::max(NT, kRmsBwdThreads)), lds, st, a);
   }
   HIP_TRY(hipGetLastError());
   return GBMW_OK;
@@ -360,36 +410,42 @@ gbmw_status launch_rms(const RmsArgs& a, bool backward, int groups, hipStream_t 
 
 template <typename T, int NT, int NJ>
 gbmw_status launch_rms(const RmsArgs& a, bool backward, int groups, hipStream_t st) {
-  return a.cols % kVec<T> ? launch_rms<T, NT, NJ, false>(a, backward, groups, st)
-                          : launch_rms<T, NT, NJ, true>(a, backward, groups, st);
+  if (a.cols % kVec<T>) return launch_rms<T, NT, NJ, false, false>(a, backward, groups, st);
+  return a.stream ? launch_rms<T, NT, NJ, true, true>(a, backward, groups, st) : launch_rms<T, NT, NJ, true, false>(a, backward, groups, st);
+}
+
+template <typename T, int NT>
+gbmw_status launch_rms(const RmsArgs& a, int nj, bool backward, int groups, hipStream_t st) {
+  if (nj == 1) return launch_rms<T, NT, 1>(a, backward, groups, st);
+  if (nj == 2) return launch_rms<T, NT, 2>(a, backward, groups, st);
+  return launch_rms<T, NT, 3>(a, backward, groups, st);
 }
 
 template <typename T>
 gbmw_status launch_rms(const RmsArgs& a, Shape s, bool backward, int groups, hipStream_t st) {
-  if (s.nt == 64) switch (s.nj) {
-    case 1: return launch_rms<T, 64, 1>(a, backward, groups, st);
-    case 2: return launch_rms<T, 64, 2>(a, backward, groups, st);
-    default: return launch_rms<T, 64, 3>(a, backward, groups, st);
-  }
-  if (s.nt == 256) switch (s.nj) {
-    case 1: return launch_rms<T, 256, 1>(a, backward, groups, st);
-    case 2: return launch_rms<T, 256, 2>(a, backward, groups, st);
-    default: return launch_rms<T, 256, 3>(a, backward, groups, st);
-  }
-  if (s.nj == 1) return launch_rms<T, 1024, 1>(a, backward, groups, st);
-  if (s.nj == 2) return launch_rms<T, 1024, 2>(a, backward, groups, st);
+  if (s.nt == 16) return launch_rms<T, 16>(a, s.nj, backward, groups, st);
+  if (s.nt == 64) return launch_rms<T, 64>(a, s.nj, backward, groups, st);
+  if (s.nt == 128) return launch_rms<T, 128, 3>(a, backward, groups, st);
+  if (s.nt == 256) return launch_rms<T, 256>(a, s.nj, backward, groups, st);
+  if (s.nt == 512) return launch_rms<T, 512>(a, s.nj, backward, groups, st);
+  if (s.nj <= 3) return launch_rms<T, 1024>(a, s.nj, backward, groups, st);
   if (s.nj == 4) return launch_rms<T, 1024, 4>(a, backward, groups, st);
   if constexpr (sizeof(T) == 4) return launch_rms<T, 1024, 8>(a, backward, groups, st);
   return fail(GBMW_ERR_UNSUPPORTED, "no kernel for %d columns", a.cols);
 }
 
 gbmw_status launch_rms(const gbmw_rms_norm_problem* p, const RmsArgs& a, bool backward, int groups) {
-  const Shape s = shape_of(p->dtype, p->cols);
+  const Shape s = rms_shape(p, backward);
   hipStream_t st = (hipStream_t)p->stream;
   if (p->dtype == GBMW_F32) return launch_rms<float>(a, s, backward, groups, st);
   if (p->dtype == GBMW_F16) return launch_rms<f16>(a, s, backward, groups, st);
   return launch_rms<bf16>(a, s, backward, groups, st);
 }
+
+// Whether a call that moves `bytes` passes the cache by: where it would not hold the results for who reads them next.
+// With a matrix product that reads them, 4096 x 5120 (168 MB) through the cache and past it: 116 and 120 us, 6144 (252 MB)
+// 167 and 162, 16384 (671 MB) 421 and 413; backward 114 and 119, 166 and 158, 406 and 395.
+bool past_cache(int64_t bytes) { return bytes >= 200000000; }
 
 // An output that is one of its inputs has to have its rows at the same places.
 gbmw_status check_place(const char* out, const void* o, int64_t os, const char* in, const void* i, int64_t is) {
@@ -445,6 +501,8 @@ extern "C" gbmw_status gbmw_rms_norm_forward(const gbmw_rms_norm_problem* p) {
   a.xs = p->x_stride, a.rs = p->residual_stride, a.hs = p->h_stride, a.ys = p->y_stride, a.qs = p->q_stride;
   a.whole_numbers = p->qtype == GBMW_I8, a.group = p->q ? p->group : 0;
   a.groups = a.group ? (p->cols + a.group - 1) / a.group : 1;
+  const int64_t n = p->rows * p->cols;
+  a.stream = past_cache(n * size * (1 + (p->residual != nullptr) + (h != nullptr) + (p->y != nullptr)) + (p->q ? n : 0));
   return launch_rms(p, a, false, rms_groups(p, false));
 }
 
@@ -471,6 +529,7 @@ extern "C" gbmw_status gbmw_rms_norm_backward(const gbmw_rms_norm_problem* p) {
     a.x = p->x, a.dy = p->dy, a.dres = p->dres, a.w = p->weight, a.dx = p->dx, a.wide = p->wdtype == GBMW_F32;
     a.xs = p->x_stride, a.dys = p->dy_stride, a.drs = p->dres_stride, a.dxs = p->dx_stride, a.rstd = p->rstd;
     a.partial = p->dweight ? (float*)p->workspace : nullptr;
+    a.stream = past_cache(p->rows * p->cols * size * (p->dres ? 4 : 3));
     CHECK(launch_rms(p, a, true, groups));
   }
   if (p->dweight) {   // without rows: zeros

@@ -39,6 +39,7 @@ __device__ __forceinline__ void row_sum(float (&s)[N], float* scratch) {
 // Rows of fewer than V columns (TINY: there may be such) have one piece, of n columns.
 template <int V, bool WHOLE, bool TINY>
 struct Span {
+  static constexpr bool kTiny = TINY;
   int c, from, n, row;
   Span() = default;
   __device__ __forceinline__ Span(int piece, int cols) : row(cols) {

@@ -86,7 +86,7 @@ def _check_backward(dx, dw, dy, h, w, rstd, dres=None):
 @pytest.mark.parametrize("types", TYPES, ids=IDS)
 @pytest.mark.parametrize("rows,cols", [(1, 1), (3, 2), (5, 7), (4, 63), (9, 64), (2, 257), (33, 500), (7, 1023), (6, 1283),
                                        (5, 2049), (3, 5120), (2, 8192), (3, 8193), (2, 16385), (1, 32768), (1500, 40),
-                                       (4100, 136), (3000, 1544)])
+                                       (4100, 136), (3000, 1544), (40, 2057), (5000, 392), (9, 12289), (3, 6145)])
 def test_sizes(rows, cols, types):
     import paper_2307_02031_amd as g
     dtype, wdtype = types
