@@ -466,7 +466,8 @@ def _refuse(message: str):
     raise GbmwError(GBMW_ERR_INVALID_ARG, message)
 
 
-# the current stream's handle without an object around it, where torch has it
+# the current device and the current stream's handle without checks and objects around them, where torch has them
+_current_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
 _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", lambda device: torch.cuda.current_stream(device).cuda_stream)
 
 
@@ -496,7 +497,7 @@ def _device_of(name: str, t, types) -> int:
     """The current device, which the first argument has to be on, with one of the types."""
     if not isinstance(t, torch.Tensor) or not t.is_cuda:
         _refuse(f"{name} is not a tensor on the GPU")
-    device = torch.cuda.current_device()
+    device = _current_device()
     if t.get_device() != device:
         _refuse(f"{name} is on {t.device}, device {device} is current")
     if t.dtype not in types:
@@ -609,9 +610,9 @@ def gbmw_attention_workspace(q, k, backward: bool, causal: bool | None = None) -
     return need
 
 
-def _new_like(t):
-    """A dense tensor like t."""
-    return torch.empty_like(t) if t.is_contiguous() else torch.empty(t.shape, dtype=t.dtype, device="cuda")
+def _new_like(t, dtype=None):
+    """A dense tensor like t, of t's type or another."""
+    return torch.empty_like(t, dtype=dtype) if t.is_contiguous() else torch.empty(t.shape, dtype=dtype or t.dtype, device="cuda")
 
 
 @_on_stream
@@ -896,15 +897,15 @@ def gbmw_rms_norm_forward(x, weight=None, eps: float = 1e-5, residual=None, qtyp
     if qtype is not None:
         p.qtype, p.group = _QTYPE.get(qtype, -1), group
         if q is None:
-            q = torch.empty(shape, dtype=qtype, device="cuda")
+            q = _new_like(x, qtype)
             p.q, p.q_stride = q.data_ptr(), p.cols
         else:
             _set_rows(p, "q", q, device, qtype, shape)
-        scale = torch.empty((*shape[:-1], -(-p.cols // group) if group > 0 else 1), dtype=torch.float32, device="cuda")
+        scale = x.new_empty((*shape[:-1], -(-p.cols // group) if group > 0 else 1), dtype=torch.float32)
         p.scale = scale.data_ptr()
     elif q is not None:
         _refuse("q without a qtype")
-    rstd = torch.empty(shape[:-1], dtype=torch.float32, device="cuda")
+    rstd = torch.empty(shape[0] if len(shape) == 2 else shape[:-1], dtype=torch.float32, device="cuda")   # a number is faster
     p.rstd = rstd.data_ptr()
     _check(_lib.gbmw_rms_norm_forward(ct.byref(p)))
     return RmsNorm(y, h, rstd, q, scale)
@@ -974,29 +975,31 @@ def _rotary(call, q, k, freq, positions, len_x, interleaved, factor, q_out, k_ou
     _check_tensor("freq", freq, device, torch.float64, freq.shape)
     if not freq.is_contiguous():
         _refuse("freq is not contiguous")
-    p = gbmw_rotary_problem(_DTYPE[dtype], B, L, Hq, Hk, D, 2 * min(freq.shape[0], 1 << 20), 1 if interleaved else 0, factor,
-                            freq.data_ptr())
+    position = position_stride = length = k_at = k_to = None
+    k_strides = k_to_strides = (0, 0, 0)
     if positions is not None:
         if not isinstance(positions, torch.Tensor) or positions.dim() != 2:
             _refuse("positions is not a tensor [B][L]")
         _check_tensor("positions", positions, device, torch.int32, (B, L))
-        if L > 1 and positions.stride(1) != 1:
+        position_stride, step = positions.stride()
+        if L > 1 and step != 1:
             _refuse("positions of one sample are not next to each other")
-        p.positions, p.position_stride = positions.data_ptr(), positions.stride(0)
+        position = positions.data_ptr()
     if len_x is not None:
-        p.len = _length("len_x", len_x, device, B)
+        length = _length("len_x", len_x, device, B)
     if q_out is None:
         q_out = _new_like(q)
     else:
         _check_tensor("q_out", q_out, device, dtype, shape)
-    _set_array(p, "q", q), _set_array(p, "q_out", q_out)
     if k is not None:
         if k_out is None:
             k_out = _new_like(k)
         else:
             _check_tensor("k_out", k_out, device, dtype, k.shape)
-        _set_array(p, "k", k), _set_array(p, "k_out", k_out)
-    p.stream = _raw_stream(device)
+        k_at, k_to, k_strides, k_to_strides = k.data_ptr(), k_out.data_ptr(), _strides("k", k), _strides("k_out", k_out)
+    p = gbmw_rotary_problem(_DTYPE[dtype], B, L, Hq, Hk, D, 2 * min(freq.shape[0], 1 << 20), 1 if interleaved else 0, factor,
+                            freq.data_ptr(), position, position_stride or 0, length, q.data_ptr(), k_at, _strides("q", q),
+                            k_strides, q_out.data_ptr(), k_to, _strides("q_out", q_out), k_to_strides, _raw_stream(device))
     _check(call(ct.byref(p)))
     return q_out, k_out
 
@@ -1102,7 +1105,7 @@ def gbmw_adamw_step(lst: AdamWList, lr, step, beta1: float = 0.9, beta2: float =
         o.step = step
     if norm is not None:
         o.norm = _scalar_now("norm", norm, torch.float32)
-    _check(_lib.gbmw_adamw_step(lst.handle, ct.byref(o), _raw_stream(torch.cuda.current_device())))
+    _check(_lib.gbmw_adamw_step(lst.handle, ct.byref(o), _raw_stream(_current_device())))
 
 
 def gbmw_adamw_list_destroy(lst: AdamWList) -> None:
