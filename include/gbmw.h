@@ -637,7 +637,8 @@ typedef struct {
   int32_t cols;              /* 1..32768                                             */
   float eps;                 /* >= 0                                                 */
   const void* x;             /* backward: h                                          */
-  int64_t x_stride;          /* elements from row to row, >= cols (inputs: >= 0)     */
+  int64_t x_stride;          /* elements from row to row, >= cols (inputs: >= 0),
+                                below 2^29                                           */
   const void* weight;        /* [cols]                                               */
   float* rstd;               /* [rows]; forward: written, backward: read             */
   const void* residual;      /* from here on forward only                            */

@@ -1010,7 +1010,8 @@ def gbmw_rotary_forward(q, k, freq, positions=None, len_x=None, interleaved: boo
     """q [B][L][Hq][D] and k [B][L][Hk][D] (or None) with the first 2 * len(freq) values of each head turned by their
     rows' positions: float32, float16 or bfloat16 GPU tensors with any strides whose last one is 1.  freq: float64,
     radians per position (gbmw_rotary_frequencies).  positions: int32 [B][L]; by default a row's number.  len_x: int32
-    [B]; rows from there on are left as they were.  q_out, k_out: made here unless given (they may be q and k).
+    [B]; rows from there on are left as they were (in outputs made here: as memory was).  q_out, k_out: made here unless
+    given (they may be q and k).
     stream=: as everywhere.  Not recorded by autograd: gradients come from gbmw_rotary_backward."""
     return _rotary(_lib.gbmw_rotary_forward, q, k, freq, positions, len_x, interleaved, factor, q_out, k_out)
 

@@ -7,7 +7,14 @@ using gbmw_detail::fail;
 namespace gbmw {
 namespace {
 
-// NT threads hold a row in registers, as in layer norm: one pass over x and the residual, and one sum.
+// NT threads hold a row in registers, as in layer norm, a wave four rows where a quarter of it holds one: one pass
+// over x and the residual, one sum, and for 8 bits the largest of a group's threads.
+//
+// Bound by HBM.  16384 x 5120 bf16 with a residual: forward 113 us, 5.9 TB/s; backward 129 to 134, 5.0 to 5.2 TB/s, of
+// which 5 to join the shares of dweight.  8192 x 5120 to 8 bits, a scale for each 128 columns: 54 us, 5.4 TB/s.  4 x 5120:
+// 4.2 us, latency of a load, a sum and a store.  Rows at odd addresses (16-bit values, an odd number a row) cost up to
+// 1.4 times as much (4096 x 10001 102 us, 4096 x 10002 72); rows that leave the registers (16-bit values beyond
+// 16384 columns) spill in the backward pass.
 struct RmsArgs {
   int64_t rows;
   int cols;
@@ -380,7 +387,7 @@ Shape rms_shape(const gbmw_rms_norm_problem* p, bool backward) {
 int rms_groups(const gbmw_rms_norm_problem* p, bool backward) {
   const Shape s = rms_shape(p, backward);
   const int64_t per = std::max(1, (backward ? kRmsBwdThreads : kRmsFwdThreads) / s.nt), all = (p->rows + per - 1) / per;
-  if (!backward) return (int)std::min<int64_t>(all, 1 << 22);
+  if (!backward) return (int)std::min<int64_t>(all, 1 << 21);
   const int64_t most = s.nt == 1024 || s.nj == 3 || all < 4 * 512 ? 256 : 512;
   if (all <= most) return (int)all;
   const int64_t turns = (all + most - 1) / most;   // of the one that has most rows: no more workgroups than that takes

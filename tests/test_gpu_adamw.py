@@ -309,7 +309,7 @@ def test_refusals():
             make(*args, **kw)
         assert err.value.status == g.GBMW_ERR_INVALID_ARG
     lst = make([p, whole[:600]], [q, q], [m, whole[600:]], [v, torch.zeros(600, device="cuda")])     # gradients may be shared
-    for kw in (dict(lr=-1.0), dict(lr=math.nan), dict(beta1=1.0), dict(beta2=-0.1), dict(eps=0.0), dict(scale=0.0), dict(max_norm=0.0), dict(step=0)):
+    for kw in (dict(lr=-1.0), dict(lr=math.nan), dict(beta1=1.0), dict(beta2=-0.1), dict(eps=0.0), dict(eps=1e-40), dict(scale=0.0), dict(max_norm=0.0), dict(step=0)):
         with pytest.raises(g.GbmwError) as err:
             g.gbmw_adamw_step(lst, **{**HOW, "step": 1, **kw})
         assert err.value.status == g.GBMW_ERR_INVALID_ARG
