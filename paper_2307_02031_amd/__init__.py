@@ -932,7 +932,7 @@ def gbmw_rms_norm_backward(dy, h, weight, rstd, dres=None, dx=None, workspace=No
     p.rstd = rstd.data_ptr()
     ref, dweight, keep = ct.byref(p), None, None
     if weight is not None:
-        dweight = torch.empty(p.cols, dtype=weight.dtype, device="cuda")
+        dweight = torch.empty_like(weight)
         p.dweight = dweight.data_ptr()
         keep = _workspace(p, workspace, _lib.gbmw_rms_norm_workspace(ref), device)
     _check(_lib.gbmw_rms_norm_backward(ref))

@@ -27,7 +27,8 @@ struct RmsArgs {
   bool whole_numbers;   // q is GBMW_I8
   int group, groups;    // columns of a scale, or 0; scales of a row
   float *scale, *rstd;
-  float* partial;  // [gridDim.x][share_stride(cols)]
+  float* partial;  // [gridDim.x][share_stride(cols)]; with one workgroup its share is
+  void* dw;        // dweight
   bool stream;     // past the cache
 };
 
@@ -337,7 +338,7 @@ __global__ __launch_bounds__(NT < kRmsBwdThreads ? kRmsBwdThreads : NT) void k_r
     }
     if constexpr (!kAhead) fetch(row + step);
   }
-  if (!a.partial) return;
+  if (!a.dw) return;
   // the shares of the G rows' threads side by side, then added in order
   __syncthreads();
 #pragma unroll
@@ -351,7 +352,9 @@ __global__ __launch_bounds__(NT < kRmsBwdThreads ? kRmsBwdThreads : NT) void k_r
     float sum = columns[col];
 #pragma unroll
     for (int k = 1; k < G; ++k) sum += columns[k * a.cols + col];
-    out[col] = sum;
+    if (gridDim.x > 1) out[col] = sum;
+    else if (a.wide) ((float*)a.dw)[col] = sum;
+    else ((T*)a.dw)[col] = (T)sum;
   }
 }
 
@@ -388,6 +391,7 @@ int rms_groups(const gbmw_rms_norm_problem* p, bool backward) {
   const Shape s = rms_shape(p, backward);
   const int64_t per = std::max(1, (backward ? kRmsBwdThreads : kRmsFwdThreads) / s.nt), all = (p->rows + per - 1) / per;
   if (!backward) return (int)std::min<int64_t>(all, 1 << 21);
+  if (all <= 4) return all > 0;   // four turns take less than joining does (4 us and a launch)
   const int64_t most = s.nt == 1024 || s.nj == 3 || all < 4 * 512 ? 256 : 512;
   if (all <= most) return (int)all;
   const int64_t turns = (all + most - 1) / most;   // of the one that has most rows: no more workgroups than that takes
@@ -535,11 +539,11 @@ extern "C" gbmw_status gbmw_rms_norm_backward(const gbmw_rms_norm_problem* p) {
     a.rows = p->rows, a.cols = p->cols;
     a.x = p->x, a.dy = p->dy, a.dres = p->dres, a.w = p->weight, a.dx = p->dx, a.wide = p->wdtype == GBMW_F32;
     a.xs = p->x_stride, a.dys = p->dy_stride, a.drs = p->dres_stride, a.dxs = p->dx_stride, a.rstd = p->rstd;
-    a.partial = p->dweight ? (float*)p->workspace : nullptr;
+    a.partial = (float*)p->workspace, a.dw = p->dweight;
     a.stream = past_cache(p->rows * p->cols * size * (p->dres ? 4 : 3));
     CHECK(launch_rms(p, a, true, groups));
   }
-  if (p->dweight) {   // without rows: zeros
+  if (p->dweight && groups != 1) {   // without rows: zeros
     const dim3 grid((p->cols + 31) / 32, 1);
     hipStream_t st = (hipStream_t)p->stream;
     const float* part = (const float*)p->workspace;
