@@ -46,11 +46,12 @@ struct AdamArgs {
   const int64_t* step_now;
 };
 
-__host__ __device__ __forceinline__ uint32_t hash(uint32_t x) {
-  x *= 0x9E3779B1u;
+constexpr uint32_t kHashBy = 0x9E3779B1u;
+__host__ __device__ __forceinline__ uint32_t hash_rest(uint32_t x) {
   x = (x ^ (x >> 15)) * 0x85EBCA77u;
   return x ^ (x >> 13);
 }
+__host__ __device__ __forceinline__ uint32_t hash(uint32_t x) { return hash_rest(x * kHashBy); }
 
 __host__ __device__ __forceinline__ uint32_t key_of(uint32_t seed, int64_t step) {
   return seed ? hash(seed + (uint32_t)step * 0x9E3779B9u) : 0;
@@ -215,7 +216,9 @@ __device__ __forceinline__ void values_of(const Few<uint8_t, 8>& code, float (&x
   }
 }
 
-// States in 8 bits: half a wave has a block, a lane eight of its elements.
+// States in 8 bits: half a wave has a block, a lane eight of its elements.  Arithmetic is what bounds this one first,
+// so a product and a sum are one operation, and the root and the quotient are the hardware's, off by one unit of their
+// last place: the states keep three of its 23 bits, the parameter takes a step that is a small part of it.
 template <typename G, typename P>
 __device__ __forceinline__ void run_of_8(const Run& run, const Rates& r) {
   constexpr int N = kRun / kThreads<true>;
@@ -231,21 +234,26 @@ __device__ __forceinline__ void run_of_8(const Run& run, const Rates& r) {
   float m[N], root[N], q[N];
   values_of(mc, m), values_of(vc, root);
   unsigned most_m = 0, most_v = 0;
+  const float m_by = ms * r.b1;
 #pragma unroll
   for (int e = 0; e < N; ++e) {
     const float d = (float)g.v[e] * r.grad, old = root[e] * vs;
-    m[e] = m[e] * ms * r.b1 + d * r.a1;
-    root[e] = __builtin_sqrtf(old * old * r.b2 + d * d * r.a2);
-    q[e] = (float)p.v[e] * keep - m[e] / (root[e] * r.root_c2 + r.eps) * r.lr_c1;
-    most_m = max(most_m, magnitude(m[e])), most_v = max(most_v, magnitude(root[e]));
+    m[e] = __builtin_fmaf(m[e], m_by, d * r.a1);
+    root[e] = __builtin_amdgcn_sqrtf(__builtin_fmaf(old * old, r.b2, d * d * r.a2));
+    const float per = __builtin_amdgcn_rcpf(__builtin_fmaf(root[e], r.root_c2, r.eps));
+    q[e] = __builtin_fmaf((float)p.v[e], keep, -(m[e] * per) * r.lr_c1);
+    // as whole numbers: a NaN is the largest; roots have no sign
+    most_m = max(most_m, magnitude(m[e])), most_v = max(most_v, __builtin_bit_cast(unsigned, root[e]));
   }
   const float new_ms = scale_of(most_of_32(most_m)), new_vs = scale_of(most_of_32(most_v));
   const float by_m = 1.0f / new_ms, by_v = 1.0f / new_vs;
   uint32_t word[N] = {}, low[N] = {};
   if (r.key) {
+    // hash(place ^ key) with its first product taken apart: the lane's eighth of a block, and the three bits below it
+    const uint32_t base = (((run.block + k) * kBlock + lane * N) ^ (r.key & ~7u)) * kHashBy;
 #pragma unroll
     for (int e = 0; e < N; ++e) {
-      word[e] = hash(((run.block + k) * kBlock + lane * N + e) ^ r.key);
+      word[e] = hash_rest(base + (e ^ (r.key & 7u)) * kHashBy);
       low[e] = word[e] << 16 | 0x8000;
       word[e] = (word[e] & 0xffff0000u) | 0x8000;
     }
