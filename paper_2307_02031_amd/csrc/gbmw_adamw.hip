@@ -9,11 +9,12 @@ using gbmw_detail::fail;
 namespace gbmw {
 namespace {
 
-// Bound by HBM: every array is read and written once, and arithmetic (about 50 and 90 vector operations an element)
-// stays below that.  A workgroup has 1024 elements and ends: the more of them there are, the closer together lies what
-// the chip has in flight, and the better memory takes it.  197M parameters, bf16 gradients and copies: states in 32 bits
-// 930 us, 5.9 TB/s; 2048 workgroups that walk runs of 16384 elements 1210, with loads and stores through the cache 1361.
-// States in 8 bits 562 us, 5.6 TB/s (667 and 776).
+// Bound by HBM: every array is read and written once, and arithmetic (about 60 vector operations an element) stays
+// below that.  A workgroup has 1024 elements and ends: the more of them there are, the closer together lies what the chip
+// has in flight, and the better memory takes it.  197M parameters, bf16 gradients and copies: states in 32 bits 918 us,
+// 6.0 TB/s; 2048 workgroups that walk runs of 16384 elements 1210, with loads and stores through the cache 1361.  States
+// in 8 bits 557 us, 5.7 TB/s (667 and 776).  Runs dealt to the dies one by one: 906 and 566 us, and 16M parameters with
+// fp32 gradients and no copies 80 us, which take 76 in lots.
 constexpr int kBlock = 256;         // elements that share a scale
 constexpr int kRun = 1024;          // elements of a workgroup
 constexpr int kMostRuns = 1 << 23;  // of a launch
@@ -296,7 +297,12 @@ template <bool BITS8>
 __global__ __launch_bounds__(kThreads<BITS8>) void k_adamw(const Run* runs, AdamArgs a) {
   Rates r = a.r;
   if (!rates_now(a, r)) return;
-  const Run run = runs[blockIdx.x];
+  // workgroups go to the eight dies in turn; lots of 128 runs are one die's, whose cache then holds whole lines of scales
+  // and descriptors
+  constexpr unsigned kLot = 7, kAll = 8u << kLot;
+  unsigned id = blockIdx.x;
+  if ((id | (kAll - 1)) < gridDim.x) id = (id & ~(kAll - 1)) | ((id & 7) << kLot) | ((id >> 3) & ((1u << kLot) - 1));
+  const Run run = runs[id];
   if (run.grad_dtype == GBMW_F32) run_of<BITS8, float>(run, r);
   else if (run.grad_dtype == GBMW_F16) run_of<BITS8, f16>(run, r);
   else run_of<BITS8, bf16>(run, r);
