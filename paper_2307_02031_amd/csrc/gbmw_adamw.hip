@@ -13,8 +13,9 @@ namespace {
 // below that.  A workgroup has 1024 elements and ends: the more of them there are, the closer together lies what the chip
 // has in flight, and the better memory takes it.  197M parameters, bf16 gradients and copies: states in 32 bits 918 us,
 // 6.0 TB/s; 2048 workgroups that walk runs of 16384 elements 1210, with loads and stores through the cache 1361.  States
-// in 8 bits 557 us, 5.7 TB/s (667 and 776).  Runs dealt to the dies one by one: 906 and 566 us, and 16M parameters with
-// fp32 gradients and no copies 80 us, which take 76 in lots.
+// in 8 bits 527 us, 6.0 TB/s (with eight elements of a lane next to each other, whose stores are half lines, 557).
+// Runs dealt to the dies one by one: 906 us in 32 bits, 1 % more in 8, and 16M parameters with fp32 gradients and no
+// copies 80 us, which take 76 in lots.
 constexpr int kBlock = 256;         // elements that share a scale
 constexpr int kRun = 1024;          // elements of a workgroup
 constexpr int kMostRuns = 1 << 23;  // of a launch
@@ -186,97 +187,106 @@ __device__ __forceinline__ float scale_of(float most) {
   return s < 0x1p-126f ? 0x1p-126f : s;
 }
 
-// Eight values in 8 bits.  By the hash the conversion adds `random` (its upper 20 bits, below the last digit that is
+// Four values in 8 bits.  By the hash the conversion adds `random` (its upper 20 bits, below the last digit that is
 // kept) and cuts off: sixteen bits of the hash, and a half behind them.
-__device__ __forceinline__ void codes_of(const float (&x)[8], uint32_t key, const uint32_t (&random)[8], Few<uint32_t, 2>& code) {
-#pragma unroll
-  for (int w = 0; w < 2; ++w) {
-    int c = 0;
-    const float* y = x + 4 * w;
-    if (key) {
-      c = __builtin_amdgcn_cvt_sr_fp8_f32(y[0], random[4 * w], c, 0);
-      c = __builtin_amdgcn_cvt_sr_fp8_f32(y[1], random[4 * w + 1], c, 1);
-      c = __builtin_amdgcn_cvt_sr_fp8_f32(y[2], random[4 * w + 2], c, 2);
-      c = __builtin_amdgcn_cvt_sr_fp8_f32(y[3], random[4 * w + 3], c, 3);
-    } else {
-      c = __builtin_amdgcn_cvt_pk_fp8_f32(y[0], y[1], c, false);
-      c = __builtin_amdgcn_cvt_pk_fp8_f32(y[2], y[3], c, true);
-    }
-    code.v[w] = (uint32_t)c;
+__device__ __forceinline__ uint32_t codes_of(const float* x, bool at_random, const uint32_t* random) {
+  int c = 0;
+  if (at_random) {
+    c = __builtin_amdgcn_cvt_sr_fp8_f32(x[0], random[0], c, 0);
+    c = __builtin_amdgcn_cvt_sr_fp8_f32(x[1], random[1], c, 1);
+    c = __builtin_amdgcn_cvt_sr_fp8_f32(x[2], random[2], c, 2);
+    c = __builtin_amdgcn_cvt_sr_fp8_f32(x[3], random[3], c, 3);
+  } else {
+    c = __builtin_amdgcn_cvt_pk_fp8_f32(x[0], x[1], c, false);
+    c = __builtin_amdgcn_cvt_pk_fp8_f32(x[2], x[3], c, true);
   }
+  return (uint32_t)c;
 }
 
-__device__ __forceinline__ void values_of(const Few<uint8_t, 8>& code, float (&x)[8]) {
-  Few<uint32_t, 2> c;
-  __builtin_memcpy(&c, &code, 8);
-#pragma unroll
-  for (int w = 0; w < 2; ++w) {
-    typedef float f32x2 __attribute__((ext_vector_type(2)));
-    const f32x2 lo = __builtin_amdgcn_cvt_pk_f32_fp8((int)c.v[w], false), hi = __builtin_amdgcn_cvt_pk_f32_fp8((int)c.v[w], true);
-    x[4 * w] = lo[0], x[4 * w + 1] = lo[1], x[4 * w + 2] = hi[0], x[4 * w + 3] = hi[1];
-  }
+__device__ __forceinline__ Few<uint8_t, 4> bytes_of(uint32_t c) {
+  Few<uint8_t, 4> b;
+  __builtin_memcpy(&b, &c, 4);
+  return b;
+}
+__device__ __forceinline__ void values_of(const Few<uint8_t, 4>& code, float* x) {
+  typedef float f32x2 __attribute__((ext_vector_type(2)));
+  const int c = __builtin_bit_cast(int, code);
+  const f32x2 lo = __builtin_amdgcn_cvt_pk_f32_fp8(c, false), hi = __builtin_amdgcn_cvt_pk_f32_fp8(c, true);
+  x[0] = lo[0], x[1] = lo[1], x[2] = hi[0], x[3] = hi[1];
 }
 
-// States in 8 bits: half a wave has a block, a lane eight of its elements.  Arithmetic is what bounds this one first,
-// so a product and a sum are one operation, and the root and the quotient are the hardware's, off by one unit of their
-// last place: the states keep three of its 23 bits, the parameter takes a step that is a small part of it.
+// States in 8 bits: half a wave has a block, a lane four elements of each half of it, so that every store of the wave is
+// whole lines.  Arithmetic comes near to binding this one, so a product and a sum are one operation, and the root and the
+// quotient are the hardware's, off by one unit of their last place: the states keep three of its 23 bits, the parameter
+// takes a step that is a small part of it.
 template <typename G, typename P>
 __device__ __forceinline__ void run_of_8(const Run& run, const Rates& r) {
-  constexpr int N = kRun / kThreads<true>;
-  static_assert(N * 32 == kBlock, "");
+  constexpr int N = 4, U = 2, kApart = kBlock / U;
+  static_assert(kRun == kThreads<true> * N * U && kApart == 32 * N, "");
   const float keep = (float)(1.0 - r.lr * (double)run.decay);
   const int k = threadIdx.x / 32, lane = threadIdx.x % 32;
   if (k * kBlock >= run.n) return;
-  const int i = k * kBlock + lane * N, n = run.n - i;   // 0 or less behind the last element
-  const Few<G, N> g = load<G, N>(run.grad, i, n);
-  const Few<P, N> p = load<P, N>(run.param, i, n);
-  const Few<uint8_t, N> mc = load<uint8_t, N>(run.m, i, n), vc = load<uint8_t, N>(run.v, i, n);
-  const float ms = run.m_scale[k], vs = run.v_scale[k];
-  float m[N], root[N], q[N];
-  values_of(mc, m), values_of(vc, root);
-  unsigned most_m = 0, most_v = 0;
-  const float m_by = ms * r.b1;
+  const int i = k * kBlock + lane * N;
+  Few<G, N> g[U];
+  Few<P, N> p[U];
+  Few<uint8_t, N> mc[U], vc[U];
 #pragma unroll
-  for (int e = 0; e < N; ++e) {
-    const float d = (float)g.v[e] * r.grad, old = root[e] * vs;
-    m[e] = __builtin_fmaf(m[e], m_by, d * r.a1);
-    root[e] = __builtin_amdgcn_sqrtf(__builtin_fmaf(old * old, r.b2, d * d * r.a2));
-    const float per = __builtin_amdgcn_rcpf(__builtin_fmaf(root[e], r.root_c2, r.eps));
-    q[e] = __builtin_fmaf((float)p.v[e], keep, -(m[e] * per) * r.lr_c1);
-    // as whole numbers: a NaN is the largest; roots have no sign
-    most_m = max(most_m, magnitude(m[e])), most_v = max(most_v, __builtin_bit_cast(unsigned, root[e]));
+  for (int u = 0; u < U; ++u) {
+    const int at = i + u * kApart, n = run.n - at;   // 0 or less behind the last element
+    g[u] = load<G, N>(run.grad, at, n), p[u] = load<P, N>(run.param, at, n);
+    mc[u] = load<uint8_t, N>(run.m, at, n), vc[u] = load<uint8_t, N>(run.v, at, n);
+  }
+  const float ms = run.m_scale[k], vs = run.v_scale[k], m_by = ms * r.b1;
+  float m[U * N], root[U * N], q[U][N];
+  unsigned most_m = 0, most_v = 0;
+#pragma unroll
+  for (int u = 0; u < U; ++u) {
+    values_of(mc[u], m + u * N), values_of(vc[u], root + u * N);
+#pragma unroll
+    for (int e = 0; e < N; ++e) {
+      float &me = m[u * N + e], &ve = root[u * N + e];
+      const float d = (float)g[u].v[e] * r.grad, old = ve * vs;
+      me = __builtin_fmaf(me, m_by, d * r.a1);
+      ve = __builtin_amdgcn_sqrtf(__builtin_fmaf(old * old, r.b2, d * d * r.a2));
+      const float per = __builtin_amdgcn_rcpf(__builtin_fmaf(ve, r.root_c2, r.eps));
+      q[u][e] = __builtin_fmaf((float)p[u].v[e], keep, -(me * per) * r.lr_c1);
+      // as whole numbers: a NaN is the largest; roots have no sign
+      most_m = max(most_m, magnitude(me)), most_v = max(most_v, __builtin_bit_cast(unsigned, ve));
+    }
   }
   const float new_ms = scale_of(most_of_32(most_m)), new_vs = scale_of(most_of_32(most_v));
   const float by_m = 1.0f / new_ms, by_v = 1.0f / new_vs;
-  uint32_t word[N] = {}, low[N] = {};
+  uint32_t high[U * N] = {}, low[U * N] = {};
   if (r.key) {
-    // hash(place ^ key) with its first product taken apart: the lane's eighth of a block, and the three bits below it
-    const uint32_t base = (((run.block + k) * kBlock + lane * N) ^ (r.key & ~7u)) * kHashBy;
 #pragma unroll
-    for (int e = 0; e < N; ++e) {
-      word[e] = hash_rest(base + (e ^ (r.key & 7u)) * kHashBy);
-      low[e] = word[e] << 16 | 0x8000;
-      word[e] = (word[e] & 0xffff0000u) | 0x8000;
+    for (int u = 0; u < U; ++u) {
+      // hash(place ^ key) with its first product taken apart: the place of the lane's four, and the two bits below it
+      const uint32_t base = (((run.block + k) * kBlock + u * kApart + lane * N) ^ (r.key & ~3u)) * kHashBy;
+#pragma unroll
+      for (int e = 0; e < N; ++e) {
+        const uint32_t word = hash_rest(base + (e ^ (r.key & 3u)) * kHashBy);
+        high[u * N + e] = (word & 0xffff0000u) | 0x8000, low[u * N + e] = word << 16 | 0x8000;
+      }
     }
   }
 #pragma unroll
-  for (int e = 0; e < N; ++e) {
+  for (int e = 0; e < U * N; ++e) {
     m[e] = __builtin_amdgcn_fmed3f(m[e] * by_m, -448.0f, 448.0f);
     root[e] = root[e] > 0.0f ? __builtin_amdgcn_fmed3f(root[e] * by_v, 0x1p-9f, 448.0f) : 0.0f;
   }
-  Few<uint32_t, 2> mw, vw;
-  codes_of(m, r.key, word, mw), codes_of(root, r.key, low, vw);
-  if (n <= 0) return;
-  Few<uint8_t, N> out;
-  __builtin_memcpy(&out, &mw, N);
-  store(run.m, i, out, n);
-  __builtin_memcpy(&out, &vw, N);
-  store(run.v, i, out, n);
-  Few<P, N> to;
 #pragma unroll
-  for (int e = 0; e < N; ++e) to.v[e] = (P)q[e];
-  store(run.param, i, to, n);
-  store_copy(run, i, q, n);
+  for (int u = 0; u < U; ++u) {
+    const int at = i + u * kApart, n = run.n - at;
+    const uint32_t mw = codes_of(m + u * N, r.key, high + u * N), vw = codes_of(root + u * N, r.key, low + u * N);
+    if (n <= 0) continue;
+    store(run.m, at, bytes_of(mw), n);
+    store(run.v, at, bytes_of(vw), n);
+    Few<P, N> to;
+#pragma unroll
+    for (int e = 0; e < N; ++e) to.v[e] = (P)q[u][e];
+    store(run.param, at, to, n);
+    store_copy(run, at, q[u], n);
+  }
   if (lane == 0) run.m_scale[k] = new_ms, run.v_scale[k] = new_vs;
 }
 
