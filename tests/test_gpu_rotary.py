@@ -179,7 +179,7 @@ def test_the_binding_refuses():
     for args, kw in [((q[0], k, freq), {}), ((q, k[:, :2], freq), {}), ((q, k.half(), freq), {}), ((q, k, freq.float()), {}),
                      ((q, k, torch.zeros(5, dtype=torch.float64, device="cuda")), {}), ((q, k, freq.cpu()), {}),
                      ((q, k, freq), dict(positions=pos.long())), ((q, k, freq), dict(positions=pos[:1])),
-                     ((q, k, freq), dict(positions=pos.t().contiguous().t())), ((q, k, freq), dict(len_x=pos[0])),
+                     ((q, k, freq), dict(positions=pos.t().contiguous().t())), ((q, k, freq), dict(len_x=pos[0])), ((q, k, freq), dict(factor=1e39)), ((q, k, freq), dict(factor=math.nan)),
                      ((q, k, freq), dict(q_out=k)), ((q, None, freq), dict(k_out=k)), ((q, k, freq), dict(factor=math.inf)),
                      ((q, k, freq), dict(q_out=q[:1].expand(2, 3, 4, 8))), ((q.transpose(1, 3).contiguous().transpose(1, 3), k, freq), {})]:
         with pytest.raises(g.GbmwError) as e:
