@@ -425,22 +425,26 @@ gbmw_status launch_rms(const RmsArgs& a, bool backward, int groups, hipStream_t 
   return a.stream ? launch_rms<T, NT, NJ, true, true>(a, backward, groups, st) : launch_rms<T, NT, NJ, true, false>(a, backward, groups, st);
 }
 
-template <typename T, int NT>
-gbmw_status launch_rms(const RmsArgs& a, int nj, bool backward, int groups, hipStream_t st) {
-  if (nj == 1) return launch_rms<T, NT, 1>(a, backward, groups, st);
-  if (nj == 2) return launch_rms<T, NT, 2>(a, backward, groups, st);
-  return launch_rms<T, NT, 3>(a, backward, groups, st);
-}
-
 template <typename T>
 gbmw_status launch_rms(const RmsArgs& a, Shape s, bool backward, int groups, hipStream_t st) {
-  if (s.nt == 16) return launch_rms<T, 16>(a, s.nj, backward, groups, st);
-  if (s.nt == 64) return launch_rms<T, 64>(a, s.nj, backward, groups, st);
-  if (s.nt == 128) return launch_rms<T, 128, 3>(a, backward, groups, st);
-  if (s.nt == 256) return launch_rms<T, 256>(a, s.nj, backward, groups, st);
-  if (s.nt == 512) return launch_rms<T, 512>(a, s.nj, backward, groups, st);
-  if (s.nj <= 3) return launch_rms<T, 1024>(a, s.nj, backward, groups, st);
-  if (s.nj == 4) return launch_rms<T, 1024, 4>(a, backward, groups, st);
+  switch (s.nt * 10 + s.nj) {
+    case 161: return launch_rms<T, 16, 1>(a, backward, groups, st);
+    case 162: return launch_rms<T, 16, 2>(a, backward, groups, st);
+    case 163: return launch_rms<T, 16, 3>(a, backward, groups, st);
+    case 641: return launch_rms<T, 64, 1>(a, backward, groups, st);
+    case 642: return launch_rms<T, 64, 2>(a, backward, groups, st);
+    case 643: return launch_rms<T, 64, 3>(a, backward, groups, st);
+    case 1283: return launch_rms<T, 128, 3>(a, backward, groups, st);
+    case 2561: return launch_rms<T, 256, 1>(a, backward, groups, st);
+    case 2562: return launch_rms<T, 256, 2>(a, backward, groups, st);
+    case 2563: return launch_rms<T, 256, 3>(a, backward, groups, st);
+    case 5122: return launch_rms<T, 512, 2>(a, backward, groups, st);
+    case 5123: return launch_rms<T, 512, 3>(a, backward, groups, st);
+    case 10242: return launch_rms<T, 1024, 2>(a, backward, groups, st);
+    case 10243: return launch_rms<T, 1024, 3>(a, backward, groups, st);
+    case 10244: return launch_rms<T, 1024, 4>(a, backward, groups, st);
+    default: break;
+  }
   if constexpr (sizeof(T) == 4) return launch_rms<T, 1024, 8>(a, backward, groups, st);
   return fail(GBMW_ERR_UNSUPPORTED, "no kernel for %d columns", a.cols);
 }
