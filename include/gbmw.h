@@ -659,8 +659,8 @@ typedef struct {
   void* dx;
   int64_t dx_stride;
   void* dweight;             /* [cols]                                               */
-  void* workspace;           /* at least gbmw_rms_norm_workspace() bytes, 16-byte    */
-  int64_t workspace_bytes;   /* aligned; backward with dweight only                  */
+  void* workspace;           /* at least gbmw_rms_norm_workspace() bytes (may be 0), */
+  int64_t workspace_bytes;   /* 16-byte aligned; backward with dweight only          */
   void* stream;
 } gbmw_rms_norm_problem;
 

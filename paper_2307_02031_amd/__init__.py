@@ -863,7 +863,7 @@ def _set_rows(p, name: str, t, device: int, dtype, shape) -> None:
 
 @_on_stream
 def gbmw_rms_norm_workspace(x, weight=None) -> int:
-    """Bytes of workspace of the backward call."""
+    """Bytes of workspace of the backward call (0 for a few rows)."""
     n = _lib.gbmw_rms_norm_workspace(ct.byref(_rms_problem(x, weight)[0]))
     if n < 0:
         raise GbmwError(GBMW_ERR_INVALID_ARG, gbmw_last_error())
@@ -940,7 +940,8 @@ def gbmw_rms_norm_backward(dy, h, weight, rstd, dres=None, dx=None, workspace=No
     if weight is not None:
         dweight = torch.empty_like(weight)
         p.dweight = dweight.data_ptr()
-        keep = _workspace(p, workspace, _lib.gbmw_rms_norm_workspace(ref), device)
+        need = _lib.gbmw_rms_norm_workspace(ref)
+        keep = _workspace(p, workspace, need, device) if need else None
     _check(_lib.gbmw_rms_norm_backward(ref))
     return dx, dweight
 

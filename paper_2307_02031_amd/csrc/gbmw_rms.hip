@@ -27,7 +27,7 @@ struct RmsArgs {
   bool whole_numbers;   // q is GBMW_I8
   int group, groups;    // columns of a scale, or 0; scales of a row
   float *scale, *rstd;
-  float* partial;  // [gridDim.x][share_stride(cols)]; with one workgroup its share is
+  float* partial;  // [gridDim.x][share_stride(cols)], with more than one workgroup
   void* dw;        // dweight
   bool stream;     // past the cache
 };
@@ -398,6 +398,11 @@ int rms_groups(const gbmw_rms_norm_problem* p, bool backward) {
   return (int)((all + turns - 1) / turns);
 }
 
+// For the workgroups' shares of dweight; one writes it itself.
+int64_t rms_workspace(const gbmw_rms_norm_problem* p, int groups) {
+  return groups > 1 ? (int64_t)groups * share_stride(p->cols) * 4 : 0;
+}
+
 template <typename T, int NT, int NJ, bool WHOLE, bool STREAM>
 gbmw_status launch_rms(const RmsArgs& a, bool backward, int groups, hipStream_t st) {
   if (!backward) {
@@ -476,7 +481,7 @@ using namespace gbmw;
 extern "C" int64_t gbmw_rms_norm_workspace(const gbmw_rms_norm_problem* p) {
   gbmw_detail::clear_error();
   if (check_rms(p) != GBMW_OK) return -1;
-  return (int64_t)rms_groups(p, true) * share_stride(p->cols) * 4;
+  return rms_workspace(p, rms_groups(p, true));
 }
 
 extern "C" gbmw_status gbmw_rms_norm_forward(const gbmw_rms_norm_problem* p) {
@@ -536,8 +541,8 @@ extern "C" gbmw_status gbmw_rms_norm_backward(const gbmw_rms_norm_problem* p) {
     if (p->weight) CHECK(check_array("weight", p->weight, wsize, 1, 0));
     CHECK(check_place("dx", p->dx, p->dx_stride, "dy", p->dy, p->dy_stride));
     CHECK(check_place("dx", p->dx, p->dx_stride, "dres", p->dres, p->dres_stride));
-    const int64_t need = (int64_t)groups * share_stride(p->cols) * 4;
-    if (p->dweight && (!p->workspace || p->workspace_bytes < need || (uintptr_t)p->workspace % 16))
+    const int64_t need = rms_workspace(p, groups);
+    if (p->dweight && need && (!p->workspace || p->workspace_bytes < need || (uintptr_t)p->workspace % 16))
       return fail(GBMW_ERR_INVALID_ARG, "workspace of %lld bytes, 16-byte aligned, is needed", (long long)need);
     RmsArgs a{};
     a.rows = p->rows, a.cols = p->cols;

@@ -229,7 +229,8 @@ def test_same_bits_on_streams_and_in_a_graph():
 
 def test_workspace_of_just_the_bytes_asked_for():
     import paper_2307_02031_amd as g
-    for rows, cols in ((1, 3), (700, 1280), (40, 9001)):
+    assert g.gbmw_rms_norm_workspace(torch.empty(2, 3, device="cuda")) == 0     # one workgroup writes dweight itself
+    for rows, cols in ((200, 3), (700, 1280), (40, 9001)):
         x, dy = (_normal(rows, cols, dtype=torch.float16, seed=50 + i) for i in range(2))
         w = _normal(cols, dtype=torch.float16, seed=52)
         r = g.gbmw_rms_norm_forward(x, w)

@@ -14,7 +14,7 @@ def _rms(g, **over):
     p = g.gbmw_rms_norm_problem()
     for i, n in enumerate(("x", "residual", "weight", "h", "y", "q", "scale", "rstd", "dy", "dres", "dx", "dweight", "workspace")):
         setattr(p, n, (i + 1) << 20)
-    p.dtype, p.wdtype, p.rows, p.cols, p.eps, p.qtype, p.group = g.GBMW_BF16, g.GBMW_F32, 10, 64, 1e-5, g.GBMW_E4M3, 32
+    p.dtype, p.wdtype, p.rows, p.cols, p.eps, p.qtype, p.group = g.GBMW_BF16, g.GBMW_F32, 1000, 64, 1e-5, g.GBMW_E4M3, 32
     for n in ("x", "residual", "h", "y", "q", "dy", "dres", "dx"):
         setattr(p, n + "_stride", 64)
     p.workspace_bytes = 1 << 20
