@@ -855,10 +855,10 @@ def _rms_problem(x, weight):
     return p, device
 
 
-def _set_rows(p, name: str, t, device: int, dtype, shape) -> None:
+def _rows(name: str, t, device: int, dtype, shape) -> tuple:
+    """Where t's rows are, and how far apart."""
     _check_tensor(name, t, device, dtype, shape)
-    setattr(p, name, t.data_ptr())
-    setattr(p, name + "_stride", _row_stride(name, t))
+    return t.data_ptr(), _row_stride(name, t)
 
 
 @_on_stream
@@ -884,17 +884,17 @@ def gbmw_rms_norm_forward(x, weight=None, eps: float = 1e-5, residual=None, qtyp
     shape, dtype = x.shape, x.dtype
     p.eps = eps
     if y is not None:
-        _set_rows(p, "y", y, device, dtype, shape)
+        p.y, p.y_stride = _rows("y", y, device, dtype, shape)
     elif want_y:
         y = _new_like(x)
         p.y, p.y_stride = y.data_ptr(), p.cols
     if residual is not None:
-        _set_rows(p, "residual", residual, device, dtype, shape)
+        p.residual, p.residual_stride = _rows("residual", residual, device, dtype, shape)
         if h is None:
             h = _new_like(x)
             p.h, p.h_stride = h.data_ptr(), p.cols
         else:
-            _set_rows(p, "h", h, device, dtype, shape)
+            p.h, p.h_stride = _rows("h", h, device, dtype, shape)
     elif h is not None:
         _refuse("h without a residual is x")
     else:
@@ -906,7 +906,7 @@ def gbmw_rms_norm_forward(x, weight=None, eps: float = 1e-5, residual=None, qtyp
             q = _new_like(x, qtype)
             p.q, p.q_stride = q.data_ptr(), p.cols
         else:
-            _set_rows(p, "q", q, device, qtype, shape)
+            p.q, p.q_stride = _rows("q", q, device, qtype, shape)
         scale = x.new_empty((*shape[:-1], -(-p.cols // group) if group > 0 else 1), dtype=torch.float32)
         p.scale = scale.data_ptr()
     elif q is not None:
@@ -924,14 +924,14 @@ def gbmw_rms_norm_backward(dy, h, weight, rstd, dres=None, dx=None, workspace=No
     dres).  stream=: as everywhere."""
     p, device = _rms_problem(h, weight)
     shape, dtype = h.shape, h.dtype
-    _set_rows(p, "dy", dy, device, dtype, shape)
+    p.dy, p.dy_stride = _rows("dy", dy, device, dtype, shape)
     if dres is not None:
-        _set_rows(p, "dres", dres, device, dtype, shape)
+        p.dres, p.dres_stride = _rows("dres", dres, device, dtype, shape)
     if dx is None:
         dx = _new_like(h)
         p.dx, p.dx_stride = dx.data_ptr(), p.cols
     else:
-        _set_rows(p, "dx", dx, device, dtype, shape)
+        p.dx, p.dx_stride = _rows("dx", dx, device, dtype, shape)
     _check_tensor("rstd", rstd, device, torch.float32, shape[:-1])
     if not rstd.is_contiguous():
         _refuse("rstd is not contiguous")
