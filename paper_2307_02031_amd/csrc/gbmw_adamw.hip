@@ -66,7 +66,7 @@ __host__ __device__ __forceinline__ double power(double x, int64_t n) {
   return p;
 }
 
-// What the device knows alone is read here.  False: the step is left out.
+// What the device knows alone is read here, with the elements on their way.  False: the step is left out.
 __device__ __forceinline__ bool rates_now(const AdamArgs& a, Rates& r) {
   if (a.norm) {
     const double norm = (double)*a.norm;
@@ -146,14 +146,16 @@ __device__ __forceinline__ void store_copy(const Run& run, int i, const float (&
 
 // States in 32 bits: a thread has four elements.
 template <typename G, typename P>
-__device__ __forceinline__ void run_of_32(const Run& run, const Rates& r) {
+__device__ __forceinline__ void run_of_32(const Run& run, const AdamArgs& a) {
   constexpr int N = kRun / kThreads<false>;
-  const float keep = (float)(1.0 - r.lr * (double)run.decay);
   const int i = threadIdx.x * N, n = run.n - i;   // 0 or less behind the last element
   if (n <= 0) return;
   const Few<G, N> g = load<G, N>(run.grad, i, n);
   Few<P, N> p = load<P, N>(run.param, i, n);
   Few<float, N> m = load<float, N>(run.m, i, n), v = load<float, N>(run.v, i, n);
+  Rates r = a.r;
+  if (!rates_now(a, r)) return;
+  const float keep = (float)(1.0 - r.lr * (double)run.decay);
   float q[N];
 #pragma unroll
   for (int e = 0; e < N; ++e) {
@@ -220,10 +222,9 @@ __device__ __forceinline__ void values_of(const Few<uint8_t, 4>& code, float* x)
 // quotient are the hardware's, off by one unit of their last place: the states keep three of its 23 bits, the parameter
 // takes a step that is a small part of it.
 template <typename G, typename P>
-__device__ __forceinline__ void run_of_8(const Run& run, const Rates& r) {
+__device__ __forceinline__ void run_of_8(const Run& run, const AdamArgs& a) {
   constexpr int N = 4, U = 2, kApart = kBlock / U;
   static_assert(kRun == kThreads<true> * N * U && kApart == 32 * N, "");
-  const float keep = (float)(1.0 - r.lr * (double)run.decay);
   const int k = threadIdx.x / 32, lane = threadIdx.x % 32;
   if (k * kBlock >= run.n) return;
   const int i = k * kBlock + lane * N;
@@ -236,7 +237,10 @@ __device__ __forceinline__ void run_of_8(const Run& run, const Rates& r) {
     g[u] = load<G, N>(run.grad, at, n), p[u] = load<P, N>(run.param, at, n);
     mc[u] = load<uint8_t, N>(run.m, at, n), vc[u] = load<uint8_t, N>(run.v, at, n);
   }
-  const float ms = run.m_scale[k], vs = run.v_scale[k], m_by = ms * r.b1;
+  const float ms = run.m_scale[k], vs = run.v_scale[k];
+  Rates r = a.r;
+  if (!rates_now(a, r)) return;
+  const float keep = (float)(1.0 - r.lr * (double)run.decay), m_by = ms * r.b1;
   float m[U * N], root[U * N], q[U][N];
   unsigned most_m = 0, most_v = 0;
 #pragma unroll
@@ -291,31 +295,29 @@ __device__ __forceinline__ void run_of_8(const Run& run, const Rates& r) {
 }
 
 template <bool BITS8, typename G, typename P>
-__device__ __forceinline__ void run_of(const Run& run, const Rates& r) {
-  if constexpr (BITS8) run_of_8<G, P>(run, r);
-  else run_of_32<G, P>(run, r);
+__device__ __forceinline__ void run_of(const Run& run, const AdamArgs& a) {
+  if constexpr (BITS8) run_of_8<G, P>(run, a);
+  else run_of_32<G, P>(run, a);
 }
 
 template <bool BITS8, typename G>
-__device__ __forceinline__ void run_of(const Run& run, const Rates& r) {
-  if (run.dtype == GBMW_F32) run_of<BITS8, G, float>(run, r);
-  else if (run.dtype == GBMW_F16) run_of<BITS8, G, f16>(run, r);
-  else run_of<BITS8, G, bf16>(run, r);
+__device__ __forceinline__ void run_of(const Run& run, const AdamArgs& a) {
+  if (run.dtype == GBMW_F32) run_of<BITS8, G, float>(run, a);
+  else if (run.dtype == GBMW_F16) run_of<BITS8, G, f16>(run, a);
+  else run_of<BITS8, G, bf16>(run, a);
 }
 
 template <bool BITS8>
 __global__ __launch_bounds__(kThreads<BITS8>) void k_adamw(const Run* runs, AdamArgs a) {
-  Rates r = a.r;
-  if (!rates_now(a, r)) return;
   // workgroups go to the eight dies in turn; lots of 128 runs are one die's, whose cache then holds whole lines of scales
   // and descriptors
   constexpr unsigned kLot = 7, kAll = 8u << kLot;
   unsigned id = blockIdx.x;
   if ((id | (kAll - 1)) < gridDim.x) id = (id & ~(kAll - 1)) | ((id & 7) << kLot) | ((id >> 3) & ((1u << kLot) - 1));
   const Run run = runs[id];
-  if (run.grad_dtype == GBMW_F32) run_of<BITS8, float>(run, r);
-  else if (run.grad_dtype == GBMW_F16) run_of<BITS8, f16>(run, r);
-  else run_of<BITS8, bf16>(run, r);
+  if (run.grad_dtype == GBMW_F32) run_of<BITS8, float>(run, a);
+  else if (run.grad_dtype == GBMW_F16) run_of<BITS8, f16>(run, a);
+  else run_of<BITS8, bf16>(run, a);
 }
 
 // ---- host ---------------------------------------------------------------------------------
