@@ -660,7 +660,8 @@ typedef struct {
   int64_t dx_stride;
   void* dweight;             /* [cols]                                               */
   void* workspace;           /* at least gbmw_rms_norm_workspace() bytes (may be 0), */
-  int64_t workspace_bytes;   /* 16-byte aligned; backward with dweight only          */
+  int64_t workspace_bytes;   /* 16-byte aligned; backward with dweight only; may be
+                                used by one call at a time                           */
   void* stream;
 } gbmw_rms_norm_problem;
 

@@ -13,7 +13,7 @@ namespace {
 // below that.  A workgroup has 1024 elements and ends: the more of them there are, the closer together lies what the chip
 // has in flight, and the better memory takes it.  197M parameters, bf16 gradients and copies: states in 32 bits 918 us,
 // 6.0 TB/s; 2048 workgroups that walk runs of 16384 elements 1210, with loads and stores through the cache 1361.  States
-// in 8 bits 527 us, 6.0 TB/s (with eight elements of a lane next to each other, whose stores are half lines, 557).
+// in 8 bits 524 us, 6.0 TB/s (with eight elements of a lane next to each other, whose stores are half lines, 557).
 // Runs dealt to the dies one by one: 906 us in 32 bits, 1 % more in 8, and 16M parameters with fp32 gradients and no
 // copies 80 us, which take 76 in lots.
 constexpr int kBlock = 256;         // elements that share a scale

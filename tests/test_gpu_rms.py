@@ -267,3 +267,40 @@ def test_gradients_against_differences():
         hi[j] += d
         lo[j] -= d
         assert abs((total(x, hi) - total(x, lo)) / (2 * d) - float(dw[j])) < 2e-3
+
+
+def test_shapes_of_one_axis_and_of_many():
+    import paper_2307_02031_amd as g
+    x, res, dy = (_normal(2, 3, 4, 130, dtype=torch.float16, seed=70 + i) for i in range(3))
+    w = _normal(130, dtype=torch.float16, seed=74)
+    r = g.gbmw_rms_norm_forward(x, w, residual=res, qtype=F8, group=64)
+    dx, dw = g.gbmw_rms_norm_backward(dy, r.h, w, r.rstd)
+    _check_forward(r, x, res, w, qtype=F8, group=64)
+    _check_backward(dx, dw, dy, r.h, w, r.rstd)
+    assert r.rstd.shape == (2, 3, 4) and r.scale.shape == (2, 3, 4, 3)
+    one = g.gbmw_rms_norm_forward(x[1, 2, 3], w, residual=res[1, 2, 3], qtype=F8, group=64)
+    assert one.rstd.shape == () and one.scale.shape == (3,)
+    assert torch.equal(one.y, r.y[1, 2, 3]) and torch.equal(one.scale, r.scale[1, 2, 3]) and one.rstd == r.rstd[1, 2, 3]
+    dx1, dw1 = g.gbmw_rms_norm_backward(dy[1, 2, 3], one.h, w, one.rstd)
+    assert torch.equal(dx1, dx[1, 2, 3]) and dw1.shape == (130,)
+    # rows that are not one stride apart have no row stride
+    with pytest.raises(g.GbmwError):
+        g.gbmw_rms_norm_forward(x[:, ::2, 1:], w)
+
+
+def test_the_binding_refuses():
+    import paper_2307_02031_amd as g
+    x, w = _normal(4, 64, dtype=torch.bfloat16, seed=1), _normal(64, dtype=torch.float32, seed=2)
+    r = g.gbmw_rms_norm_forward(x, w)
+    for kw in (dict(weight=w[:5]), dict(weight=w.half()), dict(residual=x[:2]), dict(residual=x.float()), dict(residual=x.cpu()), dict(h=x.clone()),
+               dict(q=x.to(F8)), dict(qtype=torch.uint8), dict(qtype=F8, group=16), dict(qtype=F8, group=-1), dict(qtype=F8, q=x), dict(y=x.float()),
+               dict(y=x[:, :1].expand(4, 64)), dict(want_y=False), dict(eps=-1.0), dict(eps=math.inf), dict(residual=x[:1].expand(4, 64), h=x[:1].expand(4, 64)),
+               dict(weight=torch.zeros(128, device="cuda")[::2])):
+        with pytest.raises(g.GbmwError) as e:
+            g.gbmw_rms_norm_forward(x, **{"weight": w, **kw})
+        assert e.value.status == g.GBMW_ERR_INVALID_ARG, kw
+    for args, kw in (((x[:2], x, w, r.rstd), {}), ((x, x, w, r.rstd[:2]), {}), ((x, x, w, r.rstd.half()), {}), ((x, x, w, r.rstd), dict(dres=x[:1])),
+                     ((x, x, w, r.rstd), dict(dx=x.float())), ((x.float(), x, w, r.rstd), {})):
+        with pytest.raises(g.GbmwError) as e:
+            g.gbmw_rms_norm_backward(*args, **kw)
+        assert e.value.status == g.GBMW_ERR_INVALID_ARG

@@ -119,6 +119,11 @@ def test_lengths_and_strides(D, rot):
         for out, res, ref_ in zip(outs, got, want):
             assert torch.equal(res[b, :m], ref_[b, :m])
             assert bool((out[b, m:] == 3).all()) and bool((out[..., :2] == 3).all()) and bool((out[..., D + 2:] == 3).all())
+    # lengths beyond the rows, and below none
+    off = g.gbmw_rotary_forward(dense[0], None, freq, len_x=torch.tensor([L + 9, -3, 7, 2 ** 31 - 1], dtype=torch.int32, device="cuda"),
+                                q_out=torch.zeros_like(dense[0]))[0]
+    for b, m in enumerate((L, 0, 7, L)):
+        assert torch.equal(off[b, :m], want[0][b, :m]) and bool((off[b, m:] == 0).all())
     # in place in the product's own array: v and the rows behind stay
     before = qkv.clone()
     g.gbmw_rotary_forward(q, k, freq, len_x=n, q_out=q, k_out=k)
