@@ -10,7 +10,7 @@ namespace {
 // NT threads hold a row in registers, as in layer norm, a wave four rows where a quarter of it holds one: one pass
 // over x and the residual, one sum, and for 8 bits the largest of a group's threads.
 //
-// Bound by HBM.  16384 x 5120 bf16 with a residual: forward 113 us, 5.9 TB/s; backward 129 to 134, 5.0 to 5.2 TB/s, of
+// Bound by HBM.  16384 x 5120 bf16 with a residual: forward 113 us, 5.9 TB/s; backward 125, 5.4 TB/s, of
 // which 5 to join the shares of dweight.  8192 x 5120 to 8 bits, a scale for each 128 columns: 54 us, 5.4 TB/s.  4 x 5120:
 // 4.2 us, latency of a load, a sum and a store.  Rows at odd addresses (16-bit values, an odd number a row) cost up to
 // 1.4 times as much (4096 x 10001 102 us, 4096 x 10002 72); rows that leave the registers (16-bit values beyond
@@ -33,6 +33,9 @@ struct RmsArgs {
 };
 
 constexpr int kRmsFwdThreads = 256, kRmsBwdThreads = 512;
+// Rows that a workgroup has at a time.
+template <int NT, bool BACKWARD>
+constexpr int kRows = NT < (BACKWARD ? kRmsBwdThreads : kRmsFwdThreads) ? (BACKWARD ? kRmsBwdThreads : kRmsFwdThreads) / NT : 1;
 
 template <int WORDS>
 using Words = uint32_t __attribute__((ext_vector_type(WORDS), aligned(1)));
@@ -129,8 +132,8 @@ __device__ __forceinline__ void to_codes(const float (&x)[V], float by, bool who
 }
 
 template <typename T, int NT, int NJ, bool WHOLE, bool STREAM>
-__global__ __launch_bounds__(NT < kRmsFwdThreads ? kRmsFwdThreads : NT) void k_rms_fwd(RmsArgs a) {
-  constexpr int V = kVec<T>, G = (NT < kRmsFwdThreads ? kRmsFwdThreads : NT) / NT;
+__global__ __launch_bounds__((NT * kRows<NT, false>)) void k_rms_fwd(RmsArgs a) {
+  constexpr int V = kVec<T>, G = kRows<NT, false>;
   __shared__ float scratch[2][G][kWaves<NT>];
   __shared__ unsigned most_of[G][kWaves<NT>];
   const int t = threadIdx.x % NT, g = threadIdx.x / NT;
@@ -246,8 +249,8 @@ __global__ __launch_bounds__(NT < kRmsFwdThreads ? kRmsFwdThreads : NT) void k_r
 
 // The same walk; a thread keeps its columns' share of dweight over all its rows, as layer norm's does.
 template <typename T, int NT, int NJ, bool WHOLE, bool STREAM>
-__global__ __launch_bounds__(NT < kRmsBwdThreads ? kRmsBwdThreads : NT) void k_rms_bwd(RmsArgs a) {
-  constexpr int V = kVec<T>, G = (NT < kRmsBwdThreads ? kRmsBwdThreads : NT) / NT;
+__global__ __launch_bounds__((NT * kRows<NT, true>)) void k_rms_bwd(RmsArgs a) {
+  constexpr int V = kVec<T>, G = kRows<NT, true>;
   constexpr bool kAhead = kRunsAhead<NT, NJ>;
   __shared__ float scratch[2][G][kWaves<NT>];
   extern __shared__ __attribute__((aligned(16))) float columns[];   // [V/4][pieces][4] weight, then [cols] shares
@@ -372,11 +375,14 @@ gbmw_status check_rms(const gbmw_rms_norm_problem* p) {
 
 // As layer norm's, and: 16 threads where a row of up to 48 pieces fits them (not where a scale has columns of
 // more threads than these), 128 where 256 would leave many without a piece, 512 between the rows of 256 and those of 1024.
+// Backward 320 with 16-bit values (16384 x 5120 125 us, with three pieces of 256 threads 130; forward 117 and 112, 8192 x
+// 2560 in 32 bits 62 and 60).
 Shape rms_shape(const gbmw_rms_norm_problem* p, bool backward) {
   const int vec = 16 / element_size(p->dtype), n = (p->cols + vec - 1) / vec;
   if (n <= 16 || (n <= 3 * 16 && (backward || !p->q || p->group <= 16 * vec))) return {16, (n + 15) / 16};
   if (n <= 3 * 64) return {64, (n + 63) / 64};
   if (n > 2 * 128 && n <= 3 * 128) return {128, 3};
+  if (backward && vec == 8 && n > 2 * 256 && n <= 2 * 320) return {320, 2};
   if (n <= 3 * 256) return {256, (n + 255) / 256};
   if (n <= 3 * 512) return {512, (n + 511) / 512};
   const int nj = (n + 1023) / 1024;
@@ -406,10 +412,11 @@ int64_t rms_workspace(const gbmw_rms_norm_problem* p, int groups) {
 template <typename T, int NT, int NJ, bool WHOLE, bool STREAM>
 gbmw_status launch_rms(const RmsArgs& a, bool backward, int groups, hipStream_t st) {
   if (!backward) {
-    hipLaunchKernelGGL((k_rms_fwd<T, NT, NJ, WHOLE, STREAM>), dim3(groups), dim3(std::max(NT, kRmsFwdThreads)), 0, st, a);
+    if constexpr (NT != 320)
+      hipLaunchKernelGGL((k_rms_fwd<T, NT, NJ, WHOLE, STREAM>), dim3(groups), dim3(NT * kRows<NT, false>), 0, st, a);
   } else {
     const size_t weight = 16 * (size_t)((a.cols + kVec<T> - 1) / kVec<T>) * (kVec<T> / 4);
-    const size_t lds = std::max(weight, 4 * (size_t)a.cols * std::max(1, kRmsBwdThreads / NT));
+    const size_t lds = std::max(weight, 4 * (size_t)a.cols * kRows<NT, true>);
     if (lds > 60 * 1024) {
       const hipError_t e = hipFuncSetAttribute((const void*)&k_rms_bwd<T, NT, NJ, WHOLE, STREAM>,
                                                hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
@@ -418,7 +425,7 @@ gbmw_status launch_rms(const RmsArgs& a, bool backward, int groups, hipStream_t 
         return fail(GBMW_ERR_DEVICE, "%zu bytes of shared memory: %s", lds, hipGetErrorString(e));
       }
     }
-    hipLaunchKernelGGL((k_rms_bwd<T, NT, NJ, WHOLE, STREAM>), dim3(groups), dim3(std::max(NT, kRmsBwdThreads)), lds, st, a);
+    hipLaunchKernelGGL((k_rms_bwd<T, NT, NJ, WHOLE, STREAM>), dim3(groups), dim3(NT * kRows<NT, true>), lds, st, a);
   }
   HIP_TRY(hipGetLastError());
   return GBMW_OK;
@@ -443,6 +450,9 @@ gbmw_status launch_rms(const RmsArgs& a, Shape s, bool backward, int groups, hip
     case 2561: return launch_rms<T, 256, 1>(a, backward, groups, st);
     case 2562: return launch_rms<T, 256, 2>(a, backward, groups, st);
     case 2563: return launch_rms<T, 256, 3>(a, backward, groups, st);
+    case 3202:
+      if constexpr (sizeof(T) == 2) return launch_rms<T, 320, 2>(a, backward, groups, st);
+      break;
     case 5122: return launch_rms<T, 512, 2>(a, backward, groups, st);
     case 5123: return launch_rms<T, 512, 3>(a, backward, groups, st);
     case 10242: return launch_rms<T, 1024, 2>(a, backward, groups, st);

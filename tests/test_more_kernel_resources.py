@@ -44,5 +44,5 @@ def test_norms(tmp_path):
             assert scratch == 0, (k, scratch)
             # two workgroups of 512 threads where a thread has up to two pieces, else one and a half
             assert waves >= (4 if pieces <= 2 else 3), (k, waves)
-    # fifteen shapes (one more in 32 bits), each of whole pieces, past the cache, and of any length; forward and backward
-    assert seen == (3 * 15 + 1) * 3 * 2
+    # fifteen shapes (one more in 32 bits, and one backward in 16), each of whole pieces, past the cache, and of any length
+    assert seen == ((3 * 15 + 1) * 2 + 2) * 3
