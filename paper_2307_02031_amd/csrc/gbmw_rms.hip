@@ -13,8 +13,8 @@ namespace {
 // Bound by HBM.  16384 x 5120 bf16 with a residual: forward 113 us, 5.9 TB/s; backward 125, 5.4 TB/s, of
 // which 5 to join the shares of dweight.  8192 x 5120 to 8 bits, a scale for each 128 columns: 54 us, 5.4 TB/s.  4 x 5120:
 // 4.2 us, latency of a load, a sum and a store.  Rows at odd addresses (16-bit values, an odd number a row) cost up to
-// 1.4 times as much (4096 x 10001 102 us, 4096 x 10002 72); rows that leave the registers (16-bit values beyond
-// 16384 columns) spill in the backward pass.
+// 1.4 times as much (4096 x 10001 102 us, 4096 x 10002 72); rows beyond 16384 columns spill in the backward pass
+// (2048 x 20000 bf16: 139 us, forward 62).
 struct RmsArgs {
   int64_t rows;
   int cols;
@@ -146,13 +146,17 @@ __global__ __launch_bounds__((NT * kRows<NT, false>)) void k_rms_fwd(RmsArgs a) 
     Pack<T> h[NJ], r[NJ];
     load_row<STREAM>(h, span, (const T*)a.x + at * a.xs);
     if (a.res) load_row<STREAM>(r, span, (const T*)a.res + at * a.rs);
-    float w[NJ][V];
+    // weight's loads go out with the row's, but where the row fills the registers (1024 x 32768 fp32: 99 us, else 142)
+    constexpr bool kLate = NT == 1024 && NJ > 2;
+    float w[kLate ? 1 : NJ][V];
+    auto weight_of = [&](int j, float (&w)[V]) {
 #pragma unroll
-    for (int j = 0; j < NJ; ++j) {
+      for (int i = 0; i < V; ++i) w[i] = 1.0f;
+      if (a.w) a.wide ? span[j].load(w, (const float*)a.w) : span[j].load(w, (const T*)a.w);
+    };
+    if constexpr (!kLate)
 #pragma unroll
-      for (int i = 0; i < V; ++i) w[j][i] = 1.0f;
-      if (a.w) a.wide ? span[j].load(w[j], (const float*)a.w) : span[j].load(w[j], (const T*)a.w);
-    }
+      for (int j = 0; j < NJ; ++j) weight_of(j, w[j]);
     if (a.res) {
 #pragma unroll
       for (int j = 0; j < NJ; ++j)
@@ -172,8 +176,9 @@ __global__ __launch_bounds__((NT * kRows<NT, false>)) void k_rms_fwd(RmsArgs a) 
     const float rstd = 1.0f / __builtin_sqrtf(s / (float)a.cols + a.eps);
     const bool live = row < a.rows;
     auto normed = [&](int j, float (&y)[V]) {
+      if constexpr (kLate) weight_of(j, w[0]);
 #pragma unroll
-      for (int i = 0; i < V; ++i) y[i] = (float)h[j].v[i] * rstd * w[j][i];
+      for (int i = 0; i < V; ++i) y[i] = (float)h[j].v[i] * rstd * w[kLate ? 0 : j][i];
     };
     if (live) {
       if (t == 0 && a.rstd) a.rstd[row] = rstd;
