@@ -680,7 +680,8 @@ int64_t gbmw_rms_norm_workspace(const gbmw_rms_norm_problem* p);
  * in fp64, so positions may be any int32.
  * q_out may be q and k_out may be k, with the same strides (in place); an array given
  * in place must have all its elements at different places.  k and k_out may be NULL (Hk 0).
- * Layouts and strides are attention's.
+ * Layouts and strides are attention's.  GBMW_ERR_UNSUPPORTED: arrays of 64 GB or more that
+ * take more waves than a launch has.
  */
 typedef struct {
   int32_t dtype;             /* of all arrays                                        */
