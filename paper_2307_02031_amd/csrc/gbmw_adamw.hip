@@ -87,7 +87,9 @@ __device__ __forceinline__ bool rates_now(const AdamArgs& a, Rates& r) {
 }
 
 // N elements at p of which n (0..N) are there, loaded or stored at once where all are.  Nothing is
-// read or written twice in a step, so all of it passes the cache by.
+// read or written twice in a step, so all of it passes the cache by.  Arrays that begin in the middle of a
+// line (40M parameters: 184 us become 196, in 8 bits 107 become 172) take the same way: through the cache
+// they take 280 and 161.
 template <typename T, int N>
 struct alignas(sizeof(T)) Few {
   T v[N];

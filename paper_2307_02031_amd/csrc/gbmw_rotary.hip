@@ -26,7 +26,7 @@ struct RotaryArgs {
 };
 
 // cos and sin of 2 pi x, |x| <= 1/2, by the quarter turn that x is nearest and the Taylor series of the
-// rest (at most pi / 4; the first term left out is below 2^-29 of the result).
+// rest (at most pi / 4; the first term left out is below 2^-28 of the result).
 __device__ __forceinline__ void turn_of(float x, float& c, float& s) {
   const float quarter = __builtin_rintf(4.0f * x);
   const float r = 6.28318530717958648f * __builtin_fmaf(-0.25f, quarter, x), r2 = r * r;
