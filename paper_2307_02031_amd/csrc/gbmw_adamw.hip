@@ -186,6 +186,13 @@ __device__ __forceinline__ float most_of_32(unsigned x) {   // over a half of th
   return __builtin_bit_cast(float, max((unsigned)r[0], (unsigned)r[1]));
 }
 
+// The hardware's root takes a value below 2^-126 for 0, and m / 0 would be m / eps.
+__device__ __forceinline__ float root_of(float x) {
+  constexpr int kPositiveSubnormal = 0x80;
+  if (__builtin_amdgcn_classf(x, kPositiveSubnormal)) return __builtin_amdgcn_sqrtf(x * 0x1p64f) * 0x1p-32f;
+  return __builtin_amdgcn_sqrtf(x);
+}
+
 __device__ __forceinline__ float scale_of(float most) {
   const float s = most / 448.0f;
   return s < 0x1p-126f ? 0x1p-126f : s;
@@ -253,7 +260,7 @@ __device__ __forceinline__ void run_of_8(const Run& run, const AdamArgs& a) {
       float &me = m[u * N + e], &ve = root[u * N + e];
       const float d = (float)g[u].v[e] * r.grad, old = ve * vs;
       me = __builtin_fmaf(me, m_by, d * r.a1);
-      ve = __builtin_amdgcn_sqrtf(__builtin_fmaf(old * old, r.b2, d * d * r.a2));
+      ve = root_of(__builtin_fmaf(old * old, r.b2, d * d * r.a2));
       const float per = __builtin_amdgcn_rcpf(__builtin_fmaf(ve, r.root_c2, r.eps));
       q[u][e] = __builtin_fmaf((float)p[u].v[e], keep, -(me * per) * r.lr_c1);
       // as whole numbers: a NaN is the largest; roots have no sign

@@ -316,3 +316,27 @@ def test_refusals():
     for kw in (dict(lr=torch.zeros(1)), dict(step=torch.ones(1, device="cuda")), dict(norm=torch.ones(0, device="cuda"))):
         with pytest.raises(g.GbmwError):
             g.gbmw_adamw_step(lst, **{**HOW, "step": 1, **kw})
+
+
+@pytest.mark.parametrize("seed", [0, 5])
+@pytest.mark.parametrize("bits", [8, 32])
+@pytest.mark.parametrize("grad", [1e-15, 1e-18, -1e-19])
+def test_gradients_whose_squares_are_below_the_normal_numbers(grad, bits, seed):
+    import paper_2307_02031_amd as lib
+
+    # v is g^2 (1 - beta2), with two roundings of half a step of 2^-149; a first step goes by lr g / |g|.  All values of the
+    # block are its largest, so its codes are 448 whatever the rounding
+    n = 300
+    p, g = torch.zeros(n, device="cuda"), torch.full((n,), grad, device="cuda")
+    m, v = (torch.zeros(n, device="cuda").to(F8 if bits == 8 else torch.float32) for _ in range(2))
+    scales = [torch.zeros(2, device="cuda") for _ in range(2)]
+    how = dict(m_scales=scales[:1], v_scales=scales[1:]) if bits == 8 else {}
+    lst = lib.gbmw_adamw_list_create([p], [g], [m], [v], **how)
+    lib.gbmw_adamw_step(lst, 1.0, 1, beta1=0.9, beta2=0.999, eps=2.0 ** -126, seed=seed)
+    value = float(np.float32(grad))
+    square = value * value * 1e-3
+    off = 2.0 ** -149 / square / 2 + 2.0 ** -20
+    root = _held(v, scales[1]) if bits == 8 else v.cpu().double().sqrt()
+    assert ((root - math.sqrt(square)).abs() <= off * math.sqrt(square)).all()
+    want = -value / (abs(value) + 2.0 ** -126)
+    assert ((p.cpu().double() - want).abs() <= off).all()
