@@ -723,19 +723,22 @@ gbmw_status gbmw_rotary_frequencies(int32_t rot, double theta, int32_t scaling, 
 /*
  * One AdamW step over many tensors.  For every element, with c1 = 1 - beta1^step and
  * c2 = 1 - beta2^step,
- *   g = grad * scale * (norm > max_norm ? max_norm / norm : 1),
- *   m = beta1 m + (1 - beta1) g,  v = beta2 v + (1 - beta2) g^2,
- *   param = param (1 - lr weight_decay) - (lr / c1) m / (sqrt(v) / sqrt(c2) + eps),
- * in fp32 (the factors in fp64, rounded once), param rounded to dtype.  `copy`, if given, gets
- * the new param (of GBMW_F32) rounded to copy_dtype.  norm is what gbmw_clip_gradients wrote:
- * with a list whose outputs are its inputs and max_norm +inf that call only computes it, and the
+ *   g = grad * factor,  factor = scale * (norm > max_norm ? max_norm / norm : 1),
+ *   m = m * beta1 + g * (1 - beta1),  v = v * beta2 + (g * g) * (1 - beta2),
+ *   param = param * (1 - lr weight_decay) - (m / (sqrt(v) * (1 / sqrt(c2)) + eps)) * (lr / c1),
+ * in fp32, each of these operations rounded to nearest (numbers that all elements share, factor, 1 - beta1,
+ * lr / c1 and so on, are computed in fp64 and rounded once), param then to dtype.  `copy`, if
+ * given, gets the new param (of GBMW_F32) rounded to copy_dtype.  norm is what gbmw_clip_gradients
+ * wrote: with a list whose outputs are its inputs and max_norm +inf that call only computes it, and the
  * step clips as it reads.  If *norm is NaN or infinite the step is left out: nothing is written.
  *
  * States of 32 bits: m and v in fp32.  States of 8 bits: for each block of 256 elements of a
  * tensor (the last may have fewer) m is held as codes of GBMW_E4M3 with a scale, and so is
  * r = sqrt(v) in the place of v:
- *   value = code * scale,  scale = max(largest |value| / 448, 2^-126).
- * With seed 0 value / scale is rounded to nearest even.  With another seed it goes to one of
+ *   value = code * scale,  scale = max(largest |value| * (1 / 448), 2^-126),
+ * 1 / 448 in fp32, and the arithmetic is as above (from v = r * r, to r = sqrt(v)), but that m is
+ * divided by a reciprocal that may be off by a unit of its last place.  With seed 0 value / scale
+ * (in fp32, at most 448) is rounded to nearest even.  With another seed it goes to one of
  * its two neighbours at random, with the probabilities that make it right on average, by 16
  * bits of a hash of seed, step and the element's place in the list (the same call gives the same
  * bits).  Rounding to nearest leaves a moment unchanged for ever that moves by less than half a

@@ -13,7 +13,7 @@ namespace {
 // below that.  A workgroup has 1024 elements and ends: the more of them there are, the closer together lies what the chip
 // has in flight, and the better memory takes it.  197M parameters, bf16 gradients and copies: states in 32 bits 918 us,
 // 6.0 TB/s; 2048 workgroups that walk runs of 16384 elements 1210, with loads and stores through the cache 1361.  States
-// in 8 bits 524 us, 6.0 TB/s (with eight elements of a lane next to each other, whose stores are half lines, 557).
+// in 8 bits 512 us, 6.1 TB/s (with eight elements of a lane next to each other, whose stores are half lines, 6 % more).
 // Runs dealt to the dies one by one: 906 us in 32 bits, 1 % more in 8, and 16M parameters with fp32 gradients and no
 // copies 80 us, which take 76 in lots.
 constexpr int kBlock = 256;         // elements that share a scale
@@ -186,16 +186,28 @@ __device__ __forceinline__ float most_of_32(unsigned x) {   // over a half of th
   return __builtin_bit_cast(float, max((unsigned)r[0], (unsigned)r[1]));
 }
 
-// The hardware's root takes a value below 2^-126 for 0, and m / 0 would be m / eps.
-__device__ __forceinline__ float root_of(float x) {
-  constexpr int kPositiveSubnormal = 0x80;
-  if (__builtin_amdgcn_classf(x, kPositiveSubnormal)) return __builtin_amdgcn_sqrtf(x * 0x1p64f) * 0x1p-32f;
-  return __builtin_amdgcn_sqrtf(x);
+__device__ __forceinline__ float scale_of(float most) {
+  const float s = most * (1.0f / 448.0f);
+  return s < 0x1p-126f ? 0x1p-126f : s;
 }
 
-__device__ __forceinline__ float scale_of(float most) {
-  const float s = most / 448.0f;
-  return s < 0x1p-126f ? 0x1p-126f : s;
+// x / scale, rounded once: the product with the rounded reciprocal is off by a unit of its last place, and what it leaves of
+// x, which a fused operation has exactly, puts that right.  So the codes are the formula's to the last one; rounding at
+// random carries a last place into a whole code now and then, and from there into scales (without the correction 20 of
+// 10^8 codes differ after a step).  What is left of x is no number of 32 bits where x is below 2^-103: small scales are
+// taken times 2^64 (by a factor, not a branch, which costs 11 registers: 512 us for 521), and else such an x has code 0
+// either way.  A scale that is infinite or NaN has no reciprocal: x / inf is 0.
+template <int N>
+__device__ __forceinline__ void divide(float (&x)[N], float scale) {
+  const float up = scale < 0x1p-60f ? 0x1p64f : 1.0f;
+  scale *= up;
+  const float by = 1.0f / scale, taken = by > 0.0f ? scale : 0.0f;
+#pragma unroll
+  for (int e = 0; e < N; ++e) {
+    x[e] *= up;
+    const float q = x[e] * by;
+    x[e] = __builtin_fmaf(__builtin_fmaf(-q, taken, x[e]), by, q);
+  }
 }
 
 // Four values in 8 bits.  By the hash the conversion adds `random` (its upper 20 bits, below the last digit that is
@@ -227,9 +239,8 @@ __device__ __forceinline__ void values_of(const Few<uint8_t, 4>& code, float* x)
 }
 
 // States in 8 bits: half a wave has a block, a lane four elements of each half of it, so that every store of the wave is
-// whole lines.  Arithmetic comes near to binding this one, so a product and a sum are one operation, and the root and the
-// quotient are the hardware's, off by one unit of their last place: the states keep three of its 23 bits, the parameter
-// takes a step that is a small part of it.
+// whole lines.  Moments, scales and codes are the header's formula, each operation rounded.  The parameter takes
+// the hardware's reciprocal, off by one unit of its last place (with a division 3 % more: vector operations then count).
 template <typename G, typename P>
 __device__ __forceinline__ void run_of_8(const Run& run, const AdamArgs& a) {
   constexpr int N = 4, U = 2, kApart = kBlock / U;
@@ -249,7 +260,7 @@ __device__ __forceinline__ void run_of_8(const Run& run, const AdamArgs& a) {
   const float ms = run.m_scale[k], vs = run.v_scale[k];
   Rates r = a.r;
   if (!rates_now(a, r)) return;
-  const float keep = (float)(1.0 - r.lr * (double)run.decay), m_by = ms * r.b1;
+  const float keep = (float)(1.0 - r.lr * (double)run.decay);
   float m[U * N], root[U * N], q[U][N];
   unsigned most_m = 0, most_v = 0;
 #pragma unroll
@@ -259,16 +270,20 @@ __device__ __forceinline__ void run_of_8(const Run& run, const AdamArgs& a) {
     for (int e = 0; e < N; ++e) {
       float &me = m[u * N + e], &ve = root[u * N + e];
       const float d = (float)g[u].v[e] * r.grad, old = ve * vs;
-      me = __builtin_fmaf(me, m_by, d * r.a1);
-      ve = root_of(__builtin_fmaf(old * old, r.b2, d * d * r.a2));
-      const float per = __builtin_amdgcn_rcpf(__builtin_fmaf(ve, r.root_c2, r.eps));
-      q[u][e] = __builtin_fmaf((float)p[u].v[e], keep, -(me * per) * r.lr_c1);
+      me = me * ms * r.b1 + d * r.a1;
+      ve = __builtin_sqrtf(old * old * r.b2 + d * d * r.a2);
+      q[u][e] = (float)p[u].v[e] * keep - me * __builtin_amdgcn_rcpf(ve * r.root_c2 + r.eps) * r.lr_c1;
       // as whole numbers: a NaN is the largest; roots have no sign
       most_m = max(most_m, magnitude(me)), most_v = max(most_v, __builtin_bit_cast(unsigned, ve));
     }
   }
   const float new_ms = scale_of(most_of_32(most_m)), new_vs = scale_of(most_of_32(most_v));
-  const float by_m = 1.0f / new_ms, by_v = 1.0f / new_vs;
+  divide(m, new_ms), divide(root, new_vs);
+#pragma unroll
+  for (int e = 0; e < U * N; ++e) {
+    m[e] = __builtin_amdgcn_fmed3f(m[e], -448.0f, 448.0f);
+    root[e] = root[e] > 0.0f ? __builtin_amdgcn_fmed3f(root[e], 0x1p-9f, 448.0f) : 0.0f;
+  }
   uint32_t high[U * N] = {}, low[U * N] = {};
   if (r.key) {
 #pragma unroll
@@ -281,11 +296,6 @@ __device__ __forceinline__ void run_of_8(const Run& run, const AdamArgs& a) {
         high[u * N + e] = (word & 0xffff0000u) | 0x8000, low[u * N + e] = word << 16 | 0x8000;
       }
     }
-  }
-#pragma unroll
-  for (int e = 0; e < U * N; ++e) {
-    m[e] = __builtin_amdgcn_fmed3f(m[e] * by_m, -448.0f, 448.0f);
-    root[e] = root[e] > 0.0f ? __builtin_amdgcn_fmed3f(root[e] * by_v, 0x1p-9f, 448.0f) : 0.0f;
   }
 #pragma unroll
   for (int u = 0; u < U; ++u) {

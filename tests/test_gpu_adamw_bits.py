@@ -1,0 +1,127 @@
+"""AdamW's states in 8 bits, bit for bit: the header's formula in 32 bits, each operation rounded, gives the same codes and
+scales, with no element left out.  Rounding at random turns a difference in the last place into a whole code now and then, and
+a code that is its block's largest a step later into another scale, so an arithmetic that is right to a last place is not
+enough."""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+pytestmark = pytest.mark.gpu
+
+F8 = torch.float8_e4m3fn
+BY_TOP = float(np.float32(1) / np.float32(448))
+HOW = dict(beta1=0.9, beta2=0.999, eps=1e-8)
+
+
+def _hash(x):
+    x = (x * 0x9E3779B1) & 0xFFFFFFFF
+    x = ((x ^ (x >> 15)) * 0x85EBCA77) & 0xFFFFFFFF
+    return x ^ (x >> 13)
+
+
+def _codes(x, random, root):
+    """Codes of whole blocks (values in 32 bits) and their scales."""
+    blocks = x.view(-1, 256)
+    scale = (blocks.abs().amax(1) * BY_TOP).clamp_min(2.0 ** -126)
+    c = (blocks / scale[:, None]).view(-1)
+    if root:
+        c = torch.where(x > 0, c.clamp_min(2.0 ** -9), c)
+    c = c.clamp(-448.0, 448.0)
+    if random is not None:
+        # a step of the code's three digits; what is cut off goes up where it is more than 1 less the number of [0, 1)
+        step = (((torch.frexp(c).exponent - 1).clamp_min(-6) - 3 + 127) << 23).view(torch.float32)
+        c = torch.copysign(torch.floor(c.abs() / step + random) * step, c)
+    return c.to(F8), scale
+
+
+def _step(t, grad, place, step, seed, factor=1.0):
+    """One step of states held in whole blocks, in 32 bits; place: the elements' numbers in the list."""
+    b1, b2 = HOW["beta1"], HOW["beta2"]
+    held = lambda c, s: (c.float().view(-1, 256) * s[:, None]).view(-1)
+    g = grad.float() * factor
+    m, r = held(t["m"], t["m_scale"]), held(t["v"], t["v_scale"])
+    m = m * b1 + g * (1.0 - b1)
+    v = (r * r) * b2 + (g * g) * (1.0 - b2)
+    word = _hash(place ^ _hash((seed + step * 0x9E3779B9) & 0xFFFFFFFF)) if seed else None
+    part = lambda w: None if seed == 0 else (w.float() + 0.5) / 65536.0
+    t["m"], t["m_scale"] = _codes(m, part(word >> 16 if seed else None), False)
+    # by way of 64 bits, because torch's root on the CPU is off by a last place at times: a root of 24 bits is at least 2^-27
+    # of a last place from the middle of two, so a second rounding changes nothing
+    r = torch.sqrt(v.double()).float()
+    t["v"], t["v_scale"] = _codes(r, part(word & 65535 if seed else None), True)
+
+
+def _same(t, got, n, what):
+    for name in ("m", "v", "m_scale", "v_scale"):
+        a, b = (x.view(torch.uint8 if x.element_size() == 1 else torch.int32) for x in (t[name], got[name]))
+        few = n if a.element_size() == 1 else -(-n // 256)
+        off = int((a[:few].to(b.device) != b[:few]).sum())
+        assert off == 0, (what, name, off)
+
+
+@pytest.mark.parametrize("seed", [20231, 0])
+def test_codes_and_scales_of_many_elements(seed):
+    import paper_2307_02031_amd as g
+    n = 60_000_123
+    room = -(-n // 256) * 256
+    gen = torch.Generator(device="cuda").manual_seed(7)
+    there = torch.arange(room, device="cuda") < n
+    grad = torch.where(there, torch.randn(room, generator=gen, device="cuda") * 1e-3, 0.0).bfloat16()
+    zeros = lambda: torch.zeros(room, dtype=torch.uint8, device="cuda").view(F8)
+    scales = lambda: torch.zeros(room // 256, device="cuda")
+    got = dict(m=zeros(), v=zeros(), m_scale=scales(), v_scale=scales())
+    t = {k: x.clone() for k, x in got.items()}
+    param = torch.zeros(n, device="cuda")
+    lst = g.gbmw_adamw_list_create([param], [grad[:n]], [got["m"][:n]], [got["v"][:n]], m_scales=[got["m_scale"]], v_scales=[got["v_scale"]])
+    place = torch.arange(room, device="cuda")
+    for step in range(1, 11):
+        g.gbmw_adamw_step(lst, 1e-4, step, seed=seed, **HOW)
+        _step(t, grad, place, step, seed)
+        if step in (1, 2, 10):
+            _same(t, got, n, step)
+        grad.copy_(torch.where(there, torch.randn(room, generator=gen, device="cuda") * 1e-3, 0.0))
+
+
+@pytest.mark.parametrize("seed", [5, 0])
+@pytest.mark.parametrize("spread", [1e-38, 1e-30, 1e-24, 1e-19, 1e-12, 1.0, 1e15])
+def test_codes_and_scales_of_far_sizes(spread, seed):
+    """Blocks whose scales are small, or subnormal but for their least; values of many sizes within a block; a scaled gradient;
+    several tensors, whose places go on at the next block.  The formula runs on the CPU."""
+    import paper_2307_02031_amd as g
+    sizes = [700, 256, 5001, 1]
+    gen = torch.Generator().manual_seed(11)
+    lists, plain, first = dict(param=[], grad=[], m=[], v=[], m_scale=[], v_scale=[]), [], 0
+    for n in sizes:
+        room = -(-n // 256) * 256
+        x = torch.randn(room, generator=gen) * spread * 2.0 ** torch.randint(-40, 1, (room,), generator=gen).float()
+        x[n:] = 0.0
+        t = dict(m=torch.zeros(room).to(F8), v=torch.zeros(room).to(F8), m_scale=torch.zeros(room // 256), v_scale=torch.zeros(room // 256))
+        plain.append((t, x, torch.arange(first, first + room)))
+        first += room
+        for name, y in dict(t, param=torch.zeros(n), grad=x).items():
+            lists[name].append(y[:n].cuda() if name in ("m", "v", "grad") else y.cuda())
+    lst = g.gbmw_adamw_list_create(lists["param"], lists["grad"], lists["m"], lists["v"], m_scales=lists["m_scale"], v_scales=lists["v_scale"])
+    for step in (1, 2, 3):
+        g.gbmw_adamw_step(lst, 1e-4, step, seed=seed, scale=0.75, **HOW)
+        for i, (t, x, place) in enumerate(plain):
+            _step(t, x, place, step, seed, 0.75)
+            _same({k: y.cuda() for k, y in t.items()}, {k: lists[k][i] for k in t}, sizes[i], (step, i))
+
+
+def test_an_infinite_scale():
+    """A finite gradient whose square is none makes the block's second moments' scale infinite; the first moments' stay."""
+    import paper_2307_02031_amd as g
+    grad = torch.full((256,), 1e25, device="cuda")
+    grad[1] = -3e24
+    m, v = (torch.zeros(256, dtype=torch.uint8, device="cuda").view(F8) for _ in range(2))
+    ms, vs, p = torch.zeros(1, device="cuda"), torch.zeros(1, device="cuda"), torch.ones(256, device="cuda")
+    g.gbmw_adamw_step(g.gbmw_adamw_list_create([p], [grad], [m], [v], m_scales=[ms], v_scales=[vs]), 1e-3, 1, seed=3, **HOW)
+    assert math.isinf(float(vs)) and bool((p == 1).all())      # a step of m / infinity
+    want = grad.cpu() * np.float32(1.0 - 0.9)
+    scale = want.abs().max() * BY_TOP
+    assert float(ms) == float(scale) and float(m[0].float()) == 448.0
+    assert abs(float(m[1].float()) + 0.3 * 448) <= 16       # 134.4 lies between codes 16 apart
+    held = v.float() * vs
+    assert not bool(torch.isfinite(held).any())
