@@ -615,9 +615,9 @@ void gbmw_gradient_list_destroy(gbmw_gradient_list* list);
  * not written without a residual.
  * q holds y in 8 bits, of the value in fp32 and not of y as rounded to dtype: for each row
  * and group of `group` columns (the last may have fewer; one group a row if group is 0)
- *   scale = max(largest |y| / top, 2^-126),  q = y / scale rounded to nearest even,
+ *   scale = max(largest |y| * (1 / top), 2^-126),  q = y / scale rounded to nearest even,
  * with top 448 for GBMW_E4M3 and 127 for GBMW_I8 (whose codes are whole numbers from -127
- * to 127).  A NaN in a group makes its scale NaN, and every value of a row that holds a NaN or
+ * to 127), y = (h * rstd) * weight, 1 / top and the quotient rounded to fp32.  A NaN in a group makes its scale NaN, and every value of a row that holds a NaN or
  * an infinity is one, so its scales are too; GBMW_I8's codes are then without meaning.
  * Backward, from dy (the gradient of y, or of the values that q stands for), h and rstd as
  * the forward call left them (x if there was no residual), with g = dy * weight:

@@ -13,7 +13,7 @@ namespace {
 // below that.  A workgroup has 1024 elements and ends: the more of them there are, the closer together lies what the chip
 // has in flight, and the better memory takes it.  197M parameters, bf16 gradients and copies: states in 32 bits 918 us,
 // 6.0 TB/s; 2048 workgroups that walk runs of 16384 elements 1210, with loads and stores through the cache 1361.  States
-// in 8 bits 512 us, 6.1 TB/s (with eight elements of a lane next to each other, whose stores are half lines, 6 % more).
+// in 8 bits 515 us, 6.1 TB/s (with eight elements of a lane next to each other, whose stores are half lines, 6 % more).
 // Runs dealt to the dies one by one: 906 us in 32 bits, 1 % more in 8, and 16M parameters with fp32 gradients and no
 // copies 80 us, which take 76 in lots.
 constexpr int kBlock = 256;         // elements that share a scale
@@ -186,30 +186,6 @@ __device__ __forceinline__ float most_of_32(unsigned x) {   // over a half of th
   return __builtin_bit_cast(float, max((unsigned)r[0], (unsigned)r[1]));
 }
 
-__device__ __forceinline__ float scale_of(float most) {
-  const float s = most * (1.0f / 448.0f);
-  return s < 0x1p-126f ? 0x1p-126f : s;
-}
-
-// x / scale, rounded once: the product with the rounded reciprocal is off by a unit of its last place, and what it leaves of
-// x, which a fused operation has exactly, puts that right.  So the codes are the formula's to the last one; rounding at
-// random carries a last place into a whole code now and then, and from there into scales (without the correction 20 of
-// 10^8 codes differ after a step).  What is left of x is no number of 32 bits where x is below 2^-103: small scales are
-// taken times 2^64 (by a factor, not a branch, which costs 11 registers: 512 us for 521), and else such an x has code 0
-// either way.  A scale that is infinite or NaN has no reciprocal: x / inf is 0.
-template <int N>
-__device__ __forceinline__ void divide(float (&x)[N], float scale) {
-  const float up = scale < 0x1p-60f ? 0x1p64f : 1.0f;
-  scale *= up;
-  const float by = 1.0f / scale, taken = by > 0.0f ? scale : 0.0f;
-#pragma unroll
-  for (int e = 0; e < N; ++e) {
-    x[e] *= up;
-    const float q = x[e] * by;
-    x[e] = __builtin_fmaf(__builtin_fmaf(-q, taken, x[e]), by, q);
-  }
-}
-
 // Four values in 8 bits.  By the hash the conversion adds `random` (its upper 20 bits, below the last digit that is
 // kept) and cuts off: sixteen bits of the hash, and a half behind them.
 __device__ __forceinline__ uint32_t codes_of(const float* x, bool at_random, const uint32_t* random) {
@@ -239,8 +215,10 @@ __device__ __forceinline__ void values_of(const Few<uint8_t, 4>& code, float* x)
 }
 
 // States in 8 bits: half a wave has a block, a lane four elements of each half of it, so that every store of the wave is
-// whole lines.  Moments, scales and codes are the header's formula, each operation rounded.  The parameter takes
-// the hardware's reciprocal, off by one unit of its last place (with a division 3 % more: vector operations then count).
+// whole lines.  Moments, scales and codes are the header's formula, each operation rounded: rounding at random carries a
+// last place into a whole code now and then, and from there into scales (200 of 10^8 codes a step, had products and sums
+// one rounding, and the quotient a last place to spare).  The parameter takes the hardware's reciprocal, off by one unit
+// of its last place (with a division 3 % more: vector operations then count).
 template <typename G, typename P>
 __device__ __forceinline__ void run_of_8(const Run& run, const AdamArgs& a) {
   constexpr int N = 4, U = 2, kApart = kBlock / U;
@@ -277,8 +255,8 @@ __device__ __forceinline__ void run_of_8(const Run& run, const AdamArgs& a) {
       most_m = max(most_m, magnitude(me)), most_v = max(most_v, __builtin_bit_cast(unsigned, ve));
     }
   }
-  const float new_ms = scale_of(most_of_32(most_m)), new_vs = scale_of(most_of_32(most_v));
-  divide(m, new_ms), divide(root, new_vs);
+  const float new_ms = scale_of(most_of_32(most_m), 1.0f / 448.0f), new_vs = scale_of(most_of_32(most_v), 1.0f / 448.0f);
+  divide<false>(m, new_ms), divide<false>(root, new_vs);
 #pragma unroll
   for (int e = 0; e < U * N; ++e) {
     m[e] = __builtin_amdgcn_fmed3f(m[e], -448.0f, 448.0f);

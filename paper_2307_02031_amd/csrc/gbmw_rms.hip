@@ -112,21 +112,21 @@ __device__ __forceinline__ unsigned lanes_max(unsigned x, int lanes) {
   return x;
 }
 
-// V values in 8 bits, four in a word.
+// V values over their scale in 8 bits, four in a word.
 template <int V>
-__device__ __forceinline__ void to_codes(const float (&x)[V], float by, bool whole_numbers, unsigned (&code)[V / 4]) {
+__device__ __forceinline__ void to_codes(const float (&x)[V], bool whole_numbers, unsigned (&code)[V / 4]) {
 #pragma unroll
   for (int i = 0; i < V / 4; ++i) {
     if (whole_numbers) {
       code[i] = 0;
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
-        const int n = (int)__builtin_fminf(__builtin_fmaxf(__builtin_rintf(x[4 * i + e] * by), -127.0f), 127.0f);
+        const int n = (int)__builtin_fminf(__builtin_fmaxf(__builtin_rintf(x[4 * i + e]), -127.0f), 127.0f);
         code[i] |= (unsigned)(n & 255) << (8 * e);
       }
     } else {
-      int word = __builtin_amdgcn_cvt_pk_fp8_f32(x[4 * i] * by, x[4 * i + 1] * by, 0, false);
-      code[i] = (unsigned)__builtin_amdgcn_cvt_pk_fp8_f32(x[4 * i + 2] * by, x[4 * i + 3] * by, word, true);
+      int word = __builtin_amdgcn_cvt_pk_fp8_f32(x[4 * i], x[4 * i + 1], 0, false);
+      code[i] = (unsigned)__builtin_amdgcn_cvt_pk_fp8_f32(x[4 * i + 2], x[4 * i + 3], word, true);
     }
   }
 }
@@ -198,7 +198,7 @@ __global__ __launch_bounds__((NT * kRows<NT, false>)) void k_rms_fwd(RmsArgs a) 
       }
     }
     if (!a.q) continue;
-    const float top = a.whole_numbers ? 127.0f : 448.0f;
+    const float per_top = a.whole_numbers ? 1.0f / 127.0f : 1.0f / 448.0f;
     unsigned most[NJ];
 #pragma unroll
     for (int j = 0; j < NJ; ++j) {
@@ -233,13 +233,13 @@ __global__ __launch_bounds__((NT * kRows<NT, false>)) void k_rms_fwd(RmsArgs a) 
 #pragma unroll
     for (int j = 0; j < NJ; ++j) {
       if (span[j].n == 0) continue;
-      const float most_f = __builtin_bit_cast(float, most[j]) / top;
-      const float scale = most_f < 0x1p-126f ? 0x1p-126f : most_f, by = 1.0f / scale;
+      const float scale = scale_of(__builtin_bit_cast(float, most[j]), per_top);
       if (a.group ? span[j].from % a.group == 0 : t == 0 && j == 0) scales[a.group ? span[j].from / a.group : 0] = scale;
       float y[V];
       normed(j, y);
+      divide<true>(y, scale);
       unsigned code[V / 4];
-      to_codes(y, by, a.whole_numbers, code);
+      to_codes(y, a.whole_numbers, code);
       // a piece that starts early has columns of another group: those are the piece's before it
       if (WHOLE || (span[j].n == V && span[j].c == span[j].from)) {
         __builtin_memcpy(out + span[j].c, code, V);
