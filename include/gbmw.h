@@ -592,8 +592,9 @@ int64_t gbmw_layer_norm_workspace(const gbmw_layer_norm_problem* p);
  * A list is made once for tensors that stay where they are: it copies the addresses and
  * sizes to the device and owns a workspace for the sums.  It holds no tensor alive.
  * numel[i] >= 0 elements of type in_dtype[i] at in[i]; out_dtype[i] is in_dtype[i] or
- * GBMW_F32; out[i] may be in[i] if the types are the same.  Making a list allocates and waits;
- * gbmw_clip_gradients does neither.  One list serves one stream at a time.
+ * GBMW_F32; out[i] may be in[i] if the types are the same.  out itself may be NULL, and out_dtype
+ * with it: the list is for the norm alone, and nothing else is written.  Making a list allocates and
+ * waits; gbmw_clip_gradients does neither.  One list serves one stream at a time.
  */
 typedef struct gbmw_gradient_list gbmw_gradient_list;
 
@@ -728,9 +729,11 @@ gbmw_status gbmw_rotary_frequencies(int32_t rot, double theta, int32_t scaling, 
  *   param = param * (1 - lr weight_decay) - (m / (sqrt(v) * (1 / sqrt(c2)) + eps)) * (lr / c1),
  * in fp32, each of these operations rounded to nearest (numbers that all elements share, factor, 1 - beta1,
  * lr / c1 and so on, are computed in fp64 and rounded once), param then to dtype.  `copy`, if
- * given, gets the new param (of GBMW_F32) rounded to copy_dtype.  norm is what gbmw_clip_gradients
- * wrote: with a list whose outputs are its inputs and max_norm +inf that call only computes it, and the
- * step clips as it reads.  If *norm is NaN or infinite the step is left out: nothing is written.
+ * given, gets the new param (of GBMW_F32) rounded to copy_dtype.  norm is that of grad * scale, what
+ * gbmw_clip_gradients writes with the same scale, of a list without outputs: that call leaves the
+ * gradients as they are, and the step scales and clips as it reads.  (A list whose outputs are its inputs
+ * scales them itself; the step's scale is then 1.)  If *norm is NaN or infinite the step is left
+ * out: nothing is written.
  *
  * States of 32 bits: m and v in fp32.  States of 8 bits: for each block of 256 elements of a
  * tensor (the last may have fewer) m is held as codes of GBMW_E4M3 with a scale, and so is

@@ -793,10 +793,13 @@ class GradientList:
             pass
 
 
-def gbmw_gradient_list_create(grads, outs=None) -> GradientList:
+def gbmw_gradient_list_create(grads, outs=None, norm_only: bool = False) -> GradientList:
     """A list of gradients (contiguous GPU tensors) and of the tensors that their clipped values go to, of the same
-    types or float32; by default the gradients themselves.  The tensors have to stay where they are."""
+    types or float32; by default the gradients themselves.  norm_only: the list is for the norm alone, and
+    gbmw_clip_gradients writes no tensor.  The tensors have to stay where they are."""
     grads = list(grads)
+    if norm_only and outs is not None:
+        _refuse("outputs of a list for the norm alone")
     outs = grads if outs is None else list(outs)
     if len(outs) != len(grads):
         _refuse(f"{len(grads)} gradients, {len(outs)} outputs")
@@ -809,15 +812,15 @@ def gbmw_gradient_list_create(grads, outs=None) -> GradientList:
     types = lambda ts: (ct.c_int32 * max(1, n))(*[_DTYPE.get(t.dtype, -1) for t in ts])
     numel = (ct.c_int64 * max(1, n))(*[g.numel() for g in grads])
     lst = GradientList()
-    _check(_lib.gbmw_gradient_list_create(n, pointers(grads), pointers(outs), numel, types(grads), types(outs),
-                                          ct.byref(lst.handle)))
+    _check(_lib.gbmw_gradient_list_create(n, pointers(grads), None if norm_only else pointers(outs), numel, types(grads),
+                                          None if norm_only else types(outs), ct.byref(lst.handle)))
     lst._keep = (grads, outs)
     return lst
 
 
 @_on_stream
 def gbmw_clip_gradients(lst: GradientList, max_norm: float, scale: float = 1.0, norm=None):
-    """Writes the list's outputs; returns the norm before clipping, a float32 GPU tensor [1] (norm, if given).
+    """Writes the list's outputs, if it has any; returns the norm before clipping, a float32 GPU tensor [1] (norm, if given).
     stream=: as everywhere."""
     if norm is None:
         norm = torch.empty(1, dtype=torch.float32, device="cuda")
@@ -1102,7 +1105,8 @@ def _scalar_now(name: str, t, dtype) -> int:
 def gbmw_adamw_step(lst: AdamWList, lr, step, beta1: float = 0.9, beta2: float = 0.999, eps: float = 1e-8,
                     scale: float = 1.0, norm=None, max_norm: float = float("inf"), seed: int = 0) -> None:
     """One step of the list's parameters and states.  lr: a number, or a float32 GPU tensor that is read when the step
-    runs; step: the step's number from 1 on, or an int64 GPU tensor.  norm: what gbmw_clip_gradients returned: the
+    runs; step: the step's number from 1 on, or an int64 GPU tensor.  scale: of the gradients, the inverse of a loss scale.
+    norm: of the gradients times scale, what gbmw_clip_gradients returned for a list with norm_only and the same scale: the
     gradients are clipped to max_norm as they are read, and the step is left out where it is not finite.  seed: of the
     rounding of states of 8 bits, 0 for the nearest.  stream=: as everywhere."""
     o = gbmw_adamw_options(0.0, beta1, beta2, eps, scale, max_norm, 1, seed & 0xFFFFFFFF)

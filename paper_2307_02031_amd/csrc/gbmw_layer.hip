@@ -527,6 +527,7 @@ extern "C" gbmw_status gbmw_layer_norm_backward(const gbmw_layer_norm_problem* p
 struct gbmw_gradient_list {
   gbmw_detail::DevBuf buf;   // partial sums | pieces
   int count = 0, device = 0;
+  bool writes = true;        // else it is for the norm alone
   double* partial() const { return (double*)buf.p; }
   Piece* pieces() const { return (Piece*)((char*)buf.p + 8 * kNormGroups); }
 };
@@ -537,8 +538,10 @@ extern "C" gbmw_status gbmw_gradient_list_create(int32_t n, const void* const* i
   gbmw_detail::clear_error();
   if (!list) return fail(GBMW_ERR_INVALID_ARG, "null list");
   *list = nullptr;
-  if (n < 0 || (n > 0 && (!in || !out || !numel || !in_dtype || !out_dtype)))
+  if (n < 0 || (n > 0 && (!in || !numel || !in_dtype || (out && !out_dtype))))
     return fail(GBMW_ERR_INVALID_ARG, "n=%d, or a null array", n);
+  const bool writes = out;
+  if (!writes) out = const_cast<void* const*>(in), out_dtype = in_dtype;
   int64_t count = 0;
   for (int i = 0; i < n; ++i) {
     if (!known_dtype(in_dtype[i])) return fail(GBMW_ERR_INVALID_ARG, "in_dtype[%d]=%d", i, in_dtype[i]);
@@ -562,7 +565,7 @@ extern "C" gbmw_status gbmw_gradient_list_create(int32_t n, const void* const* i
         pieces.push_back({(const char*)in[i] + at * element_size(in_dtype[i]), (char*)out[i] + at * element_size(out_dtype[i]),
                           (int32_t)std::min(kPiece, numel[i] - at), in_dtype[i], out_dtype[i], 0});
     gbmw_gradient_list* l = new gbmw_gradient_list;
-    l->count = (int)count;
+    l->count = (int)count, l->writes = writes;
     const size_t head = 8 * kNormGroups;
     gbmw_status st = l->buf.reserve(head + sizeof(Piece) * (size_t)count);
     if (st == GBMW_OK) {
@@ -599,8 +602,9 @@ extern "C" gbmw_status gbmw_clip_gradients(gbmw_gradient_list* l, float max_norm
   hipStream_t st = (hipStream_t)stream;
   const dim3 grid(std::max(1, std::min(l->count, kNormGroups))), block(256);
   hipLaunchKernelGGL(k_clip_norm, grid, block, 0, st, l->pieces(), l->count, l->partial());
-  hipLaunchKernelGGL(k_clip_scale, grid, block, 0, st, l->pieces(), l->count, l->partial(), (int)grid.x, (double)max_norm,
-                     (double)scale, norm);
+  // without outputs one workgroup writes the norm
+  hipLaunchKernelGGL(k_clip_scale, l->writes ? grid : dim3(1), block, 0, st, l->pieces(), l->writes ? l->count : 0, l->partial(),
+                     (int)grid.x, (double)max_norm, (double)scale, norm);
   HIP_TRY(hipGetLastError());
   return GBMW_OK;
 }

@@ -129,7 +129,7 @@ class Layer:
         scales = lambda: {n: torch.zeros((self.w[n].numel() + 255) // 256, device="cuda") for n in names}
         self.param, self.m, self.v, self.steps = wide, zeros(), zeros(), 0
         self.m_scale, self.v_scale = (scales(), scales()) if state_bits == 8 else ({}, {})
-        self.norm_list = g.gbmw_gradient_list_create(self.grad.values())
+        self.norm_list = g.gbmw_gradient_list_create(self.grad.values(), norm_only=True)
         self.adamw = g.gbmw_adamw_list_create(
             wide.values(), [self.grad[n] for n in names], self.m.values(), self.v.values(),
             m_scales=self.m_scale.values() if state_bits == 8 else None,
