@@ -1109,7 +1109,9 @@ def gbmw_adamw_step(lst: AdamWList, lr, step, beta1: float = 0.9, beta2: float =
     norm: of the gradients times scale, what gbmw_clip_gradients returned for a list with norm_only and the same scale: the
     gradients are clipped to max_norm as they are read, and the step is left out where it is not finite.  seed: of the
     rounding of states of 8 bits, 0 for the nearest.  stream=: as everywhere."""
-    o = gbmw_adamw_options(0.0, beta1, beta2, eps, scale, max_norm, 1, seed & 0xFFFFFFFF)
+    if not 0 <= seed < 1 << 32:
+        _refuse(f"seed={seed} is not in 0..2^32 - 1")       # its lower bits alone may be 0, which rounds to the nearest
+    o = gbmw_adamw_options(0.0, beta1, beta2, eps, scale, max_norm, 1, seed)
     if isinstance(lr, torch.Tensor):
         o.lr_now = _scalar_now("lr", lr, torch.float32)
     else:

@@ -37,17 +37,18 @@ struct Run {   // elements of one tensor
 struct Rates {
   double lr;
   float grad, b1, a1, b2, a2, eps, lr_c1, root_c2;
-  uint32_t key;   // of the random numbers; 0: round to nearest
+  uint32_t key;   // of the random numbers
 };
 
 struct AdamArgs {
   Rates r;   // of the numbers that the host knows
   double beta1, beta2, scale, max_norm, c1;
-  uint32_t seed;
+  uint32_t seed;   // 0: round to nearest
   const float *norm, *lr_now;
   const int64_t* step_now;
 };
 
+// The multipliers are xxHash's published primes; what a hash of 0 is (0) is a key like any other.
 constexpr uint32_t kHashBy = 0x9E3779B1u;
 __host__ __device__ __forceinline__ uint32_t hash_rest(uint32_t x) {
   x = (x ^ (x >> 15)) * 0x85EBCA77u;
@@ -56,7 +57,7 @@ __host__ __device__ __forceinline__ uint32_t hash_rest(uint32_t x) {
 __host__ __device__ __forceinline__ uint32_t hash(uint32_t x) { return hash_rest(x * kHashBy); }
 
 __host__ __device__ __forceinline__ uint32_t key_of(uint32_t seed, int64_t step) {
-  return seed ? hash(seed + (uint32_t)step * 0x9E3779B9u) : 0;
+  return hash(seed + (uint32_t)step * 0x9E3779B9u);
 }
 
 __host__ __device__ __forceinline__ double power(double x, int64_t n) {
@@ -263,7 +264,7 @@ __device__ __forceinline__ void run_of_8(const Run& run, const AdamArgs& a) {
     root[e] = root[e] > 0.0f ? __builtin_amdgcn_fmed3f(root[e], 0x1p-9f, 448.0f) : 0.0f;
   }
   uint32_t high[U * N] = {}, low[U * N] = {};
-  if (r.key) {
+  if (a.seed) {
 #pragma unroll
     for (int u = 0; u < U; ++u) {
       // hash(place ^ key) with its first product taken apart: the place of the lane's four, and the two bits below it
@@ -278,7 +279,7 @@ __device__ __forceinline__ void run_of_8(const Run& run, const AdamArgs& a) {
 #pragma unroll
   for (int u = 0; u < U; ++u) {
     const int at = i + u * kApart, n = run.n - at;
-    const uint32_t mw = codes_of(m + u * N, r.key, high + u * N), vw = codes_of(root + u * N, r.key, low + u * N);
+    const uint32_t mw = codes_of(m + u * N, a.seed != 0, high + u * N), vw = codes_of(root + u * N, a.seed != 0, low + u * N);
     if (n <= 0) continue;
     store(run.m, at, bytes_of(mw), n);
     store(run.v, at, bytes_of(vw), n);

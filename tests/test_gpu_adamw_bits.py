@@ -125,3 +125,22 @@ def test_an_infinite_scale():
     assert abs(float(m[1].float()) + 0.3 * 448) <= 16       # 134.4 lies between codes 16 apart
     held = v.float() * vs
     assert not bool(torch.isfinite(held).any())
+
+
+def test_a_key_of_0():
+    """A seed that step and multiplier bring to 0 rounds at random like any other."""
+    import paper_2307_02031_amd as g
+    n, step = 5000, 7
+    seed = -step * 0x9E3779B9 & 0xFFFFFFFF
+    assert seed != 0 and _hash((seed + step * 0x9E3779B9) & 0xFFFFFFFF) == 0
+    room = -(-n // 256) * 256
+    grad = torch.randn(room, generator=torch.Generator().manual_seed(2)).cuda()
+    grad[n:] = 0.0
+    t = dict(m=torch.zeros(room, device="cuda").to(F8), v=torch.zeros(room, device="cuda").to(F8),
+             m_scale=torch.zeros(room // 256, device="cuda"), v_scale=torch.zeros(room // 256, device="cuda"))
+    got = {k: x.clone() for k, x in t.items()}
+    lst = g.gbmw_adamw_list_create([torch.zeros(n, device="cuda")], [grad[:n]], [got["m"][:n]], [got["v"][:n]], m_scales=[got["m_scale"]],
+                                   v_scales=[got["v_scale"]])
+    g.gbmw_adamw_step(lst, 1e-4, step, seed=seed, **HOW)
+    _step(t, grad, torch.arange(room, device="cuda"), step, seed)
+    _same(t, got, n, "key 0")
