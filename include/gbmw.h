@@ -746,10 +746,12 @@ gbmw_status gbmw_rotary_frequencies(int32_t rot, double theta, int32_t scaling, 
  * bits of a hash of seed, step and the element's place in the list (the same call gives the same
  * bits): up (away from 0) where what is cut off, in steps of the code, and (bits + 1/2) / 65536 are 1
  * or more together.  The bits are the upper ones, for m, and the lower ones, for r, of
- *   hash(place ^ hash(seed + step * 0x9E3779B9)),  hash(x): x *= 0x9E3779B1,
- *   x = (x ^ x >> 15) * 0x85EBCA77, x ^ x >> 13, all of it modulo 2^32,
- * place being 256 for each block of the tensors before, and the element's number.  Rounding to nearest leaves a moment unchanged for ever that moves by less than half a
- * step (up to 6 %) at a time.  r > 0 is never held as 0, which would let m / r grow without bound.
+ *   hash(place ^ key),  key = hash(seed + step * 0x9E3779B9),
+ *   hash(x): x *= 0x9E3779B1, x = (x ^ x >> 15) * 0x85EBCA77, x ^ x >> 13, all of it modulo 2^32,
+ * place being 256 for each block of the tensors before, and the element's number; from place 2^32
+ * on, the upper part `high` of a place goes into the key, which is then hash(key + high * 0x9E3779B9).
+ * Rounding to nearest leaves a moment unchanged for ever that moves by less than half a step (up to
+ * 6 %) at a time.  r > 0 is never held as 0, which would let m / r grow without bound.
  * Zeroed codes and scales are states before the first step.  A NaN or an infinity in a
  * gradient leaves no state of its block finite.
  *

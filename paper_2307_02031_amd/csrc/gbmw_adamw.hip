@@ -27,10 +27,13 @@ struct Run {   // elements of one tensor
   const void* grad;
   void *param, *copy, *m, *v;
   float *m_scale, *v_scale;
+  int64_t block;    // number of the run's first block in the list
   int32_t n;
-  uint32_t block;   // number of the run's first block in the list
-  int32_t grad_dtype, dtype, copy_dtype;
+  uint32_t types;   // the gradient's, the parameter's << 8, the copy's << 16
   float decay;
+  __device__ __forceinline__ int grad_type() const { return types & 255; }
+  __device__ __forceinline__ int type() const { return types >> 8 & 255; }
+  __device__ __forceinline__ int copy_type() const { return types >> 16; }
 };
 
 // The numbers that all elements share: computed in fp64, rounded once.
@@ -55,6 +58,9 @@ __host__ __device__ __forceinline__ uint32_t hash_rest(uint32_t x) {
   return x ^ (x >> 13);
 }
 __host__ __device__ __forceinline__ uint32_t hash(uint32_t x) { return hash_rest(x * kHashBy); }
+
+// The key of a step, and of the places of 32 bits that have `high` above them, if that is not 0.
+__device__ __forceinline__ uint32_t key_above(uint32_t key, uint32_t high) { return high ? hash(key + high * 0x9E3779B9u) : key; }
 
 __host__ __device__ __forceinline__ uint32_t key_of(uint32_t seed, int64_t step) {
   return hash(seed + (uint32_t)step * 0x9E3779B9u);
@@ -134,7 +140,7 @@ __device__ __forceinline__ void store(void* p, int64_t i, const Few<T, N>& x, in
 template <int N>
 __device__ __forceinline__ void store_copy(const Run& run, int i, const float (&p)[N], int n) {
   if (!run.copy) return;
-  if (run.copy_dtype == GBMW_F16) {
+  if (run.copy_type() == GBMW_F16) {
     Few<f16, N> c;
 #pragma unroll
     for (int e = 0; e < N; ++e) c.v[e] = (f16)p[e];
@@ -265,13 +271,16 @@ __device__ __forceinline__ void run_of_8(const Run& run, const AdamArgs& a) {
   }
   uint32_t high[U * N] = {}, low[U * N] = {};
   if (a.seed) {
+    const int64_t block = run.block + k;
+    const uint32_t key = key_above(r.key, (uint32_t)(block >> 24)), first = (uint32_t)block * kBlock + lane * N;
+    static_assert(kBlock == 256, "");
 #pragma unroll
     for (int u = 0; u < U; ++u) {
       // hash(place ^ key) with its first product taken apart: the place of the lane's four, and the two bits below it
-      const uint32_t base = (((run.block + k) * kBlock + u * kApart + lane * N) ^ (r.key & ~3u)) * kHashBy;
+      const uint32_t base = ((first + u * kApart) ^ (key & ~3u)) * kHashBy;
 #pragma unroll
       for (int e = 0; e < N; ++e) {
-        const uint32_t word = hash_rest(base + (e ^ (r.key & 3u)) * kHashBy);
+        const uint32_t word = hash_rest(base + (e ^ (key & 3u)) * kHashBy);
         high[u * N + e] = (word & 0xffff0000u) | 0x8000, low[u * N + e] = word << 16 | 0x8000;
       }
     }
@@ -300,8 +309,8 @@ __device__ __forceinline__ void run_of(const Run& run, const AdamArgs& a) {
 
 template <bool BITS8, typename G>
 __device__ __forceinline__ void run_of(const Run& run, const AdamArgs& a) {
-  if (run.dtype == GBMW_F32) run_of<BITS8, G, float>(run, a);
-  else if (run.dtype == GBMW_F16) run_of<BITS8, G, f16>(run, a);
+  if (run.type() == GBMW_F32) run_of<BITS8, G, float>(run, a);
+  else if (run.type() == GBMW_F16) run_of<BITS8, G, f16>(run, a);
   else run_of<BITS8, G, bf16>(run, a);
 }
 
@@ -313,8 +322,8 @@ __global__ __launch_bounds__(kThreads<BITS8>) void k_adamw(const Run* runs, Adam
   unsigned id = blockIdx.x;
   if ((id | (kAll - 1)) < gridDim.x) id = (id & ~(kAll - 1)) | ((id & 7) << kLot) | ((id >> 3) & ((1u << kLot) - 1));
   const Run run = runs[id];
-  if (run.grad_dtype == GBMW_F32) run_of<BITS8, float>(run, a);
-  else if (run.grad_dtype == GBMW_F16) run_of<BITS8, f16>(run, a);
+  if (run.grad_type() == GBMW_F32) run_of<BITS8, float>(run, a);
+  else if (run.grad_type() == GBMW_F16) run_of<BITS8, f16>(run, a);
   else run_of<BITS8, bf16>(run, a);
 }
 
@@ -402,7 +411,7 @@ extern "C" gbmw_status gbmw_adamw_list_create(int32_t n, const gbmw_adamw_tensor
     if (bad >= 0) return fail(GBMW_ERR_INVALID_ARG, "tensor %d: an array overlaps another, and one of them is written", bad);
     std::vector<Run> runs;
     runs.reserve((size_t)count);
-    uint32_t block = 0;
+    int64_t block = 0;
     for (int i = 0; i < n; ++i) {
       const gbmw_adamw_tensor& t = tensors[i];
       const int gs = element_size(t.grad_dtype), ps = element_size(t.dtype), ss = state_bits == 8 ? 1 : 4;
@@ -413,11 +422,11 @@ extern "C" gbmw_status gbmw_adamw_list_create(int32_t n, const gbmw_adamw_tensor
         r.m = (char*)t.m + at * ss, r.v = (char*)t.v + at * ss;
         if (state_bits == 8) r.m_scale = t.m_scale + at / kBlock, r.v_scale = t.v_scale + at / kBlock;
         r.n = (int32_t)std::min<int64_t>(kRun, t.numel - at);
-        r.block = block + (uint32_t)(at / kBlock);
-        r.grad_dtype = t.grad_dtype, r.dtype = t.dtype, r.copy_dtype = t.copy_dtype, r.decay = t.weight_decay;
+        r.block = block + at / kBlock, r.decay = t.weight_decay;
+        r.types = t.grad_dtype | t.dtype << 8 | (t.copy ? t.copy_dtype << 16 : 0);
         runs.push_back(r);
       }
-      block += (uint32_t)((t.numel + kBlock - 1) / kBlock);
+      block += (t.numel + kBlock - 1) / kBlock;
     }
     gbmw_adamw_list* l = new gbmw_adamw_list;
     l->count = count, l->bits = state_bits;
