@@ -618,8 +618,11 @@ void gbmw_gradient_list_destroy(gbmw_gradient_list* list);
  * and group of `group` columns (the last may have fewer; one group a row if group is 0)
  *   scale = max(largest |y| * (1 / top), 2^-126),  q = y / scale rounded to nearest even,
  * with top 448 for GBMW_E4M3 and 127 for GBMW_I8 (whose codes are whole numbers from -127
- * to 127), y = (h * rstd) * weight, 1 / top and the quotient rounded to fp32.  A NaN in a group makes its scale NaN, and every value of a row that holds a NaN or
- * an infinity is one, so its scales are too; GBMW_I8's codes are then without meaning.
+ * to 127), y = (h * rstd) * weight, 1 / top and the quotient rounded to fp32.  A NaN in a group
+ * makes its scale NaN, and GBMW_I8's codes are then without meaning.  A row that holds a NaN is NaN
+ * throughout, with its scales.  A row that holds an infinity has rstd = 0: the infinity becomes NaN,
+ * and its group's scale with it, but the row's other values become 0, and the scales of their groups
+ * 2^-126; rstd tells.
  * Backward, from dy (the gradient of y, or of the values that q stands for), h and rstd as
  * the forward call left them (x if there was no residual), with g = dy * weight:
  *   dx = (g - xhat sum(g xhat) / cols) rstd + dres,  xhat = h rstd,
@@ -627,7 +630,7 @@ void gbmw_gradient_list_destroy(gbmw_gradient_list* list);
  * dx is the gradient of x and of the residual; dres (NULL: zeros) is the one that reaches h
  * past the norm.  weight may be NULL (ones), dweight may be NULL (not wanted).
  * y or h may be x or residual, and dx may be dy or dres, with the same row stride.
- * Squares are summed in fp32: rows with values beyond about 1e18 have rstd = 0.
+ * Squares are summed in fp32: rows with values beyond about 1e18 have rstd = 0, and are 0.
  */
 enum { GBMW_E4M3 = 3, GBMW_I8 = 4 };
 
