@@ -144,3 +144,25 @@ def test_a_key_of_0():
     g.gbmw_adamw_step(lst, 1e-4, step, seed=seed, **HOW)
     _step(t, grad, torch.arange(room, device="cuda"), step, seed)
     _same(t, got, n, "key 0")
+
+
+@pytest.mark.parametrize("seed", [0, 4])
+@pytest.mark.parametrize("bad", [float("nan"), float("inf"), float("-inf")])
+def test_no_state_of_a_block_stays_finite(bad, seed):
+    """A NaN or an infinity in a gradient: both moments' scales, and every value that is held, of its block; none of the others."""
+    import paper_2307_02031_amd as g
+    n = 1000
+    grad = torch.randn(n, generator=torch.Generator().manual_seed(1)).cuda()
+    grad[300] = bad
+    m, v = (torch.zeros(n, dtype=torch.uint8, device="cuda").view(F8) for _ in range(2))
+    ms, vs, p = torch.zeros(4, device="cuda"), torch.zeros(4, device="cuda"), torch.zeros(n, device="cuda")
+    lst = g.gbmw_adamw_list_create([p], [grad], [m], [v], m_scales=[ms], v_scales=[vs])
+    its = torch.arange(n, device="cuda") // 256 == 1
+    for step in (1, 2, 3):      # the first from zeros, then from what it left, also with gradients that are fine
+        g.gbmw_adamw_step(lst, 1e-3, step, seed=seed, **HOW)
+        for code, scale in ((m, ms), (v, vs)):
+            held = code.float() * scale.repeat_interleave(256)[:n]
+            assert not bool(torch.isfinite(held[its]).any()) and bool(torch.isfinite(held[~its]).all()), step
+            assert torch.isfinite(scale).tolist() == [True, False, True, True], step
+        assert bool(torch.isfinite(p[~its]).all()) and not bool(torch.isfinite(p[300]))
+        grad[300] = 1.0
