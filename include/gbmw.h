@@ -684,12 +684,11 @@ int64_t gbmw_rms_norm_workspace(const gbmw_rms_norm_problem* p);
  * in fp64, so positions may be any int32.
  * q_out may be q and k_out may be k, with the same strides (in place); an array given
  * in place must have all its elements at different places.  k and k_out may be NULL (Hk 0).
- * Layouts and strides are attention's.  GBMW_ERR_UNSUPPORTED: arrays of 64 GB or more that
- * take more waves than a launch has.
+ * Layouts and strides are attention's.
  */
 typedef struct {
   int32_t dtype;             /* of all arrays                                        */
-  int32_t B, L;              /* samples and rows, >= 0                               */
+  int32_t B, L;              /* samples and rows, >= 0, together below 2^31 - 64     */
   int32_t Hq, Hk;            /* heads: Hq >= 1, Hk >= 0                              */
   int32_t D;                 /* head size, 1..512                                    */
   int32_t rot;               /* even, 0..D                                           */

@@ -8,12 +8,14 @@ namespace {
 
 constexpr int kMostPairs = 256;
 constexpr int kTable = 512;    // angles of a wave
+constexpr int64_t kMostWaves = (1 << 26) - 8;   // of a launch, whose threads are counted in 32 bits
 
 struct RotaryArgs {
   int B, L, Hq, H, D, rot;   // H: query and key heads
   int pairs;                 // rot / 2
   int turning, pieces;       // pieces of a head that turn, and those with the ones that are handed through
   int tokens, heads, chunks; // of a wave: tokens and heads; waves that share a token's heads
+  int begin;                 // the launch's first token
   unsigned units;            // waves' worth of work
   Divisor of_chunk, of_head, of_row, of_pairs;
   float factor, sign;
@@ -99,7 +101,7 @@ __global__ __launch_bounds__(256) void k_rotary(RotaryArgs a) {
   const unsigned unit = blockIdx.x * 4 + wave;
   if (unit >= a.units) return;
   const int group = a.of_chunk.of((int)unit), chunk = (int)unit - group * a.chunks;
-  const int first = group * a.tokens, here = min(a.tokens, a.B * a.L - first), first_head = chunk * a.heads;
+  const int first = a.begin + group * a.tokens, here = min(a.tokens, a.B * a.L - first), first_head = chunk * a.heads;
   const int items = ONE ? min(a.heads, a.H - first_head) : here * a.H;
   float(*angles)[kTable] = table[wave];
   if constexpr (ONE) {
@@ -268,9 +270,6 @@ gbmw_status rotary(const gbmw_rotary_problem* p, float sign) {
   a.heads = a.tokens > 1 ? a.H : std::min(a.H, items);
   a.chunks = (a.H + a.heads - 1) / a.heads;
   a.heads = (a.H + a.chunks - 1) / a.chunks;
-  const int64_t units = (tokens + a.tokens - 1) / a.tokens * a.chunks;
-  if (units > (1 << 26) - 8) return fail(GBMW_ERR_UNSUPPORTED, "too many rows and heads: %lld waves", (long long)units);
-  a.units = (unsigned)units;
   a.of_chunk = divisor(a.chunks), a.of_head = divisor(a.H), a.of_row = divisor(p->L), a.of_pairs = divisor(std::max(1, a.pairs));
   // Loads and stores pass the cache by where it would not hold the results for who reads them next, and where a wave's
   // stores are whole lines of it.  With the attention that reads them, bytes read and written, through the cache and past
@@ -284,9 +283,14 @@ gbmw_status rotary(const gbmw_rotary_problem* p, float sign) {
                       through % (2 * line) == 0 && lines(p->q_out, p->q_out_stride) &&
                       (!p->Hk || lines(p->k_out, p->k_out_stride));
   hipStream_t st = (hipStream_t)p->stream;
-  if (p->dtype == GBMW_F32) return launch_rotary<float>(a, W, p->interleaved, stream, st);
-  if (p->dtype == GBMW_F16) return launch_rotary<f16>(a, W, p->interleaved, stream, st);
-  return launch_rotary<bf16>(a, W, p->interleaved, stream, st);
+  const int64_t per = kMostWaves / a.chunks * a.tokens;   // tokens of a launch
+  for (int64_t begin = 0; begin < tokens; begin += per) {
+    a.begin = (int)begin, a.units = (unsigned)((std::min(per, tokens - begin) + a.tokens - 1) / a.tokens * a.chunks);
+    if (p->dtype == GBMW_F32) CHECK(launch_rotary<float>(a, W, p->interleaved, stream, st));
+    else if (p->dtype == GBMW_F16) CHECK(launch_rotary<f16>(a, W, p->interleaved, stream, st));
+    else CHECK(launch_rotary<bf16>(a, W, p->interleaved, stream, st));
+  }
+  return GBMW_OK;
 }
 
 }  // namespace
