@@ -28,10 +28,11 @@ struct RotaryArgs {
 };
 
 // cos and sin of 2 pi x, |x| <= 1/2, by the quarter turn that x is nearest and the Taylor series of the
-// rest (at most pi / 4; the first term left out is below 2^-28 of the result).
-__device__ __forceinline__ void turn_of(float x, float& c, float& s) {
-  const float quarter = __builtin_rintf(4.0f * x);
-  const float r = 6.28318530717958648f * __builtin_fmaf(-0.25f, quarter, x), r2 = r * r;
+// rest (at most pi / 4; the first term left out is below 2^-28 of the result).  The rest is taken in fp64 and rounded
+// to fp32 last: rounded before, half a turn less 10^-9 would be half a turn, and angles off by up to 2^-23.
+__device__ __forceinline__ void turn_of(double x, float& c, float& s) {
+  const double quarter = __builtin_rint(4.0 * x);
+  const float r = (float)(6.28318530717958648 * __builtin_fma(-0.25, quarter, x)), r2 = r * r;
   const float sn = r + r * r2 * (-1.0f / 6 + r2 * (1.0f / 120 + r2 * (-1.0f / 5040 + r2 * (1.0f / 362880))));
   const float cs = 1.0f + r2 * (-0.5f + r2 * (1.0f / 24 + r2 * (-1.0f / 720 + r2 * (1.0f / 40320 - r2 * (1.0f / 3628800)))));
   const int n = (int)quarter & 3;
@@ -134,7 +135,7 @@ __global__ __launch_bounds__(256) void k_rotary(RotaryArgs a) {
         const int position = a.positions ? a.positions[b * a.ps + row] : row;
         const double angle = (double)position * (a.freq[i - t * a.pairs] * 0.15915494309189533577);
         float c, s;
-        turn_of((float)(angle - __builtin_rint(angle)), c, s);
+        turn_of(angle - __builtin_rint(angle), c, s);
         angles[0][i] = c * a.factor, angles[1][i] = s * a.factor * a.sign;
       }
       __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
