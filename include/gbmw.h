@@ -629,7 +629,8 @@ void gbmw_gradient_list_destroy(gbmw_gradient_list* list);
  *   dweight = sum over rows of dy xhat.
  * dx is the gradient of x and of the residual; dres (NULL: zeros) is the one that reaches h
  * past the norm.  weight may be NULL (ones), dweight may be NULL (not wanted).
- * y or h may be x or residual, and dx may be dy or dres, with the same row stride.
+ * y or h may be x or residual, and dx may be dy or dres, with the same row stride.  A y over x
+ * without a residual leaves no h for a backward call.
  * Squares are summed in fp32: rows with values beyond about 1e18 have rstd = 0, and are 0.
  */
 enum { GBMW_E4M3 = 3, GBMW_I8 = 4 };

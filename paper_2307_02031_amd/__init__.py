@@ -878,7 +878,7 @@ def gbmw_rms_norm_forward(x, weight=None, eps: float = 1e-5, residual=None, qtyp
                           want_y: bool = True, y=None, h=None, q=None):
     """RmsNorm(y, h, rstd, q, scale) of x, a float32, float16 or bfloat16 GPU tensor whose last axis is normed, after
     the addition of residual, if there is one.  weight: of x's type or float32.  y: like x, None unless want_y.
-    h: x + residual (x itself without a residual).  rstd: float32 of x's shape without its last axis.  qtype
+    h: x + residual; without a residual x itself, or None where y is written over it (no backward call can follow).  rstd: float32 of x's shape without its last axis.  qtype
     (torch.float8_e4m3fn or torch.int8): q holds y in 8 bits, with scale (float32, of x's shape but for the last axis)
     for each row, or for each `group` (32, 64 or 128) columns; None without a qtype.  y, h, q: made here unless given (y
     or h may be x or residual).  stream=: as everywhere.  Not recorded by autograd: gradients come from
@@ -900,7 +900,7 @@ def gbmw_rms_norm_forward(x, weight=None, eps: float = 1e-5, residual=None, qtyp
             p.h, p.h_stride = _rows("h", h, device, dtype, shape)
     elif h is not None:
         _refuse("h without a residual is x")
-    else:
+    elif y is None or y.data_ptr() != x.data_ptr() or not p.rows:
         h = x
     scale = None
     if qtype is not None:
