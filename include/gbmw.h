@@ -683,9 +683,9 @@ int64_t gbmw_rms_norm_workspace(const gbmw_rms_norm_problem* p);
  * Row r of sample b has position positions[b * position_stride + r], or r if positions is
  * NULL.  Rows from len[b] on are neither read nor written.  Angles are computed and reduced
  * in fp64, so positions may be any int32.
- * q_out may be q and k_out may be k, with the same strides (in place); an array given
- * in place must have all its elements at different places.  k and k_out may be NULL (Hk 0).
- * Layouts and strides are attention's.
+ * q_out may be q and k_out may be k, with the same strides (in place), but neither may be the
+ * other input; an array given in place must have all its elements at different places.  k and k_out
+ * may be NULL (Hk 0).  Layouts and strides are attention's.
  */
 typedef struct {
   int32_t dtype;             /* of all arrays                                        */

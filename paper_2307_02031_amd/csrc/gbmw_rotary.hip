@@ -249,6 +249,8 @@ gbmw_status rotary(const gbmw_rotary_problem* p, float sign) {
     if (p->k == p->k_out && !std::equal(p->k_stride, p->k_stride + 3, p->k_out_stride))
       return fail(GBMW_ERR_INVALID_ARG, "k_out is k, with other strides");
     if (p->k_out == p->q_out) return fail(GBMW_ERR_INVALID_ARG, "q_out and k_out are one array");
+    if (p->q_out == p->k) return fail(GBMW_ERR_INVALID_ARG, "q_out is k");   // of which heads are still to be read
+    if (p->k_out == p->q) return fail(GBMW_ERR_INVALID_ARG, "k_out is q");
     in_place = in_place && p->k == p->k_out;
   }
   RotaryArgs a{};
