@@ -1067,7 +1067,7 @@ def gbmw_adamw_list_create(params, grads, m, v, m_scales=None, v_scales=None, co
                      ("copies", copies), ("weight_decay", decay)):
         if len(ts) != n:
             _refuse(f"{n} parameters, {len(ts)} {name}")
-    if bits == 32 and not (m_scales is None and v_scales is None):
+    if bits == 32 and n and not (m_scales is None and v_scales is None):
         _refuse("states of 32 bits have no scales")
     tensors = (gbmw_adamw_tensor * max(1, n))()
     for i, t in enumerate(tensors[:n]):
