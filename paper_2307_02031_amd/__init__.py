@@ -12,7 +12,7 @@ enqueued on ``torch.cuda.current_stream()`` unless a stream is given.
 """
 from __future__ import annotations
 
-import collections
+import collections.abc
 import ctypes as ct
 import functools
 import operator
@@ -1062,7 +1062,8 @@ def gbmw_adamw_list_create(params, grads, m, v, m_scales=None, v_scales=None, co
     bits = 8 if wide == torch.float8_e4m3fn else 32
     scales = [list(s) if s is not None else [None] * n for s in (m_scales, v_scales)]
     copies = [None] * n if copies is None else list(copies)
-    decay = list(weight_decay) if isinstance(weight_decay, (list, tuple)) else [weight_decay] * n
+    decay = list(weight_decay) if isinstance(weight_decay, collections.abc.Iterable) and not hasattr(weight_decay, "__float__") \
+        else [weight_decay] * n
     for name, ts in (("gradients", grads), ("m", m), ("v", v), ("m_scales", scales[0]), ("v_scales", scales[1]),
                      ("copies", copies), ("weight_decay", decay)):
         if len(ts) != n:
