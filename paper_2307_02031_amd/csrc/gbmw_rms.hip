@@ -380,14 +380,17 @@ gbmw_status check_rms(const gbmw_rms_norm_problem* p) {
 
 // As layer norm's, and: 16 threads where a row of up to 48 pieces fits them (not where a scale has columns of
 // more threads than these), 128 where 256 would leave many without a piece, 512 between the rows of 256 and those of 1024.
-// Backward 320 with 16-bit values (16384 x 5120 125 us, with three pieces of 256 threads 130; forward 117 and 112, 8192 x
-// 2560 in 32 bits 62 and 60).
+// Backward 320 for 4097 to 5120 16-bit values, where they beat three pieces of 256 threads: up to 512 rows, which have a workgroup
+// each (512 x 4608 12.9 us for 14.2, 4609 14.2 for 14.8, 5120 the same), and from 2048 rows on of whole pieces (16384
+// x 4104 110 for 117, 4608 111 for 114, 5120 119 for 124; 2048 x 5120 25.9 for 26.8).  Not in between (1500 x 5120 24.9 for
+// 22.7), nor where rows share pieces (16384 x 4609 153 for 140, 2048 x 5119 30.9 for 28.2); forward 117 for 112, 8192 x 2560
+// in 32 bits 62 for 60.
 Shape rms_shape(const gbmw_rms_norm_problem* p, bool backward) {
   const int vec = 16 / element_size(p->dtype), n = (p->cols + vec - 1) / vec;
   if (n <= 16 || (n <= 3 * 16 && (backward || !p->q || p->group <= 16 * vec))) return {16, (n + 15) / 16};
   if (n <= 3 * 64) return {64, (n + 63) / 64};
   if (n > 2 * 128 && n <= 3 * 128) return {128, 3};
-  if (backward && vec == 8 && n > 2 * 256 && n <= 2 * 320) return {320, 2};
+  if (backward && vec == 8 && n > 2 * 256 && n <= 2 * 320 && (p->rows <= 512 || (p->rows >= 2048 && p->cols % vec == 0))) return {320, 2};
   if (n <= 3 * 256) return {256, (n + 255) / 256};
   if (n <= 3 * 512) return {512, (n + 511) / 512};
   const int nj = (n + 1023) / 1024;
