@@ -13,7 +13,7 @@ namespace {
 // below that.  A workgroup has 1024 elements and ends: the more of them there are, the closer together lies what the chip
 // has in flight, and the better memory takes it.  197M parameters, bf16 gradients and copies: states in 32 bits 918 us,
 // 6.0 TB/s; 2048 workgroups that walk runs of 16384 elements 1210, with loads and stores through the cache 1361.  States
-// in 8 bits 515 us, 6.1 TB/s (with eight elements of a lane next to each other, whose stores are half lines, 6 % more).
+// in 8 bits 516 us, 6.1 TB/s (with eight elements of a lane next to each other, whose stores are half lines, 6 % more).
 // Runs dealt to the dies one by one: 906 us in 32 bits, 1 % more in 8, and 16M parameters with fp32 gradients and no
 // copies 80 us, which take 76 in lots.
 constexpr int kBlock = 256;         // elements that share a scale
@@ -23,7 +23,7 @@ constexpr int kMostRuns = 1 << 23;  // of a launch
 template <bool BITS8>
 constexpr int kThreads = BITS8 ? 128 : 256;
 
-struct Run {   // elements of one tensor
+struct Run {   // elements of one tensor, whose places have the same upper 32 bits
   const void* grad;
   void *param, *copy, *m, *v;
   float *m_scale, *v_scale;
@@ -193,6 +193,36 @@ __device__ __forceinline__ float most_of_32(unsigned x) {   // over a half of th
   return __builtin_bit_cast(float, max((unsigned)r[0], (unsigned)r[1]));
 }
 
+// The rounded root of x = 0, x >= 2^-96, infinity or a NaN: the hardware's, s, is off by at most one unit u of its last place,
+// and the root is nearer to s - u if (s - u) s >= x, to s + u if (s + u) s < x.  What a fused operation leaves of such a
+// product has the right sign, but for smaller x, which are taken times 2^64.  (Equal to the root in 64 bits, rounded, for every
+// number of 32 bits; the hardware's differs for 15 % of them.)
+__device__ __forceinline__ float root_of(float x) {
+  const float s = __builtin_amdgcn_sqrtf(x);
+  const float below = __builtin_bit_cast(float, __builtin_bit_cast(unsigned, s) - 1);
+  const float above = __builtin_bit_cast(float, __builtin_bit_cast(unsigned, s) + 1);
+  const float root = __builtin_fmaf(-below, s, x) <= 0.0f ? below : s;   // of 0 and infinity these are NaN, or are not chosen
+  return __builtin_fmaf(-above, s, x) > 0.0f ? above : root;
+}
+template <int N>
+__device__ __forceinline__ void roots(float (&x)[N]) {
+  constexpr float kSmall = 0x1p-96f;
+  unsigned least = ~0u;   // of what is not 0
+#pragma unroll
+  for (int e = 0; e < N; ++e) least = min(least, __builtin_bit_cast(unsigned, x[e]) - 1);
+  if (least < __builtin_bit_cast(unsigned, kSmall) - 1) {
+#pragma unroll
+    for (int e = 0; e < N; ++e) {
+      const bool small = x[e] < kSmall;
+      const float root = root_of(small ? x[e] * 0x1p64f : x[e]);
+      x[e] = small ? root * 0x1p-32f : root;
+    }
+  } else {
+#pragma unroll
+    for (int e = 0; e < N; ++e) x[e] = root_of(x[e]);
+  }
+}
+
 // Four values in 8 bits.  By the hash the conversion adds `random` (its upper 20 bits, below the last digit that is
 // kept) and cuts off: sixteen bits of the hash, and a half behind them.
 __device__ __forceinline__ uint32_t codes_of(const float* x, bool at_random, const uint32_t* random) {
@@ -223,9 +253,10 @@ __device__ __forceinline__ void values_of(const Few<uint8_t, 4>& code, float* x)
 
 // States in 8 bits: half a wave has a block, a lane four elements of each half of it, so that every store of the wave is
 // whole lines.  Moments, scales and codes are the header's formula, each operation rounded: rounding at random carries a
-// last place into a whole code now and then, and from there into scales (200 of 10^8 codes a step, had products and sums
-// one rounding, and the quotient a last place to spare).  The parameter takes the hardware's reciprocal, off by one unit
-// of its last place (with a division 3 % more: vector operations then count).
+// last place into a whole code now and then, and from there into scales (181 of 10^8 codes a step, had products and sums
+// one rounding, and root and quotient a last place to spare).  Vector operations take 0.87 of the cycles, so what is exact
+// has to be short: with the compiler's root, and a key for each block, they take 1.04 and a step up to 2 % longer; the parameter
+// takes the hardware's reciprocal, off by one unit of its last place (with a division 3 % more).
 template <typename G, typename P>
 __device__ __forceinline__ void run_of_8(const Run& run, const AdamArgs& a) {
   constexpr int N = 4, U = 2, kApart = kBlock / U;
@@ -256,12 +287,19 @@ __device__ __forceinline__ void run_of_8(const Run& run, const AdamArgs& a) {
       float &me = m[u * N + e], &ve = root[u * N + e];
       const float d = (float)g[u].v[e] * r.grad, old = ve * vs;
       me = me * ms * r.b1 + d * r.a1;
-      ve = __builtin_sqrtf(old * old * r.b2 + d * d * r.a2);
+      ve = old * old * r.b2 + d * d * r.a2;
+    }
+  }
+  roots(root);
+#pragma unroll
+  for (int u = 0; u < U; ++u)
+#pragma unroll
+    for (int e = 0; e < N; ++e) {
+      const float me = m[u * N + e], ve = root[u * N + e];
       q[u][e] = (float)p[u].v[e] * keep - me * __builtin_amdgcn_rcpf(ve * r.root_c2 + r.eps) * r.lr_c1;
       // as whole numbers: a NaN is the largest; roots have no sign
       most_m = max(most_m, magnitude(me)), most_v = max(most_v, __builtin_bit_cast(unsigned, ve));
     }
-  }
   const float new_ms = scale_of(most_of_32(most_m), 1.0f / 448.0f), new_vs = scale_of(most_of_32(most_v), 1.0f / 448.0f);
   divide<false>(m, new_ms), divide<false>(root, new_vs);
 #pragma unroll
@@ -271,8 +309,7 @@ __device__ __forceinline__ void run_of_8(const Run& run, const AdamArgs& a) {
   }
   uint32_t high[U * N] = {}, low[U * N] = {};
   if (a.seed) {
-    const int64_t block = run.block + k;
-    const uint32_t key = key_above(r.key, (uint32_t)(block >> 24)), first = (uint32_t)block * kBlock + lane * N;
+    const uint32_t key = key_above(r.key, (uint32_t)(run.block >> 24)), first = ((uint32_t)run.block + k) * kBlock + lane * N;
     static_assert(kBlock == 256, "");
 #pragma unroll
     for (int u = 0; u < U; ++u) {
@@ -406,28 +443,30 @@ extern "C" gbmw_status gbmw_adamw_list_create(int32_t n, const gbmw_adamw_tensor
       total += tensors[i].numel;
       if (total > (1ll << 41)) return fail(GBMW_ERR_INVALID_ARG, "more than 2^41 elements");
     }
-    for (int i = 0; i < n; ++i) count += (tensors[i].numel + kRun - 1) / kRun;
     const int bad = overlap(all);
     if (bad >= 0) return fail(GBMW_ERR_INVALID_ARG, "tensor %d: an array overlaps another, and one of them is written", bad);
     std::vector<Run> runs;
-    runs.reserve((size_t)count);
+    runs.reserve((size_t)(total / kRun + n + (total >> 32) + 1));
     int64_t block = 0;
     for (int i = 0; i < n; ++i) {
       const gbmw_adamw_tensor& t = tensors[i];
       const int gs = element_size(t.grad_dtype), ps = element_size(t.dtype), ss = state_bits == 8 ? 1 : 4;
-      for (int64_t at = 0; at < t.numel; at += kRun) {
+      for (int64_t at = 0, next; at < t.numel; at = next) {
         Run r{};
         r.grad = (const char*)t.grad + at * gs, r.param = (char*)t.param + at * ps;
         r.copy = t.copy ? (char*)t.copy + at * 2 : nullptr;
         r.m = (char*)t.m + at * ss, r.v = (char*)t.v + at * ss;
         if (state_bits == 8) r.m_scale = t.m_scale + at / kBlock, r.v_scale = t.v_scale + at / kBlock;
-        r.n = (int32_t)std::min<int64_t>(kRun, t.numel - at);
         r.block = block + at / kBlock, r.decay = t.weight_decay;
+        const int64_t upper = (r.block | ((1 << 24) - 1)) + 1;   // block whose places' upper 32 bits are others
+        next = std::min(t.numel, at + std::min<int64_t>(kRun, (upper - r.block) * kBlock));
+        r.n = (int32_t)(next - at);
         r.types = t.grad_dtype | t.dtype << 8 | (t.copy ? t.copy_dtype << 16 : 0);
         runs.push_back(r);
       }
       block += (t.numel + kBlock - 1) / kBlock;
     }
+    count = (int64_t)runs.size();
     gbmw_adamw_list* l = new gbmw_adamw_list;
     l->count = count, l->bits = state_bits;
     gbmw_status st = l->runs.reserve(sizeof(Run) * (size_t)count);

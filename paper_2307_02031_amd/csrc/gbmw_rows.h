@@ -130,7 +130,7 @@ __device__ __forceinline__ float scale_of(float most, float per_top) {
 // x / scale, rounded once: the product with the rounded reciprocal is off by a unit of its last place, and what it leaves of
 // x, which a fused operation has exactly, puts that right.  What is left of x is no number of 32 bits where x is below
 // 2^-103: small scales are taken times 2^64, and else such an x has code 0 either way.  By a factor where registers are
-// short (AdamW 515 us, by a branch 521), or by a branch where operations are (RMS norm, 8192 x 5120: 55 us, by a factor 59, with
+// short (AdamW; a branch costs it 11), or by a branch where operations are (RMS norm, 8192 x 5120: 55 us, by a factor 59, with
 // the quotient left a last place off 53).  A scale that is infinite or NaN has no reciprocal: x / inf is 0.
 template <bool BRANCH, int N>
 __device__ __forceinline__ void divide(float (&x)[N], float scale) {
