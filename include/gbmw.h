@@ -631,7 +631,9 @@ void gbmw_gradient_list_destroy(gbmw_gradient_list* list);
  * past the norm.  weight may be NULL (ones), dweight may be NULL (not wanted).
  * y or h may be x or residual, and dx may be dy or dres, with the same row stride.  A y over x
  * without a residual leaves no h for a backward call.
- * Squares are summed in fp32: rows with values beyond about 1e18 have rstd = 0, and are 0.
+ * Squares are summed in fp32: rows with values beyond about 1e18 have rstd = 0, and are 0.  Those of values
+ * below about 1e-19 are lost beside any eps that is usual; with eps = 0 such rows, and rows of zeros, have
+ * an rstd that is too large, or infinite.
  */
 enum { GBMW_E4M3 = 3, GBMW_I8 = 4 };
 
@@ -780,7 +782,8 @@ typedef struct {
   double scale;              /* > 0: the inverse of a loss scale                     */
   double max_norm;           /* > 0, may be +inf                                     */
   int64_t step;              /* >= 1: the number of this step                        */
-  uint32_t seed;             /* states of 8 bits: 0 rounds to nearest                */
+  uint32_t seed;             /* states of 8 bits: 0 rounds to nearest (see above:
+                                a training gives another)                            */
   /* DEVICE pointers, each may be NULL: read when the step runs, for steps in a graph */
   const float* norm;
   const float* lr_now;       /* in the place of lr                                   */

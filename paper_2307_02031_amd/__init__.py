@@ -1108,8 +1108,10 @@ def gbmw_adamw_step(lst: AdamWList, lr, step, beta1: float = 0.9, beta2: float =
     """One step of the list's parameters and states.  lr: a number, or a float32 GPU tensor that is read when the step
     runs; step: the step's number from 1 on, or an int64 GPU tensor.  scale: of the gradients, the inverse of a loss scale.
     norm: of the gradients times scale, what gbmw_clip_gradients returned for a list with norm_only and the same scale: the
-    gradients are clipped to max_norm as they are read, and the step is left out where it is not finite.  seed: of the
-    rounding of states of 8 bits, 0 for the nearest.  stream=: as everywhere."""
+    gradients are clipped to max_norm as they are read, and the step is left out where it is not finite.  seed (up to
+    2^32 - 1): of the rounding of states of 8 bits.  A training with such states gives one other than 0: 0 rounds to the
+    nearest, which leaves moments that move by less than half a step at a time (second moments, by a thousandth of
+    themselves) where they are.  stream=: as everywhere."""
     if not 0 <= seed < 1 << 32:
         _refuse(f"seed={seed} is not in 0..2^32 - 1")       # its lower bits alone may be 0, which rounds to the nearest
     o = gbmw_adamw_options(0.0, beta1, beta2, eps, scale, max_norm, 1, seed)

@@ -253,7 +253,7 @@ __device__ __forceinline__ void values_of(const Few<uint8_t, 4>& code, float* x)
 
 // States in 8 bits: half a wave has a block, a lane four elements of each half of it, so that every store of the wave is
 // whole lines.  Moments, scales and codes are the header's formula, each operation rounded: rounding at random carries a
-// last place into a whole code now and then, and from there into scales (181 of 10^8 codes a step, had products and sums
+// last place into a whole code now and then, and from there into scales (184 of 10^8 codes a step, had products and sums
 // one rounding, and root and quotient a last place to spare).  Vector operations take 0.87 of the cycles, so what is exact
 // has to be short: with the compiler's root, and a key for each block, they take 1.04 and a step up to 2 % longer; the parameter
 // takes the hardware's reciprocal, off by one unit of its last place (with a division 3 % more).
