@@ -9,11 +9,11 @@ using gbmw_detail::fail;
 namespace gbmw {
 namespace {
 
-// Bound by HBM: every array is read and written once, and arithmetic (about 60 vector operations an element) stays
-// below that.  A workgroup has 1024 elements and ends: the more of them there are, the closer together lies what the chip
+// Bound by HBM: every array is read and written once, and arithmetic (in 8 bits about 80 vector operations an element)
+// stays below that.  A workgroup has 1024 elements and ends: the more of them there are, the closer together lies what the chip
 // has in flight, and the better memory takes it.  197M parameters, bf16 gradients and copies: states in 32 bits 918 us,
 // 6.0 TB/s; 2048 workgroups that walk runs of 16384 elements 1210, with loads and stores through the cache 1361.  States
-// in 8 bits 516 us, 6.1 TB/s (with eight elements of a lane next to each other, whose stores are half lines, 6 % more).
+// in 8 bits 520 us, 6.1 TB/s (with eight elements of a lane next to each other, whose stores are half lines, 6 % more).
 // Runs dealt to the dies one by one: 906 us in 32 bits, 1 % more in 8, and 16M parameters with fp32 gradients and no
 // copies 80 us, which take 76 in lots.
 constexpr int kBlock = 256;         // elements that share a scale
@@ -95,7 +95,7 @@ __device__ __forceinline__ bool rates_now(const AdamArgs& a, Rates& r) {
 
 // N elements at p of which n (0..N) are there, loaded or stored at once where all are.  Nothing is
 // read or written twice in a step, so all of it passes the cache by.  Arrays that begin in the middle of a
-// line (40M parameters: 184 us become 196, in 8 bits 107 become 172) take the same way: through the cache
+// line (40M parameters: 183 us become 196, in 8 bits 107 become 162) take the same way: through the cache
 // they take 280 and 161.
 template <typename T, int N>
 struct alignas(sizeof(T)) Few {
@@ -193,33 +193,20 @@ __device__ __forceinline__ float most_of_32(unsigned x) {   // over a half of th
   return __builtin_bit_cast(float, max((unsigned)r[0], (unsigned)r[1]));
 }
 
-// The rounded root of x = 0, x >= 2^-96, infinity or a NaN: the hardware's, s, is off by at most one unit u of its last place,
-// and the root is nearer to s - u if (s - u) s >= x, to s + u if (s + u) s < x.  What a fused operation leaves of such a
-// product has the right sign, but for smaller x, which are taken times 2^64.  (Equal to the root in 64 bits, rounded, for every
-// number of 32 bits; the hardware's differs for 15 % of them.)
-__device__ __forceinline__ float root_of(float x) {
-  const float s = __builtin_amdgcn_sqrtf(x);
-  const float below = __builtin_bit_cast(float, __builtin_bit_cast(unsigned, s) - 1);
-  const float above = __builtin_bit_cast(float, __builtin_bit_cast(unsigned, s) + 1);
-  const float root = __builtin_fmaf(-below, s, x) <= 0.0f ? below : s;   // of 0 and infinity these are NaN, or are not chosen
-  return __builtin_fmaf(-above, s, x) > 0.0f ? above : root;
-}
+// Rounded roots, of values from `least` to `most` (as bits): the root by the hardware's reciprocal root is put right by half of
+// what its square leaves of x, which a fused operation has exactly.  That is the rounded root of every number of 32 bits
+// from 2^-96 on, compared with the one in 64 bits; smaller ones and infinity go the compiler's way.
 template <int N>
-__device__ __forceinline__ void roots(float (&x)[N]) {
-  constexpr float kSmall = 0x1p-96f;
-  unsigned least = ~0u;   // of what is not 0
+__device__ __forceinline__ void roots(float (&x)[N], unsigned least, unsigned most) {
+  if (least < __builtin_bit_cast(unsigned, 0x1p-96f) || most >= __builtin_bit_cast(unsigned, __builtin_inff())) {
 #pragma unroll
-  for (int e = 0; e < N; ++e) least = min(least, __builtin_bit_cast(unsigned, x[e]) - 1);
-  if (least < __builtin_bit_cast(unsigned, kSmall) - 1) {
-#pragma unroll
-    for (int e = 0; e < N; ++e) {
-      const bool small = x[e] < kSmall;
-      const float root = root_of(small ? x[e] * 0x1p64f : x[e]);
-      x[e] = small ? root * 0x1p-32f : root;
-    }
+    for (int e = 0; e < N; ++e) x[e] = __builtin_sqrtf(x[e]);
   } else {
 #pragma unroll
-    for (int e = 0; e < N; ++e) x[e] = root_of(x[e]);
+    for (int e = 0; e < N; ++e) {
+      const float y = __builtin_amdgcn_rsqf(x[e]), root = x[e] * y;
+      x[e] = __builtin_fmaf(__builtin_fmaf(-root, root, x[e]), 0.5f * y, root);
+    }
   }
 }
 
@@ -254,9 +241,10 @@ __device__ __forceinline__ void values_of(const Few<uint8_t, 4>& code, float* x)
 // States in 8 bits: half a wave has a block, a lane four elements of each half of it, so that every store of the wave is
 // whole lines.  Moments, scales and codes are the header's formula, each operation rounded: rounding at random carries a
 // last place into a whole code now and then, and from there into scales (184 of 10^8 codes a step, had products and sums
-// one rounding, and root and quotient a last place to spare).  Vector operations take 0.87 of the cycles, so what is exact
-// has to be short: with the compiler's root, and a key for each block, they take 1.04 and a step up to 2 % longer; the parameter
-// takes the hardware's reciprocal, off by one unit of its last place (with a division 3 % more).
+// one rounding, and root and quotient a last place to spare).  Vector operations take 0.8 to 0.9 of the cycles, so what is exact
+// has to be short: with the compiler's roots, and a key for each block, they take all of them and a kernel 3 % longer; the parameter
+// takes the hardware's reciprocal, off by one unit of its last place (with a division 3 % more).  Parameters of 16 bits, which
+// move less, are bound by them: 197M bf16 378 us, 5.2 TB/s, with that last place to spare 351.
 template <typename G, typename P>
 __device__ __forceinline__ void run_of_8(const Run& run, const AdamArgs& a) {
   constexpr int N = 4, U = 2, kApart = kBlock / U;
@@ -278,7 +266,7 @@ __device__ __forceinline__ void run_of_8(const Run& run, const AdamArgs& a) {
   if (!rates_now(a, r)) return;
   const float keep = (float)(1.0 - r.lr * (double)run.decay);
   float m[U * N], root[U * N], q[U][N];
-  unsigned most_m = 0, most_v = 0;
+  unsigned most_m = 0, most_v = 0, least_v = ~0u;
 #pragma unroll
   for (int u = 0; u < U; ++u) {
     values_of(mc[u], m + u * N), values_of(vc[u], root + u * N);
@@ -288,19 +276,21 @@ __device__ __forceinline__ void run_of_8(const Run& run, const AdamArgs& a) {
       const float d = (float)g[u].v[e] * r.grad, old = ve * vs;
       me = me * ms * r.b1 + d * r.a1;
       ve = old * old * r.b2 + d * d * r.a2;
+      // as whole numbers: a NaN is the largest; squares have no sign
+      const unsigned bits = __builtin_bit_cast(unsigned, ve);
+      most_m = max(most_m, magnitude(me)), most_v = max(most_v, bits), least_v = min(least_v, bits);
     }
   }
-  roots(root);
+  roots(root, least_v, most_v);
 #pragma unroll
   for (int u = 0; u < U; ++u)
 #pragma unroll
     for (int e = 0; e < N; ++e) {
       const float me = m[u * N + e], ve = root[u * N + e];
       q[u][e] = (float)p[u].v[e] * keep - me * __builtin_amdgcn_rcpf(ve * r.root_c2 + r.eps) * r.lr_c1;
-      // as whole numbers: a NaN is the largest; roots have no sign
-      most_m = max(most_m, magnitude(me)), most_v = max(most_v, __builtin_bit_cast(unsigned, ve));
     }
-  const float new_ms = scale_of(most_of_32(most_m), 1.0f / 448.0f), new_vs = scale_of(most_of_32(most_v), 1.0f / 448.0f);
+  const float new_ms = scale_of(most_of_32(most_m), 1.0f / 448.0f);
+  const float new_vs = scale_of(__builtin_sqrtf(most_of_32(most_v)), 1.0f / 448.0f);
   divide<false>(m, new_ms), divide<false>(root, new_vs);
 #pragma unroll
   for (int e = 0; e < U * N; ++e) {
