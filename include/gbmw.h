@@ -631,9 +631,9 @@ void gbmw_gradient_list_destroy(gbmw_gradient_list* list);
  * past the norm.  weight may be NULL (ones), dweight may be NULL (not wanted).
  * y or h may be x or residual, and dx may be dy or dres, with the same row stride.  A y over x
  * without a residual leaves no h for a backward call.
- * Squares are summed in fp32: rows with values beyond about 1e18 have rstd = 0, and are 0.  Those of values
- * below about 1e-19 are lost beside any eps that is usual; with eps = 0 such rows, and rows of zeros, have
- * an rstd that is too large, or infinite.
+ * Squares are summed in fp32: rows with values beyond about 1e18 have rstd = 0, and are 0.  Squares
+ * of values below about 1e-19 lose digits, which shows with an eps of 0 alone: rstd is then too large,
+ * and infinite for rows of zeros.
  */
 enum { GBMW_E4M3 = 3, GBMW_I8 = 4 };
 
@@ -732,13 +732,13 @@ gbmw_status gbmw_rotary_frequencies(int32_t rot, double theta, int32_t scaling, 
  *   g = grad * factor,  factor = scale * (norm > max_norm ? max_norm / norm : 1),
  *   m = m * beta1 + g * (1 - beta1),  v = v * beta2 + (g * g) * (1 - beta2),
  *   param = param * (1 - lr weight_decay) - (m / (sqrt(v) * (1 / sqrt(c2)) + eps)) * (lr / c1),
- * in fp32, each of these operations rounded to nearest (numbers that all elements share, factor, 1 - beta1,
- * lr / c1 and so on, are computed in fp64 and rounded once), param then to dtype.  `copy`, if
- * given, gets the new param (of GBMW_F32) rounded to copy_dtype.  norm is that of grad * scale, what
- * gbmw_clip_gradients writes with the same scale, of a list without outputs: that call leaves the
- * gradients as they are, and the step scales and clips as it reads.  (A list whose outputs are its inputs
- * scales them itself; the step's scale is then 1.)  If *norm is NaN or infinite the step is left
- * out: nothing is written.
+ * in fp32, each of these operations rounded to nearest (numbers that all elements share, factor,
+ * 1 - beta1, lr / c1 and so on, are computed in fp64 and rounded once), param then to dtype.
+ * `copy`, if given, gets the new param (of GBMW_F32) rounded to copy_dtype.  norm is that of
+ * grad * scale, what gbmw_clip_gradients writes with the same scale, of a list without outputs: that
+ * call leaves the gradients as they are, and the step scales and clips as it reads.  (A list whose
+ * outputs are its inputs scales them itself; the step's scale is then 1.)  If *norm is NaN or infinite
+ * the step is left out: nothing is written.
  *
  * States of 32 bits: m and v in fp32.  States of 8 bits: for each block of 256 elements of a
  * tensor (the last may have fewer) m is held as codes of GBMW_E4M3 with a scale, and so is

@@ -878,10 +878,10 @@ def gbmw_rms_norm_forward(x, weight=None, eps: float = 1e-5, residual=None, qtyp
                           want_y: bool = True, y=None, h=None, q=None):
     """RmsNorm(y, h, rstd, q, scale) of x, a float32, float16 or bfloat16 GPU tensor whose last axis is normed, after
     the addition of residual, if there is one.  weight: of x's type or float32.  y: like x, None unless want_y.
-    h: x + residual; without a residual x itself, or None where y is written over it (no backward call can follow).  rstd: float32 of x's shape without its last axis.  qtype
-    (torch.float8_e4m3fn or torch.int8): q holds y in 8 bits, with scale (float32, of x's shape but for the last axis)
-    for each row, or for each `group` (32, 64 or 128) columns; None without a qtype.  y, h, q: made here unless given (y
-    or h may be x or residual).  stream=: as everywhere.  Not recorded by autograd: gradients come from
+    h: x + residual; without a residual x itself, or None where y is written over it (no backward call can follow).
+    rstd: float32 of x's shape without its last axis.  qtype (torch.float8_e4m3fn or torch.int8): q holds y in 8 bits, with
+    scale (float32, of x's shape but for the last axis) for each row, or for each `group` (32, 64 or 128) columns; None
+    without a qtype.  y, h, q: made here unless given (y or h may be x or residual).  stream=: as everywhere.  Not recorded by autograd: gradients come from
     gbmw_rms_norm_backward."""
     p, device = _rms_problem(x, weight)
     shape, dtype = x.shape, x.dtype

@@ -11,10 +11,10 @@ namespace {
 // over x and the residual, one sum, and for 8 bits the largest of a group's threads.
 //
 // Bound by HBM.  16384 x 5120 bf16 with a residual: forward 113 us, 5.9 TB/s; backward 125, 5.4 TB/s, of
-// which 5 to join the shares of dweight.  8192 x 5120 to 8 bits, a scale for each 128 columns: 54 us, 5.4 TB/s.  4 x 5120:
-// 4.2 us, latency of a load, a sum and a store.  Rows at odd addresses (16-bit values, an odd number a row) cost up to
+// which 5 to join the shares of dweight.  8192 x 5120 to 8 bits, a scale for each 128 columns: 54 us, 5.4 TB/s (int8 56).  4 x 5120:
+// 4.4 us, latency of a load, a sum and a store.  Rows at odd addresses (16-bit values, an odd number a row) cost up to
 // 1.4 times as much (4096 x 10001 102 us, 4096 x 10002 72); rows beyond 16384 columns spill in the backward pass
-// (2048 x 20000 bf16: 139 us, forward 62).
+// (2048 x 20000 bf16: 139 us, forward 62; 512 x 30000 100, 1024 x 32768 fp32 265: 2 to 4 times what their bytes take).
 struct RmsArgs {
   int64_t rows;
   int cols;
@@ -390,7 +390,8 @@ Shape rms_shape(const gbmw_rms_norm_problem* p, bool backward) {
   if (n <= 16 || (n <= 3 * 16 && (backward || !p->q || p->group <= 16 * vec))) return {16, (n + 15) / 16};
   if (n <= 3 * 64) return {64, (n + 63) / 64};
   if (n > 2 * 128 && n <= 3 * 128) return {128, 3};
-  if (backward && vec == 8 && n > 2 * 256 && n <= 2 * 320 && (p->rows <= 512 || (p->rows >= 2048 && p->cols % vec == 0))) return {320, 2};
+  const bool few = p->rows <= 512, many_whole = p->rows >= 2048 && p->cols % vec == 0;
+  if (backward && vec == 8 && n > 2 * 256 && n <= 2 * 320 && (few || many_whole)) return {320, 2};
   if (n <= 3 * 256) return {256, (n + 255) / 256};
   if (n <= 3 * 512) return {512, (n + 511) / 512};
   const int nj = (n + 1023) / 1024;

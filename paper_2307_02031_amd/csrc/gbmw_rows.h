@@ -121,7 +121,8 @@ __global__ __launch_bounds__(1024) void k_norm_join(const float* partial, int pa
   if (col < cols) out[col] = (W)total;
 }
 
-// Values in 8 bits share a scale: the largest of them in place of the largest code, by its reciprocal.  Never 0 or subnormal; a NaN stays.
+// Values in 8 bits share a scale: the largest of them over the largest code, by that one's reciprocal.  Never 0 or subnormal; a
+// NaN stays.
 __device__ __forceinline__ float scale_of(float most, float per_top) {
   const float s = most * per_top;
   return s < 0x1p-126f ? 0x1p-126f : s;
